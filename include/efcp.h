@@ -404,6 +404,122 @@ int efcp_profile_end(efcp_ctx* ctx, double* ms_out, int32_t* steps_out);
 #define EFCP_TOPK_STATIC_MAX_D (1 << 20)
 int efcp_topk_static(const float* a, int64_t d, int64_t k, int32_t* idx, float* val, void* stream);
 
+/*
+ * Lists of gradients.  The optimizer sees the model as one vector in R^d; a training program
+ * holds its gradient as a list of tensors of several types and layouts.  Three calls work on the
+ * whole list: its Euclidean norm, clipping it in place, and gathering it into the flat fp32
+ * vector efcp_step takes.  They need no handle.
+ *
+ * efcp_tensor describes one gradient.
+ *   data   : device pointer, aligned to the element size; NULL for a parameter without a gradient
+ *            in this step, which counts as zeros.
+ *   numel  : elements, 0 .. 2^40.
+ *   dtype  : EFCP_F32, EFCP_BF16 or EFCP_F16.
+ *   rank   : 0 when the elements lie one after another in the order of the flat vector; otherwise
+ *            the number of dimensions, 1..EFCP_MAX_RANK, and size / stride (in elements, >= 0)
+ *            give the layout, the last dimension running fastest in the flat vector.  A stride of
+ *            0 (a broadcast tensor) may be read, not clipped.  Any layout whose dimensions merge
+ *            into at most four is taken: permuted ones (channels-last, transposes), slices, broadcasts.
+ */
+#define EFCP_F32 0
+#define EFCP_BF16 1
+#define EFCP_F16 2
+#define EFCP_MAX_RANK 8
+typedef struct efcp_tensor {
+  void* data;
+  int64_t numel;
+  int32_t dtype;
+  int32_t rank;
+  int64_t size[EFCP_MAX_RANK];
+  int64_t stride[EFCP_MAX_RANK];
+} efcp_tensor;
+
+/*
+ *   efcp_grads_norm   : N = scale * |g|_2 over all elements of the list (fp64 sums in a fixed
+ *                       order; neither large nor tiny values overflow or vanish in the squares).
+ *   efcp_grads_clip   : g <- f g in place with f = scale * min(1, max_norm / N): the list's norm
+ *                       after `scale` is at most max_norm.  One fp32 product per element, rounded
+ *                       once to the element's type.  When f is exactly 1 nothing is written.
+ *   efcp_grads_gather : flat[0..d) = f g, tensor after tensor, d being the sum of the numels;
+ *                       f = scale * min(1, max_norm / N), or scale when max_norm is 0 (no
+ *                       clipping).  A factor of exactly 1 copies fp32 gradients bit for bit.
+ * When N is not finite (an Inf or NaN among the gradients) f is `scale`: nothing is clipped, the
+ * bad values stay where they are, and *norm and the next efcp_step's status tell of them.
+ *   grads     host, n descriptors, read before the call returns; n >= 0.
+ *   scale     finite, > 0: 1 / loss scale, 1 / number of accumulated steps, ... (else 1).
+ *   max_norm  > 0 (infinity allowed); 0 only in efcp_grads_gather.
+ *   norm      device, receives N as fp32; may be NULL except in efcp_grads_norm.
+ *   flat      device, d floats, overlapping none of the gradients.
+ *   workspace device, efcp_grads_workspace_bytes() bytes, 8-byte aligned, set to zero once
+ *             before its first use and then left to these calls; calls that may run at the same
+ *             time (other streams) need one each.  Not needed (NULL) by a gather with
+ *             max_norm == 0 and norm == NULL.
+ * Work runs on the current device and on `stream`, asynchronously, and can be captured in a graph.
+ * EFCP_EINVAL (nothing enqueued): null or misaligned pointers, sizes that do not multiply to
+ * numel, an unknown type, more than four dimensions after merging, overlapping elements in a
+ * list to be clipped, a `d` that is not the sum of the numels, scalars out of range.
+ */
+int64_t efcp_grads_workspace_bytes(void);
+int efcp_grads_norm(const efcp_tensor* grads, int32_t n, float scale, float* norm,
+                    void* workspace, void* stream);
+int efcp_grads_clip(const efcp_tensor* grads, int32_t n, float max_norm, float scale, float* norm,
+                    void* workspace, void* stream);
+int efcp_grads_gather(const efcp_tensor* grads, int32_t n, float* flat, int64_t d, float max_norm,
+                      float scale, float* norm, void* workspace, void* stream);
+
+/*
+ * Group normalisation with an activation, channels last, forward and backward.  Unlike batch
+ * normalisation it does not couple the samples of a batch, so the gradient of a mini-batch is
+ * the mean of per-sample gradients, which is what the empirical Fisher matrix is built from.
+ * With n samples, `rows` positions (height x width, ...), `channels` channels in `groups`
+ * groups of D = channels / groups, for each sample and group, over its rows * D values:
+ *     mean, var = mean((x - mean)^2), rstd = 1 / sqrt(var + eps),
+ *     h = (x - mean) rstd,   z = h w_c + b_c,   y = act(z),
+ * and, given dy, with e = dy act'(z):
+ *     dw_c = sum_{n, rows} e h,   db_c = sum_{n, rows} e,
+ *     dx = rstd (e w_c - mean_group(e w_c) - h mean_group(e w_c h)).
+ *
+ *   dtype            of x, y, dy, dx: EFCP_F32, EFCP_BF16 or EFCP_F16.
+ *   param_dtype      of weight, bias, dweight, dbias: the same choices.
+ *   act              EFCP_ACT_NONE, EFCP_ACT_RELU (derivative 0 at 0) or EFCP_ACT_SILU.
+ *   x_batch, x_row   elements between samples, and between rows (>= channels) of x; the
+ *                    channels of a row lie side by side, so x may be a channel slice of a wider
+ *                    tensor.  y_batch, y_row: the same for y, in the backward call for dx;
+ *                    dy_batch, dy_row: for dy (unused by the forward call).
+ *   weight, bias     device, `channels` entries; NULL: 1 and 0.
+ *   mean, rstd       device, n * groups floats: written by the forward call, read by the
+ *                    backward one.
+ *   dweight, dbias   device, `channels` entries, overwritten; NULL: not wanted.
+ *   workspace        device, efcp_group_norm_workspace_bytes(desc, backward) bytes, 16-byte
+ *                    aligned; its contents need not be kept and are undefined afterwards.
+ * All sums are fp32 or wider and taken in a fixed order, so results repeat bit for bit; outputs
+ * are rounded to their type once.  Outputs overlap no input.  Work runs on the current device and
+ * on `stream`, asynchronously, and can be captured in a graph.
+ * n == 0 enqueues nothing but the zeroing of dweight and dbias.
+ * EFCP_EINVAL (nothing enqueued): null or misaligned pointers, groups that do not divide
+ * channels, sizes below 1 (n below 0), channels of 2^30 or more, a product above 2^40, row strides below channels,
+ * negative batch strides, rows or samples of an output that overlap,
+ * eps negative or not finite, unknown types; EFCP_ENOMEM: a workspace that is too small;
+ * EFCP_ETOOBIG: more than 2^31 - 1 thread blocks.
+ */
+#define EFCP_ACT_NONE 0
+#define EFCP_ACT_RELU 1
+#define EFCP_ACT_SILU 2
+typedef struct efcp_group_norm {
+  int64_t n, rows, channels;
+  int32_t groups, dtype, param_dtype, act;
+  int64_t x_batch, x_row, y_batch, y_row, dy_batch, dy_row;
+  float eps;
+} efcp_group_norm;
+int64_t efcp_group_norm_workspace_bytes(const efcp_group_norm* desc, int32_t backward);
+int efcp_group_norm_forward(const efcp_group_norm* desc, const void* x, const void* weight,
+                            const void* bias, void* y, float* mean, float* rstd, void* workspace,
+                            int64_t workspace_bytes, void* stream);
+int efcp_group_norm_backward(const efcp_group_norm* desc, const void* dy, const void* x,
+                             const float* mean, const float* rstd, const void* weight,
+                             const void* bias, void* dx, void* dweight, void* dbias,
+                             void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Static description of an EFCP_* code. */
 const char* efcp_strerror(int code);
 

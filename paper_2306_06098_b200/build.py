@@ -1,13 +1,17 @@
-"""Builds csrc/*.cu into csrc/libefcp.so with nvcc for sm_100a (in-tree, no JIT cache)."""
+"""Builds csrc/*.cu into csrc/libefcp.so with nvcc for sm_100a, and csrc/efcp_marshal.cpp into
+_marshal.so against the installed torch (both in-tree, no JIT cache)."""
 import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(CSRC, "libefcp.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
+MARSHAL_SRC = os.path.join(CSRC, "efcp_marshal.cpp")
 
 
 def _sources():
@@ -16,26 +20,48 @@ def _sources():
 
 def _deps():
     return _sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(
-        os.path.join(INCLUDE, "*.h"))
+        os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(INCLUDE, "*.h"))
+
+
+def _stale(target, deps):
+    return not os.path.exists(target) or os.path.getmtime(target) < max(map(os.path.getmtime, deps))
+
+
+def build_marshal(force: bool = False) -> str:
+    """Compile _marshal.so when it is missing or older than its sources; return its path."""
+    deps = [MARSHAL_SRC] + glob.glob(os.path.join(INCLUDE, "*.h"))
+    if not force and not _stale(MARSHAL, deps):
+        return MARSHAL
+    import torch
+    root = os.path.dirname(torch.__file__)
+    lib = os.path.join(root, "lib")
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+           "-I", sysconfig.get_paths()["include"], "-I", os.path.join(root, "include"),
+           "-I", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-I", INCLUDE,
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-o", MARSHAL + ".tmp", MARSHAL_SRC,
+           "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-L", CSRC, "-l:libefcp.so",
+           f"-Wl,-rpath,{lib}", "-Wl,-rpath,$ORIGIN/csrc"]
+    subprocess.run(cmd, check=True)
+    os.replace(MARSHAL + ".tmp", MARSHAL)
+    return MARSHAL
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile when the library is missing or older than any source; return its path."""
-    if not force and os.path.exists(LIB):
-        newest = max(os.path.getmtime(p) for p in _deps())
-        if os.path.getmtime(LIB) >= newest:
-            return LIB
-    nvcc = os.environ.get("NVCC", "nvcc")
-    cmd = [nvcc, "-std=c++17", "-O3", "-lineinfo",
-           "-gencode", "arch=compute_100a,code=sm_100a",
-           "-Xcompiler", "-fPIC", "-shared", "-I", INCLUDE, "-I", CSRC,
-           "-o", LIB + ".tmp"] + _sources()
-    cmd[1:1] = os.environ.get("EFCP_NVCC_FLAGS", "").split()  # e.g. -DEFCP_DEPTH=8
-    if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-    subprocess.run(cmd, check=True)
-    os.replace(LIB + ".tmp", LIB)
+    """Compile what is missing or older than its sources; return the CUDA library's path."""
+    if force or _stale(LIB, _deps()):
+        nvcc = os.environ.get("NVCC", "nvcc")
+        cmd = [nvcc, "-std=c++17", "-O3", "-lineinfo", "--threads", "0",
+               "-gencode", "arch=compute_100a,code=sm_100a",
+               "-Xcompiler", "-fPIC", "-shared", "-I", INCLUDE, "-I", CSRC,
+               "-o", LIB + ".tmp"] + _sources()
+        cmd[1:1] = os.environ.get("EFCP_NVCC_FLAGS", "").split()  # e.g. -DEFCP_DEPTH=8
+        if verbose:
+            cmd.insert(1, "-Xptxas")
+            cmd.insert(2, "-v")
+        subprocess.run(cmd, check=True)
+        os.replace(LIB + ".tmp", LIB)
+    build_marshal(force)
     return LIB
 
 
