@@ -5,6 +5,7 @@ import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -51,15 +52,20 @@ def build(force: bool = False, verbose: bool = False) -> str:
     """Compile what is missing or older than its sources; return the CUDA library's path."""
     if force or _stale(LIB, _deps()):
         nvcc = os.environ.get("NVCC", "nvcc")
-        cmd = [nvcc, "-std=c++17", "-O3", "-lineinfo", "--threads", "0",
-               "-gencode", "arch=compute_100a,code=sm_100a",
-               "-Xcompiler", "-fPIC", "-shared", "-I", INCLUDE, "-I", CSRC,
-               "-o", LIB + ".tmp"] + _sources()
-        cmd[1:1] = os.environ.get("EFCP_NVCC_FLAGS", "").split()  # e.g. -DEFCP_DEPTH=8
+        flags = os.environ.get("EFCP_NVCC_FLAGS", "").split() + [  # e.g. -DEFCP_DEPTH=8
+            "-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",
+            "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
         if verbose:
-            cmd.insert(1, "-Xptxas")
-            cmd.insert(2, "-v")
-        subprocess.run(cmd, check=True)
+            flags = ["-Xptxas", "-v"] + flags
+        # the sources at the same time: the templates of one take as long as all the rest
+        with tempfile.TemporaryDirectory() as tmp:
+            objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in _sources()]
+            jobs = [subprocess.Popen([nvcc] + flags + ["-c", "-o", o, s])
+                    for s, o in zip(_sources(), objects)]
+            failed = [s for s, j in zip(_sources(), jobs) if j.wait() != 0]
+            if failed:
+                raise RuntimeError("nvcc failed for " + ", ".join(failed))
+            subprocess.run([nvcc, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o", LIB + ".tmp"] + objects, check=True)
         os.replace(LIB + ".tmp", LIB)
     build_marshal(force)
     return LIB

@@ -1,0 +1,1214 @@
+// Group normalisation with an activation on channels-last tensors, forward and backward (the
+// formulas stand in include/efcp.h).
+//
+// Memory bounds it: forward x is read and y written once, backward x and dy are read and
+// dx is written once.  Both directions need sums over a whole group before the first result, so the
+// input has to stay on the chip in between, or is read twice.
+//
+//   resident   A cluster of up to 16 thread blocks takes one sample's tile of channels and holds all
+//              of it in shared memory (about 200 KB per SM, in two to four blocks, so that some load
+//              while others compute); the blocks exchange their sums through each other's shared
+//              memory.  One read, one write.
+//   streamed   For samples that do not fit: one pass for the sums of chunks of rows, a small
+//              kernel that joins them, one pass for the result.
+//
+// A tile is a number of whole groups.  In both forms a thread owns V neighbouring channels
+// (one access of up to 16 bytes) and walks down rows, so what belongs to a channel - weight,
+// bias, statistics, its sums - stays with the thread.
+#pragma once
+
+#include <cooperative_groups.h>
+#include <cuda_runtime.h>
+
+#include "efcp.h"
+#include "efcp_gn.h"
+#include "efcp_num.cuh"
+
+namespace efcp {
+namespace {
+
+namespace cg = cooperative_groups;
+
+// What a thread block works on.
+struct Item {
+  long long n, r0, r1;           // sample, rows r0 .. r1 of it (none when r1 <= r0)
+  int chunk, g0, ng, c0, width;  // groups g0 .. g0 + ng, channels c0 .. c0 + width
+  int tx, ty;                    // this thread's place among the accesses side by side
+  bool on;                       // whether that place exists
+};
+
+// `chunk`: the chunk of the sample's tile, `q`: the tile among those of all samples.
+template <int V>
+__device__ __forceinline__ Item item_of(const Gn& p, unsigned chunk, unsigned q) {
+  Item it;
+  it.chunk = int(chunk);
+  unsigned s = q, tile = 0;
+  if (p.tiles > 1) {
+    s = q / unsigned(p.tiles);
+    tile = q - s * unsigned(p.tiles);
+  }
+  it.n = s;
+  it.r0 = it.chunk * p.chunk_rows;
+  it.r1 = min(p.rows, it.r0 + p.chunk_rows);
+  it.g0 = int(tile) * p.tile_groups;
+  it.ng = min(p.tile_groups, p.groups - it.g0);
+  it.c0 = it.g0 * p.per;
+  it.width = it.ng * p.per;
+  if (p.pitch_log >= 0) {
+    it.ty = int(threadIdx.x) >> p.pitch_log;
+    it.tx = int(threadIdx.x) & ((1 << p.pitch_log) - 1);
+  } else {
+    it.ty = int(threadIdx.x) / p.cols;
+    it.tx = int(threadIdx.x) - it.ty * p.cols;
+  }
+  it.on = it.tx < p.cols && it.tx * V < it.width && it.ty < p.lanes_rows;
+  return it;
+}
+
+// V elements through the read-only path (the input is not written during the launch, so loads
+// may move ahead of the stores of earlier rows).
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> load_pack(const T* p) {
+  Pack<T, V> a;
+  if constexpr (sizeof(a) == 16) {
+    *reinterpret_cast<uint4*>(&a) = __ldg(reinterpret_cast<const uint4*>(p));
+  } else if constexpr (sizeof(a) == 4) {
+    *reinterpret_cast<unsigned*>(&a) = __ldg(reinterpret_cast<const unsigned*>(p));
+  } else {
+    static_assert(sizeof(a) == 2, "2, 4 or 16 bytes");
+    *reinterpret_cast<unsigned short*>(&a) = __ldg(reinterpret_cast<const unsigned short*>(p));
+  }
+  return a;
+}
+
+// V fp32 values, two to an instruction where there are two (sm_100's packed fp32 arithmetic: the
+// same rounding as one by one, at half the instructions).
+template <int V>
+struct Vec {
+  float v[V];
+};
+template <int V>
+__device__ __forceinline__ Vec<V> fill(float x) {
+  Vec<V> r;
+#pragma unroll
+  for (int j = 0; j < V; ++j) r.v[j] = x;
+  return r;
+}
+template <int V>
+__device__ __forceinline__ Vec<V> fma(const Vec<V>& a, const Vec<V>& b, const Vec<V>& c) {
+  Vec<V> r;
+  if constexpr (V == 1) {
+    r.v[0] = fmaf(a.v[0], b.v[0], c.v[0]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; j += 2) {
+      const float2 t = __ffma2_rn(make_float2(a.v[j], a.v[j + 1]), make_float2(b.v[j], b.v[j + 1]),
+                                  make_float2(c.v[j], c.v[j + 1]));
+      r.v[j] = t.x;
+      r.v[j + 1] = t.y;
+    }
+  }
+  return r;
+}
+template <int V>
+__device__ __forceinline__ Vec<V> operator+(const Vec<V>& a, const Vec<V>& b) {
+  Vec<V> r;
+  if constexpr (V == 1) {
+    r.v[0] = a.v[0] + b.v[0];
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; j += 2) {
+      const float2 t =
+          __fadd2_rn(make_float2(a.v[j], a.v[j + 1]), make_float2(b.v[j], b.v[j + 1]));
+      r.v[j] = t.x;
+      r.v[j + 1] = t.y;
+    }
+  }
+  return r;
+}
+template <int V>
+__device__ __forceinline__ Vec<V> operator*(const Vec<V>& a, const Vec<V>& b) {
+  Vec<V> r;
+  if constexpr (V == 1) {
+    r.v[0] = a.v[0] * b.v[0];
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; j += 2) {
+      const float2 t =
+          __fmul2_rn(make_float2(a.v[j], a.v[j + 1]), make_float2(b.v[j], b.v[j + 1]));
+      r.v[j] = t.x;
+      r.v[j + 1] = t.y;
+    }
+  }
+  return r;
+}
+template <typename T, int V>
+__device__ __forceinline__ Vec<V> unpack(const Pack<T, V>& a) {
+  Vec<V> r;
+#pragma unroll
+  for (int j = 0; j < V; ++j) r.v[j] = to_f32(a.v[j]);
+  return r;
+}
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> pack(const Vec<V>& a) {
+  Pack<T, V> r;
+#pragma unroll
+  for (int j = 0; j < V; ++j) r.v[j] = from_f32<T>(a.v[j]);
+  return r;
+}
+
+// max(a, b), NaN when either is one
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// 1 / x by the hardware: 0 for an infinite x
+__device__ __forceinline__ float rcp_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// 2^x by the hardware
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+__device__ __forceinline__ float weight_of(const Gn& p, int c) {
+  return p.weight ? load_as_f32(p.weight, p.param_dtype, c) : 1.f;
+}
+__device__ __forceinline__ float bias_of(const Gn& p, int c) {
+  return p.bias ? load_as_f32(p.bias, p.param_dtype, c) : 0.f;
+}
+
+// Sum over groups of neighbouring lanes (a power of two of them), the same in all of them.
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+  for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  return v;
+}
+
+// 1 / (1 + exp(-z)) with the hardware's exponential and reciprocal, each within 2 units in the
+// last place; 0 where exp(-z) overflows.
+template <int V>
+__device__ __forceinline__ Vec<V> sigmoid_of(const Vec<V>& z) {
+  Vec<V> t = z * fill<V>(-1.44269504f);
+#pragma unroll
+  for (int j = 0; j < V; ++j) t.v[j] = exp2_fast(t.v[j]);
+  t = t + fill<V>(1.f);
+#pragma unroll
+  for (int j = 0; j < V; ++j) t.v[j] = rcp_fast(t.v[j]);
+  return t;
+}
+// act(z) and act'(z)
+template <int ACT, int V>
+__device__ __forceinline__ Vec<V> act_of(Vec<V> z) {
+  if (ACT == EFCP_ACT_RELU) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) z.v[j] = max_nan(z.v[j], 0.f);
+  }
+  if (ACT == EFCP_ACT_SILU) z = z * sigmoid_of(z);
+  return z;
+}
+template <int ACT, int V>
+__device__ __forceinline__ Vec<V> act_grad(const Vec<V>& z) {
+  if (ACT == EFCP_ACT_RELU) {
+    Vec<V> r;
+#pragma unroll
+    for (int j = 0; j < V; ++j) r.v[j] = z.v[j] <= 0.f ? 0.f : 1.f;
+    return r;
+  }
+  if (ACT == EFCP_ACT_SILU) {
+    const Vec<V> s = sigmoid_of(z);
+    return s * fma(z, fma(s, fill<V>(-1.f), fill<V>(1.f)), fill<V>(1.f));
+  }
+  return fill<V>(1.f);
+}
+
+// ------------------------------------------------------------------ sums inside a block
+// Sums a thread's N values over the rows side by side, as far as a warp reaches, and stores
+// them in val: p.val_rows rows of p.cols * N values.  Threads that are not `on` bring zeros.
+// The caller synchronises.
+template <int N>
+__device__ __forceinline__ void sum_rows(const Gn& p, const Item& it, const float* v, float* val) {
+  float s[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) s[j] = v[j];
+  if (p.pitch_log < 0) {
+    if (it.ty < p.lanes_rows) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) val[(it.ty * p.cols + it.tx) * N + j] = s[j];
+    }
+    return;
+  }
+  for (int o = 1 << p.pitch_log; o < 32; o *= 2) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) s[j] += __shfl_xor_sync(0xFFFFFFFFu, s[j], o);
+  }
+  const int warp = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31;
+  if (lane < p.cols) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) val[(warp * p.cols + lane) * N + j] = s[j];
+  }
+}
+
+// Mean and sum of squared deviations of `cnt` values per channel, the mean as k + m: k is one of
+// the values, so that a mean far from zero does not round away the deviations.  Parts are joined by
+//     mean = sum n_i mean_i / sum n_i,   M2 = sum M2_i + n_i (mean_i - mean)^2,
+// sums without cancellation whatever the data.
+template <int V>
+struct Stats {
+  Vec<V> k, m, q;
+  float cnt;
+};
+
+// From the sums of d = x - k and of d^2 over n rows, k being the first of the values.  Since k is one
+// of them, (k - mean)^2 is at most their sum of squared deviations, and what the subtraction of
+// n (k - mean)^2 loses stays below n 2^-24 of the result, n <= 64.
+template <int V>
+__device__ __forceinline__ Stats<V> stats_of(int n, const Vec<V>& k, const Vec<V>& s1,
+                                             const Vec<V>& s2) {
+  Stats<V> s;
+  s.cnt = float(n);
+  s.k = k;
+  s.m = s1 * fill<V>(n ? rcp_fast(s.cnt) : 0.f);
+#pragma unroll
+  for (int j = 0; j < V; ++j) s.q.v[j] = fmaxf(0.f, fmaf(-s.m.v[j], s1.v[j], s2.v[j]));
+  return s;
+}
+
+// Neighbouring channels of one group joined.
+template <int V>
+__device__ __forceinline__ Stats<V / 2> fold_once(const Stats<V>& s) {
+  Stats<V / 2> r;
+  r.cnt = 2.f * s.cnt;
+#pragma unroll
+  for (int j = 0; j < V / 2; ++j) {
+    const float d = (s.k.v[2 * j + 1] - s.k.v[2 * j]) + (s.m.v[2 * j + 1] - s.m.v[2 * j]);
+    r.k.v[j] = s.k.v[2 * j];
+    r.m.v[j] = fmaf(0.5f, d, s.m.v[2 * j]);
+    r.q.v[j] = fmaf(0.5f * s.cnt * d, d, s.q.v[2 * j] + s.q.v[2 * j + 1]);
+  }
+  return r;
+}
+
+// Joins the rows side by side as far as a warp reaches and stores what results in shared memory: four
+// sets (k, m, q and the counts) of p.val_rows rows of p.folded_cols values.
+template <int V>
+__device__ __forceinline__ void store_stats(const Gn& p, const Item& it, Stats<V> s, float* val) {
+  int row = it.ty, col = it.tx;
+  bool store = it.ty < p.lanes_rows;
+  if (p.pitch_log >= 0) {
+    const int lane = int(threadIdx.x) & 31, first = lane & ((1 << p.pitch_log) - 1);
+    row = int(threadIdx.x) >> 5;
+    store = lane < p.cols;
+    // the rows of a warp ascend: where its first has no values, none has
+    float all = s.cnt;
+    for (int o = 1 << p.pitch_log; o < 32; o *= 2) all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
+    const float inv = all > 0.f ? rcp_fast(all) : 0.f;
+    Vec<V> sum;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float k0 = __shfl_sync(0xFFFFFFFFu, s.k.v[j], first);
+      s.m.v[j] = s.cnt > 0.f ? (s.k.v[j] - k0) + s.m.v[j] : 0.f;
+      s.k.v[j] = k0;
+      sum.v[j] = s.cnt * s.m.v[j];
+    }
+    for (int o = 1 << p.pitch_log; o < 32; o *= 2) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum.v[j] += __shfl_xor_sync(0xFFFFFFFFu, sum.v[j], o);
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      sum.v[j] *= inv;
+      const float d = s.m.v[j] - sum.v[j];
+      s.q.v[j] = fmaf(s.cnt * d, d, s.q.v[j]);
+      s.m.v[j] = sum.v[j];
+    }
+    for (int o = 1 << p.pitch_log; o < 32; o *= 2) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) s.q.v[j] += __shfl_xor_sync(0xFFFFFFFFu, s.q.v[j], o);
+    }
+    s.cnt = all;
+  }
+  if (store) {
+    float* at = val + row * p.folded_cols + col * V;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      at[j] = s.k.v[j];
+      at[p.val_floats + j] = s.m.v[j];
+      at[2 * p.val_floats + j] = s.q.v[j];
+      at[3 * p.val_floats + j] = s.cnt;
+    }
+  }
+}
+template <int V>
+__device__ __forceinline__ void fold_stats(const Gn& p, const Item& it, const Stats<V>& s,
+                                           int fold, float* val) {
+  if constexpr (V == 1) {
+    store_stats(p, it, s, val);
+  } else {
+    if (fold == 1) store_stats(p, it, s, val);
+    else fold_stats(p, it, fold_once(s), fold >> 1, val);
+  }
+}
+
+// The statistics of group g over the block, from what store_stats left (the caller has
+// synchronised): the same in all of the group's lanes.  `rows`: of the block.
+__device__ __forceinline__ Stats<1> group_stats(const Gn& p, int g, bool exists, float rows,
+                                                const float* val) {
+  const int lanes = 1 << p.lanes_log, lane = int(threadIdx.x) & (lanes - 1);
+  const int per = p.folded_per, used = p.folded_cols;
+  // lanes over a row's values, or over the rows
+  const bool along = per >= lanes;
+  const int d0 = along ? lane : 0, dstep = along ? lanes : 1;
+  const int t0 = along ? 0 : lane, tstep = along ? 1 : lanes;
+  const float* k = val + g * per;
+  const float *m = k + p.val_floats, *q = m + p.val_floats, *n = q + p.val_floats;
+  Stats<1> s;
+  s.cnt = rows * float(p.per);
+  s.k.v[0] = exists ? k[0] : 0.f;
+  float sum = 0.f;
+  if (exists) {
+    for (int t = t0; t < p.val_rows; t += tstep)
+      for (int d = d0; d < per; d += dstep)
+        sum = fmaf(n[t * used + d], (k[t * used + d] - s.k.v[0]) + m[t * used + d], sum);
+  }
+  const float mean = rows > 0.f ? lanes_sum(sum, lanes) / s.cnt : lanes_sum(0.f, lanes);
+  sum = 0.f;
+  if (exists) {
+    for (int t = t0; t < p.val_rows; t += tstep) {
+      for (int d = d0; d < per; d += dstep) {
+        const float e = ((k[t * used + d] - s.k.v[0]) + m[t * used + d]) - mean;
+        sum += fmaf(n[t * used + d] * e, e, q[t * used + d]);
+      }
+    }
+  }
+  s.m.v[0] = mean;
+  s.q.v[0] = lanes_sum(sum, lanes);
+  return s;
+}
+
+// The group of lane j of an access at column tx, counted from the tile's first: one division.
+struct GroupWalk {
+  int g, left;  // group; channels left in it, this one included
+  __device__ __forceinline__ GroupWalk(int c, int per) : g(c / per), left(per - c % per) {}
+  __device__ __forceinline__ void next(int per) {
+    if (--left == 0) {
+      ++g;
+      left = per;
+    }
+  }
+};
+
+// Per-group values of the channels of an access at channel c of the tile.
+template <int V>
+__device__ __forceinline__ Vec<V> of_groups(const float* values, int c, int per) {
+  Vec<V> r;
+  GroupWalk w(c, per);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    r.v[j] = values[w.g];
+    w.next(per);
+  }
+  return r;
+}
+// Values of V channels from a 16-byte aligned array in shared memory, c a multiple of V.
+template <int V>
+__device__ __forceinline__ Vec<V> of_channels(const float* values, int c) {
+  constexpr int Q = V < 4 ? V : 4;
+  Vec<V> r;
+#pragma unroll
+  for (int h = 0; h < V; h += Q) {
+    const Pack<float, Q> q = *reinterpret_cast<const Pack<float, Q>*>(values + c + h);
+#pragma unroll
+    for (int j = 0; j < Q; ++j) r.v[h + j] = q.v[j];
+  }
+  return r;
+}
+template <int V>
+__device__ __forceinline__ Vec<V> minus(Vec<V> a) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) a.v[j] = -a.v[j];
+  return a;
+}
+
+// The place of a block in its cluster, and of the cluster in the grid.
+__device__ __forceinline__ unsigned cluster_rank() {
+  unsigned r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ unsigned cluster_index() {
+  unsigned r;
+  asm("mov.u32 %0, %%clusterid.x;" : "=r"(r));
+  return r;
+}
+// The cluster's barrier where nothing is handed over: a block that has read the others' sums
+// arrives, and waits before it ends, since its own may still be read.
+__device__ __forceinline__ void leave_arrive() {
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void leave_wait() {
+  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+}
+
+// This thread's number of rows of the item.
+__device__ __forceinline__ int rows_of_thread(const Gn& p, const Item& it) {
+  const int rows = int(it.r1 - it.r0) - it.ty;
+  if (!it.on || rows <= 0) return 0;
+  if (p.pitch_log >= 0) return (rows + p.lanes_rows - 1) >> p.lanes_rows_log;
+  return (rows + p.lanes_rows - 1) / p.lanes_rows;
+}
+
+// ------------------------------------------------------------------ resident: shared memory
+// Copies one access from global to shared memory without passing through registers, where the
+// hardware has a copy of that size (4, 8, 16 bytes).
+template <typename T, int V>
+__device__ __forceinline__ void copy_in(void* dst, const T* src) {
+  if constexpr (sizeof(T) * V == 2) {
+    *static_cast<unsigned short*>(dst) = __ldg(reinterpret_cast<const unsigned short*>(src));
+  } else {
+    const unsigned d = static_cast<unsigned>(__cvta_generic_to_shared(dst));
+    if constexpr (sizeof(T) * V == 16)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+    else
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(d), "l"(src) : "memory");
+  }
+}
+// Waits for this thread's copies.  (Every thread reads only what it has copied itself.)
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// ------------------------------------------------------------------ resident, forward
+// The channels of group g get minus the mean and rstd times the weight; `lane` of `lanes` threads.
+__device__ __forceinline__ void finish_group(const Gn& p, const Item& it, int g, float mean,
+                                             float m2, float* cmean, float* wei, int lane,
+                                             int lanes) {
+  const float rstd = rsqrtf(m2 * p.inv_total + p.eps);
+  for (int k = g * p.per + lane; k < (g + 1) * p.per; k += lanes) {
+    cmean[k] = -mean;
+    wei[k] *= rstd;
+  }
+  if (it.chunk == 0 && lane == 0) {
+    p.mean[it.n * p.groups + it.g0 + g] = mean;
+    p.rstd[it.n * p.groups + it.g0 + g] = rstd;
+  }
+}
+
+template <typename T, int V, int ACT, int TH>
+__global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_fwd(const Gn p) {
+  extern __shared__ __align__(32) float sm[];
+  const int wide = (p.tile_groups * p.per + 3) & ~3, tg = (p.tile_groups + 3) & ~3;
+  float* val = sm;
+  float* cmean = val + 4 * p.val_floats;  // per channel: minus the mean,
+  float* wei = cmean + wide;              // the weight, later times rstd,
+  float* bia = wei + wide;                // the bias
+  float* bk = bia + wide;                 // per group the block's statistics, read by the others
+  float* bm = bk + tg;
+  float* bq = bm + tg;
+  // [row of this thread] [thread] of V elements
+  Pack<T, V>* data = reinterpret_cast<Pack<T, V>*>(bq + tg) + int(threadIdx.x);
+  const Item it = item_of<V>(p, cluster_rank(), cluster_index());
+  const int mine = rows_of_thread(p, it);
+  const int c = it.tx * V;
+  {
+    const T* px = static_cast<const T*>(p.x) + it.n * p.x_batch + it.c0 +
+                  (it.r0 + it.ty) * p.x_row + c;
+    const long long step = p.lanes_rows * p.x_row;
+#pragma unroll 4
+    for (int k = 0; k < mine; ++k, px += step) copy_in<T, V>(data + k * TH, px);
+  }
+  for (int k = threadIdx.x; k < it.width; k += TH) {
+    wei[k] = weight_of(p, it.c0 + k);
+    bia[k] = bias_of(p, it.c0 + k);
+  }
+  copies_done();
+  {
+    Vec<V> k0 = fill<V>(0.f), s1 = k0, s2 = k0;
+    if (mine) {
+      k0 = unpack(data[0]);
+      const Vec<V> neg = minus(k0);
+#pragma unroll 4
+      for (int k = 1; k < mine; ++k) {
+        const Vec<V> d = unpack(data[k * TH]) + neg;
+        s1 = s1 + d;
+        s2 = fma(d, d, s2);
+      }
+    }
+    fold_stats(p, it, stats_of(mine, k0, s1, s2), p.fold, val);
+  }
+  __syncthreads();
+  cg::cluster_group cluster = cg::this_cluster();
+  const float rows = float(max(0, int(it.r1 - it.r0)));
+  const int lanes = 1 << p.lanes_log, lane = int(threadIdx.x) & (lanes - 1);
+  for (int g0 = 0; g0 < it.ng; g0 += TH >> p.lanes_log) {
+    const int g = g0 + (int(threadIdx.x) >> p.lanes_log);
+    const Stats<1> s = group_stats(p, g, g < it.ng, rows, val);
+    if (g < it.ng) {
+      if (p.chunks == 1) {
+        finish_group(p, it, g, s.k.v[0] + s.m.v[0], s.q.v[0], cmean, wei, lane, lanes);
+      } else if (lane == 0) {
+        bk[g] = s.k.v[0];
+        bm[g] = s.m.v[0];
+        bq[g] = s.q.v[0];
+      }
+    }
+  }
+  if (p.chunks > 1) {
+    cluster.sync();
+    // a group's blocks are joined by neighbouring lanes, one each
+    const int links = 1 << p.links_log, r = int(threadIdx.x) & (links - 1);
+    const float have =
+        float(max(0, min(int(p.chunk_rows), int(p.rows) - r * int(p.chunk_rows))));
+    for (int g0 = 0; g0 < it.ng; g0 += TH >> p.links_log) {
+      const int g = g0 + (int(threadIdx.x) >> p.links_log);
+      float k = 0.f, m = 0.f, q = 0.f;
+      const bool there = g < it.ng && r < p.chunks && have > 0.f;
+      if (there) {
+        k = cluster.map_shared_rank(bk, r)[g];
+        m = cluster.map_shared_rank(bm, r)[g];
+        q = cluster.map_shared_rank(bq, r)[g];
+      }
+      const float k0 = __shfl_sync(0xFFFFFFFFu, k, int(threadIdx.x) & 31 & ~(links - 1));
+      m = there ? (k - k0) + m : 0.f;
+      const float mean = lanes_sum(have * m, links) * p.inv_rows;
+      const float d = m - mean;
+      q = lanes_sum(there ? fmaf(have * float(p.per) * d, d, q) : 0.f, links);
+      if (g < it.ng) finish_group(p, it, g, k0 + mean, q, cmean, wei, r, links);
+    }
+  }
+  __syncthreads();
+  if (p.chunks > 1) leave_arrive();
+  if (mine) {
+    const Vec<V> m = of_channels<V>(cmean, c), f = of_channels<V>(wei, c);
+    const Vec<V> b = of_channels<V>(bia, c);
+    T* py = static_cast<T*>(p.y) + it.n * p.y_batch + it.c0 + (it.r0 + it.ty) * p.y_row + c;
+    const long long step = p.lanes_rows * p.y_row;
+#pragma unroll 4
+    for (int k = 0; k < mine; ++k, py += step)
+      *reinterpret_cast<Pack<T, V>*>(py) =
+          pack<T, V>(act_of<ACT>(fma(unpack(data[k * TH]) + m, f, b)));
+  }
+  if (p.chunks > 1) leave_wait();
+}
+
+// ------------------------------------------------------------------ resident, backward
+// A thread's V fp32 values in shared memory: 16 bytes of neighbouring threads side by side, so
+// that a warp's access is free of bank conflicts.  The slot holds dy's access before.
+template <int V, int TH>
+struct Slot {
+  static constexpr int Q = V < 4 ? V : 4;
+  static constexpr int kFloats = TH * V;  // per row of this thread
+  static __device__ __forceinline__ float* at(float* base) { return base + int(threadIdx.x) * Q; }
+  static __device__ __forceinline__ void put(float* s, const Vec<V>& v) {
+#pragma unroll
+    for (int h = 0; h < V / Q; ++h) {
+      Pack<float, Q> q;
+#pragma unroll
+      for (int j = 0; j < Q; ++j) q.v[j] = v.v[h * Q + j];
+      *reinterpret_cast<Pack<float, Q>*>(s + h * TH * Q) = q;
+    }
+  }
+  static __device__ __forceinline__ Vec<V> get(const float* s) {
+    Vec<V> v;
+#pragma unroll
+    for (int h = 0; h < V / Q; ++h) {
+      const Pack<float, Q> q = *reinterpret_cast<const Pack<float, Q>*>(s + h * TH * Q);
+#pragma unroll
+      for (int j = 0; j < Q; ++j) v.v[h * Q + j] = q.v[j];
+    }
+    return v;
+  }
+};
+
+// Per channel P = sum e h and Q = sum e over the block's rows, from them the group's sums of
+// e w h and e w over the cluster, then dx = rstd (e w - mean(e w) - h mean(e w h)).  The channels'
+// sums of the whole sample go to `part` for dweight and dbias.
+//
+// silu's derivative takes two of the hardware's special functions per element, of which an SM has
+// 16 lanes: computed in both passes they alone would take as long as the memory.  The first
+// pass leaves e in shared memory (fp32, in place of dy) for the second.
+template <typename T, int V, int ACT, int TH>
+__global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_bwd(const Gn p) {
+  constexpr bool kStash = ACT == EFCP_ACT_SILU;
+  using S = Slot<V, TH>;
+  using P = Pack<T, V>;
+  extern __shared__ __align__(32) float sm[];
+  const int wide = (p.tile_groups * p.per + 3) & ~3, tg = (p.tile_groups + 3) & ~3;
+  float* val0 = sm;
+  float* val1 = val0 + p.val_floats;
+  float* wei = val1 + p.val_floats;  // per channel: weight,
+  float* bia = wei + wide;     // bias,
+  float* cm = bia + wide;      // minus the mean,
+  float* cr = cm + wide;       // rstd,
+  float* tot0 = cr + wide;     // P and Q of this block,
+  float* tot1 = tot0 + wide;
+  float* cqb = tot1 + wide;    // and minus rstd times the group's means of e w h and of e w
+  float* cqa = cqb + wide;
+  float* gb = cqa + wide;      // per group: sums of e w h and of e w of this block
+  float* ga = gb + tg;
+  float* data = ga + tg;
+  const Item it = item_of<V>(p, cluster_rank(), cluster_index());
+  const int mine = rows_of_thread(p, it);
+  const int most = p.thread_rows;  // rows a thread of this launch has room for
+  // x: [row of this thread] [thread]; then dy the same way, or in the slots that take e
+  P* dx_ = reinterpret_cast<P*>(data) + int(threadIdx.x);
+  float* rest = data + size_t(most) * (TH * V * sizeof(T) / 4);
+  float* slot = S::at(rest);
+  P* dd = reinterpret_cast<P*>(rest) + int(threadIdx.x);
+  const long long row = it.r0 + it.ty;
+  const int c = it.tx * V, at = it.c0 + c;
+  {
+    const T* px = static_cast<const T*>(p.x) + it.n * p.x_batch + row * p.x_row + at;
+    const T* pd = static_cast<const T*>(p.dy) + it.n * p.dy_batch + row * p.dy_row + at;
+    const long long xstep = p.lanes_rows * p.x_row, dstep = p.lanes_rows * p.dy_row;
+#pragma unroll 4
+    for (int k = 0; k < mine; ++k, px += xstep, pd += dstep) {
+      copy_in<T, V>(dx_ + k * TH, px);
+      copy_in<T, V>(kStash ? static_cast<void*>(slot + k * S::kFloats)
+                           : static_cast<void*>(dd + k * TH),
+                    pd);
+    }
+  }
+  for (int k = threadIdx.x; k < it.width; k += TH) {
+    const long long g = it.n * p.groups + it.g0 + k / p.per;
+    wei[k] = weight_of(p, it.c0 + k);
+    bia[k] = bias_of(p, it.c0 + k);
+    cm[k] = -p.mean[g];
+    cr[k] = p.rstd[g];
+  }
+  __syncthreads();
+  copies_done();
+  Vec<V> s0 = fill<V>(0.f), s1 = s0;
+  if (mine) {
+    const Vec<V> m = of_channels<V>(cm, c), b = of_channels<V>(bia, c);
+    const Vec<V> f = of_channels<V>(cr, c) * of_channels<V>(wei, c);
+#pragma unroll 2
+    for (int k = 0; k < mine; ++k) {
+      const Vec<V> u = unpack(dx_[k * TH]) + m;
+      Vec<V> e = unpack(kStash ? *reinterpret_cast<const P*>(slot + k * S::kFloats) : dd[k * TH]);
+      if (ACT != EFCP_ACT_NONE) e = e * act_grad<ACT>(fma(u, f, b));
+      if (kStash) S::put(slot + k * S::kFloats, e);
+      s0 = fma(e, u, s0);
+      s1 = s1 + e;
+    }
+    s0 = s0 * of_channels<V>(cr, c);
+  }
+  sum_rows<V>(p, it, s0.v, val0);
+  sum_rows<V>(p, it, s1.v, val1);
+  __syncthreads();
+  cg::cluster_group cluster = cg::this_cluster();
+  const int used = p.cols * V;
+  const bool grads = p.dweight || p.dbias;
+  float* part = p.part + it.n * 2 * p.channels + it.c0;
+  {
+    const int lanes = 1 << p.lanes_log, lane = int(threadIdx.x) & (lanes - 1);
+    const bool along = p.per >= lanes;  // lanes over a row's values, or over the rows
+    const int d0 = along ? lane : 0, dstep = along ? lanes : 1;
+    const int t0 = along ? 0 : lane, tstep = along ? 1 : lanes;
+    for (int g0 = 0; g0 < it.ng; g0 += TH >> p.lanes_log) {
+      const int g = g0 + (int(threadIdx.x) >> p.lanes_log);
+      float sb = 0.f, sa = 0.f;
+      if (g < it.ng) {
+        for (int d = g * p.per + d0; d < (g + 1) * p.per; d += dstep) {
+          float t1 = 0.f, t2 = 0.f;
+          for (int t = t0; t < p.val_rows; t += tstep) {
+            t1 += val0[t * used + d];
+            t2 += val1[t * used + d];
+          }
+          sb = fmaf(wei[d], t1, sb);
+          sa = fmaf(wei[d], t2, sa);
+        }
+      }
+      sb = lanes_sum(sb, lanes);
+      sa = lanes_sum(sa, lanes);
+      if (g < it.ng) {
+        if (p.chunks == 1) {
+          for (int k = g * p.per + lane; k < (g + 1) * p.per; k += lanes) {
+            cqb[k] = -cr[k] * (sb * p.inv_total);
+            cqa[k] = -cr[k] * (sa * p.inv_total);
+          }
+        } else if (lane == 0) {
+          gb[g] = sb;
+          ga[g] = sa;
+        }
+      }
+    }
+  }
+  if (grads) {
+    // (from the far end: the first threads have the groups' sums to form)
+    for (int k = TH - 1 - int(threadIdx.x); k < it.width; k += TH) {
+      float t0 = 0.f, t1 = 0.f;
+#pragma unroll 4
+      for (int t = 0; t < p.val_rows; ++t) {
+        t0 += val0[t * used + k];
+        t1 += val1[t * used + k];
+      }
+      if (p.chunks == 1) {
+        part[k] = t0;
+        part[p.channels + k] = t1;
+      } else {
+        tot0[k] = t0;
+        tot1[k] = t1;
+      }
+    }
+  }
+  if (p.chunks > 1) {
+    cluster.sync();
+    // a group's blocks are joined by neighbouring lanes, one each
+    const int links = 1 << p.links_log, r = int(threadIdx.x) & (links - 1);
+    for (int g0 = 0; g0 < it.ng; g0 += TH >> p.links_log) {
+      const int g = g0 + (int(threadIdx.x) >> p.links_log);
+      float sb = 0.f, sa = 0.f;
+      if (g < it.ng && r < p.chunks) {
+        sb = cluster.map_shared_rank(gb, r)[g];
+        sa = cluster.map_shared_rank(ga, r)[g];
+      }
+      sb = lanes_sum(sb, links) * p.inv_total;
+      sa = lanes_sum(sa, links) * p.inv_total;
+      if (g < it.ng) {
+        for (int k = g * p.per + r; k < (g + 1) * p.per; k += links) {
+          cqb[k] = -cr[k] * sb;
+          cqa[k] = -cr[k] * sa;
+        }
+      }
+    }
+    if (grads) {  // each block of the cluster joins its share of the channels
+      const int share = (it.width + p.chunks - 1) / p.chunks;
+      const int c1 = min(it.width, (it.chunk + 1) * share);
+      for (int k = it.chunk * share + TH - 1 - int(threadIdx.x); k < c1; k += TH) {
+        float t0 = 0.f, t1 = 0.f;
+#pragma unroll 4
+        for (int q = 0; q < p.chunks; ++q) {
+          t0 += cluster.map_shared_rank(tot0, q)[k];
+          t1 += cluster.map_shared_rank(tot1, q)[k];
+        }
+        part[k] = t0;
+        part[p.channels + k] = t1;
+      }
+    }
+  }
+  __syncthreads();
+  if (p.chunks > 1) leave_arrive();
+  if (mine) {
+    const Vec<V> m = of_channels<V>(cm, c), rs = of_channels<V>(cr, c);
+    const Vec<V> f = rs * of_channels<V>(wei, c), b = of_channels<V>(bia, c);
+    const Vec<V> qa = of_channels<V>(cqa, c), qb = of_channels<V>(cqb, c);
+    T* po = static_cast<T*>(p.y) + it.n * p.y_batch + row * p.y_row + at;
+    const long long step = p.lanes_rows * p.y_row;
+#pragma unroll 2
+    for (int k = 0; k < mine; ++k, po += step) {
+      const Vec<V> u = unpack(dx_[k * TH]) + m;
+      Vec<V> e;
+      if (kStash) {
+        e = S::get(slot + k * S::kFloats);
+      } else {
+        e = unpack(dd[k * TH]);
+        if (ACT != EFCP_ACT_NONE) e = e * act_grad<ACT>(fma(u, f, b));
+      }
+      *reinterpret_cast<P*>(po) = pack<T, V>(fma(u * rs, qb, fma(e, f, qa)));
+    }
+  }
+  if (p.chunks > 1) leave_wait();
+}
+
+// ------------------------------------------------------------------ streamed
+// Accesses in flight per thread and input: about 32 registers' worth.
+template <typename T, int V>
+constexpr int kAhead = sizeof(T) * V == 16 ? 4 : 8;
+
+// The statistics of every group over a chunk of rows: k, m and q one after another.
+template <typename T, int V>
+__global__ void __launch_bounds__(kGnThreads, 3) k_gn_stats(const Gn p) {
+  constexpr int U = kAhead<T, V>;
+  extern __shared__ __align__(32) float sm[];
+  float* val = sm;
+  const Item it = item_of<V>(p, blockIdx.x % unsigned(p.chunks), blockIdx.x / unsigned(p.chunks));
+  const T* x = static_cast<const T*>(p.x) + it.n * p.x_batch + it.c0;
+  Vec<V> k0 = fill<V>(0.f), s1 = k0, s2 = k0, neg = k0;
+  int n = 0;
+  if (it.on) {
+    // (more than one round only where a single group is wider than the block)
+    for (int c = it.tx; c < it.width / V; c += p.cols) {
+      for (long long r = it.r0 + it.ty; r < it.r1; r += U * p.lanes_rows) {
+        Pack<T, V> a[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const long long rr = r + (long long)u * p.lanes_rows;
+          if (rr < it.r1) a[u] = load_pack<T, V>(x + rr * p.x_row + (long long)c * V);
+        }
+        if (!n) {
+          k0 = unpack(a[0]);
+          neg = minus(k0);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (r + (long long)u * p.lanes_rows < it.r1) {
+            const Vec<V> d = unpack(a[u]) + neg;
+            ++n;
+            s1 = s1 + d;
+            s2 = fma(d, d, s2);
+          }
+        }
+      }
+    }
+  }
+  Stats<V> st = stats_of(n, k0, s1, s2);
+  fold_stats(p, it, st, p.fold, val);
+  __syncthreads();
+  float* part = p.part + ((it.n * p.chunks + it.chunk) * p.groups + it.g0) * 3;
+  for (int g0 = 0; g0 < it.ng; g0 += kGnThreads >> p.lanes_log) {
+    const int g = g0 + (int(threadIdx.x) >> p.lanes_log);
+    const Stats<1> s = group_stats(p, g, g < it.ng, float(it.r1 - it.r0), val);
+    if (g < it.ng && (int(threadIdx.x) & ((1 << p.lanes_log) - 1)) == 0) {
+      part[3 * g] = s.k.v[0];
+      part[3 * g + 1] = s.m.v[0];
+      part[3 * g + 2] = s.q.v[0];
+    }
+  }
+}
+
+// mean and rstd of every sample and group from the chunks' statistics: a warp each
+__global__ void __launch_bounds__(kGnThreads) k_gn_join_stats(const Gn p) {
+  const long long i = (long long)blockIdx.x * (kGnThreads / 32) + (threadIdx.x >> 5);
+  if (i >= p.n * p.groups) return;
+  const int lane = threadIdx.x & 31;
+  const long long n = i / p.groups;
+  const int g = int(i - n * p.groups);
+  const float* part = p.part + (n * p.chunks * p.groups + g) * 3;
+  const long long pitch = 3ll * p.groups;
+  const float k0 = part[0];
+  float s = 0.f;
+  for (int c = lane; c < p.chunks; c += 32) {
+    const float have = float(min(p.chunk_rows, p.rows - c * p.chunk_rows));
+    s = fmaf(have, (part[c * pitch] - k0) + part[c * pitch + 1], s);
+  }
+  const float mean = lanes_sum(s, 32) / float(p.rows);
+  float m2 = 0.f;
+  for (int c = lane; c < p.chunks; c += 32) {
+    const float have = float(min(p.chunk_rows, p.rows - c * p.chunk_rows)) * float(p.per);
+    const float d = ((part[c * pitch] - k0) + part[c * pitch + 1]) - mean;
+    m2 += fmaf(have * d, d, part[c * pitch + 2]);
+  }
+  m2 = lanes_sum(m2, 32);
+  if (lane == 0) {
+    p.mean[i] = k0 + mean;
+    p.rstd[i] = rsqrtf(m2 / (float(p.rows) * float(p.per)) + p.eps);
+  }
+}
+
+// V parameters from channel c on; the type is looked at once.
+template <int V>
+__device__ __forceinline__ Vec<V> params_at(const void* q, int dtype, int c, float absent) {
+  Vec<V> r = fill<V>(absent);
+  if (!q) return r;
+  if (dtype == EFCP_F32) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) r.v[j] = static_cast<const float*>(q)[c + j];
+  } else if (dtype == EFCP_BF16) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) r.v[j] = to_f32(static_cast<const __nv_bfloat16*>(q)[c + j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) r.v[j] = to_f32(static_cast<const __half*>(q)[c + j]);
+  }
+  return r;
+}
+
+// A thread's channel constants.
+template <int V>
+struct Lane {
+  Vec<V> m, r, f, b;  // -mean, rstd, rstd weight, bias
+  __device__ __forceinline__ void load(const Gn& p, const Item& it, int col) {
+    const long long g = it.n * p.groups + it.g0;
+    m = of_groups<V>(p.mean + g, col * V, p.per);
+    r = of_groups<V>(p.rstd + g, col * V, p.per);
+#pragma unroll
+    for (int j = 0; j < V; ++j) m.v[j] = -m.v[j];
+    f = r * params_at<V>(p.weight, p.param_dtype, it.c0 + col * V, 1.f);
+    b = params_at<V>(p.bias, p.param_dtype, it.c0 + col * V, 0.f);
+  }
+};
+
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kGnThreads, 3) k_gn_apply(const Gn p) {
+  constexpr int U = kAhead<T, V>;
+  const Item it = item_of<V>(p, blockIdx.x % unsigned(p.chunks), blockIdx.x / unsigned(p.chunks));
+  if (!it.on) return;
+  const T* x = static_cast<const T*>(p.x) + it.n * p.x_batch + it.c0;
+  T* y = static_cast<T*>(p.y) + it.n * p.y_batch + it.c0;
+  for (int c = it.tx; c < it.width / V; c += p.cols) {
+    Lane<V> ln;
+    ln.load(p, it, c);
+    for (long long r = it.r0 + it.ty; r < it.r1; r += U * p.lanes_rows) {
+      Pack<T, V> a[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const long long rr = r + (long long)u * p.lanes_rows;
+        if (rr < it.r1) a[u] = load_pack<T, V>(x + rr * p.x_row + (long long)c * V);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const long long rr = r + (long long)u * p.lanes_rows;
+        if (rr < it.r1)
+          *reinterpret_cast<Pack<T, V>*>(y + rr * p.y_row + (long long)c * V) =
+              pack<T, V>(act_of<ACT>(fma(unpack(a[u]) + ln.m, ln.f, ln.b)));
+      }
+    }
+  }
+}
+
+// Per channel and chunk of rows: sum e h, then sum e.
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kGnThreads, 2) k_gn_bwd_sums(const Gn p) {
+  constexpr int U = kAhead<T, V>;
+  extern __shared__ __align__(32) float sm[];
+  float* val0 = sm;
+  float* val1 = val0 + p.val_floats;
+  const Item it = item_of<V>(p, blockIdx.x % unsigned(p.chunks), blockIdx.x / unsigned(p.chunks));
+  const T* x = static_cast<const T*>(p.x) + it.n * p.x_batch + it.c0;
+  const T* dy = static_cast<const T*>(p.dy) + it.n * p.dy_batch + it.c0;
+  float* part = p.part + (it.n * p.chunks + it.chunk) * 2 * p.channels + it.c0;
+  // the same rounds for every thread: there is a barrier inside
+  for (int c0 = 0; c0 < it.width / V; c0 += p.cols) {
+    const int c = c0 + it.tx;
+    Vec<V> s0 = fill<V>(0.f), s1 = s0;
+    if (it.on && c < it.width / V) {
+      Lane<V> ln;
+      ln.load(p, it, c);
+      for (long long r = it.r0 + it.ty; r < it.r1; r += U * p.lanes_rows) {
+        Pack<T, V> a[U], d[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const long long rr = r + (long long)u * p.lanes_rows;
+          if (rr < it.r1) {
+            a[u] = load_pack<T, V>(x + rr * p.x_row + (long long)c * V);
+            d[u] = load_pack<T, V>(dy + rr * p.dy_row + (long long)c * V);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (r + (long long)u * p.lanes_rows < it.r1) {
+            const Vec<V> q = unpack(a[u]) + ln.m;
+            Vec<V> e = unpack(d[u]);
+            if (ACT != EFCP_ACT_NONE) e = e * act_grad<ACT>(fma(q, ln.f, ln.b));
+            s0 = fma(e, q, s0);
+            s1 = s1 + e;
+          }
+        }
+      }
+      s0 = s0 * ln.r;
+    }
+    sum_rows<V>(p, it, s0.v, val0);
+    sum_rows<V>(p, it, s1.v, val1);
+    __syncthreads();
+    const int used = p.cols * V;
+    for (int k = threadIdx.x; k < used && c0 * V + k < it.width; k += kGnThreads) {
+      float t0 = 0.f, t1 = 0.f;
+      for (int t = 0; t < p.val_rows; ++t) {
+        t0 += val0[t * used + k];
+        t1 += val1[t * used + k];
+      }
+      part[c0 * V + k] = t0;
+      part[p.channels + c0 * V + k] = t1;
+    }
+    __syncthreads();
+  }
+}
+
+// The group's means of e w and e w h from the chunks' channel sums: a warp per sample and group
+__global__ void __launch_bounds__(kGnThreads) k_gn_join_grads(const Gn p) {
+  const long long i = (long long)blockIdx.x * (kGnThreads / 32) + (threadIdx.x >> 5);
+  if (i >= p.n * p.groups) return;
+  const int lane = threadIdx.x & 31;
+  const long long n = i / p.groups;
+  const int c0 = int(i - n * p.groups) * p.per;
+  const float* part = p.part + n * p.chunks * 2 * p.channels;
+  float sb = 0.f, sa = 0.f;
+  if (p.per >= 32) {
+    for (int c = c0 + lane; c < c0 + p.per; c += 32) {
+      const float w = weight_of(p, c);
+      for (int k = 0; k < p.chunks; ++k) {
+        const float* q = part + 2ll * k * p.channels + c;
+        sb = fmaf(w, q[0], sb);
+        sa = fmaf(w, q[p.channels], sa);
+      }
+    }
+  } else {
+    for (int c = c0; c < c0 + p.per; ++c) {
+      const float w = weight_of(p, c);
+      for (int k = lane; k < p.chunks; k += 32) {
+        const float* q = part + 2ll * k * p.channels + c;
+        sb = fmaf(w, q[0], sb);
+        sa = fmaf(w, q[p.channels], sa);
+      }
+    }
+  }
+  sb = lanes_sum(sb, 32);
+  sa = lanes_sum(sa, 32);
+  if (lane == 0) {
+    const float total = float(p.rows) * float(p.per);
+    p.joint[2 * i] = sa / total;
+    p.joint[2 * i + 1] = sb / total;
+  }
+}
+
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kGnThreads, 2) k_gn_bwd_apply(const Gn p) {
+  constexpr int U = kAhead<T, V>;
+  const Item it = item_of<V>(p, blockIdx.x % unsigned(p.chunks), blockIdx.x / unsigned(p.chunks));
+  if (!it.on) return;
+  const T* x = static_cast<const T*>(p.x) + it.n * p.x_batch + it.c0;
+  const T* dy = static_cast<const T*>(p.dy) + it.n * p.dy_batch + it.c0;
+  T* dx = static_cast<T*>(p.y) + it.n * p.y_batch + it.c0;
+  const float* joint = p.joint + 2 * (it.n * p.groups + it.g0);
+  for (int c = it.tx; c < it.width / V; c += p.cols) {
+    Lane<V> ln;
+    ln.load(p, it, c);
+    Vec<V> qa, qb;
+    GroupWalk walk(c * V, p.per);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      qa.v[j] = -joint[2 * walk.g];
+      qb.v[j] = -joint[2 * walk.g + 1];
+      walk.next(p.per);
+    }
+    qa = qa * ln.r;
+    qb = qb * ln.r;
+    for (long long r = it.r0 + it.ty; r < it.r1; r += U * p.lanes_rows) {
+      Pack<T, V> a[U], d[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const long long rr = r + (long long)u * p.lanes_rows;
+        if (rr < it.r1) {
+          a[u] = load_pack<T, V>(x + rr * p.x_row + (long long)c * V);
+          d[u] = load_pack<T, V>(dy + rr * p.dy_row + (long long)c * V);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const long long rr = r + (long long)u * p.lanes_rows;
+        if (rr < it.r1) {
+          const Vec<V> q = unpack(a[u]) + ln.m;
+          Vec<V> e = unpack(d[u]);
+          if (ACT != EFCP_ACT_NONE) e = e * act_grad<ACT>(fma(q, ln.f, ln.b));
+          *reinterpret_cast<Pack<T, V>*>(dx + rr * p.y_row + (long long)c * V) =
+              pack<T, V>(fma(q * ln.r, qb, fma(e, ln.f, qa)));
+        }
+      }
+    }
+  }
+}
+
+// dweight and dbias: column sums over `rows` rows of channel sums, in fp64 and a fixed order.
+// 32 channels per block, the rows shared among its warps.
+constexpr int kGnSumWarps = 32;
+__global__ void __launch_bounds__(32 * kGnSumWarps)
+    k_gn_param_grads(const float* __restrict__ part, long long rows, int channels, int dtype,
+                     void* dweight, void* dbias) {
+  __shared__ double sh[2][kGnSumWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int c = int(blockIdx.x) * 32 + lane;
+  double s0 = 0.0, s1 = 0.0;
+  if (c < channels) {
+#pragma unroll 8
+    for (long long i = warp; i < rows; i += kGnSumWarps) {
+      s0 += double(part[i * 2 * channels + c]);
+      s1 += double(part[(i * 2 + 1) * channels + c]);
+    }
+  }
+  sh[0][warp][lane] = s0;
+  sh[1][warp][lane] = s1;
+  __syncthreads();
+  if (warp < 2 && c < channels) {
+    double s = 0.0;
+    for (int k = 0; k < kGnSumWarps; ++k) s += sh[warp][k][lane];
+    void* out = warp == 0 ? dweight : dbias;
+    if (out) store_from_f32(out, dtype, c, float(s));
+  }
+}
+
+// ------------------------------------------------------------------ launches
+// One cluster of p.chunks blocks per item.
+template <class Kernel>
+cudaError_t launch_cluster(Kernel kern, int threads, const Gn& p, const GnLaunch& l) {
+  if (p.chunks > 8) {
+    const cudaError_t e =
+        cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+  }
+  if (l.smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               int(l.smem));
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = unsigned(p.chunks);
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(l.blocks);
+  cfg.blockDim = dim3(unsigned(threads));
+  cfg.dynamicSmemBytes = l.smem;
+  cfg.stream = l.st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, p);
+}
+
+template <class Kernel>
+cudaError_t launch_streamed(Kernel kern, const Gn& p, const GnLaunch& l, size_t smem) {
+  if (smem > 48 * 1024) {
+    const cudaError_t e =
+        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    if (e != cudaSuccess) return e;
+  }
+  kern<<<l.blocks, kGnThreads, smem, l.st>>>(p);
+  return cudaGetLastError();
+}
+
+inline cudaError_t launch_params(const Gn& p, long long rows, cudaStream_t st) {
+  if (!p.dweight && !p.dbias) return cudaSuccess;
+  k_gn_param_grads<<<unsigned((p.channels + 31) / 32), 32 * kGnSumWarps, 0, st>>>(
+      p.part, rows, p.channels, p.param_dtype, p.dweight, p.dbias);
+  return cudaGetLastError();
+}
+
+template <typename T, int V, int ACT, int TH>
+cudaError_t launch_resident(const Gn& p, const GnLaunch& l) {
+  if (!l.backward) return launch_cluster(k_gn_resident_fwd<T, V, ACT, TH>, TH, p, l);
+  const cudaError_t e = launch_cluster(k_gn_resident_bwd<T, V, ACT, TH>, TH, p, l);
+  return e != cudaSuccess ? e : launch_params(p, p.n, l.st);
+}
+
+template <typename T, int V, int ACT>
+cudaError_t launch_act(const Gn& p, const GnLaunch& l) {
+  if (l.resident == 256) return launch_resident<T, V, ACT, 256>(p, l);
+  if (l.resident == 512) return launch_resident<T, V, ACT, 512>(p, l);
+  const size_t smem = gn_streamed_floats(p.val_floats, l.backward) * 4;
+  const unsigned joins = unsigned((p.n * p.groups + kGnThreads / 32 - 1) / (kGnThreads / 32));
+  cudaError_t e;
+  if (!l.backward) {
+    e = launch_streamed(k_gn_stats<T, V>, p, l, smem);
+    if (e != cudaSuccess) return e;
+    k_gn_join_stats<<<joins, kGnThreads, 0, l.st>>>(p);
+    return launch_streamed(k_gn_apply<T, V, ACT>, p, l, 0);
+  }
+  e = launch_streamed(k_gn_bwd_sums<T, V, ACT>, p, l, smem);
+  if (e != cudaSuccess) return e;
+  k_gn_join_grads<<<joins, kGnThreads, 0, l.st>>>(p);
+  e = launch_streamed(k_gn_bwd_apply<T, V, ACT>, p, l, 0);
+  return e != cudaSuccess ? e : launch_params(p, p.n * p.chunks, l.st);
+}
+
+template <typename T, int V>
+cudaError_t launch_vec(const Gn& p, const GnLaunch& l) {
+  if (l.act == EFCP_ACT_NONE) return launch_act<T, V, EFCP_ACT_NONE>(p, l);
+  if (l.act == EFCP_ACT_RELU) return launch_act<T, V, EFCP_ACT_RELU>(p, l);
+  return launch_act<T, V, EFCP_ACT_SILU>(p, l);
+}
+
+}  // namespace
+}  // namespace efcp
