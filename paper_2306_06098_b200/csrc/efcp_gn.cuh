@@ -6,9 +6,9 @@
 // input has to stay on the chip in between, or is read twice.
 //
 //   resident   A cluster of up to 16 thread blocks takes one sample's tile of channels and holds all
-//              of it in shared memory (about 200 KB per SM, in two to four blocks, so that some load
-//              while others compute); the blocks exchange their sums through each other's shared
-//              memory.  One read, one write.
+//              of it in shared memory (about 200 KB per SM in four blocks, so that some load while
+//              others compute); the blocks exchange their sums through each other's shared memory.
+//              One read, one write.
 //   streamed   For samples that do not fit: one pass for the sums of chunks of rows, a small
 //              kernel that joins them, one pass for the result.
 //
@@ -496,8 +496,8 @@ __device__ __forceinline__ void finish_group(const Gn& p, const Item& it, int g,
   }
 }
 
-template <typename T, int V, int ACT, int TH>
-__global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_fwd(const Gn p) {
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_fwd(const Gn p) {
   extern __shared__ __align__(32) float sm[];
   const int wide = (p.tile_groups * p.per + 3) & ~3, tg = (p.tile_groups + 3) & ~3;
   float* val = sm;
@@ -517,9 +517,9 @@ __global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_fwd(const Gn p) {
                   (it.r0 + it.ty) * p.x_row + c;
     const long long step = p.lanes_rows * p.x_row;
 #pragma unroll 4
-    for (int k = 0; k < mine; ++k, px += step) copy_in<T, V>(data + k * TH, px);
+    for (int k = 0; k < mine; ++k, px += step) copy_in<T, V>(data + k * kGnThreads, px);
   }
-  for (int k = threadIdx.x; k < it.width; k += TH) {
+  for (int k = threadIdx.x; k < it.width; k += kGnThreads) {
     wei[k] = weight_of(p, it.c0 + k);
     bia[k] = bias_of(p, it.c0 + k);
   }
@@ -531,7 +531,7 @@ __global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_fwd(const Gn p) {
       const Vec<V> neg = minus(k0);
 #pragma unroll 4
       for (int k = 1; k < mine; ++k) {
-        const Vec<V> d = unpack(data[k * TH]) + neg;
+        const Vec<V> d = unpack(data[k * kGnThreads]) + neg;
         s1 = s1 + d;
         s2 = fma(d, d, s2);
       }
@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_fwd(const Gn p) {
   cg::cluster_group cluster = cg::this_cluster();
   const float rows = float(max(0, int(it.r1 - it.r0)));
   const int lanes = 1 << p.lanes_log, lane = int(threadIdx.x) & (lanes - 1);
-  for (int g0 = 0; g0 < it.ng; g0 += TH >> p.lanes_log) {
+  for (int g0 = 0; g0 < it.ng; g0 += kGnThreads >> p.lanes_log) {
     const int g = g0 + (int(threadIdx.x) >> p.lanes_log);
     const Stats<1> s = group_stats(p, g, g < it.ng, rows, val);
     if (g < it.ng) {
@@ -561,7 +561,7 @@ __global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_fwd(const Gn p) {
     const int links = 1 << p.links_log, r = int(threadIdx.x) & (links - 1);
     const float have =
         float(max(0, min(int(p.chunk_rows), int(p.rows) - r * int(p.chunk_rows))));
-    for (int g0 = 0; g0 < it.ng; g0 += TH >> p.links_log) {
+    for (int g0 = 0; g0 < it.ng; g0 += kGnThreads >> p.links_log) {
       const int g = g0 + (int(threadIdx.x) >> p.links_log);
       float k = 0.f, m = 0.f, q = 0.f;
       const bool there = g < it.ng && r < p.chunks && have > 0.f;
@@ -588,51 +588,22 @@ __global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_fwd(const Gn p) {
 #pragma unroll 4
     for (int k = 0; k < mine; ++k, py += step)
       *reinterpret_cast<Pack<T, V>*>(py) =
-          pack<T, V>(act_of<ACT>(fma(unpack(data[k * TH]) + m, f, b)));
+          pack<T, V>(act_of<ACT>(fma(unpack(data[k * kGnThreads]) + m, f, b)));
   }
   if (p.chunks > 1) leave_wait();
 }
 
 // ------------------------------------------------------------------ resident, backward
-// A thread's V fp32 values in shared memory: 16 bytes of neighbouring threads side by side, so
-// that a warp's access is free of bank conflicts.  The slot holds dy's access before.
-template <int V, int TH>
-struct Slot {
-  static constexpr int Q = V < 4 ? V : 4;
-  static constexpr int kFloats = TH * V;  // per row of this thread
-  static __device__ __forceinline__ float* at(float* base) { return base + int(threadIdx.x) * Q; }
-  static __device__ __forceinline__ void put(float* s, const Vec<V>& v) {
-#pragma unroll
-    for (int h = 0; h < V / Q; ++h) {
-      Pack<float, Q> q;
-#pragma unroll
-      for (int j = 0; j < Q; ++j) q.v[j] = v.v[h * Q + j];
-      *reinterpret_cast<Pack<float, Q>*>(s + h * TH * Q) = q;
-    }
-  }
-  static __device__ __forceinline__ Vec<V> get(const float* s) {
-    Vec<V> v;
-#pragma unroll
-    for (int h = 0; h < V / Q; ++h) {
-      const Pack<float, Q> q = *reinterpret_cast<const Pack<float, Q>*>(s + h * TH * Q);
-#pragma unroll
-      for (int j = 0; j < Q; ++j) v.v[h * Q + j] = q.v[j];
-    }
-    return v;
-  }
-};
-
 // Per channel P = sum e h and Q = sum e over the block's rows, from them the group's sums of
 // e w h and e w over the cluster, then dx = rstd (e w - mean(e w) - h mean(e w h)).  The channels'
 // sums of the whole sample go to `part` for dweight and dbias.
 //
-// silu's derivative takes two of the hardware's special functions per element, of which an SM has
-// 16 lanes: computed in both passes they alone would take as long as the memory.  The first
-// pass leaves e in shared memory (fp32, in place of dy) for the second.
-template <typename T, int V, int ACT, int TH>
-__global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_bwd(const Gn p) {
-  constexpr bool kStash = ACT == EFCP_ACT_SILU;
-  using S = Slot<V, TH>;
+// x and dy stay in shared memory and e is computed in both passes: an e in fp32 in the place of dy
+// would spare the second pass silu's two special functions per element, but halves the rows a
+// thread has room for, and few rows do not pay for the sums in between (184 us with it, 107 us without, for
+// 256 x 56 x 56 x 64 bf16 with silu).
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_bwd(const Gn p) {
   using P = Pack<T, V>;
   extern __shared__ __align__(32) float sm[];
   const int wide = (p.tile_groups * p.per + 3) & ~3, tg = (p.tile_groups + 3) & ~3;
@@ -651,12 +622,9 @@ __global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_bwd(const Gn p) {
   float* data = ga + tg;
   const Item it = item_of<V>(p, cluster_rank(), cluster_index());
   const int mine = rows_of_thread(p, it);
-  const int most = p.thread_rows;  // rows a thread of this launch has room for
-  // x: [row of this thread] [thread]; then dy the same way, or in the slots that take e
-  P* dx_ = reinterpret_cast<P*>(data) + int(threadIdx.x);
-  float* rest = data + size_t(most) * (TH * V * sizeof(T) / 4);
-  float* slot = S::at(rest);
-  P* dd = reinterpret_cast<P*>(rest) + int(threadIdx.x);
+  // x, then dy: [row of this thread] [thread] of V elements
+  P* xs = reinterpret_cast<P*>(data) + int(threadIdx.x);
+  P* ds = xs + p.thread_rows * kGnThreads;
   const long long row = it.r0 + it.ty;
   const int c = it.tx * V, at = it.c0 + c;
   {
@@ -665,13 +633,11 @@ __global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_bwd(const Gn p) {
     const long long xstep = p.lanes_rows * p.x_row, dstep = p.lanes_rows * p.dy_row;
 #pragma unroll 4
     for (int k = 0; k < mine; ++k, px += xstep, pd += dstep) {
-      copy_in<T, V>(dx_ + k * TH, px);
-      copy_in<T, V>(kStash ? static_cast<void*>(slot + k * S::kFloats)
-                           : static_cast<void*>(dd + k * TH),
-                    pd);
+      copy_in<T, V>(xs + k * kGnThreads, px);
+      copy_in<T, V>(ds + k * kGnThreads, pd);
     }
   }
-  for (int k = threadIdx.x; k < it.width; k += TH) {
+  for (int k = threadIdx.x; k < it.width; k += kGnThreads) {
     const long long g = it.n * p.groups + it.g0 + k / p.per;
     wei[k] = weight_of(p, it.c0 + k);
     bia[k] = bias_of(p, it.c0 + k);
@@ -684,12 +650,11 @@ __global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_bwd(const Gn p) {
   if (mine) {
     const Vec<V> m = of_channels<V>(cm, c), b = of_channels<V>(bia, c);
     const Vec<V> f = of_channels<V>(cr, c) * of_channels<V>(wei, c);
-#pragma unroll 2
+#pragma unroll 4
     for (int k = 0; k < mine; ++k) {
-      const Vec<V> u = unpack(dx_[k * TH]) + m;
-      Vec<V> e = unpack(kStash ? *reinterpret_cast<const P*>(slot + k * S::kFloats) : dd[k * TH]);
+      const Vec<V> u = unpack(xs[k * kGnThreads]) + m;
+      Vec<V> e = unpack(ds[k * kGnThreads]);
       if (ACT != EFCP_ACT_NONE) e = e * act_grad<ACT>(fma(u, f, b));
-      if (kStash) S::put(slot + k * S::kFloats, e);
       s0 = fma(e, u, s0);
       s1 = s1 + e;
     }
@@ -707,7 +672,7 @@ __global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_bwd(const Gn p) {
     const bool along = p.per >= lanes;  // lanes over a row's values, or over the rows
     const int d0 = along ? lane : 0, dstep = along ? lanes : 1;
     const int t0 = along ? 0 : lane, tstep = along ? 1 : lanes;
-    for (int g0 = 0; g0 < it.ng; g0 += TH >> p.lanes_log) {
+    for (int g0 = 0; g0 < it.ng; g0 += kGnThreads >> p.lanes_log) {
       const int g = g0 + (int(threadIdx.x) >> p.lanes_log);
       float sb = 0.f, sa = 0.f;
       if (g < it.ng) {
@@ -738,7 +703,7 @@ __global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_bwd(const Gn p) {
   }
   if (grads) {
     // (from the far end: the first threads have the groups' sums to form)
-    for (int k = TH - 1 - int(threadIdx.x); k < it.width; k += TH) {
+    for (int k = kGnThreads - 1 - int(threadIdx.x); k < it.width; k += kGnThreads) {
       float t0 = 0.f, t1 = 0.f;
 #pragma unroll 4
       for (int t = 0; t < p.val_rows; ++t) {
@@ -758,7 +723,7 @@ __global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_bwd(const Gn p) {
     cluster.sync();
     // a group's blocks are joined by neighbouring lanes, one each
     const int links = 1 << p.links_log, r = int(threadIdx.x) & (links - 1);
-    for (int g0 = 0; g0 < it.ng; g0 += TH >> p.links_log) {
+    for (int g0 = 0; g0 < it.ng; g0 += kGnThreads >> p.links_log) {
       const int g = g0 + (int(threadIdx.x) >> p.links_log);
       float sb = 0.f, sa = 0.f;
       if (g < it.ng && r < p.chunks) {
@@ -777,7 +742,7 @@ __global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_bwd(const Gn p) {
     if (grads) {  // each block of the cluster joins its share of the channels
       const int share = (it.width + p.chunks - 1) / p.chunks;
       const int c1 = min(it.width, (it.chunk + 1) * share);
-      for (int k = it.chunk * share + TH - 1 - int(threadIdx.x); k < c1; k += TH) {
+      for (int k = it.chunk * share + kGnThreads - 1 - int(threadIdx.x); k < c1; k += kGnThreads) {
         float t0 = 0.f, t1 = 0.f;
 #pragma unroll 4
         for (int q = 0; q < p.chunks; ++q) {
@@ -797,16 +762,11 @@ __global__ void __launch_bounds__(TH, 1024 / TH) k_gn_resident_bwd(const Gn p) {
     const Vec<V> qa = of_channels<V>(cqa, c), qb = of_channels<V>(cqb, c);
     T* po = static_cast<T*>(p.y) + it.n * p.y_batch + row * p.y_row + at;
     const long long step = p.lanes_rows * p.y_row;
-#pragma unroll 2
+#pragma unroll 4
     for (int k = 0; k < mine; ++k, po += step) {
-      const Vec<V> u = unpack(dx_[k * TH]) + m;
-      Vec<V> e;
-      if (kStash) {
-        e = S::get(slot + k * S::kFloats);
-      } else {
-        e = unpack(dd[k * TH]);
-        if (ACT != EFCP_ACT_NONE) e = e * act_grad<ACT>(fma(u, f, b));
-      }
+      const Vec<V> u = unpack(xs[k * kGnThreads]) + m;
+      Vec<V> e = unpack(ds[k * kGnThreads]);
+      if (ACT != EFCP_ACT_NONE) e = e * act_grad<ACT>(fma(u, f, b));
       *reinterpret_cast<P*>(po) = pack<T, V>(fma(u * rs, qb, fma(e, f, qa)));
     }
   }
@@ -820,7 +780,7 @@ constexpr int kAhead = sizeof(T) * V == 16 ? 4 : 8;
 
 // The statistics of every group over a chunk of rows: k, m and q one after another.
 template <typename T, int V>
-__global__ void __launch_bounds__(kGnThreads, 3) k_gn_stats(const Gn p) {
+__global__ void __launch_bounds__(kGnThreads, 6) k_gn_stats(const Gn p) {
   constexpr int U = kAhead<T, V>;
   extern __shared__ __align__(32) float sm[];
   float* val = sm;
@@ -932,7 +892,7 @@ struct Lane {
 };
 
 template <typename T, int V, int ACT>
-__global__ void __launch_bounds__(kGnThreads, 3) k_gn_apply(const Gn p) {
+__global__ void __launch_bounds__(kGnThreads, 6) k_gn_apply(const Gn p) {
   constexpr int U = kAhead<T, V>;
   const Item it = item_of<V>(p, blockIdx.x % unsigned(p.chunks), blockIdx.x / unsigned(p.chunks));
   if (!it.on) return;
@@ -961,7 +921,7 @@ __global__ void __launch_bounds__(kGnThreads, 3) k_gn_apply(const Gn p) {
 
 // Per channel and chunk of rows: sum e h, then sum e.
 template <typename T, int V, int ACT>
-__global__ void __launch_bounds__(kGnThreads, 2) k_gn_bwd_sums(const Gn p) {
+__global__ void __launch_bounds__(kGnThreads, 4) k_gn_bwd_sums(const Gn p) {
   constexpr int U = kAhead<T, V>;
   extern __shared__ __align__(32) float sm[];
   float* val0 = sm;
@@ -1055,7 +1015,7 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_join_grads(const Gn p) {
 }
 
 template <typename T, int V, int ACT>
-__global__ void __launch_bounds__(kGnThreads, 2) k_gn_bwd_apply(const Gn p) {
+__global__ void __launch_bounds__(kGnThreads, 4) k_gn_bwd_apply(const Gn p) {
   constexpr int U = kAhead<T, V>;
   const Item it = item_of<V>(p, blockIdx.x % unsigned(p.chunks), blockIdx.x / unsigned(p.chunks));
   if (!it.on) return;
@@ -1132,7 +1092,7 @@ __global__ void __launch_bounds__(32 * kGnSumWarps)
 // ------------------------------------------------------------------ launches
 // One cluster of p.chunks blocks per item.
 template <class Kernel>
-cudaError_t launch_cluster(Kernel kern, int threads, const Gn& p, const GnLaunch& l) {
+cudaError_t launch_cluster(Kernel kern, const Gn& p, const GnLaunch& l) {
   if (p.chunks > 8) {
     const cudaError_t e =
         cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
@@ -1150,7 +1110,7 @@ cudaError_t launch_cluster(Kernel kern, int threads, const Gn& p, const GnLaunch
   attr[0].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(l.blocks);
-  cfg.blockDim = dim3(unsigned(threads));
+  cfg.blockDim = dim3(kGnThreads);
   cfg.dynamicSmemBytes = l.smem;
   cfg.stream = l.st;
   cfg.attrs = attr;
@@ -1176,17 +1136,13 @@ inline cudaError_t launch_params(const Gn& p, long long rows, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-template <typename T, int V, int ACT, int TH>
-cudaError_t launch_resident(const Gn& p, const GnLaunch& l) {
-  if (!l.backward) return launch_cluster(k_gn_resident_fwd<T, V, ACT, TH>, TH, p, l);
-  const cudaError_t e = launch_cluster(k_gn_resident_bwd<T, V, ACT, TH>, TH, p, l);
-  return e != cudaSuccess ? e : launch_params(p, p.n, l.st);
-}
-
 template <typename T, int V, int ACT>
 cudaError_t launch_act(const Gn& p, const GnLaunch& l) {
-  if (l.resident == 256) return launch_resident<T, V, ACT, 256>(p, l);
-  if (l.resident == 512) return launch_resident<T, V, ACT, 512>(p, l);
+  if (l.resident) {
+    if (!l.backward) return launch_cluster(k_gn_resident_fwd<T, V, ACT>, p, l);
+    const cudaError_t e = launch_cluster(k_gn_resident_bwd<T, V, ACT>, p, l);
+    return e != cudaSuccess ? e : launch_params(p, p.n, l.st);
+  }
   const size_t smem = gn_streamed_floats(p.val_floats, l.backward) * 4;
   const unsigned joins = unsigned((p.n * p.groups + kGnThreads / 32 - 1) / (kGnThreads / 32));
   cudaError_t e;

@@ -7,7 +7,11 @@
 
 namespace efcp {
 
-constexpr int kGnThreads = 256;  // of the streamed kernels
+// Threads of a block.  The sums between the passes cost a warp about a thousand instructions whatever
+// its rows, so few threads with many rows are better than many with few: forward 256 x 56 x 56 x 64
+// bf16 62 us with 256 threads, 53 us with 128.
+constexpr int kGnThreads = 128;
+static_assert((kGnThreads & (kGnThreads - 1)) == 0, "rows are shared out by shifts");
 
 struct Gn {
   const void* x;
@@ -47,7 +51,7 @@ struct GnLaunch {
   int vec;        // elements per access: as many as fill 16 or 4 bytes, or 1
   int act;        // EFCP_ACT_*
   bool backward;
-  int resident;   // threads per block when a cluster of `chunks` blocks holds a sample's tile, or 0
+  bool resident;  // a cluster of `chunks` blocks holds a sample's tile
   unsigned blocks;
   size_t smem;    // resident: dynamic shared memory
   cudaStream_t st;
@@ -61,9 +65,8 @@ constexpr int64_t gn_resident_fixed_bytes(int64_t val_floats, int tile_groups, i
   return 4 * (backward ? 2 * val_floats + 8 * wide + 2 * tg
                        : 4 * val_floats + 3 * wide + 3 * tg);
 }
-constexpr int64_t gn_resident_row_bytes(int threads, int vec, int size, bool backward,
-                                        bool stash) {
-  return int64_t(threads) * vec * (backward ? size + (stash ? 4 : size) : size);
+constexpr int64_t gn_resident_row_bytes(int vec, int size, bool backward) {
+  return int64_t(kGnThreads) * vec * size * (backward ? 2 : 1);
 }
 constexpr int64_t gn_streamed_floats(int64_t val_floats, bool backward) {
   return (backward ? 2 : 4) * val_floats;

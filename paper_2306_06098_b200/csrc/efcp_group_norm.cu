@@ -14,9 +14,8 @@ namespace efcp {
 namespace {
 
 constexpr int kTypeBytes[3] = {4, 2, 2};
-constexpr int kStreamedBlocksPerSM = 6;
+constexpr int kStreamedBlocksPerSM = 12;
 constexpr int kMaxRowsPerThread = 64;  // see the error bound in efcp_gn.cuh
-constexpr int kMaxCluster = 16;
 
 bool valid(const efcp_group_norm* d) {
   if (!d || d->n < 0 || d->rows < 1 || d->channels < 1 || d->groups < 1) return false;
@@ -105,51 +104,49 @@ void set_tiles(const efcp_group_norm& d, int unit, int64_t groups, Gn* p) {
   p->tiles = int(ceil_div(d.groups, p->tile_groups));
 }
 
-// Shared memory of one of the four (256 threads) or two (512 threads) blocks of an SM: of its
-// 228 KB, 1 KB per block is the system's.
-constexpr int64_t kSmem256 = 56 * 1024, kSmem512 = 113 * 1024;
+// Shared memory of a block when an SM is to hold four, three or two: of its 228 KB, 1 KB per block is
+// the system's.
+constexpr int64_t kSmemOf4 = 56 * 1024, kSmemOf3 = 75 * 1024, kSmemOf2 = 113 * 1024;
 
-// Whether a sample's tile fits the shared memory of a cluster; then tiles and the cluster's size.
-// Returns the threads per block, or 0.  Four small blocks per SM come before two large ones, as
-// long as 8 of them hold the tile (larger clusters leave parts of the GPU idle); a tile's rows should
-// be 128 bytes wide (whole lines), 64 bytes where that is too much for 8 large blocks, and up to 16
-// large blocks are taken where nothing else fits.  A GPU not filled by the tiles gets larger
-// clusters, as long as a thread keeps two rows.
-int plan_resident(const efcp_group_norm& d, int vec, bool backward, int sms, Gn* p) {
+// Whether a sample's tile fits on chip; then tiles, the cluster's size and the shared memory of a
+// block.  A tile's rows should be 128 bytes wide (whole lines), 64 bytes where that needs too many
+// blocks; small clusters come before large ones, and small blocks before large ones, which leave an
+// SM less to do while they wait.  A GPU not filled by the tiles gets larger clusters, as
+// long as a thread keeps two rows.
+bool plan_resident(const efcp_group_norm& d, int vec, bool backward, int sms, Gn* p,
+                   size_t* smem) {
   const int size = kTypeBytes[d.dtype], per = p->per, unit = vec / gcd(per, vec);
-  const bool stash = d.act == EFCP_ACT_SILU;
+  if (int64_t(unit) * per / vec > kGnThreads) return false;
+  const int64_t widest = int64_t(kGnThreads) * vec / per;  // groups a block is wide enough for
+  const int64_t row = gn_resident_row_bytes(vec, size, backward);
   struct Try {
-    int bytes, threads;
-    int64_t most;
+    int bytes;
+    int64_t smem, most;
   };
-  for (const Try t : {Try{128, 256, 8}, Try{128, 256, 16}, Try{64, 256, 8}, Try{64, 256, 16},
-                      Try{64, 512, kMaxCluster}}) {
-    if (int64_t(unit) * per / vec > t.threads) continue;
-    const int64_t widest = int64_t(t.threads) * vec / per;  // groups a block is wide enough for
+  for (const Try t : {Try{128, kSmemOf4, 8}, Try{128, kSmemOf4, 16}, Try{64, kSmemOf4, 8},
+                      Try{64, kSmemOf4, 16}, Try{64, kSmemOf3, 16}, Try{64, kSmemOf2, 16}}) {
     const int64_t groups = std::max<int64_t>(1, ceil_div(t.bytes / size, per));
     set_tiles(d, unit, std::min(ceil_div(groups, unit) * unit, widest), p);
-    set_layout(t.threads, vec, p);
-    const int64_t lanes_rows = p->lanes_rows;
+    set_layout(kGnThreads, vec, p);
     const int64_t fixed = gn_resident_fixed_bytes(p->val_floats, p->tile_groups,
                                                   p->tile_groups * per, backward);
-    const int64_t row = gn_resident_row_bytes(t.threads, vec, size, backward, stash);
-    const int64_t room = (t.threads == 256 ? kSmem256 : kSmem512) - fixed;
-    const int64_t deep = std::min<int64_t>(room / row, kMaxRowsPerThread);
-    if (lanes_rows < 1 || deep < 1) continue;
-    int64_t blocks = ceil_div(d.rows, lanes_rows * deep);
+    const int64_t deep = std::min<int64_t>((t.smem - fixed) / row, kMaxRowsPerThread);
+    if (deep < 1) continue;
+    int64_t blocks = ceil_div(d.rows, p->lanes_rows * deep);
     if (blocks > t.most) continue;
     const int64_t items = std::max<int64_t>(1, d.n * p->tiles);
     if (items * blocks < 2 * sms && blocks < 8) {
       const int64_t fill = std::min<int64_t>(8, ceil_div(2 * sms, items));
-      blocks = std::max(blocks, std::min(fill, d.rows / (2 * lanes_rows)));
+      blocks = std::max(blocks, std::min(fill, d.rows / (2 * p->lanes_rows)));
     }
     p->chunk_rows = ceil_div(d.rows, blocks);
     p->chunks = int(blocks);
-    p->thread_rows = int(ceil_div(p->chunk_rows, lanes_rows));
+    p->thread_rows = int(ceil_div(p->chunk_rows, p->lanes_rows));
     p->links_log = floor_log2(blocks) + ((1 << floor_log2(blocks)) < blocks);
-    return t.threads;
+    *smem = size_t(fixed + p->thread_rows * row);
+    return true;
   }
-  return 0;
+  return false;
 }
 
 // The widest tiles, and as many chunks as fill the GPU, with no thread taking more than
@@ -195,13 +192,8 @@ int make_plan(const efcp_group_norm& d, const Tensor* t, int nt, bool backward, 
   l.vec = pick_vec(d, t, nt);
   l.act = d.act;
   l.backward = backward;
-  l.resident = plan_resident(d, l.vec, backward, sms, &p);
+  l.resident = plan_resident(d, l.vec, backward, sms, &p, &l.smem);
   if (!l.resident) plan_streamed(d, l.vec, sms, &p);
-  if (l.resident)
-    l.smem = size_t(gn_resident_fixed_bytes(p.val_floats, p.tile_groups, p.tile_groups * p.per,
-                                            backward) +
-                    p.thread_rows * gn_resident_row_bytes(l.resident, l.vec, kTypeBytes[d.dtype],
-                                                          backward, d.act == EFCP_ACT_SILU));
   const int64_t blocks = d.n * p.tiles * p.chunks;
   if (blocks >= (1ll << 31) || d.n * d.groups >= (1ll << 33)) return EFCP_ETOOBIG;
   l.blocks = unsigned(blocks);
