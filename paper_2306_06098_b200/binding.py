@@ -1,5 +1,5 @@
 """Thin binding over libefcp.so (argument marshalling only): ctypes, and _marshal.so for the
-calls that take a list of tensors.
+calls on lists of gradients and on activations.
 
 The names mirror include/efcp.h.  PyTorch is used for device memory and streams; every
 step of the method runs inside the CUDA library.  Importing this module fails loudly
@@ -23,7 +23,7 @@ GGT_MAX_M = 160
 F32, BF16, F16 = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "silu": ACT_SILU}
+ACTS = ("none", "relu", "silu")
 MAX_RANK = 8
 
 for _path in (LIB_PATH, MARSHAL_PATH):
@@ -150,100 +150,33 @@ def topk_static(a: torch.Tensor, k: int, idx: torch.Tensor, val: torch.Tensor, s
 
 
 # ---------------------------------------------------------------------------------------
-# Lists of gradients
+# Lists of gradients.  `stream`: a torch.cuda.Stream to run on instead of the current one; memory
+# the call allocates then belongs to it.
 
-_GRADS_WORKSPACE = int(_lib.efcp_grads_workspace_bytes())
-_workspaces = {}  # (device, stream) -> the scratch memory calls on that stream share
-
-
-def _grads_workspace(index: int, stream: int) -> torch.Tensor:
-    """Scratch memory for the calls on one stream; a graph being captured gets its own (it may
-    be replayed on any stream)."""
-    if torch.cuda.is_current_stream_capturing():
-        return torch.zeros(_GRADS_WORKSPACE, dtype=torch.uint8, device=index)
-    ws = _workspaces.get((index, stream))
-    if ws is None:
-        ws = torch.zeros(_GRADS_WORKSPACE, dtype=torch.uint8, device=index)
-        _workspaces[index, stream] = ws
-    return ws
-
-
-def _on(device: torch.device, stream, call, *args):
-    """Runs call(index, raw stream, *args) with `device` current, on `stream` (a
-    torch.cuda.Stream, or None for the device's current one).  Memory the call allocates
-    then belongs to that stream too."""
-    if device.type != "cuda":
-        raise ValueError(f"CUDA tensors expected, got {device}")
-    index = device.index
-    if stream is not None:
-        with torch.cuda.stream(stream):
-            return call(index, stream.cuda_stream, *args)
-    if index != torch.cuda.current_device():
-        with torch.cuda.device(index):
-            return call(index, torch._C._cuda_getCurrentRawStream(index), *args)
-    return call(index, torch._C._cuda_getCurrentRawStream(index), *args)
-
-
-def _list_device(tensors, *others) -> torch.device:
-    for t in others:
-        if t is not None:
-            return t.device
-    for t in tensors:
-        if isinstance(t, torch.Tensor):
-            return t.device
-    return torch.device("cuda", torch.cuda.current_device())
-
-
-def _norm_out(out, index):
-    if out is None:
-        return torch.empty((), dtype=torch.float32, device=index)
-    if out.dtype != torch.float32 or out.numel() != 1 or out.device.index != index:
-        raise ValueError("out: one fp32 value on the gradients' device expected")
-    return out
-
-
-def _grad_norm(index, stream, tensors, scale, out):
-    out = _norm_out(out, index)
-    rc = _marshal.grads_norm(tensors, index, scale, out.data_ptr(),
-                             _grads_workspace(index, stream).data_ptr(), stream)
-    if rc != OK:
-        raise EfcpError(rc, "efcp_grads_norm")
-    return out
+def _done(result, where):
+    """The result of a native call, or the error whose code it returned."""
+    if type(result) is int:
+        raise EfcpError(result, where)
+    return result
 
 
 def grad_norm(tensors, scale: float = 1.0, out: torch.Tensor = None, stream=None) -> torch.Tensor:
     """efcp_grads_norm: scale * |g|_2 over a list of gradients (fp32, bfloat16, fp16, any
     strides, one CUDA device) as an fp32 scalar on the device; asynchronous."""
-    return _on(_list_device(tensors, out), stream, _grad_norm, tensors, scale, out)
-
-
-def _clip_grads(index, stream, tensors, max_norm, scale, out):
-    out = _norm_out(out, index)
-    rc = _marshal.grads_clip(tensors, index, max_norm, scale, out.data_ptr(),
-                             _grads_workspace(index, stream).data_ptr(), stream)
-    if rc != OK:
-        raise EfcpError(rc, "efcp_grads_clip")
-    return out
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return grad_norm(tensors, scale, out)
+    return _done(_marshal.grads_norm(tensors, scale, out), "efcp_grads_norm")
 
 
 def clip_grads(tensors, max_norm: float, scale: float = 1.0, out: torch.Tensor = None,
                stream=None) -> torch.Tensor:
     """efcp_grads_clip: g <- scale * min(1, max_norm / N) g in place over a list of gradients;
     returns N = scale * |g|_2 of before (fp32 scalar on the device); asynchronous."""
-    return _on(_list_device(tensors, out), stream, _clip_grads, tensors, max_norm, scale, out)
-
-
-def _gather_grads(index, stream, tensors, flat, max_norm, scale, norm, out):
-    if flat.dtype != torch.float32 or not flat.is_contiguous():
-        raise ValueError("flat: a contiguous fp32 tensor expected")
-    want = norm or out is not None
-    out = _norm_out(out, index) if want else None
-    ws = _grads_workspace(index, stream).data_ptr() if want or max_norm > 0 else 0
-    rc = _marshal.grads_gather(tensors, index, flat.data_ptr(), flat.numel(), max_norm, scale,
-                               out.data_ptr() if want else 0, ws, stream)
-    if rc != OK:
-        raise EfcpError(rc, "efcp_grads_gather")
-    return out
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return clip_grads(tensors, max_norm, scale, out)
+    return _done(_marshal.grads_clip(tensors, max_norm, scale, out), "efcp_grads_clip")
 
 
 def gather_grads(tensors, flat: torch.Tensor, max_norm: float = 0.0, scale: float = 1.0,
@@ -253,105 +186,15 @@ def gather_grads(tensors, flat: torch.Tensor, max_norm: float = 0.0, scale: floa
     norm.  An int in the list stands for a parameter without a gradient: that many zeros.
     Returns scale * |g|_2 (fp32 scalar on the device) when `norm` is set or `out` given, else
     None; asynchronous."""
-    return _on(_list_device(tensors, flat), stream, _gather_grads, tensors, flat, max_norm, scale,
-               norm, out)
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return gather_grads(tensors, flat, max_norm, scale, norm, out)
+    return _done(_marshal.grads_gather(tensors, flat, max_norm, scale, norm, out),
+                 "efcp_grads_gather")
 
 
 # ---------------------------------------------------------------------------------------
 # Group normalisation, channels last
-
-def _rows_layout(x: torch.Tensor):
-    """(batch stride, row stride) when the channels of x (n, channels, *positions) lie side by
-    side and its positions at one distance, else None."""
-    shape, stride = x.shape, x.stride()
-    channels = shape[1]
-    if channels != 1 and stride[1] != 1:
-        return None
-    row, count = 0, 1  # the merged positions so far, from the last dimension on
-    for size, st in zip(reversed(shape[2:]), reversed(stride[2:])):
-        if size == 1:
-            continue
-        if count == 1:
-            row = st
-        elif st != row * count:
-            return None
-        count *= size
-    if count == 1:
-        row = channels
-    batch = stride[0] if shape[0] != 1 else row * count
-    return (batch, row) if row >= channels else None
-
-
-def _channels_last(x: torch.Tensor):
-    """x itself with its strides, or a channels-last copy when its layout is another."""
-    if x.numel() == 0:
-        return x, (x.shape[1], x.shape[1])
-    layout = _rows_layout(x)
-    if layout is None:
-        order = (0, *range(2, x.dim()), 1)
-        back = (0, x.dim() - 1, *range(1, x.dim() - 1))
-        x = x.permute(order).contiguous().permute(back)
-        layout = _rows_layout(x)
-    return x, layout
-
-
-def _new_channels_last(x: torch.Tensor, index: int):
-    """An empty channels-last tensor of x's shape and type."""
-    shape = x.shape
-    channels, strides, step = shape[1], [0] * len(shape), shape[1]
-    for k in range(len(shape) - 1, 1, -1):
-        strides[k] = step
-        step *= shape[k]
-    strides[0], strides[1] = step, 1
-    return (torch.empty_strided(shape, strides, dtype=x.dtype, device=index),
-            (step, channels))
-
-
-def _gn_desc(x, groups, weight, bias, eps, act):
-    if x.dim() < 2 or x.dtype not in DTYPES:
-        raise ValueError("x: (n, channels, ...) in fp32, bfloat16 or fp16 expected")
-    if act not in ACTS:
-        raise ValueError(f"act: one of {', '.join(ACTS)} expected, got {act!r}")
-    params = [t for t in (weight, bias) if t is not None]
-    for t in params:
-        if (t.device != x.device or t.dtype not in DTYPES or t.dtype != params[0].dtype or
-                t.numel() != x.shape[1] or not t.is_contiguous()):
-            raise ValueError("weight, bias: contiguous, one value per channel, one type "
-                             "(fp32, bfloat16 or fp16), on x's device")
-    rows = 1
-    for size in x.shape[2:]:
-        rows *= size
-    return GroupNormDesc(n=x.shape[0], rows=rows, channels=x.shape[1], groups=groups,
-                         dtype=DTYPES[x.dtype],
-                         param_dtype=DTYPES[params[0].dtype] if params else F32, act=ACTS[act],
-                         eps=eps)
-
-
-def _gn_workspace(desc, backward, index):
-    size = int(_lib.efcp_group_norm_workspace_bytes(C.byref(desc), backward))
-    if size < 0:
-        raise EfcpError(EINVAL, "efcp_group_norm_workspace_bytes")
-    return torch.empty(size, dtype=torch.uint8, device=index), size
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
-
-
-def _group_norm_forward(index, stream, x, groups, weight, bias, eps, act):
-    desc = _gn_desc(x, groups, weight, bias, eps, act)
-    ws, ws_bytes = _gn_workspace(desc, 0, index)
-    x, (desc.x_batch, desc.x_row) = _channels_last(x)
-    y, (desc.y_batch, desc.y_row) = _new_channels_last(x, index)
-    mean = torch.empty((x.shape[0], groups), dtype=torch.float32, device=index)
-    rstd = torch.empty_like(mean)
-    rc = _lib.efcp_group_norm_forward(C.byref(desc), x.data_ptr(), _ptr(weight), _ptr(bias),
-                                      y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
-                                      ws.data_ptr(), ws_bytes, stream)
-    if rc != OK:
-        raise EfcpError(rc, "efcp_group_norm_forward")
-    return y, mean, rstd
-
 
 def group_norm_forward(x: torch.Tensor, groups: int, weight: torch.Tensor = None,
                        bias: torch.Tensor = None, eps: float = 1e-5, act: str = "none",
@@ -360,30 +203,11 @@ def group_norm_forward(x: torch.Tensor, groups: int, weight: torch.Tensor = None
     channel slice of a wider tensor too; other layouts are copied first).  act: "none", "relu"
     or "silu".  Returns (y, mean, rstd): y channels last in x's type, the statistics (n, groups)
     in fp32.  Asynchronous."""
-    return _on(x.device, stream, _group_norm_forward, x, groups, weight, bias, eps, act)
-
-
-def _group_norm_backward(index, stream, dy, x, mean, rstd, groups, weight, bias, act):
-    desc = _gn_desc(x, groups, weight, bias, 0.0, act)
-    if dy.shape != x.shape or dy.dtype != x.dtype or dy.device != x.device:
-        raise ValueError("dy: x's shape, type and device expected")
-    for t in (mean, rstd):
-        if (t.dtype != torch.float32 or t.numel() != x.shape[0] * groups or
-                not t.is_contiguous() or t.device != x.device):
-            raise ValueError("mean, rstd: as group_norm_forward returned them")
-    ws, ws_bytes = _gn_workspace(desc, 1, index)
-    x, (desc.x_batch, desc.x_row) = _channels_last(x)
-    dy, (desc.dy_batch, desc.dy_row) = _channels_last(dy)
-    dx, (desc.y_batch, desc.y_row) = _new_channels_last(x, index)
-    dweight = None if weight is None else torch.empty_like(weight)
-    dbias = None if bias is None else torch.empty_like(bias)
-    rc = _lib.efcp_group_norm_backward(C.byref(desc), dy.data_ptr(), x.data_ptr(),
-                                       mean.data_ptr(), rstd.data_ptr(), _ptr(weight), _ptr(bias),
-                                       dx.data_ptr(), _ptr(dweight), _ptr(dbias), ws.data_ptr(),
-                                       ws_bytes, stream)
-    if rc != OK:
-        raise EfcpError(rc, "efcp_group_norm_backward")
-    return dx, dweight, dbias
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return group_norm_forward(x, groups, weight, bias, eps, act)
+    return _done(_marshal.group_norm_forward(x, groups, weight, bias, eps, act),
+                 "efcp_group_norm_forward")
 
 
 def group_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
@@ -392,7 +216,11 @@ def group_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
     """efcp_group_norm_backward: (dx, dweight, dbias) for the gradient dy of
     group_norm_forward's y, with the statistics that call returned; dx channels last in x's type,
     dweight and dbias in the parameters' type (None where there is no parameter).  Asynchronous."""
-    return _on(x.device, stream, _group_norm_backward, dy, x, mean, rstd, groups, weight, bias, act)
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return group_norm_backward(dy, x, mean, rstd, groups, weight, bias, act)
+    return _done(_marshal.group_norm_backward(dy, x, mean, rstd, groups, weight, bias, act),
+                 "efcp_group_norm_backward")
 
 
 def _np_ptr(a: np.ndarray):

@@ -39,9 +39,10 @@ def build_marshal(force: bool = False) -> str:
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
            "-I", sysconfig.get_paths()["include"], "-I", os.path.join(root, "include"),
            "-I", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-I", INCLUDE,
+           "-I", os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include"),
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            "-o", MARSHAL + ".tmp", MARSHAL_SRC,
-           "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-L", CSRC, "-l:libefcp.so",
+           "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-L", CSRC, "-l:libefcp.so",
            f"-Wl,-rpath,{lib}", "-Wl,-rpath,$ORIGIN/csrc"]
     subprocess.run(cmd, check=True)
     os.replace(MARSHAL + ".tmp", MARSHAL)
@@ -65,7 +66,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
             failed = [s for s, j in zip(_sources(), jobs) if j.wait() != 0]
             if failed:
                 raise RuntimeError("nvcc failed for " + ", ".join(failed))
-            subprocess.run([nvcc, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o", LIB + ".tmp"] + objects, check=True)
+            subprocess.run([nvcc, "-shared", "-gencode", "arch=compute_100a,code=sm_100a",
+                            "-o", LIB + ".tmp"] + objects, check=True)
         os.replace(LIB + ".tmp", LIB)
     build_marshal(force)
     return LIB

@@ -167,39 +167,48 @@ def test_group_norm_pointers():
 
 
 def test_layouts_of_torch_tensors():
+    from paper_2306_06098_b200._marshal import as_channels_last, like_channels_last, rows_layout
     x = torch.zeros(2, 6, 5, 4)
-    assert B._rows_layout(x) is None
+    assert rows_layout(x) is None
     cl = x.contiguous(memory_format=torch.channels_last)
-    assert B._rows_layout(cl) == (120, 6)
-    assert B._rows_layout(cl[:, 1:4]) == (120, 6)
-    assert B._rows_layout(cl[:, :, 1:3]) == (120, 6)
-    assert B._rows_layout(cl[:, :, :, 1:3]) is None
-    assert B._rows_layout(cl[:, :, :, :1]) == (120, 24)
-    assert B._rows_layout(cl[1:]) == (120, 6)
-    assert B._rows_layout(x[:, :, :1, :1]) is None
-    assert B._rows_layout(torch.zeros(3, 7)) == (7, 7)
-    assert B._rows_layout(torch.zeros(3, 1, 4, 4)) == (16, 1)
-    assert B._rows_layout(torch.zeros(1, 6).expand(3, 6)) == (0, 6)
-    assert B._rows_layout(torch.zeros(1, 6, 1).expand(2, 6, 9)) is None
-    for t in (x, cl, cl[:, :, :, 1:3], torch.zeros(2, 6, 5, 4, 3), torch.zeros(1, 6, 1).expand(2, 6, 9)):
-        c, layout = B._channels_last(t)
-        assert c.shape == t.shape and layout is not None and torch.equal(c, t)
-    y, (batch, row) = B._new_channels_last(x, "cpu")
-    assert y.shape == x.shape and y.is_contiguous(memory_format=torch.channels_last) and (batch, row) == (120, 6)
+    assert rows_layout(cl) == (120, 6)
+    assert rows_layout(cl[:, 1:4]) == (120, 6)
+    assert rows_layout(cl[:, :, 1:3]) == (120, 6)
+    assert rows_layout(cl[:, :, :, 1:3]) is None
+    assert rows_layout(cl[:, :, :, :1]) == (120, 24)
+    assert rows_layout(cl[1:]) == (120, 6)
+    assert rows_layout(x[:, :, :1, :1]) is None
+    assert rows_layout(torch.zeros(3, 7)) == (7, 7)
+    assert rows_layout(torch.zeros(3, 1, 4, 4)) == (16, 1)
+    assert rows_layout(torch.zeros(1, 6).expand(3, 6)) == (0, 6)
+    assert rows_layout(torch.zeros(1, 6, 1).expand(2, 6, 9)) is None
+    assert rows_layout(torch.zeros(0, 6, 5, 4)) == (6, 6)
+    g = torch.Generator().manual_seed(0)
+    for t in (torch.randn(x.shape, generator=g), cl, torch.randn(2, 6, 5, 4, generator=g)[:, :, :, 1:3],
+              torch.randn(2, 6, 5, 4, 3, generator=g), torch.randn(1, 6, 1, generator=g).expand(2, 6, 9),
+              torch.randn(1, generator=g).expand(2, 6, 3, 3)):
+        c = as_channels_last(t)
+        assert c.shape == t.shape and rows_layout(c) is not None and torch.equal(c, t)
+    assert as_channels_last(cl).data_ptr() == cl.data_ptr()
+    y = like_channels_last(x)
+    assert y.shape == x.shape and y.is_contiguous(memory_format=torch.channels_last)
+    with pytest.raises(TypeError):
+        rows_layout(3)
 
 
 def test_marshalling_refuses_what_it_cannot_describe():
-    from paper_2306_06098_b200 import _marshal
-    for bad, err in (([torch.zeros(3)], ValueError), ([None], TypeError), ([3], TypeError), (3, TypeError),
+    for bad, err in (([torch.zeros(3)], ValueError), (3, TypeError), ("abc", TypeError),
                      ([torch.zeros(3).to_sparse()], ValueError)):
         with pytest.raises(err):
-            _marshal.grads_norm(bad, 0, 1.0, FAKE, FAKE, 0)
+            B.grad_norm(bad)
+    with pytest.raises(ValueError):
+        B.gather_grads([torch.zeros(3)], torch.zeros(3))
     with pytest.raises(TypeError):
-        _marshal.grads_gather([None], 0, FAKE, 3, 0.0, 1.0, 0, 0, 0)
-    assert _marshal.grads_gather([3, -1], 0, FAKE, 2, 0.0, 1.0, 0, 0, 0) == B.EINVAL
-    with pytest.raises(OverflowError):
-        _marshal.grads_gather([1 << 70], 0, FAKE, 2, 0.0, 1.0, 0, 0, 0)
-    with pytest.raises(ValueError):
-        B.grad_norm([torch.zeros(3)])
-    with pytest.raises(ValueError):
-        B.group_norm_forward(torch.zeros(2, 4, 3), 2)
+        B.gather_grads([torch.zeros(3)], None)
+    for call in (lambda: B.group_norm_forward(torch.zeros(2, 4, 3), 2),
+                 lambda: B.group_norm_forward(torch.zeros(4), 2),
+                 lambda: B.group_norm_forward(torch.zeros(2, 4, dtype=torch.float64), 2)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(TypeError):
+        B.group_norm_forward(None, 2)
