@@ -4,15 +4,16 @@
 // All three are streams over memory with a handful of operations per element: HBM bounds them when
 // the list is large, the launch when it is small.  The list travels in the kernel's parameters (up to
 // 32 KB of constant memory: no copy to wait for, no host buffer that has to outlive the
-// call).  It is cut into chunks of 16 KB that the thread blocks take in turn, so that one
-// large matrix and hundreds of short vectors both keep every SM busy.
+// call).  It is cut into chunks of 32 KB that the thread blocks take in turn, so that one
+// large matrix and hundreds of short vectors both keep every SM busy (smaller chunks when there are too
+// few of them for that).
 #include "efcp.h"
 
 #include <cuda_runtime.h>
 
 #include <algorithm>
 #include <cmath>
-#include <cstring>
+#include <vector>
 
 #include "efcp_common.cuh"
 #include "efcp_device.h"
@@ -24,25 +25,30 @@ namespace {
 constexpr int kGrThreads = 256;
 constexpr int kGrBlocksPerSM = 8;
 constexpr int kGrMaxBlocks = 4096;    // partial sums the workspace has room for
-constexpr int kGrChunkBytes = 16384;  // of the source; 64 bytes per thread
+constexpr int kGrChunkLog = 15;     // 32 KB of the source: 128 bytes per thread
+constexpr int kGrChunkLogMin = 11;  // 2 KB
 
 // A tensor's layout when its elements do not lie one after another: up to four merged
 // dimensions, [0] running fastest in the flat vector.
 struct Geom {
   long long size[3];  // of dimensions 0..2 (dimension 3 is what is left)
   long long stride[4];
+  // n / size[k] = n * mul[k] >> shift[k] for n < 2^31
+  unsigned mul[3];
+  unsigned char shift[3];
 };
 
-// What a launch works on.  first[i] is the number of the first chunk of tensor i.
+// What a launch works on.  first[i] is the number of the first chunk of tensor i.  M: how many tensors
+// may need a Geom; with 0 the kernels leave the code for them out, which takes twice the registers.
 template <int N, int M>
 struct Table {
   static constexpr int kN = N, kM = M;
   const void* ptr[N];
   long long numel[N];
   long long dst[N];  // position in the flat vector
-  Geom geom[M];
+  Geom geom[M > 0 ? M : 1];
   unsigned first[N + 1];
-  int n;
+  int n, chunk_log;
   short shape[N];  // index into geom, -1: one after another
   unsigned char dtype[N];
 };
@@ -55,8 +61,8 @@ struct Work {
 };
 
 // ------------------------------------------------------------------ device
-__device__ __forceinline__ int chunk_elems(int dtype) {
-  return dtype == EFCP_F32 ? kGrChunkBytes / 4 : kGrChunkBytes / 2;
+__device__ __forceinline__ int chunk_elems(int chunk_log, int dtype) {
+  return 1 << (chunk_log - (dtype == EFCP_F32 ? 2 : 1));
 }
 
 // The tensor that chunk c belongs to: the last i with first[i] <= c.
@@ -74,12 +80,12 @@ __device__ __forceinline__ int find_tensor(const Tab& tab, unsigned c) {
 // Position of element e of a strided tensor.
 __device__ __forceinline__ long long strided_pos(const Geom& g, long long e, bool small) {
   long long pos = 0;
-  if (small) {  // fewer than 2^31 elements: 32-bit divisions
+  if (small) {  // fewer than 2^31 elements
     unsigned r = unsigned(e);
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-      const unsigned s = unsigned(g.size[k]), q = r / s;
-      pos += (long long)(r - q * s) * g.stride[k];
+      const unsigned q = unsigned((unsigned long long)r * g.mul[k] >> g.shift[k]);
+      pos += (long long)(r - q * unsigned(g.size[k])) * g.stride[k];
       r = q;
     }
     return pos + (long long)r * g.stride[3];
@@ -93,23 +99,41 @@ __device__ __forceinline__ long long strided_pos(const Geom& g, long long e, boo
   return pos + e * g.stride[3];
 }
 
-// Sum of the squares of V values.  fp32 products and sums are exact to a few 2^-24 as long as
-// they neither overflow nor vanish; otherwise the same values are squared in fp64.
-template <int V>
-__device__ __forceinline__ double sumsq_of(const float (&v)[V]) {
-  float s = 0.f;
+// fp32 sums of squares are good to a few 2^-24 as long as they neither overflow nor vanish.
+__device__ __forceinline__ bool in_range(float s) { return s > 1e-28f && s < 1e37f; }
+
+// The squares of N values added to t, two products to an instruction.
+template <int N>
+__device__ __forceinline__ void add_squares(const float (&v)[N], float2& t) {
 #pragma unroll
-  for (int j = 0; j < V; ++j) s = fmaf(v[j], v[j], s);
-  if (s > 1e-28f && s < 1e37f) return double(s);
-  double t = 0.0;
+  for (int j = 0; j < N; j += 2) {
+    const float2 x = make_float2(v[j], v[j + 1]);
+    t = __ffma2_rn(x, x, t);
+  }
+}
+
+template <int N>
+__device__ __forceinline__ double sumsq_wide(const float (&v)[N]) {
+  double d = 0.0;
 #pragma unroll
-  for (int j = 0; j < V; ++j) t = fma(double(v[j]), double(v[j]), t);
-  return t;
+  for (int j = 0; j < N; ++j) d = fma(double(v[j]), double(v[j]), d);
+  return d;
+}
+
+template <typename T, int V>
+__device__ __forceinline__ double sumsq_of(const Pack<T, V>& a) {
+  float v[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) v[j] = to_f32(a.v[j]);
+  float2 t = make_float2(0.f, 0.f);
+  add_squares(v, t);
+  const float s = t.x + t.y;
+  return in_range(s) ? double(s) : sumsq_wide(v);
 }
 
 template <typename T>
 __device__ __forceinline__ double chunk_sumsq(const T* p, int len) {
-  constexpr int V = 16 / int(sizeof(T));
+  constexpr int V = 16 / int(sizeof(T)), U = 4;
   using P = Pack<T, V>;
   // elements before the first 16-byte boundary
   const int skew = int((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
@@ -117,18 +141,34 @@ __device__ __forceinline__ double chunk_sumsq(const T* p, int len) {
   const int nv = (len - head) / V;
   const P* q = reinterpret_cast<const P*>(p + head);
   double acc = 0.0;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < nv; i += kGrThreads) {
-    const P a = q[i];
-    float v[V];
+  int i = threadIdx.x;
+  for (; i + (U - 1) * kGrThreads < nv; i += U * kGrThreads) {
+    P a[U];
 #pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = to_f32(a.v[j]);
-    acc += sumsq_of(v);
+    for (int u = 0; u < U; ++u) a[u] = q[i + u * kGrThreads];
+    // four sums of at most 8 products each
+    float2 t[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float v[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = to_f32(a[u].v[j]);
+      add_squares(v, t[u & 1]);
+    }
+    const float s = (t[0].x + t[0].y) + (t[1].x + t[1].y);
+    if (in_range(s)) {
+      acc += double(s);
+    } else {
+#pragma unroll 1
+      for (int u = 0; u < U; ++u) acc += sumsq_of(q[i + u * kGrThreads]);
+    }
   }
+#pragma unroll 1
+  for (; i < nv; i += kGrThreads) acc += sumsq_of(q[i]);
   const int rest = len - head - nv * V;  // the ends: fewer than 2 V elements
   if (int(threadIdx.x) < head + rest) {
-    const int i = int(threadIdx.x) < head ? int(threadIdx.x) : nv * V + int(threadIdx.x);
-    const double x = double(to_f32(p[i]));
+    const int k = int(threadIdx.x) < head ? int(threadIdx.x) : nv * V + int(threadIdx.x);
+    const double x = double(to_f32(p[k]));
     acc += x * x;
   }
   return acc;
@@ -138,6 +178,7 @@ template <typename T>
 __device__ double chunk_sumsq_strided(const T* p, const Geom& g, long long begin, int len,
                                       bool small) {
   double acc = 0.0;
+#pragma unroll 2
   for (int i = threadIdx.x; i < len; i += kGrThreads) {
     const double x = double(to_f32(p[strided_pos(g, begin + i, small)]));
     acc += x * x;
@@ -175,18 +216,18 @@ __device__ __forceinline__ float factor_of(const Work* ws, double max_norm, doub
 }
 
 template <class Tab>
-__global__ void __launch_bounds__(kGrThreads)
+__global__ void __launch_bounds__(kGrThreads, Tab::kM > 0 ? 3 : kGrBlocksPerSM)
     k_grads_sumsq(const __grid_constant__ Tab tab, Work* ws, bool first_launch, double scale,
                   float* norm) {
   double acc = 0.0;
   const unsigned total = tab.first[tab.n];
   for (unsigned c = blockIdx.x; c < total; c += gridDim.x) {
     const int i = find_tensor(tab, c);
-    const int dtype = tab.dtype[i], per = chunk_elems(dtype);
+    const int dtype = tab.dtype[i], per = chunk_elems(tab.chunk_log, dtype);
     const long long begin = (long long)(c - tab.first[i]) * per;
     const int len = int(min((long long)per, tab.numel[i] - begin));
-    const int g = tab.shape[i];
-    if (g < 0) {
+    const int g = Tab::kM > 0 ? tab.shape[i] : -1;
+    if (Tab::kM == 0 || g < 0) {
       if (dtype == EFCP_F32)
         acc += chunk_sumsq(static_cast<const float*>(tab.ptr[i]) + begin, len);
       else if (dtype == EFCP_BF16)
@@ -243,7 +284,7 @@ __device__ void chunk_scale_strided(T* p, const Geom& g, long long begin, int le
 // The chunks run from the last to the first: the norm has just read them from the first to the
 // last, and what it read last is still in L2.
 template <class Tab>
-__global__ void __launch_bounds__(kGrThreads)
+__global__ void __launch_bounds__(kGrThreads, Tab::kM > 0 ? 3 : kGrBlocksPerSM)
     k_grads_scale(const __grid_constant__ Tab tab, const Work* ws, double max_norm, double scale) {
   const float f = factor_of(ws, max_norm, scale);
   if (f == 1.f) return;
@@ -251,20 +292,20 @@ __global__ void __launch_bounds__(kGrThreads)
   for (unsigned b = blockIdx.x; b < total; b += gridDim.x) {
     const unsigned c = total - 1 - b;
     const int i = find_tensor(tab, c);
-    const int dtype = tab.dtype[i], per = chunk_elems(dtype);
+    const int dtype = tab.dtype[i], per = chunk_elems(tab.chunk_log, dtype);
     const long long begin = (long long)(c - tab.first[i]) * per;
     const int len = int(min((long long)per, tab.numel[i] - begin));
-    const int g = tab.shape[i];
+    const int g = Tab::kM > 0 ? tab.shape[i] : -1;
     void* p = const_cast<void*>(tab.ptr[i]);
     const bool small = tab.numel[i] < (1ll << 31);
     if (dtype == EFCP_F32) {
-      if (g < 0) chunk_scale(static_cast<float*>(p) + begin, len, f);
+      if (Tab::kM == 0 || g < 0) chunk_scale(static_cast<float*>(p) + begin, len, f);
       else chunk_scale_strided(static_cast<float*>(p), tab.geom[g], begin, len, small, f);
     } else if (dtype == EFCP_BF16) {
-      if (g < 0) chunk_scale(static_cast<__nv_bfloat16*>(p) + begin, len, f);
+      if (Tab::kM == 0 || g < 0) chunk_scale(static_cast<__nv_bfloat16*>(p) + begin, len, f);
       else chunk_scale_strided(static_cast<__nv_bfloat16*>(p), tab.geom[g], begin, len, small, f);
     } else {
-      if (g < 0) chunk_scale(static_cast<__half*>(p) + begin, len, f);
+      if (Tab::kM == 0 || g < 0) chunk_scale(static_cast<__half*>(p) + begin, len, f);
       else chunk_scale_strided(static_cast<__half*>(p), tab.geom[g], begin, len, small, f);
     }
   }
@@ -275,54 +316,104 @@ __device__ __forceinline__ float scaled(float v, float f) {
   return __uint_as_float(f == 1.f ? __float_as_uint(v) : __float_as_uint(__fmul_rn(v, f)));
 }
 
-// One chunk into the flat vector; with ACC its sum of squares is returned.  Four elements per
-// access: the stores are then 16 bytes from consecutive lanes whatever the source's type.
-template <typename T, bool ACC>
-__device__ __forceinline__ double chunk_gather(const T* p, float* dst, int len, float f) {
-  using P = Pack<T, 4>;
+// One chunk into the flat vector; with ACC its sum of squares is returned.  A thread stores four
+// elements at a time, at 16-byte boundaries of the flat vector; it loads them by one access where the
+// source is aligned to that, and one by one, out of L1, where it is not.
+// U: such stores under way at a time.
+template <typename T, bool ACC, int U, class Load>
+__device__ __forceinline__ double gather_by_fours(float* dst, int len, float f, Load load) {
+  const int skew = int((reinterpret_cast<uintptr_t>(dst) & 15) / 4);
+  const int head = min(len, skew ? 4 - skew : 0);
+  const int nv = (len - head) / 4;
+  float4* out = reinterpret_cast<float4*>(dst + head);
   double acc = 0.0;
-  int done = 0;
-  if (!(reinterpret_cast<uintptr_t>(p) & (sizeof(P) - 1)) &&
-      !(reinterpret_cast<uintptr_t>(dst) & 15)) {
-    const P* q = reinterpret_cast<const P*>(p);
-    float4* o = reinterpret_cast<float4*>(dst);
-    const int nv = len / 4;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < nv; i += kGrThreads) {
-      const P a = q[i];
-      float v[4];
+  const auto put = [&](int i, const Pack<T, 4>& a) {
+    float v[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = to_f32(a.v[j]);
-      if (ACC) acc += sumsq_of(v);
-      o[i] = make_float4(scaled(v[0], f), scaled(v[1], f), scaled(v[2], f), scaled(v[3], f));
+    for (int j = 0; j < 4; ++j) v[j] = to_f32(a.v[j]);
+    if (ACC) acc += sumsq_of(a);
+    out[i] = make_float4(scaled(v[0], f), scaled(v[1], f), scaled(v[2], f), scaled(v[3], f));
+  };
+  int i = threadIdx.x;
+  if (U > 1) {
+    for (; i + (U - 1) * kGrThreads < nv; i += U * kGrThreads) {
+      Pack<T, 4> a[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) a[u] = load.four(head + 4 * (i + u * kGrThreads));
+#pragma unroll
+      for (int u = 0; u < U; ++u) put(i + u * kGrThreads, a[u]);
     }
-    done = nv * 4;
   }
-#pragma unroll 4
-  for (int i = done + threadIdx.x; i < len; i += kGrThreads) {
-    const float v = to_f32(p[i]);
+#pragma unroll 1
+  for (; i < nv; i += kGrThreads) put(i, load.four(head + 4 * i));
+  const int rest = len - head - nv * 4;  // the ends: fewer than 8 elements
+  if (int(threadIdx.x) < head + rest) {
+    const int k = int(threadIdx.x) < head ? int(threadIdx.x) : nv * 4 + int(threadIdx.x);
+    const float v = to_f32(load.one(k));
     if (ACC) acc += double(v) * double(v);
-    dst[i] = scaled(v, f);
+    dst[k] = scaled(v, f);
   }
   return acc;
+}
+
+template <typename T>
+struct LoadAligned {
+  const T* p;
+  __device__ __forceinline__ Pack<T, 4> four(int i) const {
+    return *reinterpret_cast<const Pack<T, 4>*>(p + i);
+  }
+  __device__ __forceinline__ T one(int i) const { return p[i]; }
+};
+template <typename T>
+struct LoadSingly {
+  const T* p;
+  __device__ __forceinline__ Pack<T, 4> four(int i) const {
+    Pack<T, 4> a;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a.v[j] = p[i + j];
+    return a;
+  }
+  __device__ __forceinline__ T one(int i) const { return p[i]; }
+};
+struct LoadZeros {
+  __device__ __forceinline__ Pack<float, 4> four(int) const { return {{0.f, 0.f, 0.f, 0.f}}; }
+  __device__ __forceinline__ float one(int) const { return 0.f; }
+};
+template <typename T>
+struct LoadStrided {
+  const T* p;
+  const Geom& g;
+  long long begin;
+  bool small;
+  __device__ __forceinline__ Pack<T, 4> four(int i) const {
+    Pack<T, 4> a;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a.v[j] = one(i + j);
+    return a;
+  }
+  __device__ __forceinline__ T one(int i) const { return p[strided_pos(g, begin + i, small)]; }
+};
+
+template <typename T, bool ACC>
+__device__ __forceinline__ double chunk_gather(const T* p, float* dst, int len, float f) {
+  // (the address of the first element that goes to a 16-byte boundary of the flat vector)
+  const int skew = int((reinterpret_cast<uintptr_t>(dst) & 15) / 4);
+  const uintptr_t first = reinterpret_cast<uintptr_t>(p + (skew ? 4 - skew : 0));
+  if (first % sizeof(Pack<T, 4>) == 0)
+    return gather_by_fours<T, ACC, 4>(dst, len, f, LoadAligned<T>{p});
+  return gather_by_fours<T, ACC, 2>(dst, len, f, LoadSingly<T>{p});
 }
 
 template <typename T, bool ACC>
 __device__ double chunk_gather_strided(const T* p, const Geom& g, long long begin, float* dst,
                                        int len, bool small, float f) {
-  double acc = 0.0;
-  for (int i = threadIdx.x; i < len; i += kGrThreads) {
-    const float v = to_f32(p[strided_pos(g, begin + i, small)]);
-    if (ACC) acc += double(v) * double(v);
-    dst[i] = scaled(v, f);
-  }
-  return acc;
+  return gather_by_fours<T, ACC, 1>(dst, len, f, LoadStrided<T>{p, g, begin, small});
 }
 
 // CLIP: the factor comes from the norm a launch before has left in ws.  ACC: there is no
 // clipping, and the norm is taken in the same pass.
 template <class Tab, bool CLIP, bool ACC>
-__global__ void __launch_bounds__(kGrThreads)
+__global__ void __launch_bounds__(kGrThreads, Tab::kM > 0 ? 3 : kGrBlocksPerSM)
     k_grads_gather(const __grid_constant__ Tab tab, float* flat, Work* ws, bool first_launch,
                    double max_norm, double scale, float* norm) {
   const float f = CLIP ? factor_of(ws, max_norm, scale) : float(scale);
@@ -331,27 +422,27 @@ __global__ void __launch_bounds__(kGrThreads)
   for (unsigned b = blockIdx.x; b < total; b += gridDim.x) {
     const unsigned c = CLIP ? total - 1 - b : b;  // backwards after a norm, as k_grads_scale
     const int i = find_tensor(tab, c);
-    const int dtype = tab.dtype[i], per = chunk_elems(dtype);
+    const int dtype = tab.dtype[i], per = chunk_elems(tab.chunk_log, dtype);
     const long long begin = (long long)(c - tab.first[i]) * per;
     const int len = int(min((long long)per, tab.numel[i] - begin));
-    const int g = tab.shape[i];
+    const int g = Tab::kM > 0 ? tab.shape[i] : -1;
     const void* p = tab.ptr[i];
     float* dst = flat + tab.dst[i] + begin;
     const bool small = tab.numel[i] < (1ll << 31);
     if (!p) {
-      for (int j = threadIdx.x; j < len; j += kGrThreads) dst[j] = 0.f;
+      gather_by_fours<float, false, 1>(dst, len, 1.f, LoadZeros{});
     } else if (dtype == EFCP_F32) {
       const float* q = static_cast<const float*>(p);
-      acc += g < 0 ? chunk_gather<float, ACC>(q + begin, dst, len, f)
+      acc += Tab::kM == 0 || g < 0 ? chunk_gather<float, ACC>(q + begin, dst, len, f)
                    : chunk_gather_strided<float, ACC>(q, tab.geom[g], begin, dst, len, small, f);
     } else if (dtype == EFCP_BF16) {
       const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p);
-      acc += g < 0 ? chunk_gather<__nv_bfloat16, ACC>(q + begin, dst, len, f)
+      acc += Tab::kM == 0 || g < 0 ? chunk_gather<__nv_bfloat16, ACC>(q + begin, dst, len, f)
                    : chunk_gather_strided<__nv_bfloat16, ACC>(q, tab.geom[g], begin, dst, len,
                                                               small, f);
     } else {
       const __half* q = static_cast<const __half*>(p);
-      acc += g < 0 ? chunk_gather<__half, ACC>(q + begin, dst, len, f)
+      acc += Tab::kM == 0 || g < 0 ? chunk_gather<__half, ACC>(q + begin, dst, len, f)
                    : chunk_gather_strided<__half, ACC>(q, tab.geom[g], begin, dst, len, small, f);
     }
   }
@@ -417,16 +508,34 @@ Layout layout_of(const Dim* dims, int n, bool* overlaps) {
 
 enum class Op { kNorm, kClip, kGather };
 
-int check_list(const efcp_tensor* grads, int n, Op op, int64_t* sum) {
+// A tensor of the list that a launch has to deal with.
+struct Entry {
+  void* data;
+  int64_t numel, dst;
+  int dtype, dims;  // dims 0: no layout needed
+  Dim dim[4];
+};
+
+// Checks the list and describes its tensors; `sum` receives the number of elements.  Empty tensors are
+// left out, absent ones too unless the list is gathered.  A layout is noted where the elements lie
+// neither one after another nor, if any order will do, close together.
+int read_list(const efcp_tensor* grads, int n, Op op, std::vector<Entry>* out, int64_t* sum) {
   int64_t total = 0;
   if (n < 0 || (n && !grads)) return EFCP_EINVAL;
+  out->reserve(size_t(n));
   for (int i = 0; i < n; ++i) {
     const efcp_tensor& t = grads[i];
-    if (t.numel < 0 || t.numel > (1ll << 40) || t.rank < 0 || t.rank > EFCP_MAX_RANK || t.dtype < 0 || t.dtype > 2)
+    if (t.numel < 0 || t.numel > (1ll << 40) || t.rank < 0 || t.rank > EFCP_MAX_RANK ||
+        t.dtype < 0 || t.dtype > 2)
       return EFCP_EINVAL;
     if (total > INT64_MAX / 8 - t.numel) return EFCP_EINVAL;
+    Entry e{t.data, t.numel, total, t.dtype, 0, {}};
     total += t.numel;
-    if (!t.numel || !t.data) continue;
+    if (!t.numel) continue;
+    if (!t.data) {
+      if (op == Op::kGather) out->push_back(e);
+      continue;
+    }
     const uintptr_t size = t.dtype == EFCP_F32 ? 4 : 2;
     if (reinterpret_cast<uintptr_t>(t.data) % size) return EFCP_EINVAL;
     if (t.rank) {
@@ -436,75 +545,91 @@ int check_list(const efcp_tensor* grads, int n, Op op, int64_t* sum) {
       if (nd < 0) return EFCP_EINVAL;
       const Layout l = layout_of(dims, nd, &overlaps);
       if (overlaps && op == Op::kClip) return EFCP_EINVAL;
-      if (nd > 4 && (l == Layout::kStrided || op == Op::kGather)) return EFCP_EINVAL;
+      if (l == Layout::kStrided || (l == Layout::kDense && op == Op::kGather)) {
+        if (nd > 4) return EFCP_EINVAL;
+        e.dims = nd;
+        std::copy(dims, dims + nd, e.dim);
+      }
     }
+    out->push_back(e);
   }
   *sum = total;
   return EFCP_OK;
 }
 
-// Fills the table from grads[*at] on, until it is full or the list ends.  Chunk numbers are
-// 32-bit: a tensor has at most 2^28 chunks, and no tensor is added to 2^30 of them.
+// n / d = n * mul >> shift for n < 2^31: with 2^b >= d, mul = floor(2^(31 + b) / d) + 1 is off from
+// 2^(31 + b) / d by at most 1, so the quotient by less than n / 2^(31 + b) < 1 / d.
+void set_divisor(long long d, unsigned* mul, unsigned char* shift) {
+  if (d >= (1ll << 31)) d = (1ll << 31) - 1;  // (not used: such a tensor takes 64-bit divisions)
+  int b = 0;
+  while ((1ll << b) < d) ++b;
+  *shift = static_cast<unsigned char>(31 + b);
+  *mul = unsigned(((1ull << (31 + b)) / static_cast<unsigned long long>(d)) + 1);
+}
+
+// Fills the table from list[*at] on, until it is full or the list ends.  Chunk numbers are 32-bit: a
+// tensor has at most 2^28 chunks of 32 KB (only short lists have smaller ones), and no
+// tensor is added to 2^30 of them.
 template <class Tab>
-void fill(Tab& tab, const efcp_tensor* grads, int n, Op op, int* at, int64_t* dst) {
+void fill(Tab& tab, const std::vector<Entry>& list, int chunk_log, size_t* at) {
+  tab.chunk_log = chunk_log;
   int used = 0, shapes = 0;
   unsigned chunks = 0;
-  for (; *at < n && used < Tab::kN && shapes < Tab::kM && chunks < (1u << 30); ++*at) {
-    const efcp_tensor& t = grads[*at];
-    const int64_t here = *dst;
-    *dst += t.numel;
-    if (!t.numel || (!t.data && op != Op::kGather)) continue;
+  for (; *at < list.size() && used < Tab::kN && chunks < (1u << 30); ++*at, ++used) {
+    const Entry& e = list[*at];
     int shape = -1;
-    if (t.rank && t.data) {
-      Dim dims[EFCP_MAX_RANK];
-      bool overlaps;
-      const int nd = merge_dims(t, dims);
-      const Layout l = layout_of(dims, nd, &overlaps);
-      if (l == Layout::kStrided || (l == Layout::kDense && op == Op::kGather)) {
-        shape = shapes++;
-        Geom& g = tab.geom[shape];
-        for (int k = 0; k < 3; ++k) g.size[k] = k < nd ? dims[k].size : 1;
-        for (int k = 0; k < 4; ++k) g.stride[k] = k < nd ? dims[k].stride : 0;
-      }
+    if (Tab::kM > 0 && e.dims) {
+      if (shapes == Tab::kM) break;
+      shape = shapes++;
+      Geom& g = tab.geom[shape];
+      for (int k = 0; k < 3; ++k) g.size[k] = k < e.dims ? e.dim[k].size : 1;
+      for (int k = 0; k < 4; ++k) g.stride[k] = k < e.dims ? e.dim[k].stride : 0;
+      for (int k = 0; k < 3; ++k) set_divisor(g.size[k], &g.mul[k], &g.shift[k]);
     }
-    const int64_t per = kGrChunkBytes / (t.dtype == EFCP_F32 ? 4 : 2);
-    tab.ptr[used] = t.data;
-    tab.numel[used] = t.numel;
-    tab.dst[used] = here;
+    const int64_t per = 1ll << (chunk_log - (e.dtype == EFCP_F32 ? 2 : 1));
+    tab.ptr[used] = e.data;
+    tab.numel[used] = e.numel;
+    tab.dst[used] = e.dst;
     tab.first[used] = chunks;
     tab.shape[used] = short(shape);
-    tab.dtype[used] = static_cast<unsigned char>(t.dtype);
-    chunks += unsigned((t.numel + per - 1) / per);
-    ++used;
+    tab.dtype[used] = static_cast<unsigned char>(e.dtype);
+    chunks += unsigned((e.numel + per - 1) / per);
   }
   tab.n = used;
   tab.first[used] = chunks;
 }
 
 struct Args {
-  const efcp_tensor* grads;
-  int n;
+  const std::vector<Entry>& list;
   float* flat;
   double max_norm, scale;
   float* norm;
   Work* ws;
   cudaStream_t st;
-  int sms;
+  int sms, chunk_log;
 };
+
+// The largest chunks that still give every SM four of them.
+int pick_chunk_log(const std::vector<Entry>& list, int sms) {
+  int64_t bytes = 0;
+  for (const Entry& e : list)
+    if (e.data) bytes += e.numel * (e.dtype == EFCP_F32 ? 4 : 2);
+  int log = kGrChunkLog;
+  while (log > kGrChunkLogMin && (bytes >> log) < 4ll * sms) --log;
+  return log;
+}
 
 enum class Kernel { kSumsq, kScale, kGather, kGatherClip, kGatherNorm };
 
 // One pass over the list: a launch for as many tensors at a time as a table holds.
 template <class Tab>
-int run_pass(const Args& a, Op op, Kernel kern) {
+int run_pass(const Args& a, Kernel kern) {
   Tab tab;
-  int at = 0;
-  int64_t dst = 0;
+  size_t at = 0;
   bool first = true;
-  while (at < a.n) {
-    fill(tab, a.grads, a.n, op, &at, &dst);
+  while (at < a.list.size()) {
+    fill(tab, a.list, a.chunk_log, &at);
     const unsigned chunks = tab.first[tab.n];
-    if (!chunks) continue;
     const unsigned grid = std::min<unsigned>(
         chunks, unsigned(std::min(a.sms * kGrBlocksPerSM, kGrMaxBlocks)));
     switch (kern) {
@@ -538,17 +663,32 @@ int run_pass(const Args& a, Op op, Kernel kern) {
 }
 
 // The table's size follows the list's: parameters are copied with every launch.
-using SmallTable = Table<64, 24>;
-using MidTable = Table<320, 96>;
-using LargeTable = Table<600, 200>;
-static_assert(sizeof(LargeTable) + 64 <= 32764, "kernel parameters");
+using LargeTable = Table<600, 150>;
+using LargeDenseTable = Table<960, 0>;
+static_assert(sizeof(LargeTable) + 64 <= 32764 && sizeof(LargeDenseTable) + 64 <= 32764,
+              "kernel parameters");
 
-int run_pass_sized(const Args& a, Op op, Kernel kern) {
-  int shapes = 0;
-  for (int i = 0; i < a.n; ++i) shapes += a.grads[i].rank > 0;
-  if (a.n <= SmallTable::kN && shapes <= SmallTable::kM) return run_pass<SmallTable>(a, op, kern);
-  if (a.n <= MidTable::kN && shapes <= MidTable::kM) return run_pass<MidTable>(a, op, kern);
-  return run_pass<LargeTable>(a, op, kern);
+int run_pass_sized(const Args& a, Kernel kern) {
+  size_t shapes = 0;
+  const size_t n = a.list.size();
+  for (const Entry& e : a.list) shapes += e.dims > 0;
+  if (!shapes) {
+    if (n <= 96) return run_pass<Table<96, 0>>(a, kern);
+    if (n <= 320) return run_pass<Table<320, 0>>(a, kern);
+    return run_pass<LargeDenseTable>(a, kern);
+  }
+  if (n <= 96 && shapes <= 32) return run_pass<Table<96, 32>>(a, kern);
+  return run_pass<LargeTable>(a, kern);
+}
+
+// The host side keeps the list in a vector: running out of memory is an error code, not an exception.
+template <class F>
+int guarded(F f) {
+  try {
+    return f();
+  } catch (...) {
+    return EFCP_ENOMEM;
+  }
 }
 
 bool bad_scalar(float v) { return !(v > 0.f) || !std::isfinite(v); }
@@ -564,52 +704,65 @@ int64_t efcp_grads_workspace_bytes(void) { return int64_t(sizeof(Work)); }
 
 int efcp_grads_norm(const efcp_tensor* grads, int32_t n, float scale, float* norm,
                     void* workspace, void* stream) {
-  int64_t d = 0;
   if (!norm || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 7) || bad_scalar(scale))
     return EFCP_EINVAL;
-  const int rc = check_list(grads, n, Op::kNorm, &d);
-  if (rc != EFCP_OK) return rc;
-  Args a{grads, n, nullptr, 0.0, double(scale), norm, static_cast<Work*>(workspace),
-         static_cast<cudaStream_t>(stream), device_sms()};
-  if (a.sms < 1) return EFCP_ECUDA;
-  return run_pass_sized(a, Op::kNorm, Kernel::kSumsq);
+  return guarded([&] {
+    std::vector<Entry> list;
+    int64_t sum = 0;
+    const int rc = read_list(grads, n, Op::kNorm, &list, &sum);
+    if (rc != EFCP_OK) return rc;
+    Args a{list, nullptr, 0.0, double(scale), norm, static_cast<Work*>(workspace),
+           static_cast<cudaStream_t>(stream), device_sms(), 0};
+    if (a.sms < 1) return EFCP_ECUDA;
+    a.chunk_log = pick_chunk_log(list, a.sms);
+    return run_pass_sized(a, Kernel::kSumsq);
+  });
 }
 
 int efcp_grads_clip(const efcp_tensor* grads, int32_t n, float max_norm, float scale, float* norm,
                     void* workspace, void* stream) {
-  int64_t d = 0;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 7) || bad_scalar(scale) ||
       !(max_norm > 0.f))
     return EFCP_EINVAL;
-  int rc = check_list(grads, n, Op::kClip, &d);
-  if (rc != EFCP_OK) return rc;
-  Args a{grads, n, nullptr, double(max_norm), double(scale), norm,
-         static_cast<Work*>(workspace), static_cast<cudaStream_t>(stream), device_sms()};
-  if (a.sms < 1) return EFCP_ECUDA;
-  rc = run_pass_sized(a, Op::kNorm, Kernel::kSumsq);
-  return rc != EFCP_OK ? rc : run_pass_sized(a, Op::kClip, Kernel::kScale);
+  return guarded([&] {
+    std::vector<Entry> list;
+    int64_t sum = 0;
+    int rc = read_list(grads, n, Op::kClip, &list, &sum);
+    if (rc != EFCP_OK) return rc;
+    Args a{list, nullptr, double(max_norm), double(scale), norm, static_cast<Work*>(workspace),
+           static_cast<cudaStream_t>(stream), device_sms(), 0};
+    if (a.sms < 1) return EFCP_ECUDA;
+    a.chunk_log = pick_chunk_log(list, a.sms);
+    rc = run_pass_sized(a, Kernel::kSumsq);
+    return rc != EFCP_OK ? rc : run_pass_sized(a, Kernel::kScale);
+  });
 }
 
 int efcp_grads_gather(const efcp_tensor* grads, int32_t n, float* flat, int64_t d, float max_norm,
                       float scale, float* norm, void* workspace, void* stream) {
-  int64_t sum = 0;
   if ((!flat && d != 0) || (reinterpret_cast<uintptr_t>(flat) & 3) || bad_scalar(scale) ||
       !(max_norm >= 0.f))
     return EFCP_EINVAL;
   if ((max_norm > 0.f || norm) &&
       (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 7)))
     return EFCP_EINVAL;
-  int rc = check_list(grads, n, Op::kGather, &sum);
-  if (rc != EFCP_OK) return rc;
-  if (sum != d) return EFCP_EINVAL;
-  Args a{grads, n, flat, double(max_norm), double(scale), norm, static_cast<Work*>(workspace),
-         static_cast<cudaStream_t>(stream), device_sms()};
-  if (a.sms < 1) return EFCP_ECUDA;
-  if (max_norm > 0.f) {
-    rc = run_pass_sized(a, Op::kNorm, Kernel::kSumsq);
-    return rc != EFCP_OK ? rc : run_pass_sized(a, Op::kGather, Kernel::kGatherClip);
-  }
-  return run_pass_sized(a, Op::kGather, norm ? Kernel::kGatherNorm : Kernel::kGather);
+  return guarded([&] {
+    std::vector<Entry> list, unordered;
+    int64_t sum = 0;
+    int rc = read_list(grads, n, Op::kGather, &list, &sum);
+    if (rc != EFCP_OK) return rc;
+    if (sum != d) return EFCP_EINVAL;
+    Args a{list, flat, double(max_norm), double(scale), norm, static_cast<Work*>(workspace),
+           static_cast<cudaStream_t>(stream), device_sms(), 0};
+    if (a.sms < 1) return EFCP_ECUDA;
+    a.chunk_log = pick_chunk_log(list, a.sms);
+    if (max_norm == 0.f) return run_pass_sized(a, norm ? Kernel::kGatherNorm : Kernel::kGather);
+    rc = read_list(grads, n, Op::kNorm, &unordered, &sum);  // most layouts do not matter to the norm
+    if (rc != EFCP_OK) return rc;
+    Args b{unordered, nullptr, 0.0, a.scale, norm, a.ws, a.st, a.sms, a.chunk_log};
+    rc = run_pass_sized(b, Kernel::kSumsq);
+    return rc != EFCP_OK ? rc : run_pass_sized(a, Kernel::kGatherClip);
+  });
 }
 
 }  // extern "C"
