@@ -13,6 +13,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <utility>
 #include <vector>
 
 #include "efcp_common.cuh"
@@ -215,10 +216,17 @@ __device__ __forceinline__ float factor_of(const Work* ws, double max_norm, doub
   return float(norm > max_norm && isfinite(norm) ? scale * (max_norm / norm) : scale);
 }
 
+// The kernel before in the stream has ended, and its results are visible; the one behind may begin.
+__device__ __forceinline__ void take_turn() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+}
+
 template <class Tab>
 __global__ void __launch_bounds__(kGrThreads, Tab::kM > 0 ? 3 : kGrBlocksPerSM)
     k_grads_sumsq(const __grid_constant__ Tab tab, Work* ws, bool first_launch, double scale,
                   float* norm) {
+  take_turn();
   double acc = 0.0;
   const unsigned total = tab.first[tab.n];
   for (unsigned c = blockIdx.x; c < total; c += gridDim.x) {
@@ -286,6 +294,7 @@ __device__ void chunk_scale_strided(T* p, const Geom& g, long long begin, int le
 template <class Tab>
 __global__ void __launch_bounds__(kGrThreads, Tab::kM > 0 ? 3 : kGrBlocksPerSM)
     k_grads_scale(const __grid_constant__ Tab tab, const Work* ws, double max_norm, double scale) {
+  take_turn();
   const float f = factor_of(ws, max_norm, scale);
   if (f == 1.f) return;
   const unsigned total = tab.first[tab.n];
@@ -416,6 +425,7 @@ template <class Tab, bool CLIP, bool ACC>
 __global__ void __launch_bounds__(kGrThreads, Tab::kM > 0 ? 3 : kGrBlocksPerSM)
     k_grads_gather(const __grid_constant__ Tab tab, float* flat, Work* ws, bool first_launch,
                    double max_norm, double scale, float* norm) {
+  take_turn();
   const float f = CLIP ? factor_of(ws, max_norm, scale) : float(scale);
   const unsigned total = tab.first[tab.n];
   double acc = 0.0;
@@ -621,6 +631,22 @@ int pick_chunk_log(const std::vector<Entry>& list, int sms) {
 
 enum class Kernel { kSumsq, kScale, kGather, kGatherClip, kGatherNorm };
 
+// A launch that may begin while the kernel before it in the stream ends: the kernels here wait for
+// that (griddepcontrol.wait) before they touch memory, and let their successor begin at once.
+template <class... P, class... A>
+cudaError_t launch(void (*kern)(P...), unsigned grid, cudaStream_t st, A&&... args) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kGrThreads);
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, std::forward<A>(args)...);
+}
+
 // One pass over the list: a launch for as many tensors at a time as a table holds.
 template <class Tab>
 int run_pass(const Args& a, Kernel kern) {
@@ -632,27 +658,32 @@ int run_pass(const Args& a, Kernel kern) {
     const unsigned chunks = tab.first[tab.n];
     const unsigned grid = std::min<unsigned>(
         chunks, unsigned(std::min(a.sms * kGrBlocksPerSM, kGrMaxBlocks)));
+    cudaError_t e = cudaSuccess;
     switch (kern) {
       case Kernel::kSumsq:
-        k_grads_sumsq<<<grid, kGrThreads, 0, a.st>>>(tab, a.ws, first, a.scale, a.norm);
+        e = launch(k_grads_sumsq<Tab>, grid, a.st, tab, a.ws, first, a.scale, a.norm);
         break;
       case Kernel::kScale:
-        k_grads_scale<<<grid, kGrThreads, 0, a.st>>>(tab, a.ws, a.max_norm, a.scale);
+        e = launch(k_grads_scale<Tab>, grid, a.st, tab, static_cast<const Work*>(a.ws), a.max_norm,
+                   a.scale);
         break;
       case Kernel::kGather:
-        k_grads_gather<Tab, false, false><<<grid, kGrThreads, 0, a.st>>>(
-            tab, a.flat, a.ws, first, a.max_norm, a.scale, a.norm);
+        e = launch(k_grads_gather<Tab, false, false>, grid, a.st, tab, a.flat, a.ws, first, a.max_norm,
+                   a.scale, a.norm);
         break;
       case Kernel::kGatherClip:
-        k_grads_gather<Tab, true, false><<<grid, kGrThreads, 0, a.st>>>(
-            tab, a.flat, a.ws, first, a.max_norm, a.scale, a.norm);
+        e = launch(k_grads_gather<Tab, true, false>, grid, a.st, tab, a.flat, a.ws, first, a.max_norm,
+                   a.scale, a.norm);
         break;
       case Kernel::kGatherNorm:
-        k_grads_gather<Tab, false, true><<<grid, kGrThreads, 0, a.st>>>(
-            tab, a.flat, a.ws, first, a.max_norm, a.scale, a.norm);
+        e = launch(k_grads_gather<Tab, false, true>, grid, a.st, tab, a.flat, a.ws, first, a.max_norm,
+                   a.scale, a.norm);
         break;
     }
-    if (cudaGetLastError() != cudaSuccess) return EFCP_ECUDA;
+    if (e != cudaSuccess) {
+      (void)cudaGetLastError();
+      return EFCP_ECUDA;
+    }
     first = false;
   }
   if (first && (kern == Kernel::kSumsq || kern == Kernel::kGatherNorm)) {
