@@ -61,7 +61,7 @@ __device__ __forceinline__ Item item_of(const Gn& p, unsigned chunk, unsigned q)
     it.ty = int(threadIdx.x) / p.cols;
     it.tx = int(threadIdx.x) - it.ty * p.cols;
   }
-  it.on = it.tx < p.cols && it.tx * V < it.width && it.ty < p.lanes_rows;
+  it.on = it.tx * V < it.width && it.ty < p.lanes_rows;
   return it;
 }
 
@@ -829,32 +829,72 @@ __global__ void __launch_bounds__(kGnThreads, 6) k_gn_stats(const Gn p) {
   }
 }
 
-// mean and rstd of every sample and group from the chunks' statistics: a warp each
-__global__ void __launch_bounds__(kGnThreads) k_gn_join_stats(const Gn p) {
-  const long long i = (long long)blockIdx.x * (kGnThreads / 32) + (threadIdx.x >> 5);
-  if (i >= p.n * p.groups) return;
-  const int lane = threadIdx.x & 31;
-  const long long n = i / p.groups;
-  const int g = int(i - n * p.groups);
-  const float* part = p.part + (n * p.chunks * p.groups + g) * 3;
+// The kernels between the two passes: 32 columns (groups, channels) per block, the rows shared among its
+// warps, so that loads of neighbouring columns are loads of neighbouring addresses.
+constexpr int kGnSumWarps = 32;
+
+// Sum over the block's warps of their lane's value, in a fixed order, the same in all of them.
+__device__ __forceinline__ float warps_sum(float v, float (*sh)[32]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __syncthreads();
+  sh[warp][lane] = v;
+  __syncthreads();
+  float s = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < kGnSumWarps; ++k) s += sh[k][lane];
+  return s;
+}
+
+// mean and rstd of a sample's groups from the chunks' statistics
+__global__ void __launch_bounds__(32 * kGnSumWarps) k_gn_join_stats(const Gn p, int blocks) {
+  __shared__ float sh[kGnSumWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long n = blockIdx.x / unsigned(blocks);
+  const int g = int(blockIdx.x - n * blocks) * 32 + lane;
+  const bool on = g < p.groups;
+  const float* part = p.part + (n * p.chunks * p.groups + (on ? g : 0)) * 3;
   const long long pitch = 3ll * p.groups;
   const float k0 = part[0];
   float s = 0.f;
-  for (int c = lane; c < p.chunks; c += 32) {
+#pragma unroll 4
+  for (int c = warp; c < p.chunks; c += kGnSumWarps) {
     const float have = float(min(p.chunk_rows, p.rows - c * p.chunk_rows));
     s = fmaf(have, (part[c * pitch] - k0) + part[c * pitch + 1], s);
   }
-  const float mean = lanes_sum(s, 32) / float(p.rows);
+  const float mean = warps_sum(s, sh) / float(p.rows);
   float m2 = 0.f;
-  for (int c = lane; c < p.chunks; c += 32) {
+#pragma unroll 4
+  for (int c = warp; c < p.chunks; c += kGnSumWarps) {
     const float have = float(min(p.chunk_rows, p.rows - c * p.chunk_rows)) * float(p.per);
     const float d = ((part[c * pitch] - k0) + part[c * pitch + 1]) - mean;
     m2 += fmaf(have * d, d, part[c * pitch + 2]);
   }
-  m2 = lanes_sum(m2, 32);
-  if (lane == 0) {
-    p.mean[i] = k0 + mean;
-    p.rstd[i] = rsqrtf(m2 / (float(p.rows) * float(p.per)) + p.eps);
+  m2 = warps_sum(m2, sh);
+  if (on && warp == 0) {
+    p.mean[n * p.groups + g] = k0 + mean;
+    p.rstd[n * p.groups + g] = rsqrtf(m2 / (float(p.rows) * float(p.per)) + p.eps);
+  }
+}
+
+// A sample's channel sums (sum e h, sum e) from those of its chunks
+__global__ void __launch_bounds__(32 * kGnSumWarps) k_gn_join_grads(const Gn p, int blocks) {
+  __shared__ float sh[kGnSumWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long n = blockIdx.x / unsigned(blocks);
+  const int c = int(blockIdx.x - n * blocks) * 32 + lane;
+  const bool on = c < p.channels;
+  const float* part = p.part + n * p.chunks * 2 * p.channels + (on ? c : 0);
+  float s0 = 0.f, s1 = 0.f;
+#pragma unroll 4
+  for (int k = warp; k < p.chunks; k += kGnSumWarps) {
+    s0 += part[2ll * k * p.channels];
+    s1 += part[(2ll * k + 1) * p.channels];
+  }
+  s0 = warps_sum(s0, sh);
+  s1 = warps_sum(s1, sh);
+  if (on && warp == 0) {
+    p.total[n * 2 * p.channels + c] = s0;
+    p.total[(n * 2 + 1) * p.channels + c] = s1;
   }
 }
 
@@ -977,52 +1017,38 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_bwd_sums(const Gn p) {
   }
 }
 
-// The group's means of e w and e w h from the chunks' channel sums: a warp per sample and group
-__global__ void __launch_bounds__(kGnThreads) k_gn_join_grads(const Gn p) {
-  const long long i = (long long)blockIdx.x * (kGnThreads / 32) + (threadIdx.x >> 5);
-  if (i >= p.n * p.groups) return;
-  const int lane = threadIdx.x & 31;
-  const long long n = i / p.groups;
-  const int c0 = int(i - n * p.groups) * p.per;
-  const float* part = p.part + n * p.chunks * 2 * p.channels;
-  float sb = 0.f, sa = 0.f;
-  if (p.per >= 32) {
-    for (int c = c0 + lane; c < c0 + p.per; c += 32) {
-      const float w = weight_of(p, c);
-      for (int k = 0; k < p.chunks; ++k) {
-        const float* q = part + 2ll * k * p.channels + c;
-        sb = fmaf(w, q[0], sb);
-        sa = fmaf(w, q[p.channels], sa);
-      }
-    }
-  } else {
-    for (int c = c0; c < c0 + p.per; ++c) {
-      const float w = weight_of(p, c);
-      for (int k = lane; k < p.chunks; k += 32) {
-        const float* q = part + 2ll * k * p.channels + c;
-        sb = fmaf(w, q[0], sb);
-        sa = fmaf(w, q[p.channels], sa);
-      }
-    }
-  }
-  sb = lanes_sum(sb, 32);
-  sa = lanes_sum(sa, 32);
-  if (lane == 0) {
-    const float total = float(p.rows) * float(p.per);
-    p.joint[2 * i] = sa / total;
-    p.joint[2 * i + 1] = sb / total;
-  }
-}
-
 template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kGnThreads, 4) k_gn_bwd_apply(const Gn p) {
   constexpr int U = kAhead<T, V>;
   const Item it = item_of<V>(p, blockIdx.x % unsigned(p.chunks), blockIdx.x / unsigned(p.chunks));
+  // the groups' means of e w and of e w h
+  extern __shared__ __align__(32) float joint[];
+  {
+    const float* total = p.total + it.n * 2 * p.channels + it.c0;
+    const int lanes = 1 << p.lanes_log, lane = int(threadIdx.x) & (lanes - 1);
+    for (int g0 = 0; g0 < it.ng; g0 += kGnThreads >> p.lanes_log) {
+      const int g = g0 + (int(threadIdx.x) >> p.lanes_log);
+      float sb = 0.f, sa = 0.f;
+      if (g < it.ng) {
+        for (int k = g * p.per + lane; k < (g + 1) * p.per; k += lanes) {
+          const float w = weight_of(p, it.c0 + k);
+          sb = fmaf(w, total[k], sb);
+          sa = fmaf(w, total[p.channels + k], sa);
+        }
+      }
+      sb = lanes_sum(sb, lanes);
+      sa = lanes_sum(sa, lanes);
+      if (g < it.ng && lane == 0) {
+        joint[2 * g] = sa * p.inv_total;
+        joint[2 * g + 1] = sb * p.inv_total;
+      }
+    }
+  }
+  __syncthreads();
   if (!it.on) return;
   const T* x = static_cast<const T*>(p.x) + it.n * p.x_batch + it.c0;
   const T* dy = static_cast<const T*>(p.dy) + it.n * p.dy_batch + it.c0;
   T* dx = static_cast<T*>(p.y) + it.n * p.y_batch + it.c0;
-  const float* joint = p.joint + 2 * (it.n * p.groups + it.g0);
   for (int c = it.tx; c < it.width / V; c += p.cols) {
     Lane<V> ln;
     ln.load(p, it, c);
@@ -1062,8 +1088,6 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_bwd_apply(const Gn p) {
 }
 
 // dweight and dbias: column sums over `rows` rows of channel sums, in fp64 and a fixed order.
-// 32 channels per block, the rows shared among its warps.
-constexpr int kGnSumWarps = 32;
 __global__ void __launch_bounds__(32 * kGnSumWarps)
     k_gn_param_grads(const float* __restrict__ part, long long rows, int channels, int dtype,
                      void* dweight, void* dbias) {
@@ -1129,10 +1153,10 @@ cudaError_t launch_streamed(Kernel kern, const Gn& p, const GnLaunch& l, size_t 
   return cudaGetLastError();
 }
 
-inline cudaError_t launch_params(const Gn& p, long long rows, cudaStream_t st) {
+inline cudaError_t launch_params(const Gn& p, const float* sums, cudaStream_t st) {
   if (!p.dweight && !p.dbias) return cudaSuccess;
   k_gn_param_grads<<<unsigned((p.channels + 31) / 32), 32 * kGnSumWarps, 0, st>>>(
-      p.part, rows, p.channels, p.param_dtype, p.dweight, p.dbias);
+      sums, p.n, p.channels, p.param_dtype, p.dweight, p.dbias);
   return cudaGetLastError();
 }
 
@@ -1141,22 +1165,24 @@ cudaError_t launch_act(const Gn& p, const GnLaunch& l) {
   if (l.resident) {
     if (!l.backward) return launch_cluster(k_gn_resident_fwd<T, V, ACT>, p, l);
     const cudaError_t e = launch_cluster(k_gn_resident_bwd<T, V, ACT>, p, l);
-    return e != cudaSuccess ? e : launch_params(p, p.n, l.st);
+    return e != cudaSuccess ? e : launch_params(p, p.part, l.st);
   }
-  const size_t smem = gn_streamed_floats(p.val_floats, l.backward) * 4;
-  const unsigned joins = unsigned((p.n * p.groups + kGnThreads / 32 - 1) / (kGnThreads / 32));
+  const size_t smem = size_t(gn_streamed_floats(p.val_floats, l.backward)) * 4;
+  const int joins = ((l.backward ? p.channels : p.groups) + 31) / 32;
+  if (p.n * joins >= (1ll << 31)) return cudaErrorInvalidConfiguration;
+  const unsigned blocks = unsigned(p.n * joins);
   cudaError_t e;
   if (!l.backward) {
     e = launch_streamed(k_gn_stats<T, V>, p, l, smem);
     if (e != cudaSuccess) return e;
-    k_gn_join_stats<<<joins, kGnThreads, 0, l.st>>>(p);
+    k_gn_join_stats<<<blocks, 32 * kGnSumWarps, 0, l.st>>>(p, joins);
     return launch_streamed(k_gn_apply<T, V, ACT>, p, l, 0);
   }
   e = launch_streamed(k_gn_bwd_sums<T, V, ACT>, p, l, smem);
   if (e != cudaSuccess) return e;
-  k_gn_join_grads<<<joins, kGnThreads, 0, l.st>>>(p);
-  e = launch_streamed(k_gn_bwd_apply<T, V, ACT>, p, l, 0);
-  return e != cudaSuccess ? e : launch_params(p, p.n * p.chunks, l.st);
+  k_gn_join_grads<<<blocks, 32 * kGnSumWarps, 0, l.st>>>(p, joins);
+  e = launch_streamed(k_gn_bwd_apply<T, V, ACT>, p, l, size_t(p.tile_groups) * 8);
+  return e != cudaSuccess ? e : launch_params(p, p.total, l.st);
 }
 
 template <typename T, int V>

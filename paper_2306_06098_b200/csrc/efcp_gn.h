@@ -22,7 +22,7 @@ struct Gn {
   float* mean;
   float* rstd;
   float* part;   // sums of chunks (streamed) or of samples (resident, backward)
-  float* joint;  // streamed, backward: per sample and group the means of e w and of e w h
+  float* total;  // streamed, backward: sums of samples
   void* dweight;
   void* dbias;
   long long x_batch, x_row, y_batch, y_row, dy_batch, dy_row;
@@ -34,7 +34,7 @@ struct Gn {
   // How the threads of a block lie over rows and channels, the same for every tile (in a last,
   // smaller one some have nothing to do), and what follows from that for its sums.
   int cols;                       // accesses of a row side by side
-  int pitch_log;                  // threads per row: 2^pitch_log (at most 32), or cols if negative
+  int pitch_log;                  // log2(cols) where cols is a power of two up to 32, else -1
   int lanes_rows, lanes_rows_log; // rows side by side (and its logarithm if pitch_log >= 0)
   int lanes_log;                  // 2^lanes_log lanes add up a group
   int fold;                       // channels of an access that always belong to one group

@@ -14,7 +14,7 @@ namespace efcp {
 namespace {
 
 constexpr int kTypeBytes[3] = {4, 2, 2};
-constexpr int kStreamedBlocksPerSM = 12;
+constexpr int kStreamedBlocksPerSM = 4;
 constexpr int kMaxRowsPerThread = 64;  // see the error bound in efcp_gn.cuh
 
 bool valid(const efcp_group_norm* d) {
@@ -74,19 +74,15 @@ int floor_log2(int64_t v) {
   return n;
 }
 
-// How `threads` threads lie over rows of the tile's channels.  Rows of up to 32 accesses get a power
-// of two of threads, so that the lanes of a warp that share a channel can add up by shuffles.
+// How `threads` threads lie over rows of the tile's channels.  Where a row has a power of two of
+// accesses, up to 32, the lanes of a warp that share a channel add up by shuffles.  (Filling other rows up to
+// a power of two with idle threads was slower: 65 us against 56 us for 8 x 64 x 64 x 320 fp32 backward.)
 void set_layout(int threads, int vec, Gn* p) {
   const int64_t width = int64_t(p->tile_groups) * p->per;
   p->cols = int(std::min<int64_t>(threads, width / vec));
   p->pitch_log = -1;
-  int pitch = p->cols;
-  if (p->cols <= 32) {
-    p->pitch_log = floor_log2(p->cols);
-    if ((1 << p->pitch_log) < p->cols) ++p->pitch_log;
-    pitch = 1 << p->pitch_log;
-  }
-  p->lanes_rows = threads / pitch;
+  if (p->cols <= 32 && (p->cols & (p->cols - 1)) == 0) p->pitch_log = floor_log2(p->cols);
+  p->lanes_rows = threads / p->cols;
   p->lanes_rows_log = floor_log2(p->lanes_rows);
   p->fold = gcd(p->per, vec);
   p->folded_cols = p->cols * (vec / p->fold);
@@ -104,15 +100,16 @@ void set_tiles(const efcp_group_norm& d, int unit, int64_t groups, Gn* p) {
   p->tiles = int(ceil_div(d.groups, p->tile_groups));
 }
 
-// Shared memory of a block when an SM is to hold four, three or two: of its 228 KB, 1 KB per block is
+// Shared memory of a block when an SM is to hold four or two: of its 228 KB, 1 KB per block is
 // the system's.
-constexpr int64_t kSmemOf4 = 56 * 1024, kSmemOf3 = 75 * 1024, kSmemOf2 = 113 * 1024;
+constexpr int64_t kSmemOf4 = 56 * 1024, kSmemOf2 = 113 * 1024;
 
 // Whether a sample's tile fits on chip; then tiles, the cluster's size and the shared memory of a
-// block.  A tile's rows should be 128 bytes wide (whole lines), 64 bytes where that needs too many
-// blocks; small clusters come before large ones, and small blocks before large ones, which leave an
-// SM less to do while they wait.  A GPU not filled by the tiles gets larger clusters, as
-// long as a thread keeps two rows.
+// block.  Narrow tiles come first, as they need smaller clusters: 64 bytes a row with 16-byte accesses
+// (256 x 28 x 28 x 128 bf16 forward 27 us against 29 us with 128), 128 with narrower ones
+// (200 x 30 x 30 x 37 forward 16 us against 21 us with 64), 32 where nothing else fits; clusters
+// of 8 blocks before larger ones, and four blocks per SM before two.  A GPU not filled by the tiles
+// gets larger clusters, as long as a thread keeps two rows.
 bool plan_resident(const efcp_group_norm& d, int vec, bool backward, int sms, Gn* p,
                    size_t* smem) {
   const int size = kTypeBytes[d.dtype], per = p->per, unit = vec / gcd(per, vec);
@@ -123,8 +120,9 @@ bool plan_resident(const efcp_group_norm& d, int vec, bool backward, int sms, Gn
     int bytes;
     int64_t smem, most;
   };
-  for (const Try t : {Try{128, kSmemOf4, 8}, Try{128, kSmemOf4, 16}, Try{64, kSmemOf4, 8},
-                      Try{64, kSmemOf4, 16}, Try{64, kSmemOf3, 16}, Try{64, kSmemOf2, 16}}) {
+  const int wide = vec * size == 16 ? 64 : 128;
+  for (const Try t : {Try{wide, kSmemOf4, 8}, Try{wide, kSmemOf4, 16}, Try{32, kSmemOf4, 16},
+                      Try{wide, kSmemOf2, 16}, Try{32, kSmemOf2, 16}}) {
     const int64_t groups = std::max<int64_t>(1, ceil_div(t.bytes / size, per));
     set_tiles(d, unit, std::min(ceil_div(groups, unit) * unit, widest), p);
     set_layout(kGnThreads, vec, p);
@@ -169,7 +167,7 @@ void plan_streamed(const efcp_group_norm& d, int vec, int sms, Gn* p) {
 struct Plan {
   Gn gn;
   GnLaunch launch;
-  int64_t part, joint;  // floats of the workspace
+  int64_t part, total;  // floats of the workspace
 };
 
 int make_plan(const efcp_group_norm& d, const Tensor* t, int nt, bool backward, int sms,
@@ -197,10 +195,10 @@ int make_plan(const efcp_group_norm& d, const Tensor* t, int nt, bool backward, 
   const int64_t blocks = d.n * p.tiles * p.chunks;
   if (blocks >= (1ll << 31) || d.n * d.groups >= (1ll << 33)) return EFCP_ETOOBIG;
   l.blocks = unsigned(blocks);
-  out->part = out->joint = 0;
+  out->part = out->total = 0;
   if (backward) {
     out->part = (l.resident ? d.n : d.n * p.chunks) * 2 * d.channels;
-    out->joint = l.resident ? 0 : d.n * d.groups * 2;
+    out->total = l.resident ? 0 : d.n * 2 * d.channels;
   } else if (!l.resident) {
     out->part = d.n * p.chunks * 3 * d.groups;
   }
@@ -239,7 +237,7 @@ int64_t efcp_group_norm_workspace_bytes(const efcp_group_norm* desc, int32_t bac
     Plan plan;
     const Tensor t{reinterpret_cast<const void*>(align), 0, 0};
     if (make_plan(*desc, &t, 1, backward != 0, sms, &plan) == EFCP_OK)
-      most = std::max(most, plan.part + plan.joint);
+      most = std::max(most, plan.part + plan.total);
   }
   return std::max<int64_t>(16, most * 4);
 }
@@ -299,12 +297,12 @@ int efcp_group_norm_backward(const efcp_group_norm* desc, const void* dy, const 
                        {dx, desc->y_batch, desc->y_row}};
   const int rc = make_plan(*desc, t, 3, true, sms, &plan);
   if (rc != EFCP_OK) return rc;
-  if (workspace_bytes < (plan.part + plan.joint) * 4) return EFCP_ENOMEM;
+  if (workspace_bytes < (plan.part + plan.total) * 4) return EFCP_ENOMEM;
   Gn& p = plan.gn;
   p.x = x; p.dy = dy; p.y = dx; p.weight = weight; p.bias = bias;
   p.mean = const_cast<float*>(mean); p.rstd = const_cast<float*>(rstd);
   p.part = static_cast<float*>(workspace);
-  p.joint = p.part + plan.part;
+  p.total = p.part + plan.part;
   p.dweight = dweight; p.dbias = dbias;
   return run(plan, desc->dtype, st);
 }
