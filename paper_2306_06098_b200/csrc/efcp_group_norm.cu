@@ -92,12 +92,24 @@ void set_layout(int threads, int vec, Gn* p) {
   p->val_floats = (p->val_rows * p->cols * vec + 3) / 4 * 4;
 }
 
-// Tiles of about `groups` groups, all of nearly the same size and a multiple of `unit`.
-void set_tiles(const efcp_group_norm& d, int unit, int64_t groups, Gn* p) {
-  const int64_t most = std::max<int64_t>(unit, groups / unit * unit);
-  p->tiles = int(ceil_div(d.groups, most));
-  p->tile_groups = int(ceil_div(ceil_div(d.groups, p->tiles), unit) * unit);
-  p->tiles = int(ceil_div(d.groups, p->tile_groups));
+// Tiles of at most `groups` groups and not much less than half of that, a multiple of `unit` and all of
+// nearly the same size: those that leave the fewest threads without work (65 columns on 128 threads would
+// leave half of them).
+void set_tiles(const efcp_group_norm& d, int vec, int unit, int64_t groups, Gn* p) {
+  const int64_t most = std::max<int64_t>(1, groups / unit);
+  double best = 0;
+  for (int64_t k = most; k >= (most + 1) / 2; --k) {
+    int64_t tiles = ceil_div(d.groups, k * unit);
+    const int64_t size = ceil_div(ceil_div(d.groups, tiles), unit) * unit;
+    tiles = ceil_div(d.groups, size);
+    const int64_t cols = std::min<int64_t>(kGnThreads, size * p->per / vec);
+    const double use = double(kGnThreads / cols) / double(tiles);
+    if (use > best * 1.001) {
+      best = use;
+      p->tiles = int(tiles);
+      p->tile_groups = int(size);
+    }
+  }
 }
 
 // Shared memory of a block when an SM is to hold four or two: of its 228 KB, 1 KB per block is
@@ -124,7 +136,7 @@ bool plan_resident(const efcp_group_norm& d, int vec, bool backward, int sms, Gn
   for (const Try t : {Try{wide, kSmemOf4, 8}, Try{wide, kSmemOf4, 16}, Try{32, kSmemOf4, 16},
                       Try{wide, kSmemOf2, 16}, Try{32, kSmemOf2, 16}}) {
     const int64_t groups = std::max<int64_t>(1, ceil_div(t.bytes / size, per));
-    set_tiles(d, unit, std::min(ceil_div(groups, unit) * unit, widest), p);
+    set_tiles(d, vec, unit, std::min(ceil_div(groups, unit) * unit, widest), p);
     set_layout(kGnThreads, vec, p);
     const int64_t fixed = gn_resident_fixed_bytes(p->val_floats, p->tile_groups,
                                                   p->tile_groups * per, backward);
@@ -151,7 +163,7 @@ bool plan_resident(const efcp_group_norm& d, int vec, bool backward, int sms, Gn
 // kMaxRowsPerThread rows.
 void plan_streamed(const efcp_group_norm& d, int vec, int sms, Gn* p) {
   const int per = p->per, unit = vec / gcd(per, vec);
-  set_tiles(d, unit, std::max<int64_t>(1, int64_t(kGnThreads) * vec / per), p);
+  set_tiles(d, vec, unit, std::max<int64_t>(1, int64_t(kGnThreads) * vec / per), p);
   set_layout(kGnThreads, vec, p);
   const int64_t lanes_rows = p->lanes_rows;
   const int64_t rounds = ceil_div(int64_t(p->tile_groups) * per / vec, p->cols);
