@@ -22,6 +22,7 @@
 
 #include "efcp.h"
 #include "efcp_gn.h"
+#include "efcp_launch.cuh"
 #include "efcp_num.cuh"
 
 namespace efcp {
@@ -510,6 +511,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_fwd(const Gn p) {
   // [row of this thread] [thread] of V elements
   Pack<T, V>* data = reinterpret_cast<Pack<T, V>*>(bq + tg) + int(threadIdx.x);
   const Item it = item_of<V>(p, cluster_rank(), cluster_index());
+  take_turn();
   const int mine = rows_of_thread(p, it);
   const int c = it.tx * V;
   {
@@ -621,6 +623,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_bwd(const Gn p) {
   float* ga = gb + tg;
   float* data = ga + tg;
   const Item it = item_of<V>(p, cluster_rank(), cluster_index());
+  take_turn();
   const int mine = rows_of_thread(p, it);
   // x, then dy: [row of this thread] [thread] of V elements
   P* xs = reinterpret_cast<P*>(data) + int(threadIdx.x);
@@ -785,6 +788,7 @@ __global__ void __launch_bounds__(kGnThreads, 6) k_gn_stats(const Gn p) {
   extern __shared__ __align__(32) float sm[];
   float* val = sm;
   const Item it = item_of<V>(p, blockIdx.x % unsigned(p.chunks), blockIdx.x / unsigned(p.chunks));
+  take_turn();
   const T* x = static_cast<const T*>(p.x) + it.n * p.x_batch + it.c0;
   Vec<V> k0 = fill<V>(0.f), s1 = k0, s2 = k0, neg = k0;
   int n = 0;
@@ -854,6 +858,7 @@ __global__ void __launch_bounds__(32 * kGnSumWarps) k_gn_join_stats(const Gn p, 
   const bool on = g < p.groups;
   const float* part = p.part + (n * p.chunks * p.groups + (on ? g : 0)) * 3;
   const long long pitch = 3ll * p.groups;
+  take_turn();
   const float k0 = part[0];
   float s = 0.f;
 #pragma unroll 4
@@ -884,6 +889,7 @@ __global__ void __launch_bounds__(32 * kGnSumWarps) k_gn_join_grads(const Gn p, 
   const int c = int(blockIdx.x - n * blocks) * 32 + lane;
   const bool on = c < p.channels;
   const float* part = p.part + n * p.chunks * 2 * p.channels + (on ? c : 0);
+  take_turn();
   float s0 = 0.f, s1 = 0.f;
 #pragma unroll 4
   for (int k = warp; k < p.chunks; k += kGnSumWarps) {
@@ -935,6 +941,7 @@ template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kGnThreads, 6) k_gn_apply(const Gn p) {
   constexpr int U = kAhead<T, V>;
   const Item it = item_of<V>(p, blockIdx.x % unsigned(p.chunks), blockIdx.x / unsigned(p.chunks));
+  take_turn();
   if (!it.on) return;
   const T* x = static_cast<const T*>(p.x) + it.n * p.x_batch + it.c0;
   T* y = static_cast<T*>(p.y) + it.n * p.y_batch + it.c0;
@@ -967,6 +974,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_bwd_sums(const Gn p) {
   float* val0 = sm;
   float* val1 = val0 + p.val_floats;
   const Item it = item_of<V>(p, blockIdx.x % unsigned(p.chunks), blockIdx.x / unsigned(p.chunks));
+  take_turn();
   const T* x = static_cast<const T*>(p.x) + it.n * p.x_batch + it.c0;
   const T* dy = static_cast<const T*>(p.dy) + it.n * p.dy_batch + it.c0;
   float* part = p.part + (it.n * p.chunks + it.chunk) * 2 * p.channels + it.c0;
@@ -1021,6 +1029,7 @@ template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kGnThreads, 4) k_gn_bwd_apply(const Gn p) {
   constexpr int U = kAhead<T, V>;
   const Item it = item_of<V>(p, blockIdx.x % unsigned(p.chunks), blockIdx.x / unsigned(p.chunks));
+  take_turn();
   // the groups' means of e w and of e w h
   extern __shared__ __align__(32) float joint[];
   {
@@ -1087,101 +1096,73 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_bwd_apply(const Gn p) {
   }
 }
 
-// dweight and dbias: column sums over `rows` rows of channel sums, in fp64 and a fixed order.
+// dweight and dbias: column sums over `rows` rows of channel sums, in fp64 and a fixed order.  Eight
+// channels per block, a sector of memory, so that few channels of many samples still occupy some SMs.
+constexpr int kGnParamCols = 8;
 __global__ void __launch_bounds__(32 * kGnSumWarps)
     k_gn_param_grads(const float* __restrict__ part, long long rows, int channels, int dtype,
                      void* dweight, void* dbias) {
-  __shared__ double sh[2][kGnSumWarps][32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int c = int(blockIdx.x) * 32 + lane;
+  constexpr int kRows = 32 * kGnSumWarps / kGnParamCols;
+  __shared__ double sh[2][kGnSumWarps][kGnParamCols];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = lane % kGnParamCols;
+  const int c = int(blockIdx.x) * kGnParamCols + col;
   double s0 = 0.0, s1 = 0.0;
+  take_turn();
   if (c < channels) {
-#pragma unroll 8
-    for (long long i = warp; i < rows; i += kGnSumWarps) {
+#pragma unroll 4
+    for (long long i = threadIdx.x / kGnParamCols; i < rows; i += kRows) {
       s0 += double(part[i * 2 * channels + c]);
       s1 += double(part[(i * 2 + 1) * channels + c]);
     }
   }
-  sh[0][warp][lane] = s0;
-  sh[1][warp][lane] = s1;
+#pragma unroll
+  for (int d = kGnParamCols; d < 32; d *= 2) {
+    s0 += __shfl_xor_sync(~0u, s0, d);
+    s1 += __shfl_xor_sync(~0u, s1, d);
+  }
+  if (lane < kGnParamCols) {
+    sh[0][warp][col] = s0;
+    sh[1][warp][col] = s1;
+  }
   __syncthreads();
-  if (warp < 2 && c < channels) {
+  if (warp < 2 && lane < kGnParamCols && c < channels) {
     double s = 0.0;
-    for (int k = 0; k < kGnSumWarps; ++k) s += sh[warp][k][lane];
+#pragma unroll
+    for (int k = 0; k < kGnSumWarps; ++k) s += sh[warp][k][col];
     void* out = warp == 0 ? dweight : dbias;
     if (out) store_from_f32(out, dtype, c, float(s));
   }
 }
 
 // ------------------------------------------------------------------ launches
-// One cluster of p.chunks blocks per item.
-template <class Kernel>
-cudaError_t launch_cluster(Kernel kern, const Gn& p, const GnLaunch& l) {
-  if (p.chunks > 8) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e != cudaSuccess) return e;
-  }
-  if (l.smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               int(l.smem));
-    if (e != cudaSuccess) return e;
-  }
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = unsigned(p.chunks);
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(l.blocks);
-  cfg.blockDim = dim3(kGnThreads);
-  cfg.dynamicSmemBytes = l.smem;
-  cfg.stream = l.st;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, p);
-}
-
-template <class Kernel>
-cudaError_t launch_streamed(Kernel kern, const Gn& p, const GnLaunch& l, size_t smem) {
-  if (smem > 48 * 1024) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
-    if (e != cudaSuccess) return e;
-  }
-  kern<<<l.blocks, kGnThreads, smem, l.st>>>(p);
-  return cudaGetLastError();
-}
-
 inline cudaError_t launch_params(const Gn& p, const float* sums, cudaStream_t st) {
   if (!p.dweight && !p.dbias) return cudaSuccess;
-  k_gn_param_grads<<<unsigned((p.channels + 31) / 32), 32 * kGnSumWarps, 0, st>>>(
-      sums, p.n, p.channels, p.param_dtype, p.dweight, p.dbias);
-  return cudaGetLastError();
+  const Shape s{unsigned((p.channels + kGnParamCols - 1) / kGnParamCols), 32 * kGnSumWarps, 0, 0};
+  return launch(k_gn_param_grads, s, st, sums, p.n, p.channels, p.param_dtype, p.dweight, p.dbias);
 }
 
 template <typename T, int V, int ACT>
 cudaError_t launch_act(const Gn& p, const GnLaunch& l) {
   if (l.resident) {
-    if (!l.backward) return launch_cluster(k_gn_resident_fwd<T, V, ACT>, p, l);
-    const cudaError_t e = launch_cluster(k_gn_resident_bwd<T, V, ACT>, p, l);
+    const Shape s{l.blocks, kGnThreads, l.smem, unsigned(p.chunks)};
+    if (!l.backward) return launch(k_gn_resident_fwd<T, V, ACT>, s, l.st, p);
+    const cudaError_t e = launch(k_gn_resident_bwd<T, V, ACT>, s, l.st, p);
     return e != cudaSuccess ? e : launch_params(p, p.part, l.st);
   }
-  const size_t smem = size_t(gn_streamed_floats(p.val_floats, l.backward)) * 4;
+  const Shape sums{l.blocks, kGnThreads, size_t(gn_streamed_floats(p.val_floats, l.backward)) * 4, 0};
   const int joins = ((l.backward ? p.channels : p.groups) + 31) / 32;
   if (p.n * joins >= (1ll << 31)) return cudaErrorInvalidConfiguration;
-  const unsigned blocks = unsigned(p.n * joins);
+  const Shape join{unsigned(p.n * joins), 32 * kGnSumWarps, 0, 0};
+  const Shape apply{l.blocks, kGnThreads, l.backward ? size_t(p.tile_groups) * 8 : 0, 0};
   cudaError_t e;
   if (!l.backward) {
-    e = launch_streamed(k_gn_stats<T, V>, p, l, smem);
-    if (e != cudaSuccess) return e;
-    k_gn_join_stats<<<blocks, 32 * kGnSumWarps, 0, l.st>>>(p, joins);
-    return launch_streamed(k_gn_apply<T, V, ACT>, p, l, 0);
+    e = launch(k_gn_stats<T, V>, sums, l.st, p);
+    if (e == cudaSuccess) e = launch(k_gn_join_stats, join, l.st, p, joins);
+    return e != cudaSuccess ? e : launch(k_gn_apply<T, V, ACT>, apply, l.st, p);
   }
-  e = launch_streamed(k_gn_bwd_sums<T, V, ACT>, p, l, smem);
-  if (e != cudaSuccess) return e;
-  k_gn_join_grads<<<blocks, 32 * kGnSumWarps, 0, l.st>>>(p, joins);
-  e = launch_streamed(k_gn_bwd_apply<T, V, ACT>, p, l, size_t(p.tile_groups) * 8);
+  e = launch(k_gn_bwd_sums<T, V, ACT>, sums, l.st, p);
+  if (e == cudaSuccess) e = launch(k_gn_join_grads, join, l.st, p, joins);
+  if (e == cudaSuccess) e = launch(k_gn_bwd_apply<T, V, ACT>, apply, l.st, p);
   return e != cudaSuccess ? e : launch_params(p, p.total, l.st);
 }
 

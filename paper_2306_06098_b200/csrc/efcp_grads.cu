@@ -13,11 +13,11 @@
 
 #include <algorithm>
 #include <cmath>
-#include <utility>
 #include <vector>
 
 #include "efcp_common.cuh"
 #include "efcp_device.h"
+#include "efcp_launch.cuh"
 #include "efcp_num.cuh"
 
 namespace efcp {
@@ -214,12 +214,6 @@ __device__ bool finish_sum(double acc, Work* ws, bool first_launch) {
 __device__ __forceinline__ float factor_of(const Work* ws, double max_norm, double scale) {
   const double norm = scale * sqrt(ws->sumsq);
   return float(norm > max_norm && isfinite(norm) ? scale * (max_norm / norm) : scale);
-}
-
-// The kernel before in the stream has ended, and its results are visible; the one behind may begin.
-__device__ __forceinline__ void take_turn() {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;");
 }
 
 template <class Tab>
@@ -631,22 +625,6 @@ int pick_chunk_log(const std::vector<Entry>& list, int sms) {
 
 enum class Kernel { kSumsq, kScale, kGather, kGatherClip, kGatherNorm };
 
-// A launch that may begin while the kernel before it in the stream ends: the kernels here wait for
-// that (griddepcontrol.wait) before they touch memory, and let their successor begin at once.
-template <class... P, class... A>
-cudaError_t launch(void (*kern)(P...), unsigned grid, cudaStream_t st, A&&... args) {
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(kGrThreads);
-  cfg.stream = st;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, std::forward<A>(args)...);
-}
-
 // One pass over the list: a launch for as many tensors at a time as a table holds.
 template <class Tab>
 int run_pass(const Args& a, Kernel kern) {
@@ -656,27 +634,28 @@ int run_pass(const Args& a, Kernel kern) {
   while (at < a.list.size()) {
     fill(tab, a.list, a.chunk_log, &at);
     const unsigned chunks = tab.first[tab.n];
-    const unsigned grid = std::min<unsigned>(
-        chunks, unsigned(std::min(a.sms * kGrBlocksPerSM, kGrMaxBlocks)));
+    const Shape shape{
+        std::min<unsigned>(chunks, unsigned(std::min(a.sms * kGrBlocksPerSM, kGrMaxBlocks))),
+        kGrThreads, 0, 0};
     cudaError_t e = cudaSuccess;
     switch (kern) {
       case Kernel::kSumsq:
-        e = launch(k_grads_sumsq<Tab>, grid, a.st, tab, a.ws, first, a.scale, a.norm);
+        e = launch(k_grads_sumsq<Tab>, shape, a.st, tab, a.ws, first, a.scale, a.norm);
         break;
       case Kernel::kScale:
-        e = launch(k_grads_scale<Tab>, grid, a.st, tab, static_cast<const Work*>(a.ws), a.max_norm,
+        e = launch(k_grads_scale<Tab>, shape, a.st, tab, static_cast<const Work*>(a.ws), a.max_norm,
                    a.scale);
         break;
       case Kernel::kGather:
-        e = launch(k_grads_gather<Tab, false, false>, grid, a.st, tab, a.flat, a.ws, first, a.max_norm,
+        e = launch(k_grads_gather<Tab, false, false>, shape, a.st, tab, a.flat, a.ws, first, a.max_norm,
                    a.scale, a.norm);
         break;
       case Kernel::kGatherClip:
-        e = launch(k_grads_gather<Tab, true, false>, grid, a.st, tab, a.flat, a.ws, first, a.max_norm,
+        e = launch(k_grads_gather<Tab, true, false>, shape, a.st, tab, a.flat, a.ws, first, a.max_norm,
                    a.scale, a.norm);
         break;
       case Kernel::kGatherNorm:
-        e = launch(k_grads_gather<Tab, false, true>, grid, a.st, tab, a.flat, a.ws, first, a.max_norm,
+        e = launch(k_grads_gather<Tab, false, true>, shape, a.st, tab, a.flat, a.ws, first, a.max_norm,
                    a.scale, a.norm);
         break;
     }
