@@ -42,7 +42,8 @@ def build_marshal(force: bool = False) -> str:
            "-I", os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include"),
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            "-o", MARSHAL + ".tmp", MARSHAL_SRC,
-           "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-L", CSRC, "-l:libefcp.so",
+           "-L", lib, "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda",
+           "-L", CSRC, "-l:libefcp.so",
            f"-Wl,-rpath,{lib}", "-Wl,-rpath,$ORIGIN/csrc"]
     subprocess.run(cmd, check=True)
     os.replace(MARSHAL + ".tmp", MARSHAL)

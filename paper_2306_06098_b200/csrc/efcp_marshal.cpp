@@ -6,6 +6,8 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -80,10 +82,17 @@ std::optional<at::Tensor> maybe_tensor(PyObject* o, const char* name) {
 struct Place {
   c10::cuda::CUDAGuard guard;
   c10::cuda::CUDAStream stream;
-  at::TensorOptions f32;
   explicit Place(c10::Device d)
-      : guard(d), stream(c10::cuda::getCurrentCUDAStream(d.index())),
-        f32(at::TensorOptions().dtype(at::kFloat).device(d)) {}
+      : guard(d), stream(c10::cuda::getCurrentCUDAStream(d.index())) {}
+
+  // An output, without the way through the operators' dispatch (a call makes up to four).
+  at::Tensor empty(at::IntArrayRef sizes, at::ScalarType type = at::kFloat) const {
+    return at::detail::empty_cuda(sizes, type, stream.device(), std::nullopt);
+  }
+  // Scratch memory until the end of the call, in the stream's order like a tensor's.
+  c10::DataPtr scratch(int64_t bytes) const {
+    return c10::cuda::CUDACachingAllocator::get()->allocate(size_t(bytes));
+  }
 };
 
 // ------------------------------------------------------------------ lists of gradients
@@ -166,7 +175,9 @@ std::vector<efcp_tensor> describe_list(PyObject* seq, c10::Device device, Use us
 // replayed on any stream.  (Never freed: streams live as long as the process.)
 at::Tensor list_workspace(const Place& place) {
   static const int64_t bytes = efcp_grads_workspace_bytes();
-  const auto fresh = [&] { return at::zeros({bytes}, place.f32.dtype(at::kByte)); };
+  const auto fresh = [&] {
+    return at::zeros({bytes}, at::TensorOptions().dtype(at::kByte).device(place.stream.device()));
+  };
   if (c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None)
     return fresh();
   static auto* known = new std::map<std::pair<int, void*>, at::Tensor>;  // (under the GIL)
@@ -176,7 +187,7 @@ at::Tensor list_workspace(const Place& place) {
 }
 
 at::Tensor norm_out(const std::optional<at::Tensor>& out, const Place& place) {
-  if (!out) return at::empty({}, place.f32);
+  if (!out) return place.empty({});
   require(out->scalar_type() == at::kFloat && out->numel() == 1 &&
               out->device() == place.stream.device(),
           "out: one fp32 value on the gradients' device expected");
@@ -298,6 +309,8 @@ at::Tensor new_channels_last(const at::Tensor& x, Rows* rows) {
   strides[0] = step;
   strides[1] = 1;
   *rows = Rows{step, x.size(1)};
+  if (x.is_cuda())
+    return at::detail::empty_strided_cuda(x.sizes(), strides, x.scalar_type(), x.device());
   return at::empty_strided(x.sizes(), strides, x.options());
 }
 
@@ -336,12 +349,6 @@ efcp_group_norm group_norm_desc(const at::Tensor& x, int groups,
   return d;
 }
 
-at::Tensor workspace_for(const efcp_group_norm& d, bool backward, const Place& place,
-                         int64_t* bytes) {
-  *bytes = efcp_group_norm_workspace_bytes(&d, backward);
-  return *bytes < 0 ? at::Tensor() : at::empty({*bytes}, place.f32.dtype(at::kByte));
-}
-
 const void* data_of(const std::optional<at::Tensor>& t) {
   return t ? t->const_data_ptr() : nullptr;
 }
@@ -367,20 +374,20 @@ PyObject* group_norm_forward(PyObject*, PyObject* args) {
     const auto weight = maybe_tensor(w_, "weight"), bias = maybe_tensor(b_, "bias");
     efcp_group_norm d = group_norm_desc(given, groups, weight, bias, eps, act);
     const Place place(given.device());
-    int64_t bytes;
-    const at::Tensor ws = workspace_for(d, false, place, &bytes);
+    const int64_t bytes = efcp_group_norm_workspace_bytes(&d, false);
     if (bytes < 0) return PyLong_FromLong(EFCP_EINVAL);
+    const c10::DataPtr ws = place.scratch(bytes);
     Rows in, out;
     const at::Tensor x = channels_last(given, &in), y = new_channels_last(x, &out);
     d.x_batch = in.batch;
     d.x_row = in.row;
     d.y_batch = out.batch;
     d.y_row = out.row;
-    const at::Tensor mean = at::empty({d.n, groups}, place.f32);
-    const at::Tensor rstd = at::empty({d.n, groups}, place.f32);
+    const at::Tensor mean = place.empty({d.n, groups});
+    const at::Tensor rstd = place.empty({d.n, groups});
     const int rc = efcp_group_norm_forward(
         &d, x.const_data_ptr(), data_of(weight), data_of(bias), y.mutable_data_ptr(),
-        mean.mutable_data_ptr<float>(), rstd.mutable_data_ptr<float>(), ws.mutable_data_ptr(), bytes,
+        mean.mutable_data_ptr<float>(), rstd.mutable_data_ptr<float>(), ws.get(), bytes,
         place.stream.stream());
     return triple(rc, y, mean, rstd);
   });
@@ -406,9 +413,9 @@ PyObject* group_norm_backward(PyObject*, PyObject* args) {
                   t->device() == given.device(),
               "mean, rstd: as group_norm_forward returned them");
     const Place place(given.device());
-    int64_t bytes;
-    const at::Tensor ws = workspace_for(d, true, place, &bytes);
+    const int64_t bytes = efcp_group_norm_workspace_bytes(&d, true);
     if (bytes < 0) return PyLong_FromLong(EFCP_EINVAL);
+    const c10::DataPtr ws = place.scratch(bytes);
     Rows in, grad, out;
     const at::Tensor x = channels_last(given, &in), dy = channels_last(given_dy, &grad);
     const at::Tensor dx = new_channels_last(x, &out);
@@ -418,13 +425,13 @@ PyObject* group_norm_backward(PyObject*, PyObject* args) {
     d.dy_row = grad.row;
     d.y_batch = out.batch;
     d.y_row = out.row;
-    const at::Tensor dw = weight ? at::empty_like(*weight) : at::Tensor();
-    const at::Tensor db = bias ? at::empty_like(*bias) : at::Tensor();
+    const at::Tensor dw = weight ? place.empty(weight->sizes(), weight->scalar_type()) : at::Tensor();
+    const at::Tensor db = bias ? place.empty(bias->sizes(), bias->scalar_type()) : at::Tensor();
     const int rc = efcp_group_norm_backward(
         &d, dy.const_data_ptr(), x.const_data_ptr(), mean.const_data_ptr<float>(),
         rstd.const_data_ptr<float>(), data_of(weight), data_of(bias), dx.mutable_data_ptr(),
         dw.defined() ? dw.mutable_data_ptr() : nullptr,
-        db.defined() ? db.mutable_data_ptr() : nullptr, ws.mutable_data_ptr(), bytes,
+        db.defined() ? db.mutable_data_ptr() : nullptr, ws.get(), bytes,
         place.stream.stream());
     return triple(rc, dx, dw, db);
   });
