@@ -123,8 +123,10 @@ constexpr int64_t kSmemOf4 = 56 * 1024, kSmemOf2 = 113 * 1024;
 // of 8 blocks before larger ones, and four blocks per SM before two.  Where a sample has few rows the tiles
 // are wider, up to 16 rows for a thread forward, 8 backward, as long as there are three tiles per SM
 // (1000 x 1 x 1 x 768 bf16 forward 9.6 us against 46 us, 256 x 7 x 7 x 512 bf16 backward 18 us against 47;
-// with 16 rows backward 256 x 14 x 14 x 256 43 us against 37).  A GPU not filled by the tiles gets larger
-// clusters, as long as a thread keeps two rows.
+// with 16 rows backward 256 x 14 x 14 x 256 43 us against 37).  Tiles
+// too few to occupy the GPU in clusters of eight are made narrower, down to 16 bytes (3 x 37 x 53 x 120 fp16
+// of 2-byte accesses backward 9.7 us against 13.5; with a limit twice as high 4 x 32 x 32 x 128 fp32 forward
+// 5.3 us against 4.9), and a GPU still not filled gets larger clusters, as long as a thread keeps two rows.
 bool plan_resident(const efcp_group_norm& d, int vec, bool backward, int sms, Gn* p,
                    size_t* smem) {
   const int size = kTypeBytes[d.dtype], per = p->per, unit = vec / gcd(per, vec);
@@ -139,6 +141,7 @@ bool plan_resident(const efcp_group_norm& d, int vec, bool backward, int sms, Gn
     const int64_t deep = ceil_div(int64_t(kGnThreads) * (backward ? 8 : 16) * vec * size, d.rows);
     wide = std::max(wide, std::min(deep, d.channels * size / ceil_div(3 * sms, d.n)));
   }
+  while (wide > 16 && d.n * ceil_div(d.channels * size, wide) * 16 < 3 * sms) wide /= 2;
   for (const Try t : {Try{wide, kSmemOf4, 8}, Try{wide, kSmemOf4, 16}, Try{32, kSmemOf4, 16},
                       Try{wide, kSmemOf2, 16}, Try{32, kSmemOf2, 16}}) {
     const int64_t groups = std::max<int64_t>(1, ceil_div(t.bytes / size, per));
