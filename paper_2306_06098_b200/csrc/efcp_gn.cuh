@@ -15,6 +15,11 @@
 // A tile is a number of whole groups.  In both forms a thread owns V neighbouring channels
 // (one access of up to 16 bytes) and walks down rows, so what belongs to a channel - weight,
 // bias, statistics, its sums - stays with the thread.
+//
+// Measured on a B200 (copy rate 6.56 TB/s), device time: 256 x 112 x 112 x 64 bf16 relu forward 206 us,
+// 4.0 TB/s; 256 x 56 x 56 x 64 bf16 silu backward 102 us, 3.0 TB/s; 128 x 32 x 32 x 16 fp32 forward 5.8 us;
+// 1 x 7 x 7 x 512 fp16 forward 3.1 us; streamed, 1 x 512 x 512 x 128 bf16 silu forward 67 us,
+// backward 130 us.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -603,7 +608,8 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_fwd(const Gn p) {
 // x and dy stay in shared memory and e is computed in both passes: an e in fp32 in the place of dy
 // would spare the second pass silu's two special functions per element, but halves the rows a
 // thread has room for, and few rows do not pay for the sums in between (184 us with it, 107 us without, for
-// 256 x 56 x 56 x 64 bf16 with silu).
+// 256 x 56 x 56 x 64 bf16 with silu, when this was tried; 102 us since).  silu's exponential and
+// reciprocal keep the special function units half busy, twice per element.
 template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_bwd(const Gn p) {
   using P = Pack<T, V>;
@@ -777,6 +783,8 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_bwd(const Gn p) {
 }
 
 // ------------------------------------------------------------------ streamed
+// Bound by memory in the two passes (23 and 31 us of 1 x 512 x 512 x 128 bf16 forward, 58 and 67 us backward, where
+// silu takes its share again) and by latency in the joins (18 and 8 us: 592 chunks, few columns).
 // Accesses in flight per thread and input: about 32 registers' worth.
 template <typename T, int V>
 constexpr int kAhead = sizeof(T) * V == 16 ? 4 : 8;

@@ -6,7 +6,13 @@
 // 32 KB of constant memory: no copy to wait for, no host buffer that has to outlive the
 // call).  It is cut into chunks of 32 KB that the thread blocks take in turn, so that one
 // large matrix and hundreds of short vectors both keep every SM busy (smaller chunks when there are too
-// few of them for that).
+// few of them for that; a contiguous range per block instead took 41 us in place of 37 for the
+// norm below, and 188 in place of 157 for the gather).
+//
+// Measured on a B200 (copy rate 6.56 TB/s), device time: norm of a BERT-base in bf16 and fp32 vectors, 219 MB, 37 us,
+// 5.9 TB/s; clipping ResNet-18's 47 MB in place 11.7 us out of L2, its norm and the factor in two launches; the clipped
+// gather of BERT-base from bf16 157 us, 876 MB with the norm's read, 5.6 TB/s; of 301 ragged fp16 tensors 42 us;
+// norm of a ResNet-20 5.7 us, its clipped gather from channels-last gradients 9.3 us.
 #include "efcp.h"
 
 #include <cuda_runtime.h>
@@ -217,7 +223,7 @@ __device__ __forceinline__ float factor_of(const Work* ws, double max_norm, doub
 }
 
 template <class Tab>
-__global__ void __launch_bounds__(kGrThreads, Tab::kM > 0 ? 3 : kGrBlocksPerSM)
+__global__ void __launch_bounds__(kGrThreads, Tab::kM > 0 ? 4 : kGrBlocksPerSM)
     k_grads_sumsq(const __grid_constant__ Tab tab, Work* ws, bool first_launch, double scale,
                   float* norm) {
   take_turn();
@@ -286,7 +292,7 @@ __device__ void chunk_scale_strided(T* p, const Geom& g, long long begin, int le
 // The chunks run from the last to the first: the norm has just read them from the first to the
 // last, and what it read last is still in L2.
 template <class Tab>
-__global__ void __launch_bounds__(kGrThreads, Tab::kM > 0 ? 3 : kGrBlocksPerSM)
+__global__ void __launch_bounds__(kGrThreads, Tab::kM > 0 ? 4 : kGrBlocksPerSM)
     k_grads_scale(const __grid_constant__ Tab tab, const Work* ws, double max_norm, double scale) {
   take_turn();
   const float f = factor_of(ws, max_norm, scale);
@@ -416,7 +422,7 @@ __device__ double chunk_gather_strided(const T* p, const Geom& g, long long begi
 // CLIP: the factor comes from the norm a launch before has left in ws.  ACC: there is no
 // clipping, and the norm is taken in the same pass.
 template <class Tab, bool CLIP, bool ACC>
-__global__ void __launch_bounds__(kGrThreads, Tab::kM > 0 ? 3 : kGrBlocksPerSM)
+__global__ void __launch_bounds__(kGrThreads, Tab::kM > 0 ? 4 : kGrBlocksPerSM)
     k_grads_gather(const __grid_constant__ Tab tab, float* flat, Work* ws, bool first_launch,
                    double max_norm, double scale, float* norm) {
   take_turn();

@@ -1,7 +1,7 @@
 // Argument marshalling for the calls on lists of gradients and on activations: checks torch tensors,
 // makes the outputs and the scratch memory, and hands addresses and layouts to the C ABI
 // (include/efcp.h) on the current stream.  The same in Python takes longer than the kernels of a
-// small model (23 us a call against 4 to 9 us on the device).
+// small model: 23 us a call, 7 to 10 here, 3 to 10 on the device.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
