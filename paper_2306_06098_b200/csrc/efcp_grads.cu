@@ -327,7 +327,8 @@ __device__ __forceinline__ float scaled(float v, float f) {
 
 // One chunk into the flat vector; with ACC its sum of squares is returned.  A thread stores four
 // elements at a time, at 16-byte boundaries of the flat vector; it loads them by one access where the
-// source is aligned to that, and one by one, out of L1, where it is not.
+// source is aligned to that, and one by one, out of L1, where it is not (cutting them out of two
+// aligned accesses was slower: 45 us against 42 for the 301 ragged fp16 tensors).
 // U: such stores under way at a time.
 template <typename T, bool ACC, int U, class Load>
 __device__ __forceinline__ double gather_by_fours(float* dst, int len, float f, Load load) {
