@@ -1159,7 +1159,6 @@ cudaError_t launch_act(const Gn& p, const GnLaunch& l) {
   }
   const Shape sums{l.blocks, kGnThreads, size_t(gn_streamed_floats(p.val_floats, l.backward)) * 4, 0};
   const int joins = ((l.backward ? p.channels : p.groups) + 31) / 32;
-  if (p.n * joins >= (1ll << 31)) return cudaErrorInvalidConfiguration;
   const Shape join{unsigned(p.n * joins), 32 * kGnSumWarps, 0, 0};
   const Shape apply{l.blocks, kGnThreads, l.backward ? size_t(p.tile_groups) * 8 : 0, 0};
   cudaError_t e;

@@ -214,7 +214,9 @@ int make_plan(const efcp_group_norm& d, const Tensor* t, int nt, bool backward, 
   l.resident = plan_resident(d, l.vec, backward, sms, &p, &l.smem);
   if (!l.resident) plan_streamed(d, l.vec, sms, &p);
   const int64_t blocks = d.n * p.tiles * p.chunks;
-  if (blocks >= (1ll << 31) || d.n * d.groups >= (1ll << 33)) return EFCP_ETOOBIG;
+  const int64_t joins = d.n * ceil_div(backward ? d.channels : d.groups, 32);
+  if (blocks >= (1ll << 31) || joins >= (1ll << 31) || d.n * d.groups >= (1ll << 33))
+    return EFCP_ETOOBIG;
   l.blocks = unsigned(blocks);
   out->part = out->total = 0;
   if (backward) {

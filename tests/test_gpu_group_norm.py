@@ -143,6 +143,26 @@ def test_forward(size, dtype):
     check_forward(inputs(n, c, pos, dtype, 3, mean=0.5), groups, w, b, act=act)
 
 
+# where the cut into tiles and blocks changes: many samples of few rows (wide tiles), few samples
+# (narrow ones), odd channel counts whose columns do not fill the threads, samples too large to stay on chip
+CUTS = [
+    (600, 96, 12, (1,)), (500, 200, 8, (2, 3)), (450, 130, 26, (3, 3)), (460, 185, 37, (4,)),
+    (445, 64, 8, (8, 8)), (1, 35, 7, (40, 53)), (2, 33, 11, (100, 30)), (1, 256, 32, (14, 14)),
+    (4, 185, 37, (50, 50)), (2, 130, 26, (128, 128)), (1, 1260, 42, (60, 60)),
+    (2, 320, 32, (160, 160)), (3, 65, 13, (200, 160)),
+]
+
+
+@pytest.mark.parametrize("dtype", list(HALF_ULP))
+@pytest.mark.parametrize("size", CUTS)
+def test_where_the_work_is_cut_differently(size, dtype):
+    n, c, groups, pos = size
+    w, b = rand((c,), 1, mean=1.0, size=0.3), rand((c,), 2, size=0.3)
+    x = inputs(n, c, pos, dtype, 3, mean=0.5)
+    check_forward(x, groups, w, b, act="silu")
+    check_backward(inputs(n, c, pos, dtype, 4), x, groups, w, b, 1e-3, "silu")
+
+
 def away_from_the_jump(x, groups, w, b, eps):
     """relu's derivative jumps at z = 0: values of x whose z is too near for fp32 to tell the side
     are moved until there are none."""
