@@ -190,7 +190,8 @@ __device__ __forceinline__ float bias_of(const Gn& p, int c) {
 }
 
 // Sum over groups of neighbouring lanes (a power of two of them), the same in all of them.
-__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+template <typename F>
+__device__ __forceinline__ F lanes_sum(F v, int lanes) {
   for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
   return v;
 }
@@ -259,13 +260,16 @@ __device__ __forceinline__ void sum_rows(const Gn& p, const Item& it, const floa
   }
 }
 
-// Mean and sum of squared deviations of `cnt` values per channel, the mean as k + m: k is one of
-// the values, so that a mean far from zero does not round away the deviations.  Parts are joined by
+// Mean and sum of squared deviations M2 of `cnt` values per channel.  Parts are joined by
 //     mean = sum n_i mean_i / sum n_i,   M2 = sum M2_i + n_i (mean_i - mean)^2,
-// sums without cancellation whatever the data.
+// sums without cancellation whatever the data.  The means are held and joined in 64 bits: every join in
+// fp32 would round by up to half a unit of the parts' distance from each other, and a chain of them is
+// further off than one sum over the group in fp32 (128 x 32 x 32 x 16 fp32: mean and y off by 2.3e-7 with fp32
+// joins, 6.7e-8 now; it costs the small calls 0.3 us on the device, 6.0 for 5.7 there).
 template <int V>
 struct Stats {
-  Vec<V> k, m, q;
+  double mean[V];
+  Vec<V> q;  // M2
   float cnt;
 };
 
@@ -277,10 +281,13 @@ __device__ __forceinline__ Stats<V> stats_of(int n, const Vec<V>& k, const Vec<V
                                              const Vec<V>& s2) {
   Stats<V> s;
   s.cnt = float(n);
-  s.k = k;
-  s.m = s1 * fill<V>(n ? rcp_fast(s.cnt) : 0.f);
+  const double inv = n ? 1.0 / double(n) : 0.0;
+  const Vec<V> m = s1 * fill<V>(float(inv));
 #pragma unroll
-  for (int j = 0; j < V; ++j) s.q.v[j] = fmaxf(0.f, fmaf(-s.m.v[j], s1.v[j], s2.v[j]));
+  for (int j = 0; j < V; ++j) {
+    s.mean[j] = __fma_rn(double(s1.v[j]), inv, double(k.v[j]));
+    s.q.v[j] = fmaxf(0.f, fmaf(-m.v[j], s1.v[j], s2.v[j]));
+  }
   return s;
 }
 
@@ -291,46 +298,39 @@ __device__ __forceinline__ Stats<V / 2> fold_once(const Stats<V>& s) {
   r.cnt = 2.f * s.cnt;
 #pragma unroll
   for (int j = 0; j < V / 2; ++j) {
-    const float d = (s.k.v[2 * j + 1] - s.k.v[2 * j]) + (s.m.v[2 * j + 1] - s.m.v[2 * j]);
-    r.k.v[j] = s.k.v[2 * j];
-    r.m.v[j] = fmaf(0.5f, d, s.m.v[2 * j]);
+    const float d = float(s.mean[2 * j + 1] - s.mean[2 * j]);
+    r.mean[j] = 0.5 * (s.mean[2 * j] + s.mean[2 * j + 1]);
     r.q.v[j] = fmaf(0.5f * s.cnt * d, d, s.q.v[2 * j] + s.q.v[2 * j + 1]);
   }
   return r;
 }
 
-// Joins the rows side by side as far as a warp reaches and stores what results in shared memory: four
-// sets (k, m, q and the counts) of p.val_rows rows of p.folded_cols values.
+// Joins the rows side by side as far as a warp reaches and stores what results in shared memory: p.val_rows
+// rows of p.folded_cols values each of the means (64 bits), of M2 and of the counts.
 template <int V>
 __device__ __forceinline__ void store_stats(const Gn& p, const Item& it, Stats<V> s, float* val) {
   int row = it.ty, col = it.tx;
   bool store = it.ty < p.lanes_rows;
   if (p.pitch_log >= 0) {
-    const int lane = int(threadIdx.x) & 31, first = lane & ((1 << p.pitch_log) - 1);
+    const int lane = int(threadIdx.x) & 31;
     row = int(threadIdx.x) >> 5;
     store = lane < p.cols;
-    // the rows of a warp ascend: where its first has no values, none has
     float all = s.cnt;
     for (int o = 1 << p.pitch_log; o < 32; o *= 2) all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
-    const float inv = all > 0.f ? rcp_fast(all) : 0.f;
-    Vec<V> sum;
+    const double inv = all > 0.f ? 1.0 / double(all) : 0.0;
+    double sum[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const float k0 = __shfl_sync(0xFFFFFFFFu, s.k.v[j], first);
-      s.m.v[j] = s.cnt > 0.f ? (s.k.v[j] - k0) + s.m.v[j] : 0.f;
-      s.k.v[j] = k0;
-      sum.v[j] = s.cnt * s.m.v[j];
-    }
+    for (int j = 0; j < V; ++j) sum[j] = double(s.cnt) * s.mean[j];
     for (int o = 1 << p.pitch_log; o < 32; o *= 2) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) sum.v[j] += __shfl_xor_sync(0xFFFFFFFFu, sum.v[j], o);
+      for (int j = 0; j < V; ++j) sum[j] += __shfl_xor_sync(0xFFFFFFFFu, sum[j], o);
     }
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      sum.v[j] *= inv;
-      const float d = s.m.v[j] - sum.v[j];
+      const double mean = sum[j] * inv;
+      const float d = float(s.mean[j] - mean);
       s.q.v[j] = fmaf(s.cnt * d, d, s.q.v[j]);
-      s.m.v[j] = sum.v[j];
+      s.mean[j] = mean;
     }
     for (int o = 1 << p.pitch_log; o < 32; o *= 2) {
 #pragma unroll
@@ -339,13 +339,14 @@ __device__ __forceinline__ void store_stats(const Gn& p, const Item& it, Stats<V
     s.cnt = all;
   }
   if (store) {
-    float* at = val + row * p.folded_cols + col * V;
+    const int at = row * p.folded_cols + col * V;
+    double* mean = reinterpret_cast<double*>(val) + at;
+    float *q = val + 2 * p.val_floats + at, *n = q + p.val_floats;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      at[j] = s.k.v[j];
-      at[p.val_floats + j] = s.m.v[j];
-      at[2 * p.val_floats + j] = s.q.v[j];
-      at[3 * p.val_floats + j] = s.cnt;
+      mean[j] = s.mean[j];
+      q[j] = s.q.v[j];
+      n[j] = s.cnt;
     }
   }
 }
@@ -360,39 +361,41 @@ __device__ __forceinline__ void fold_stats(const Gn& p, const Item& it, const St
   }
 }
 
-// The statistics of group g over the block, from what store_stats left (the caller has
+// Mean and M2 of group g over the block, from what store_stats left (the caller has
 // synchronised): the same in all of the group's lanes.  `rows`: of the block.
-__device__ __forceinline__ Stats<1> group_stats(const Gn& p, int g, bool exists, float rows,
-                                                const float* val) {
+struct Joined {
+  double mean;
+  float q;
+};
+__device__ __forceinline__ Joined group_stats(const Gn& p, int g, bool exists, float rows,
+                                              const float* val) {
   const int lanes = 1 << p.lanes_log, lane = int(threadIdx.x) & (lanes - 1);
   const int per = p.folded_per, used = p.folded_cols;
   // lanes over a row's values, or over the rows
   const bool along = per >= lanes;
   const int d0 = along ? lane : 0, dstep = along ? lanes : 1;
   const int t0 = along ? 0 : lane, tstep = along ? 1 : lanes;
-  const float* k = val + g * per;
-  const float *m = k + p.val_floats, *q = m + p.val_floats, *n = q + p.val_floats;
-  Stats<1> s;
-  s.cnt = rows * float(p.per);
-  s.k.v[0] = exists ? k[0] : 0.f;
-  float sum = 0.f;
+  const double* mean = reinterpret_cast<const double*>(val) + g * per;
+  const float *q = val + 2 * p.val_floats + g * per, *n = q + p.val_floats;
+  double sum = 0.0;
   if (exists) {
     for (int t = t0; t < p.val_rows; t += tstep)
       for (int d = d0; d < per; d += dstep)
-        sum = fmaf(n[t * used + d], (k[t * used + d] - s.k.v[0]) + m[t * used + d], sum);
+        sum = __fma_rn(double(n[t * used + d]), mean[t * used + d], sum);
   }
-  const float mean = rows > 0.f ? lanes_sum(sum, lanes) / s.cnt : lanes_sum(0.f, lanes);
-  sum = 0.f;
+  sum = lanes_sum(sum, lanes);
+  Joined s;
+  s.mean = rows > 0.f ? sum / (double(rows) * double(p.per)) : 0.0;
+  float m2 = 0.f;
   if (exists) {
     for (int t = t0; t < p.val_rows; t += tstep) {
       for (int d = d0; d < per; d += dstep) {
-        const float e = ((k[t * used + d] - s.k.v[0]) + m[t * used + d]) - mean;
-        sum += fmaf(n[t * used + d] * e, e, q[t * used + d]);
+        const float e = float(mean[t * used + d] - s.mean);
+        m2 += fmaf(n[t * used + d] * e, e, q[t * used + d]);
       }
     }
   }
-  s.m.v[0] = mean;
-  s.q.v[0] = lanes_sum(sum, lanes);
+  s.q = lanes_sum(m2, lanes);
   return s;
 }
 
@@ -510,9 +513,9 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_fwd(const Gn p) {
   float* cmean = val + 4 * p.val_floats;  // per channel: minus the mean,
   float* wei = cmean + wide;              // the weight, later times rstd,
   float* bia = wei + wide;                // the bias
-  float* bk = bia + wide;                 // per group the block's statistics, read by the others
-  float* bm = bk + tg;
-  float* bq = bm + tg;
+  // per group the block's mean and M2, read by the others
+  double* bm = reinterpret_cast<double*>(bia + wide);
+  float* bq = reinterpret_cast<float*>(bm + tg);
   // [row of this thread] [thread] of V elements
   Pack<T, V>* data = reinterpret_cast<Pack<T, V>*>(bq + tg) + int(threadIdx.x);
   const Item it = item_of<V>(p, cluster_rank(), cluster_index());
@@ -551,14 +554,13 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_fwd(const Gn p) {
   const int lanes = 1 << p.lanes_log, lane = int(threadIdx.x) & (lanes - 1);
   for (int g0 = 0; g0 < it.ng; g0 += kGnThreads >> p.lanes_log) {
     const int g = g0 + (int(threadIdx.x) >> p.lanes_log);
-    const Stats<1> s = group_stats(p, g, g < it.ng, rows, val);
+    const Joined s = group_stats(p, g, g < it.ng, rows, val);
     if (g < it.ng) {
       if (p.chunks == 1) {
-        finish_group(p, it, g, s.k.v[0] + s.m.v[0], s.q.v[0], cmean, wei, lane, lanes);
+        finish_group(p, it, g, float(s.mean), s.q, cmean, wei, lane, lanes);
       } else if (lane == 0) {
-        bk[g] = s.k.v[0];
-        bm[g] = s.m.v[0];
-        bq[g] = s.q.v[0];
+        bm[g] = s.mean;
+        bq[g] = s.q;
       }
     }
   }
@@ -570,19 +572,17 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_fwd(const Gn p) {
         float(max(0, min(int(p.chunk_rows), int(p.rows) - r * int(p.chunk_rows))));
     for (int g0 = 0; g0 < it.ng; g0 += kGnThreads >> p.links_log) {
       const int g = g0 + (int(threadIdx.x) >> p.links_log);
-      float k = 0.f, m = 0.f, q = 0.f;
+      double m = 0.0;
+      float q = 0.f;
       const bool there = g < it.ng && r < p.chunks && have > 0.f;
       if (there) {
-        k = cluster.map_shared_rank(bk, r)[g];
         m = cluster.map_shared_rank(bm, r)[g];
         q = cluster.map_shared_rank(bq, r)[g];
       }
-      const float k0 = __shfl_sync(0xFFFFFFFFu, k, int(threadIdx.x) & 31 & ~(links - 1));
-      m = there ? (k - k0) + m : 0.f;
-      const float mean = lanes_sum(have * m, links) * p.inv_rows;
-      const float d = m - mean;
+      const double mean = lanes_sum(there ? double(have) * m : 0.0, links) * p.inv_rows;
+      const float d = float(m - mean);
       q = lanes_sum(there ? fmaf(have * float(p.per) * d, d, q) : 0.f, links);
-      if (g < it.ng) finish_group(p, it, g, k0 + mean, q, cmean, wei, r, links);
+      if (g < it.ng) finish_group(p, it, g, float(mean), q, cmean, wei, r, links);
     }
   }
   __syncthreads();
@@ -789,7 +789,8 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_bwd(const Gn p) {
 template <typename T, int V>
 constexpr int kAhead = sizeof(T) * V == 16 ? 4 : 8;
 
-// The statistics of every group over a chunk of rows: k, m and q one after another.
+// The statistics of every group over a chunk of rows: the mean as two floats (its fp32 value and what
+// that leaves) and M2, one after another.
 template <typename T, int V>
 __global__ void __launch_bounds__(kGnThreads, 6) k_gn_stats(const Gn p) {
   constexpr int U = kAhead<T, V>;
@@ -832,11 +833,11 @@ __global__ void __launch_bounds__(kGnThreads, 6) k_gn_stats(const Gn p) {
   float* part = p.part + ((it.n * p.chunks + it.chunk) * p.groups + it.g0) * 3;
   for (int g0 = 0; g0 < it.ng; g0 += kGnThreads >> p.lanes_log) {
     const int g = g0 + (int(threadIdx.x) >> p.lanes_log);
-    const Stats<1> s = group_stats(p, g, g < it.ng, float(it.r1 - it.r0), val);
+    const Joined s = group_stats(p, g, g < it.ng, float(it.r1 - it.r0), val);
     if (g < it.ng && (int(threadIdx.x) & ((1 << p.lanes_log) - 1)) == 0) {
-      part[3 * g] = s.k.v[0];
-      part[3 * g + 1] = s.m.v[0];
-      part[3 * g + 2] = s.q.v[0];
+      part[3 * g] = float(s.mean);
+      part[3 * g + 1] = float(s.mean - double(part[3 * g]));
+      part[3 * g + 2] = s.q;
     }
   }
 }
@@ -846,12 +847,13 @@ __global__ void __launch_bounds__(kGnThreads, 6) k_gn_stats(const Gn p) {
 constexpr int kGnSumWarps = 32;
 
 // Sum over the block's warps of their lane's value, in a fixed order, the same in all of them.
-__device__ __forceinline__ float warps_sum(float v, float (*sh)[32]) {
+template <typename F>
+__device__ __forceinline__ F warps_sum(F v, F (*sh)[32]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   __syncthreads();
   sh[warp][lane] = v;
   __syncthreads();
-  float s = 0.f;
+  F s = 0;
 #pragma unroll 8
   for (int k = 0; k < kGnSumWarps; ++k) s += sh[k][lane];
   return s;
@@ -859,6 +861,7 @@ __device__ __forceinline__ float warps_sum(float v, float (*sh)[32]) {
 
 // mean and rstd of a sample's groups from the chunks' statistics
 __global__ void __launch_bounds__(32 * kGnSumWarps) k_gn_join_stats(const Gn p, int blocks) {
+  __shared__ double wide[kGnSumWarps][32];
   __shared__ float sh[kGnSumWarps][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long n = blockIdx.x / unsigned(blocks);
@@ -867,24 +870,22 @@ __global__ void __launch_bounds__(32 * kGnSumWarps) k_gn_join_stats(const Gn p, 
   const float* part = p.part + (n * p.chunks * p.groups + (on ? g : 0)) * 3;
   const long long pitch = 3ll * p.groups;
   take_turn();
-  const float k0 = part[0];
-  float s = 0.f;
+  const auto mean_of = [&](int c) { return double(part[c * pitch]) + double(part[c * pitch + 1]); };
+  double s = 0.0;
 #pragma unroll 4
-  for (int c = warp; c < p.chunks; c += kGnSumWarps) {
-    const float have = float(min(p.chunk_rows, p.rows - c * p.chunk_rows));
-    s = fmaf(have, (part[c * pitch] - k0) + part[c * pitch + 1], s);
-  }
-  const float mean = warps_sum(s, sh) / float(p.rows);
+  for (int c = warp; c < p.chunks; c += kGnSumWarps)
+    s = __fma_rn(double(min(p.chunk_rows, p.rows - c * p.chunk_rows)), mean_of(c), s);
+  const double mean = warps_sum(s, wide) / double(p.rows);
   float m2 = 0.f;
 #pragma unroll 4
   for (int c = warp; c < p.chunks; c += kGnSumWarps) {
     const float have = float(min(p.chunk_rows, p.rows - c * p.chunk_rows)) * float(p.per);
-    const float d = ((part[c * pitch] - k0) + part[c * pitch + 1]) - mean;
+    const float d = float(mean_of(c) - mean);
     m2 += fmaf(have * d, d, part[c * pitch + 2]);
   }
   m2 = warps_sum(m2, sh);
   if (on && warp == 0) {
-    p.mean[n * p.groups + g] = k0 + mean;
+    p.mean[n * p.groups + g] = float(mean);
     p.rstd[n * p.groups + g] = rsqrtf(m2 / (float(p.rows) * float(p.per)) + p.eps);
   }
 }

@@ -41,7 +41,8 @@ struct Gn {
   int folded_cols, folded_per;    // values of a row, and of a group in it, after adding those
   int val_rows, val_floats;       // rows of partial sums in shared memory; floats of one set
   int links_log;                  // 2^links_log lanes join the blocks of a cluster
-  float inv_rows, inv_total;      // 1 / rows, 1 / (rows per)
+  double inv_rows;                // 1 / rows
+  float inv_total;                // 1 / (rows per)
   int param_dtype;
   float eps;
 };

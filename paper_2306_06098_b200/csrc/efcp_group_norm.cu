@@ -202,7 +202,7 @@ int make_plan(const efcp_group_norm& d, const Tensor* t, int nt, bool backward, 
   p.per = int(d.channels / d.groups);
   p.param_dtype = d.param_dtype;
   p.eps = d.eps;
-  p.inv_rows = float(1.0 / double(d.rows));
+  p.inv_rows = 1.0 / double(d.rows);
   p.inv_total = float(1.0 / (double(d.rows) * double(p.per)));
   p.x_batch = d.x_batch; p.x_row = d.x_row;
   p.y_batch = d.y_batch; p.y_row = d.y_row;

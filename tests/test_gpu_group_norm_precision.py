@@ -1,0 +1,53 @@
+"""Group norm: how exact the statistics are, against 64 bits, where sums in fp32 are easily spoilt."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = (torch.float32, torch.bfloat16, torch.float16)
+
+
+def channels_last(n, c, pos, dtype, seed, spread=True):
+    """(n, c, *pos), channels last; with `spread` the channels differ in mean and size."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn((n, *pos, c), generator=g, device="cuda")
+    if spread:
+        x.mul_(torch.exp(0.3 * torch.randn(c, generator=g, device="cuda")))
+        x.add_(torch.randn(c, generator=g, device="cuda"))
+    return x.to(dtype).permute(0, len(pos) + 1, *range(1, len(pos) + 1))
+
+
+def statistics64(x, groups, eps=1e-5):
+    v = x.double().reshape(x.shape[0], groups, -1)
+    mean = v.mean(2, keepdim=True)
+    var = (v - mean).square().mean(2)
+    return mean[..., 0], (var + eps).rsqrt(), var.sqrt()
+
+
+def statistics(x, groups):
+    from paper_2306_06098_b200 import binding
+    return binding.group_norm_forward(x, groups)[1:]
+
+
+# one block a sample, clusters, several tiles, every access width, samples that are streamed
+SIZES = [(128, 16, 8, (32, 32)), (2, 1380, 23, (24, 5)), (25, 300, 5, (68, 3)), (43, 58, 2, (3, 2)), (2, 68, 4, (8, 37)),
+         (144, 114, 3, (1, 32)), (2, 1036, 28, (101, 61)), (161, 444, 12, (43, 3)), (1, 128, 32, (130, 130)),
+         (3, 65, 13, (200, 160)), (64, 64, 32, (56, 56))]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", SIZES)
+def test_error_of_the_mean(size, dtype):
+    n, c, groups, pos = size
+    x = channels_last(n, c, pos, dtype, 5)
+    mean, _ = statistics(x, groups)
+    m64, _, sigma = statistics64(x, groups)
+    # rounding the result: U |mean| at most.  A thread's fp32 sum of n <= 64 differences of about
+    # sigma: its partial sums grow to n sigma, their roundings together to U sigma sqrt(n) / 3
+    # <= 2.7 U sigma, and the independent ones of the group's 16 threads and more average out to
+    # less than 0.7 U sigma.  What follows is held in 64 bits.
+    err = (mean.double() - m64).square().mean().sqrt().item()
+    assert err <= U * (sigma + m64.abs()).square().mean().sqrt().item(), err / U
