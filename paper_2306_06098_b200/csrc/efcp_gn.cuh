@@ -148,6 +148,13 @@ __device__ __forceinline__ Vec<V> operator*(const Vec<V>& a, const Vec<V>& b) {
   }
   return r;
 }
+template <int V>
+__device__ __forceinline__ Vec<V> minus(Vec<V> a) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) a.v[j] = -a.v[j];
+  return a;
+}
+
 template <typename T, int V>
 __device__ __forceinline__ Vec<V> unpack(const Pack<T, V>& a) {
   Vec<V> r;
@@ -273,23 +280,85 @@ struct Stats {
   float cnt;
 };
 
-// From the sums of d = x - k and of d^2 over n rows, k being the first of the values.  Since k is one
-// of them, (k - mean)^2 is at most their sum of squared deviations, and what the subtraction of
-// n (k - mean)^2 loses stays below n 2^-24 of the result, n <= 64.
+// A thread's own values: sums of d = x - k and of d^2 over n of them, then M2 = sum d^2 - (sum d)^2 / n.
+// The subtraction loses what the squares' sum is larger than M2, a factor of 1 + n (k - mean)^2 / M2,
+// so k has to be near the mean whatever the data.  With k a mean of c of the values, (k - mean)^2 is at most
+// M2 / c, and the factor at most 1 + n / c: 9 on chip (n <= 32 and c = 4, n <= 64 and c = 8).  (k the first value: up to n + 1, rstd
+// off by 520 units of 2^-24 where columns of 64 values begin with one far from the rest.)
+
+// M2 of n values from those sums; `inv` = 1 / n.
+__device__ __forceinline__ float m2_of(float s1, float s2, float inv) {
+  return fmaxf(0.f, fmaf(-(s1 * inv), s1, s2));
+}
+
 template <int V>
 __device__ __forceinline__ Stats<V> stats_of(int n, const Vec<V>& k, const Vec<V>& s1,
                                              const Vec<V>& s2) {
   Stats<V> s;
   s.cnt = float(n);
   const double inv = n ? 1.0 / double(n) : 0.0;
-  const Vec<V> m = s1 * fill<V>(float(inv));
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     s.mean[j] = __fma_rn(double(s1.v[j]), inv, double(k.v[j]));
-    s.q.v[j] = fmaxf(0.f, fmaf(-m.v[j], s1.v[j], s2.v[j]));
+    s.q.v[j] = m2_of(s1.v[j], s2.v[j], float(inv));
   }
   return s;
 }
+
+// The same for values that come a batch at a time: segments of at most twice as many values as came before,
+// each around the mean so far (a factor of 3 at most), joined one after another.  Segments end at 64
+// values, so that the sums of a long run (a group wider than the block) stay short too.
+template <int V>
+struct Running {
+  Vec<V> neg = fill<V>(0.f);  // minus the mean of the n values joined
+  Vec<V> q = neg, s1 = neg, s2 = neg;
+  int n = 0, open = 0;  // values joined, of the segment
+
+  // m > 0 of the U values of a batch exist.
+  template <typename T, int U>
+  __device__ __forceinline__ void add(const Pack<T, V> (&a)[U], int m) {
+    if (n == 0) {  // the first segment is this batch, around its own mean
+      const Vec<V> first = minus(unpack(a[0]));
+      Vec<V> s = fill<V>(0.f);
+#pragma unroll
+      for (int u = 1; u < U; ++u)
+        if (u < m) s = s + (unpack(a[u]) + first);
+      neg = fma(s, fill<V>(-rcp_fast(float(m))), first);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u < m) {
+        const Vec<V> d = unpack(a[u]) + neg;
+        s1 = s1 + d;
+        s2 = fma(d, d, s2);
+      }
+    }
+    open += m;
+    if (open >= min(64, 2 * n)) join();
+  }
+  __device__ __forceinline__ void join() {
+    if (open == 0) return;
+    const float inv = rcp_fast(float(open)), w = float(open) * rcp_fast(float(n + open));
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float d = s1.v[j] * inv;
+      q.v[j] += fmaf(float(n) * w * d, d, m2_of(s1.v[j], s2.v[j], inv));
+      neg.v[j] = fmaf(-w, d, neg.v[j]);
+    }
+    s1 = s2 = fill<V>(0.f);
+    n += open;
+    open = 0;
+  }
+  __device__ __forceinline__ Stats<V> done() {
+    join();
+    Stats<V> s;
+    s.cnt = float(n);
+    s.q = q;
+#pragma unroll
+    for (int j = 0; j < V; ++j) s.mean[j] = -double(neg.v[j]);
+    return s;
+  }
+};
 
 // Neighbouring channels of one group joined.
 template <int V>
@@ -436,13 +505,6 @@ __device__ __forceinline__ Vec<V> of_channels(const float* values, int c) {
   }
   return r;
 }
-template <int V>
-__device__ __forceinline__ Vec<V> minus(Vec<V> a) {
-#pragma unroll
-  for (int j = 0; j < V; ++j) a.v[j] = -a.v[j];
-  return a;
-}
-
 // The place of a block in its cluster, and of the cluster in the grid.
 __device__ __forceinline__ unsigned cluster_rank() {
   unsigned r;
@@ -535,18 +597,27 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_fwd(const Gn p) {
   }
   copies_done();
   {
-    Vec<V> k0 = fill<V>(0.f), s1 = k0, s2 = k0;
+    Vec<V> centre = fill<V>(0.f), s1 = centre, s2 = centre;
     if (mine) {
-      k0 = unpack(data[0]);
-      const Vec<V> neg = minus(k0);
+      // of 4 rows, of 8 where there are more than 32, spread over the thread's (fewer come twice)
+      const int some = mine > 32 ? 3 : 2;
+      const Vec<V> first = unpack(data[0]), from = minus(first);
+      for (int h = 0; h < (mine > 1 ? 1 << some : 0); h += 4) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          s1 = s1 + (unpack(data[((h + k) * mine >> some) * kGnThreads]) + from);
+      }
+      centre = fma(s1, fill<V>(some == 3 ? 0.125f : 0.25f), first);
+      s1 = fill<V>(0.f);
+      const Vec<V> neg = minus(centre);
 #pragma unroll 4
-      for (int k = 1; k < mine; ++k) {
+      for (int k = 0; k < mine; ++k) {
         const Vec<V> d = unpack(data[k * kGnThreads]) + neg;
         s1 = s1 + d;
         s2 = fma(d, d, s2);
       }
     }
-    fold_stats(p, it, stats_of(mine, k0, s1, s2), p.fold, val);
+    fold_stats(p, it, stats_of(mine, centre, s1, s2), p.fold, val);
   }
   __syncthreads();
   cg::cluster_group cluster = cg::this_cluster();
@@ -789,46 +860,37 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_bwd(const Gn p) {
 template <typename T, int V>
 constexpr int kAhead = sizeof(T) * V == 16 ? 4 : 8;
 
+// (Six blocks an SM, as k_gn_apply has, would spill here: 68 us against 65.5 for the call above.)
 // The statistics of every group over a chunk of rows: the mean as two floats (its fp32 value and what
 // that leaves) and M2, one after another.
 template <typename T, int V>
-__global__ void __launch_bounds__(kGnThreads, 6) k_gn_stats(const Gn p) {
+__global__ void __launch_bounds__(kGnThreads, 5) k_gn_stats(const Gn p) {
   constexpr int U = kAhead<T, V>;
   extern __shared__ __align__(32) float sm[];
   float* val = sm;
   const Item it = item_of<V>(p, blockIdx.x % unsigned(p.chunks), blockIdx.x / unsigned(p.chunks));
   take_turn();
   const T* x = static_cast<const T*>(p.x) + it.n * p.x_batch + it.c0;
-  Vec<V> k0 = fill<V>(0.f), s1 = k0, s2 = k0, neg = k0;
-  int n = 0;
+  Running<V> sums;
   if (it.on) {
     // (more than one round only where a single group is wider than the block)
     for (int c = it.tx; c < it.width / V; c += p.cols) {
       for (long long r = it.r0 + it.ty; r < it.r1; r += U * p.lanes_rows) {
         Pack<T, V> a[U];
+        int m = 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const long long rr = r + (long long)u * p.lanes_rows;
-          if (rr < it.r1) a[u] = load_pack<T, V>(x + rr * p.x_row + (long long)c * V);
-        }
-        if (!n) {
-          k0 = unpack(a[0]);
-          neg = minus(k0);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if (r + (long long)u * p.lanes_rows < it.r1) {
-            const Vec<V> d = unpack(a[u]) + neg;
-            ++n;
-            s1 = s1 + d;
-            s2 = fma(d, d, s2);
+          if (rr < it.r1) {
+            a[u] = load_pack<T, V>(x + rr * p.x_row + (long long)c * V);
+            m = u + 1;
           }
         }
+        sums.add(a, m);
       }
     }
   }
-  Stats<V> st = stats_of(n, k0, s1, s2);
-  fold_stats(p, it, st, p.fold, val);
+  fold_stats(p, it, sums.done(), p.fold, val);
   __syncthreads();
   float* part = p.part + ((it.n * p.chunks + it.chunk) * p.groups + it.g0) * 3;
   for (int g0 = 0; g0 < it.ng; g0 += kGnThreads >> p.lanes_log) {

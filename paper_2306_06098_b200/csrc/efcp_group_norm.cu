@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kTypeBytes[3] = {4, 2, 2};
 constexpr int kStreamedBlocksPerSM = 4;
-constexpr int kMaxRowsPerThread = 64;  // see the error bound in efcp_gn.cuh
+constexpr int kMaxRowsPerThread = 64;  // keeps a thread's sums short: see Stats in efcp_gn.cuh
 
 bool valid(const efcp_group_norm* d) {
   if (!d || d->n < 0 || d->rows < 1 || d->channels < 1 || d->groups < 1) return false;

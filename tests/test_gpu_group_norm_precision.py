@@ -51,3 +51,39 @@ def test_error_of_the_mean(size, dtype):
     # less than 0.7 U sigma.  What follows is held in 64 bits.
     err = (mean.double() - m64).square().mean().sqrt().item()
     assert err <= U * (sigma + m64.abs()).square().mean().sqrt().item(), err / U
+
+
+# groups of one channel (a thread then has a whole column, or a chunk of it, to itself) and larger
+# ones; resident and streamed
+FIRST = [(3, 127, 127, (64,)), (400, 7, 7, (1152,)), (8, 32, 32, (16, 16)), (1, 512, 512, (150, 150)), (2, 130, 26, (128, 128)),
+         (400, 8, 1, (4096,)), (1, 8, 2, (64, 64)), (1, 1030, 1, (3, 5))]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("far", [1, 2, 18, 64])
+@pytest.mark.parametrize("size", FIRST)
+def test_first_positions_far_from_the_rest(size, far, dtype):
+    """A border of other values, where every thread's sums begin."""
+    n, c, groups, pos = size
+    x = channels_last(n, c, (math.prod(pos),), dtype, 6, spread=False)
+    x = x.clone(memory_format=torch.preserve_format)
+    x[:, :, :far] += 1000.0
+    mean, rstd = statistics(x, groups)
+    m64, r64, sigma = statistics64(x, groups)
+    # a thread's squares add up to at most 9 times its sum of squared deviations (the centre is the
+    # mean of eight of its values, or of an eighth); 64 of them in fp32 come within 4 U as a rule, all
+    # columns taken 6 U: 54 U, halved by the root; joins and the root itself a few U
+    assert ((rstd.double() - r64).abs() <= r64 * 36 * U).all(), ((rstd / r64 - 1).abs().max() / U).item()
+    assert ((mean.double() - m64).abs() <= 16 * U * (sigma + m64.abs())).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [1, 3])
+@pytest.mark.parametrize("c", [65_537, 300_001, 1_048_577, 262_144])
+def test_one_group_of_very_many_channels(c, rows, dtype):
+    x = channels_last(1, c, (rows,), dtype, 7, spread=False).clone(memory_format=torch.preserve_format)
+    x[:, :128] += 1000.0  # where a thread's sums begin
+    mean, rstd = statistics(x, 1)
+    m64, r64, sigma = statistics64(x, 1)
+    assert ((rstd.double() - r64).abs() <= r64 * 36 * U).all(), ((rstd / r64 - 1).abs().max() / U).item()
+    assert ((mean.double() - m64).abs() <= 16 * U * (sigma + m64.abs())).all()
