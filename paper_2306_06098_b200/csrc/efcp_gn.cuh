@@ -215,7 +215,7 @@ __device__ __forceinline__ Vec<V> sigmoid_of(const Vec<V>& z) {
   for (int j = 0; j < V; ++j) t.v[j] = rcp_fast(t.v[j]);
   return t;
 }
-// act(z) and act'(z)
+// act(z)
 template <int ACT, int V>
 __device__ __forceinline__ Vec<V> act_of(Vec<V> z) {
   if (ACT == EFCP_ACT_RELU) {
@@ -225,19 +225,18 @@ __device__ __forceinline__ Vec<V> act_of(Vec<V> z) {
   if (ACT == EFCP_ACT_SILU) z = z * sigmoid_of(z);
   return z;
 }
+// dy act'(z).  relu's derivative selects: what arrives where it is 0 does not matter, infinite or not.
 template <int ACT, int V>
-__device__ __forceinline__ Vec<V> act_grad(const Vec<V>& z) {
+__device__ __forceinline__ Vec<V> through_act(Vec<V> dy, const Vec<V>& z) {
   if (ACT == EFCP_ACT_RELU) {
-    Vec<V> r;
 #pragma unroll
-    for (int j = 0; j < V; ++j) r.v[j] = z.v[j] <= 0.f ? 0.f : 1.f;
-    return r;
+    for (int j = 0; j < V; ++j) dy.v[j] = z.v[j] <= 0.f ? 0.f : dy.v[j];
   }
   if (ACT == EFCP_ACT_SILU) {
     const Vec<V> s = sigmoid_of(z);
-    return s * fma(z, fma(s, fill<V>(-1.f), fill<V>(1.f)), fill<V>(1.f));
+    dy = dy * (s * fma(z, fma(s, fill<V>(-1.f), fill<V>(1.f)), fill<V>(1.f)));
   }
-  return fill<V>(1.f);
+  return dy;
 }
 
 // ------------------------------------------------------------------ sums inside a block
@@ -734,7 +733,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_bwd(const Gn p) {
     for (int k = 0; k < mine; ++k) {
       const Vec<V> u = unpack(xs[k * kGnThreads]) + m;
       Vec<V> e = unpack(ds[k * kGnThreads]);
-      if (ACT != EFCP_ACT_NONE) e = e * act_grad<ACT>(fma(u, f, b));
+      if (ACT != EFCP_ACT_NONE) e = through_act<ACT>(e, fma(u, f, b));
       s0 = fma(e, u, s0);
       s1 = s1 + e;
     }
@@ -846,7 +845,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_bwd(const Gn p) {
     for (int k = 0; k < mine; ++k, po += step) {
       const Vec<V> u = unpack(xs[k * kGnThreads]) + m;
       Vec<V> e = unpack(ds[k * kGnThreads]);
-      if (ACT != EFCP_ACT_NONE) e = e * act_grad<ACT>(fma(u, f, b));
+      if (ACT != EFCP_ACT_NONE) e = through_act<ACT>(e, fma(u, f, b));
       *reinterpret_cast<P*>(po) = pack<T, V>(fma(u * rs, qb, fma(e, f, qa)));
     }
   }
@@ -1071,7 +1070,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_bwd_sums(const Gn p) {
           if (r + (long long)u * p.lanes_rows < it.r1) {
             const Vec<V> q = unpack(a[u]) + ln.m;
             Vec<V> e = unpack(d[u]);
-            if (ACT != EFCP_ACT_NONE) e = e * act_grad<ACT>(fma(q, ln.f, ln.b));
+            if (ACT != EFCP_ACT_NONE) e = through_act<ACT>(e, fma(q, ln.f, ln.b));
             s0 = fma(e, q, s0);
             s1 = s1 + e;
           }
@@ -1158,7 +1157,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_bwd_apply(const Gn p) {
         if (rr < it.r1) {
           const Vec<V> q = unpack(a[u]) + ln.m;
           Vec<V> e = unpack(d[u]);
-          if (ACT != EFCP_ACT_NONE) e = e * act_grad<ACT>(fma(q, ln.f, ln.b));
+          if (ACT != EFCP_ACT_NONE) e = through_act<ACT>(e, fma(q, ln.f, ln.b));
           *reinterpret_cast<Pack<T, V>*>(dx + rr * p.y_row + (long long)c * V) =
               pack<T, V>(fma(q * ln.r, qb, fma(e, ln.f, qa)));
         }
