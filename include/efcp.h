@@ -457,7 +457,9 @@ typedef struct efcp_tensor {
  * Work runs on the current device and on `stream`, asynchronously, and can be captured in a graph.
  * EFCP_EINVAL (nothing enqueued): null or misaligned pointers, sizes that do not multiply to
  * numel, an unknown type, more than four dimensions after merging, overlapping elements in a
- * list to be clipped, a `d` that is not the sum of the numels, scalars out of range.
+ * list to be clipped, inside a tensor or of two (slices side by side, as the columns of a matrix, are
+ * told apart; layouts of unlike strides that interleave without sharing an element may be refused too), a
+ * `d` that is not the sum of the numels, scalars out of range.
  */
 int64_t efcp_grads_workspace_bytes(void);
 int efcp_grads_norm(const efcp_tensor* grads, int32_t n, float scale, float* norm,

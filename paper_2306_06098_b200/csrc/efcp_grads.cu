@@ -485,6 +485,7 @@ int merge_dims(const efcp_tensor& t, Dim (&dims)[EFCP_MAX_RANK]) {
   for (int k = t.rank - 1; k >= 0; --k) {
     const long long s = t.size[k], st = t.stride[k];
     if (s < 0 || st < 0) return -1;
+    if (s > 1 && st > (1ll << 56) / s) return -1;  // beyond any address space
     if (s != 0 && prod > t.numel / s) return -1;  // the product would exceed numel
     prod *= s;
     if (s == 1) continue;
@@ -516,6 +517,75 @@ Layout layout_of(const Dim* dims, int n, bool* overlaps) {
   }
   return dense ? Layout::kDense : Layout::kStrided;
 }
+
+// Whether two tensors of a list share a byte.  Their positions in bytes are
+//     a + sum i_k s_k  and  b + sum j_k t_k,   0 <= i_k < n_k, 0 <= j_k < m_k,
+// and they share one where the difference of two positions lies between minus the width of an element of the
+// one and the width of one of the other.  As a sum over all dimensions, largest stride first, every index is
+// bounded by what the smaller strides can still make up for, which for slices of one tensor (columns of a
+// matrix, channels of a kernel) leaves one or two values of it.  Layouts that need more than kShareSteps
+// steps count as sharing.
+class Sharing {
+ public:
+  struct Side {
+    long long at;  // address
+    int width, n;  // bytes of an element; dimensions
+    const Dim* dim;
+  };
+  static bool any(const Side& a, const Side& b) {
+    Sharing s;
+    for (const Side* t : {&a, &b}) {
+      for (int k = 0; k < t->n; ++k) {
+        if (t->dim[k].size < 2) continue;
+        const bool first = t == &a;
+        s.term_[s.terms_++] = {t->dim[k].stride * t->width, first ? 0 : 1 - t->dim[k].size,
+                               first ? t->dim[k].size - 1 : 0};
+      }
+    }
+    std::sort(s.term_, s.term_ + s.terms_, [](const Term& x, const Term& y) { return x.step > y.step; });
+    // equal strides are one term
+    int n = 0;
+    for (int k = 0; k < s.terms_; ++k) {
+      if (n && s.term_[n - 1].step == s.term_[k].step) {
+        s.term_[n - 1].lo += s.term_[k].lo;
+        s.term_[n - 1].hi += s.term_[k].hi;
+      } else {
+        s.term_[n++] = s.term_[k];
+      }
+    }
+    s.terms_ = n;
+    for (int k = n; k-- > 0;) {
+      s.low_[k] = s.low_[k + 1] + s.term_[k].step * s.term_[k].lo;
+      s.high_[k] = s.high_[k + 1] + s.term_[k].step * s.term_[k].hi;
+    }
+    // position in a minus position in b: above -width of a, below width of b
+    return s.reach(0, b.at - a.at - a.width + 1, b.at - a.at + b.width - 1);
+  }
+
+ private:
+  struct Term {
+    long long step, lo, hi;  // bytes; bounds of the index
+  };
+  static constexpr int kShareSteps = 4096;
+  Term term_[2 * EFCP_MAX_RANK];
+  long long low_[2 * EFCP_MAX_RANK + 1] = {}, high_[2 * EFCP_MAX_RANK + 1] = {};  // of the terms from k on
+  int terms_ = 0, steps_ = 0;
+
+  static long long floor_div(long long a, long long b) { return a / b - (a % b < 0); }
+  // Whether the terms from k on can add up to something from lo to hi.
+  bool reach(int k, long long lo, long long hi) {
+    if (++steps_ > kShareSteps) return true;
+    if (hi < low_[k] || lo > high_[k]) return false;
+    if (k == terms_) return true;
+    const Term& t = term_[k];
+    if (t.step == 0) return reach(k + 1, lo, hi);
+    const long long first = std::max(t.lo, -floor_div(high_[k + 1] - lo, t.step));
+    const long long last = std::min(t.hi, floor_div(hi - low_[k + 1], t.step));
+    for (long long i = first; i <= last; ++i)
+      if (reach(k + 1, lo - i * t.step, hi - i * t.step)) return true;
+    return false;
+  }
+};
 
 enum class Op { kNorm, kClip, kGather };
 
@@ -566,6 +636,50 @@ int read_list(const efcp_tensor* grads, int n, Op op, std::vector<Entry>* out, i
   }
   *sum = total;
   return EFCP_OK;
+}
+
+// Whether two of the tensors share memory.
+bool list_overlaps(const efcp_tensor* grads, int n) {
+  struct Range {
+    long long begin, end;  // addresses
+    int index;
+  };
+  std::vector<Range> r;
+  r.reserve(size_t(n));
+  const auto side = [&](int i, Dim (&dims)[EFCP_MAX_RANK]) {
+    const efcp_tensor& t = grads[i];
+    const int nd = merge_dims(t, dims);
+    return Sharing::Side{static_cast<long long>(reinterpret_cast<intptr_t>(t.data)),
+                         t.dtype == EFCP_F32 ? 4 : 2, nd, dims};
+  };
+  bool sorted = true;
+  long long reached = 0;
+  for (int i = 0; i < n; ++i) {
+    if (!grads[i].numel || !grads[i].data) continue;
+    Dim dims[EFCP_MAX_RANK];
+    const Sharing::Side s = side(i, dims);
+    long long last = 0;
+    for (int k = 0; k < s.n; ++k) last += (dims[k].size - 1) * dims[k].stride;
+    const Range q{s.at, s.at + (last + 1) * s.width, i};
+    sorted = sorted && q.begin >= reached;
+    reached = q.end;
+    r.push_back(q);
+  }
+  if (sorted) return false;
+  std::sort(r.begin(), r.end(), [](const Range& a, const Range& b) { return a.begin < b.begin; });
+  // ranges that begin inside an earlier one: that pair has to be looked at
+  std::vector<const Range*> open;
+  for (const Range& q : r) {
+    open.erase(std::remove_if(open.begin(), open.end(),
+                              [&](const Range* o) { return o->end <= q.begin; }),
+               open.end());
+    for (const Range* o : open) {
+      Dim a[EFCP_MAX_RANK], b[EFCP_MAX_RANK];
+      if (Sharing::any(side(o->index, a), side(q.index, b))) return true;
+    }
+    open.push_back(&q);
+  }
+  return false;
 }
 
 // n / d = n * mul >> shift for n < 2^31: with 2^b >= d, mul = floor(2^(31 + b) / d) + 1 is off from
@@ -747,6 +861,7 @@ int efcp_grads_clip(const efcp_tensor* grads, int32_t n, float max_norm, float s
     int64_t sum = 0;
     int rc = read_list(grads, n, Op::kClip, &list, &sum);
     if (rc != EFCP_OK) return rc;
+    if (list_overlaps(grads, n)) return EFCP_EINVAL;
     Args a{list, nullptr, double(max_norm), double(scale), norm, static_cast<Work*>(workspace),
            static_cast<cudaStream_t>(stream), device_sms(), 0};
     if (a.sms < 1) return EFCP_ECUDA;
