@@ -35,6 +35,8 @@ namespace {
 
 namespace cg = cooperative_groups;
 
+static_assert(kGnSmemOf2 <= int64_t(kMaxDynamicSmem), "what a launch may ask for");
+
 // What a thread block works on.
 struct Item {
   long long n, r0, r1;           // sample, rows r0 .. r1 of it (none when r1 <= r0)

@@ -58,6 +58,10 @@ struct GnLaunch {
   cudaStream_t st;
 };
 
+// Shared memory of a block when an SM is to hold four or two: of its 228 KB, 1 KB per block is
+// the system's.
+constexpr int64_t kGnSmemOf4 = 56 * 1024, kGnSmemOf2 = 113 * 1024;
+
 // Shared memory of the kernels (the arrays at their start say what for).  Resident: what does not
 // depend on the rows, and what a row of every thread takes.
 constexpr int64_t gn_resident_fixed_bytes(int64_t val_floats, int tile_groups, int width,

@@ -112,10 +112,6 @@ void set_tiles(const efcp_group_norm& d, int vec, int unit, int64_t groups, Gn* 
   }
 }
 
-// Shared memory of a block when an SM is to hold four or two: of its 228 KB, 1 KB per block is
-// the system's.
-constexpr int64_t kSmemOf4 = 56 * 1024, kSmemOf2 = 113 * 1024;
-
 // Whether a sample's tile fits on chip; then tiles, the cluster's size and the shared memory of a
 // block.  Narrow tiles come first, as they need smaller clusters: 64 bytes a row with 16-byte accesses
 // (256 x 28 x 28 x 128 bf16 forward 27 us against 29 us with 128), 128 with narrower ones
@@ -142,8 +138,8 @@ bool plan_resident(const efcp_group_norm& d, int vec, bool backward, int sms, Gn
     wide = std::max(wide, std::min(deep, d.channels * size / ceil_div(3 * sms, d.n)));
   }
   while (wide > 16 && d.n * ceil_div(d.channels * size, wide) * 16 < 3 * sms) wide /= 2;
-  for (const Try t : {Try{wide, kSmemOf4, 8}, Try{wide, kSmemOf4, 16}, Try{32, kSmemOf4, 16},
-                      Try{wide, kSmemOf2, 16}, Try{32, kSmemOf2, 16}}) {
+  for (const Try t : {Try{wide, kGnSmemOf4, 8}, Try{wide, kGnSmemOf4, 16}, Try{32, kGnSmemOf4, 16},
+                      Try{wide, kGnSmemOf2, 16}, Try{32, kGnSmemOf2, 16}}) {
     const int64_t groups = std::max<int64_t>(1, ceil_div(t.bytes / size, per));
     set_tiles(d, vec, unit, std::min(ceil_div(groups, unit) * unit, widest), p);
     set_layout(kGnThreads, vec, p);

@@ -15,12 +15,17 @@ __device__ __forceinline__ void take_turn() {
   asm volatile("griddepcontrol.launch_dependents;");
 }
 
+// The largest dynamic shared memory that a launch may ask for: an SM then holds two blocks.
+constexpr size_t kMaxDynamicSmem = 113 * 1024;
+
 struct Shape {
   unsigned blocks, threads;
   size_t smem;       // dynamic shared memory
   unsigned cluster;  // blocks of a cluster, 0: none
 };
 
+// A kernel's attributes belong to the device, and other host threads may launch the same kernel with other
+// shapes: they are set to the same values every time, never to this launch's own.
 template <class... P, class... A>
 cudaError_t launch(void (*kern)(P...), const Shape& s, cudaStream_t st, A&&... args) {
   if (s.cluster > 8) {
@@ -29,8 +34,9 @@ cudaError_t launch(void (*kern)(P...), const Shape& s, cudaStream_t st, A&&... a
     if (e != cudaSuccess) return e;
   }
   if (s.smem > 48 * 1024) {
+    if (s.smem > kMaxDynamicSmem) return cudaErrorInvalidValue;
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               int(s.smem));
+                                               int(kMaxDynamicSmem));
     if (e != cudaSuccess) return e;
   }
   cudaLaunchAttribute attr[2];
