@@ -91,6 +91,8 @@ class SparseMFAC(torch.optim.Optimizer):
         g = p.grad
         if g is None:
             return p.numel()
+        if g.is_neg():  # a view whose sign is a flag
+            g = g.resolve_neg()
         if g.dtype not in binding.DTYPES:
             return g.float()
         if g.dim() > 4 and not g.is_contiguous():  # might not merge into four dimensions
