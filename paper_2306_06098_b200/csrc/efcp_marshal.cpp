@@ -7,6 +7,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/InferenceMode.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAGuard.h>
@@ -124,8 +125,9 @@ void describe(PyObject* o, c10::Device device, Use use, Py_ssize_t i, efcp_tenso
   out->data = nullptr;
   if (!out->numel) return;
   if (use == Use::kWrite) {
+    if (t.is_inference() && !c10::InferenceMode::is_enabled())
+      refuse(PyExc_RuntimeError, at() + "an inference tensor changed outside of inference mode");
     out->data = t.mutable_data_ptr();
-    t.unsafeGetTensorImpl()->bump_version();  // autograd's record of changes in place
   } else {
     out->data = const_cast<void*>(t.const_data_ptr());
   }
@@ -138,6 +140,14 @@ void describe(PyObject* o, c10::Device device, Use use, Py_ssize_t i, efcp_tenso
       out->stride[k] = t.stride(k);
     }
   }
+}
+
+// Autograd's record of a change in place, once the call has succeeded.  (Inference tensors have none.)
+void written(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+void written(const std::optional<at::Tensor>& t) {
+  if (t) written(*t);
 }
 
 // The list's device: that of `first` if given, else of its first tensor, else the current one.
@@ -208,10 +218,11 @@ PyObject* grads_norm(PyObject*, PyObject* args) {
     const Place place(list_device(seq, out));
     const auto list = describe_list(seq, place.stream.device(), Use::kRead);
     const at::Tensor norm = norm_out(out, place), ws = list_workspace(place);
-    return result(efcp_grads_norm(list.data(), int32_t(list.size()), scale,
-                                  norm.mutable_data_ptr<float>(), ws.mutable_data_ptr(),
-                                  place.stream.stream()),
-                  norm);
+    const int rc = efcp_grads_norm(list.data(), int32_t(list.size()), scale,
+                                   norm.mutable_data_ptr<float>(), ws.mutable_data_ptr(),
+                                   place.stream.stream());
+    if (rc == EFCP_OK) written(out);
+    return result(rc, norm);
   });
 }
 
@@ -224,10 +235,15 @@ PyObject* grads_clip(PyObject*, PyObject* args) {
     const Place place(list_device(seq, out));
     const auto list = describe_list(seq, place.stream.device(), Use::kWrite);
     const at::Tensor norm = norm_out(out, place), ws = list_workspace(place);
-    return result(efcp_grads_clip(list.data(), int32_t(list.size()), max_norm, scale,
-                                  norm.mutable_data_ptr<float>(), ws.mutable_data_ptr(),
-                                  place.stream.stream()),
-                  norm);
+    const int rc = efcp_grads_clip(list.data(), int32_t(list.size()), max_norm, scale,
+                                   norm.mutable_data_ptr<float>(), ws.mutable_data_ptr(),
+                                   place.stream.stream());
+    if (rc == EFCP_OK) {
+      for (Py_ssize_t i = 0; i < Py_ssize_t(list.size()); ++i)
+        if (list[size_t(i)].numel) written(THPVariable_Unpack(PySequence_Fast_GET_ITEM(seq, i)));
+      written(out);
+    }
+    return result(rc, norm);
   });
 }
 
@@ -251,7 +267,11 @@ PyObject* grads_gather(PyObject*, PyObject* args) {
         list.data(), int32_t(list.size()), flat.mutable_data_ptr<float>(), flat.numel(), max_norm,
         scale, norm.defined() ? norm.mutable_data_ptr<float>() : nullptr,
         ws.defined() ? ws.mutable_data_ptr() : nullptr, place.stream.stream());
-    if (rc == EFCP_OK && !norm.defined()) Py_RETURN_NONE;
+    if (rc == EFCP_OK) {
+      written(flat);
+      written(out);
+      if (!norm.defined()) Py_RETURN_NONE;
+    }
     return result(rc, norm);
   });
 }
