@@ -33,7 +33,12 @@ for _path in (LIB_PATH, MARSHAL_PATH):
             "(nvcc, sm_100a). There is no CPU fallback.")
 
 _lib = C.CDLL(LIB_PATH)
-from . import _marshal  # noqa: E402  (links against the library just loaded)
+try:
+    from . import _marshal  # noqa: E402  (links against the library just loaded)
+except ImportError as _e:
+    raise ImportError(
+        f"{MARSHAL_PATH} does not load with torch {torch.__version__}: rebuild it with "
+        f"`python -m paper_2306_06098_b200.build` ({_e})") from _e
 
 _vp, _i32, _i64, _f32, _u32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_uint32
 

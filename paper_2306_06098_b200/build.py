@@ -28,10 +28,25 @@ def _stale(target, deps):
     return not os.path.exists(target) or os.path.getmtime(target) < max(map(os.path.getmtime, deps))
 
 
+def _bound_to() -> str:
+    """What a build of _marshal.so fits: torch's C++ interface and the interpreter's."""
+    import torch
+    return f"torch {torch.__version__}, Python {sys.version_info.major}.{sys.version_info.minor}"
+
+
+def _built_for() -> str:
+    try:
+        with open(MARSHAL + ".built_for") as f:
+            return f.read()
+    except OSError:
+        return ""
+
+
 def build_marshal(force: bool = False) -> str:
-    """Compile _marshal.so when it is missing or older than its sources; return its path."""
+    """Compile _marshal.so when it is missing, older than its sources or built for another torch;
+    return its path."""
     deps = [MARSHAL_SRC] + glob.glob(os.path.join(INCLUDE, "*.h"))
-    if not force and not _stale(MARSHAL, deps):
+    if not force and not _stale(MARSHAL, deps) and _built_for() == _bound_to():
         return MARSHAL
     import torch
     root = os.path.dirname(torch.__file__)
@@ -47,6 +62,8 @@ def build_marshal(force: bool = False) -> str:
            f"-Wl,-rpath,{lib}", "-Wl,-rpath,$ORIGIN/csrc"]
     subprocess.run(cmd, check=True)
     os.replace(MARSHAL + ".tmp", MARSHAL)
+    with open(MARSHAL + ".built_for", "w") as f:
+        f.write(_bound_to())
     return MARSHAL
 
 
