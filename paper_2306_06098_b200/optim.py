@@ -36,6 +36,10 @@ class SparseMFAC(torch.optim.Optimizer):
                  max_grad_norm: float = 0.0, grad_scale: float = 1.0):
         if lr < 0 or weight_decay < 0 or clip_norm < 0 or max_grad_norm < 0:
             raise ValueError("lr, weight_decay, clip_norm and max_grad_norm must be non-negative")
+        if not max_grad_norm >= 0:
+            raise ValueError("max_grad_norm must be a number of 0 or more")
+        if not 0 < grad_scale < float("inf"):
+            raise ValueError("grad_scale must be finite and positive")
         super().__init__(params, dict(lr=lr, weight_decay=weight_decay))
         plist = [p for g in self.param_groups for p in g["params"]]
         if not plist:
