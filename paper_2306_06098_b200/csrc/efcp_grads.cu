@@ -138,6 +138,14 @@ __device__ __forceinline__ double sumsq_of(const Pack<T, V>& a) {
   return in_range(s) ? double(s) : sumsq_wide(v);
 }
 
+// The bits of an access's values, without their signs, joined: 0 where all are zeros.
+template <typename T, int V>
+__device__ __forceinline__ unsigned bits_of(const Pack<T, V>& a) {
+  static_assert(sizeof(a) == 16, "four words");
+  const uint4 w = *reinterpret_cast<const uint4*>(&a);
+  return (w.x | w.y | w.z | w.w) & (sizeof(T) == 4 ? 0x7FFFFFFFu : 0x7FFF7FFFu);
+}
+
 template <typename T>
 __device__ __forceinline__ double chunk_sumsq(const T* p, int len) {
   constexpr int V = 16 / int(sizeof(T)), U = 4;
@@ -148,6 +156,12 @@ __device__ __forceinline__ double chunk_sumsq(const T* p, int len) {
   const int nv = (len - head) / V;
   const P* q = reinterpret_cast<const P*>(p + head);
   double acc = 0.0;
+  const int rest = len - head - nv * V;  // the ends: fewer than 2 V elements
+  if (int(threadIdx.x) < head + rest) {
+    const int k = int(threadIdx.x) < head ? int(threadIdx.x) : nv * V + int(threadIdx.x);
+    const double x = double(to_f32(p[k]));
+    acc += x * x;
+  }
   int i = threadIdx.x;
   for (; i + (U - 1) * kGrThreads < nv; i += U * kGrThreads) {
     P a[U];
@@ -155,15 +169,18 @@ __device__ __forceinline__ double chunk_sumsq(const T* p, int len) {
     for (int u = 0; u < U; ++u) a[u] = q[i + u * kGrThreads];
     // four sums of at most 8 products each
     float2 t[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    unsigned bits = 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      bits |= bits_of(a[u]);
       float v[V];
 #pragma unroll
       for (int j = 0; j < V; ++j) v[j] = to_f32(a[u].v[j]);
       add_squares(v, t[u & 1]);
     }
     const float s = (t[0].x + t[0].y) + (t[1].x + t[1].y);
-    if (in_range(s)) {
+    // zeros are common (an embedding's rows without a token)
+    if (in_range(s) | (bits == 0)) {
       acc += double(s);
     } else {
 #pragma unroll 1
@@ -172,12 +189,6 @@ __device__ __forceinline__ double chunk_sumsq(const T* p, int len) {
   }
 #pragma unroll 1
   for (; i < nv; i += kGrThreads) acc += sumsq_of(q[i]);
-  const int rest = len - head - nv * V;  // the ends: fewer than 2 V elements
-  if (int(threadIdx.x) < head + rest) {
-    const int k = int(threadIdx.x) < head ? int(threadIdx.x) : nv * V + int(threadIdx.x);
-    const double x = double(to_f32(p[k]));
-    acc += x * x;
-  }
   return acc;
 }
 
