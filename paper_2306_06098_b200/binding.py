@@ -156,7 +156,19 @@ def topk_static(a: torch.Tensor, k: int, idx: torch.Tensor, val: torch.Tensor, s
 
 # ---------------------------------------------------------------------------------------
 # Lists of gradients.  `stream`: a torch.cuda.Stream to run on instead of the current one; memory
-# the call allocates then belongs to it.
+# the call allocates then belongs to it.  The call is not noted on the tensors it is given: as with any work on
+# another stream than their own, they have to be ready when it starts (wait_stream) and to be kept until
+# it has run (record_stream, or a wait before they are freed or written).
+
+def _on(stream, tensors):
+    """The stream as a context, once it is known to be of the tensors' device."""
+    for t in tensors:
+        if isinstance(t, torch.Tensor):
+            if t.device != stream.device:
+                raise ValueError(f"stream: one of the tensors' device expected ({t.device}), not of {stream.device}")
+            break
+    return torch.cuda.stream(stream)
+
 
 def _done(result, where):
     """The result of a native call, or the error whose code it returned."""
@@ -169,7 +181,7 @@ def grad_norm(tensors, scale: float = 1.0, out: torch.Tensor = None, stream=None
     """efcp_grads_norm: scale * |g|_2 over a list of gradients (fp32, bfloat16, fp16, any
     strides, one CUDA device) as an fp32 scalar on the device; asynchronous."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, (out, *tensors)):
             return grad_norm(tensors, scale, out)
     return _done(_marshal.grads_norm(tensors, scale, out), "efcp_grads_norm")
 
@@ -179,7 +191,7 @@ def clip_grads(tensors, max_norm: float, scale: float = 1.0, out: torch.Tensor =
     """efcp_grads_clip: g <- scale * min(1, max_norm / N) g in place over a list of gradients;
     returns N = scale * |g|_2 of before (fp32 scalar on the device); asynchronous."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, (out, *tensors)):
             return clip_grads(tensors, max_norm, scale, out)
     return _done(_marshal.grads_clip(tensors, max_norm, scale, out), "efcp_grads_clip")
 
@@ -192,7 +204,7 @@ def gather_grads(tensors, flat: torch.Tensor, max_norm: float = 0.0, scale: floa
     Returns scale * |g|_2 (fp32 scalar on the device) when `norm` is set or `out` given, else
     None; asynchronous."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, (flat,)):
             return gather_grads(tensors, flat, max_norm, scale, norm, out)
     return _done(_marshal.grads_gather(tensors, flat, max_norm, scale, norm, out),
                  "efcp_grads_gather")
@@ -209,7 +221,7 @@ def group_norm_forward(x: torch.Tensor, groups: int, weight: torch.Tensor = None
     or "silu".  Returns (y, mean, rstd): y channels last in x's type, the statistics (n, groups)
     in fp32.  Asynchronous."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, (x,)):
             return group_norm_forward(x, groups, weight, bias, eps, act)
     return _done(_marshal.group_norm_forward(x, groups, weight, bias, eps, act),
                  "efcp_group_norm_forward")
@@ -222,7 +234,7 @@ def group_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
     group_norm_forward's y, with the statistics that call returned; dx channels last in x's type,
     dweight and dbias in the parameters' type (None where there is no parameter).  Asynchronous."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, (x,)):
             return group_norm_backward(dy, x, mean, rstd, groups, weight, bias, act)
     return _done(_marshal.group_norm_backward(dy, x, mean, rstd, groups, weight, bias, act),
                  "efcp_group_norm_backward")
