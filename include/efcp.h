@@ -435,8 +435,9 @@ typedef struct efcp_tensor {
 } efcp_tensor;
 
 /*
- *   efcp_grads_norm   : N = scale * |g|_2 over all elements of the list (fp64 sums in a fixed
- *                       order; neither large nor tiny values overflow or vanish in the squares).
+ *   efcp_grads_norm   : N = scale * |g|_2 over all elements of the list, in a fixed order: up to
+ *                       32 squares at a time in fp32 (four sums of eight; fp64 where they would
+ *                       overflow or vanish), everything else in fp64.
  *   efcp_grads_clip   : g <- f g in place with f = scale * min(1, max_norm / N): the list's norm
  *                       after `scale` is at most max_norm.  One fp32 product per element, rounded
  *                       once to the element's type.  When f is exactly 1 nothing is written.
@@ -471,9 +472,8 @@ int efcp_grads_gather(const efcp_tensor* grads, int32_t n, float* flat, int64_t 
 
 /*
  * Group normalisation with an activation, channels last, forward and backward.  Unlike batch
- * normalisation it does not couple the samples of a batch, so the gradient of a mini-batch is
- * the mean of per-sample gradients, which is what the empirical Fisher matrix is built from.
- * With n samples, `rows` positions (height x width, ...), `channels` channels in `groups`
+ * normalisation it does not couple the samples of a batch, and its results do not depend on the
+ * batch size.  With n samples, `rows` positions (height x width, ...), `channels` channels in `groups`
  * groups of D = channels / groups, for each sample and group, over its rows * D values:
  *     mean, var = mean((x - mean)^2), rstd = 1 / sqrt(var + eps),
  *     h = (x - mean) rstd,   z = h w_c + b_c,   y = act(z),

@@ -16,10 +16,10 @@
 // (one access of up to 16 bytes) and walks down rows, so what belongs to a channel - weight,
 // bias, statistics, its sums - stays with the thread.
 //
-// Measured on a B200 (copy rate 6.56 TB/s), device time: 256 x 112 x 112 x 64 bf16 relu forward 206 us,
-// 4.0 TB/s; 256 x 56 x 56 x 64 bf16 silu backward 102 us, 3.0 TB/s; 128 x 32 x 32 x 16 fp32 forward 5.8 us;
-// 1 x 7 x 7 x 512 fp16 forward 3.1 us; streamed, 1 x 512 x 512 x 128 bf16 silu forward 67 us,
-// backward 130 us.
+// Measured on a B200 (copy rate 6.56 TB/s), device time: 256 x 112 x 112 x 64 bf16 relu forward 199 us,
+// 4.1 TB/s; 256 x 56 x 56 x 64 bf16 silu backward 102 us, 3.0 TB/s; 128 x 32 x 32 x 16 fp32 forward 6.2 us;
+// 1 x 7 x 7 x 512 fp16 forward 3.4 us; streamed, 1 x 512 x 512 x 128 bf16 silu forward 65 us,
+// backward 129 us.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -205,8 +205,9 @@ __device__ __forceinline__ F lanes_sum(F v, int lanes) {
   return v;
 }
 
-// 1 / (1 + exp(-z)) with the hardware's exponential and reciprocal, each within 2 units in the
-// last place; 0 where exp(-z) overflows.
+// 1 / (1 + exp(-z)) with the hardware's reciprocal and power of two, each within 2 units in the last place.
+// The power's argument is rounded to fp32, so exp(-z) is off by up to another |z| units or so; where that is many, z
+// far below 0, the result is small.  0 where exp(-z) overflows.
 template <int V>
 __device__ __forceinline__ Vec<V> sigmoid_of(const Vec<V>& z) {
   Vec<V> t = z * fill<V>(-1.44269504f);
@@ -273,7 +274,7 @@ __device__ __forceinline__ void sum_rows(const Gn& p, const Item& it, const floa
 // sums without cancellation whatever the data.  The means are held and joined in 64 bits: every join in
 // fp32 would round by up to half a unit of the parts' distance from each other, and a chain of them is
 // further off than one sum over the group in fp32 (128 x 32 x 32 x 16 fp32: mean and y off by 2.3e-7 with fp32
-// joins, 6.7e-8 now; it costs the small calls 0.3 us on the device, 6.0 for 5.7 there).
+// joins, 6.7e-8 now; it cost the small calls 0.3 us on the device, 6.0 for 5.7 there).
 template <int V>
 struct Stats {
   double mean[V];
@@ -855,8 +856,8 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_bwd(const Gn p) {
 }
 
 // ------------------------------------------------------------------ streamed
-// Bound by memory in the two passes (23 and 31 us of 1 x 512 x 512 x 128 bf16 forward, 58 and 67 us backward, where
-// silu takes its share again) and by latency in the joins (18 and 8 us: 592 chunks, few columns).
+// Bound by memory in the two passes (20 and 31 us of 1 x 512 x 512 x 128 bf16 forward, 58 and 67 us backward, where
+// silu takes its share again) and by latency in the joins (15 and 8 us: 592 chunks, few columns).
 // Accesses in flight per thread and input: about 32 registers' worth.
 template <typename T, int V>
 constexpr int kAhead = sizeof(T) * V == 16 ? 4 : 8;

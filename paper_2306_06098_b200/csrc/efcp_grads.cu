@@ -9,10 +9,11 @@
 // few of them for that; a contiguous range per block instead took 41 us in place of 37 for the
 // norm below, and 188 in place of 157 for the gather).
 //
-// Measured on a B200 (copy rate 6.56 TB/s), device time: norm of a BERT-base in bf16 and fp32 vectors, 219 MB, 37 us,
-// 5.9 TB/s; clipping ResNet-18's 47 MB in place 11.7 us out of L2, its norm and the factor in two launches; the clipped
-// gather of BERT-base from bf16 157 us, 876 MB with the norm's read, 5.6 TB/s; of 301 ragged fp16 tensors 42 us;
-// norm of a ResNet-20 5.7 us, its clipped gather from channels-last gradients 9.3 us.
+// Measured on a B200 (copy rate 6.56 TB/s): norm of a BERT-base in bf16 and fp32 vectors, 219 MB, 37 us,
+// 5.9 TB/s; clipping ResNet-18's 47 MB in place 28 us, its norm and the factor in two launches (11 where it is in L2
+// already); the clipped gather of BERT-base from bf16 157 us, 876 MB with the norm's read, 5.6 TB/s; of 301 ragged
+// fp16 tensors 41 us; norm of a ResNet-20 6.0 us, its clipped gather from channels-last gradients 9.7 us.  From fp32
+// gradients one after another, not clipped: ResNet-18 13.9 us, BERT-base 146 us, 6.0 TB/s.
 #include "efcp.h"
 
 #include <cuda_runtime.h>

@@ -115,8 +115,10 @@ void set_tiles(const efcp_group_norm& d, int vec, int unit, int64_t groups, Gn* 
 // Whether a sample's tile fits on chip; then tiles, the cluster's size and the shared memory of a
 // block.  Narrow tiles come first, as they need smaller clusters: 64 bytes a row with 16-byte accesses
 // (256 x 28 x 28 x 128 bf16 forward 27 us against 29 us with 128), 128 with narrower ones
-// (200 x 30 x 30 x 37 forward 16 us against 21 us with 64), 32 where nothing else fits; clusters
-// of 8 blocks before larger ones, and four blocks per SM before two.  Where a sample has few rows the tiles
+// (200 x 30 x 30 x 37 forward 16 us against 21 us with 64), 32 where nothing else fits; of equal tiles
+// clusters of 8 blocks before larger ones, and four blocks per SM before two.  (Tiles of 32 bytes in clusters of
+// 8 before wider ones in up to 16: 128 x 90 x 90 x 64 fp16 forward 77 us against 70, 64 x 60 x 60 x 128 fp32
+// backward 114 against 105, but 200 x 50 x 50 x 37 bf16 forward 49 against 74.)  Where a sample has few rows the tiles
 // are wider, up to 16 rows for a thread forward, 8 backward, as long as there are three tiles per SM
 // (1000 x 1 x 1 x 768 bf16 forward 9.6 us against 46 us, 256 x 7 x 7 x 512 bf16 backward 18 us against 47;
 // with 16 rows backward 256 x 14 x 14 x 256 43 us against 37).  Tiles

@@ -1,9 +1,8 @@
 """Group normalisation for training with torch.autograd (argument marshalling only): both
 directions run in the CUDA library behind `binding`.
 
-Group normalisation takes the statistics of each sample by itself, so the gradient of a
-mini-batch is a mean of per-sample gradients - what the empirical Fisher matrix of Section 2.1 is made of - and
-the statistics do not depend on the batch size.
+Group normalisation takes the statistics of each sample by itself: samples of a batch do not depend on each
+other, and results not on the batch size.  The optimizer works with any model; this is one that a model may use.
 """
 from typing import Optional
 
