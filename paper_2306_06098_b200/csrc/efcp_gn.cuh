@@ -18,7 +18,7 @@
 //
 // Measured on a B200 (copy rate 6.56 TB/s), device time: 256 x 112 x 112 x 64 bf16 relu forward 199 us,
 // 4.1 TB/s; 256 x 56 x 56 x 64 bf16 silu backward 102 us, 3.0 TB/s; 128 x 32 x 32 x 16 fp32 forward 6.2 us;
-// 1 x 7 x 7 x 512 fp16 forward 3.4 us; streamed, 1 x 512 x 512 x 128 bf16 silu forward 65 us,
+// 1 x 7 x 7 x 512 fp16 forward 3.4 us; streamed, 1 x 512 x 512 x 128 bf16 silu forward 67 us,
 // backward 129 us.
 #pragma once
 
@@ -309,10 +309,12 @@ __device__ __forceinline__ Stats<V> stats_of(int n, const Vec<V>& k, const Vec<V
 
 // The same for values that come a batch at a time: segments of at most twice as many values as came before,
 // each around the mean so far (a factor of 3 at most), joined one after another.  Segments end at 64
-// values, so that the sums of a long run (a group wider than the block) stay short too.
+// values, so that the sums of a long run (a group wider than the block) stay short too.  The mean is kept with
+// what its rounding to fp32 leaves: without that, rstd was off by 190 units for values 10^5 deviations from zero.
 template <int V>
 struct Running {
-  Vec<V> neg = fill<V>(0.f);  // minus the mean of the n values joined
+  Vec<V> neg = fill<V>(0.f);  // minus the mean of the n values joined, rounded to fp32,
+  Vec<V> rest = neg;          // and what that leaves of it
   Vec<V> q = neg, s1 = neg, s2 = neg;
   int n = 0, open = 0;  // values joined, of the segment
 
@@ -343,9 +345,11 @@ struct Running {
     const float inv = rcp_fast(float(open)), w = float(open) * rcp_fast(float(n + open));
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const float d = s1.v[j] * inv;
+      const float d = fmaf(s1.v[j], inv, -rest.v[j]);  // the segment's mean, less the mean so far
       q.v[j] += fmaf(float(n) * w * d, d, m2_of(s1.v[j], s2.v[j], inv));
-      neg.v[j] = fmaf(-w, d, neg.v[j]);
+      const float up = fmaf(w, d, rest.v[j]), old = neg.v[j];
+      neg.v[j] = old - up;
+      rest.v[j] = up - (old - neg.v[j]);
     }
     s1 = s2 = fill<V>(0.f);
     n += open;
@@ -357,7 +361,7 @@ struct Running {
     s.cnt = float(n);
     s.q = q;
 #pragma unroll
-    for (int j = 0; j < V; ++j) s.mean[j] = -double(neg.v[j]);
+    for (int j = 0; j < V; ++j) s.mean[j] = double(rest.v[j]) - double(neg.v[j]);
     return s;
   }
 };
@@ -862,7 +866,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) k_gn_resident_bwd(const Gn p) {
 template <typename T, int V>
 constexpr int kAhead = sizeof(T) * V == 16 ? 4 : 8;
 
-// (Six blocks an SM, as k_gn_apply has, would spill here: 68 us against 65.5 for the call above.)
+// (Six blocks an SM, as k_gn_apply has, would spill here: 68 us against 65.5 for the call above when it was tried.)
 // The statistics of every group over a chunk of rows: the mean as two floats (its fp32 value and what
 // that leaves) and M2, one after another.
 template <typename T, int V>

@@ -87,3 +87,17 @@ def test_one_group_of_very_many_channels(c, rows, dtype):
     m64, r64, sigma = statistics64(x, 1)
     assert ((rstd.double() - r64).abs() <= r64 * 36 * U).all(), ((rstd / r64 - 1).abs().max() / U).item()
     assert ((mean.double() - m64).abs() <= 16 * U * (sigma + m64.abs())).all()
+
+
+@pytest.mark.parametrize("size", [(1, 64, 8, (400, 400)), (1, 128, 32, (512, 512)), (2, 130, 26, (128, 128)), (4, 32, 8, (40, 40)), (25, 300, 5, (68, 3))])
+@pytest.mark.parametrize("mean", [0.0, 1e3, -3e4, 1e5])
+def test_deviations_of_data_far_from_zero(size, mean):
+    """The mean's rounding is 1/170 of a deviation at 1e5: the squares must not feel it."""
+    n, c, groups, pos = size
+    x = channels_last(n, c, pos, torch.float32, 8, spread=False) + mean
+    got, rstd = statistics(x, groups)
+    m64, r64, sigma = statistics64(x, groups)
+    # squares near the centre 4 U, joins and the root a few U, as above; the centre itself is off by U |mean| at
+    # most, which squares of differences taken about it and corrected by their sum do not feel
+    assert ((rstd.double() - r64).abs() <= r64 * 16 * U).all(), ((rstd / r64 - 1).abs().max() / U).item()
+    assert ((got.double() - m64).abs() <= U * (m64.abs() + 2 * sigma)).all()
