@@ -522,6 +522,70 @@ int efcp_group_norm_backward(const efcp_group_norm* desc, const void* dy, const 
                              const void* bias, void* dx, void* dweight, void* dbias,
                              void* workspace, int64_t workspace_bytes, void* stream);
 
+/*
+ * Root-mean-square norm of a residual stream, and dropout.  For each of `rows` rows of `d` values
+ *     s = dropout(x),   h = s + residual rounded to its type,   r = 1 / sqrt(mean(h^2) + eps),
+ *     y = h r w,
+ * without a residual and with p == 0: h = x.  Given dy and dh (gradients of y and of h; dh NULL: zeros),
+ *     dresidual = r (dy w - h r^2 mean(dy w h)) + dh,   dx = dropout'(dresidual),   dw = sum_rows dy h r.
+ *
+ * Dropout of share p keeps no mask.  Element e of the logical order (row * d + column) has a 16-bit number
+ * from Philox4x32-10: half-word e % 8 (low halves first) of the four words for the counter
+ * (e / 8, offset) - four 32-bit words, low ones first - and the key `seed`.  It becomes 0 (whatever it was, NaN too) when the
+ * number is below T = round(65536 p), else it is multiplied by 65536 / (65536 - T).  The backward pass names
+ * the same seed and offset.
+ *
+ *   dtype            of x, residual, y, h, dy, dh, dx, dresidual: EFCP_F32, EFCP_BF16 or EFCP_F16.
+ *   param_dtype      of weight and dweight: the same choices.
+ *   p                0 .. 1; 0: no dropout, and seed, offset and rng are not looked at.
+ *   rng              device, (seed, offset), 8-byte aligned, read when the work runs: a captured graph
+ *                    takes what is there at each replay.  NULL: the fields `seed` and `offset`.
+ *   *_row            elements between rows of that input (>= 0; 0 repeats a row); values of a row lie
+ *                    side by side.  Outputs lie row after row.
+ *   weight           device, d entries; NULL: 1.
+ *   h                device, rows * d; needed with a residual or p > 0, else it is x and not written.
+ *   rstd             device, rows floats: r, for the backward call; NULL: not wanted.
+ *   dx, dresidual, dweight   NULL: not wanted.  With p == 0 the first two are equal: ask for one.
+ *   workspace        device, efcp_rms_norm_workspace_bytes(desc) bytes, 16-byte aligned, undefined
+ *                    afterwards; not needed (NULL) without dweight.
+ * efcp_rms_norm_quantize gives y in 8 bits: with `block` columns sharing a scale (32, 64, 128; 0: the whole
+ * row; the last block of a row may be shorter) and m their largest |h r w| in fp32,
+ *     scale = m / 448 (EFCP_E4M3) or m / 127 (EFCP_INT8), q = h r w / scale to the nearest, ties to even;
+ * scale 1 where m is 0, and scale NaN with q 0 where m is not finite.
+ *   q        device, rows * d bytes.   scales   device, rows * ceil(d / block) floats (rows, when block is 0).
+ * Squares and sums are fp32 (a mean of squares beyond its range, rows of 2^64 and more, gives r = 0), in a fixed
+ * order, so results repeat bit for bit; outputs are rounded to their type once.  Outputs overlap no input.  Work runs on the current device and on `stream`, asynchronously, and can be
+ * captured in a graph.  rows == 0 enqueues nothing but the zeroing of dweight.
+ * EFCP_EINVAL (nothing enqueued): null or misaligned pointers, rows < 0, d outside 1 .. 2^30 - 1, a
+ * product above 2^40, negative strides, eps negative or not finite, p outside 0 .. 1, unknown types, formats or blocks;
+ * EFCP_ENOMEM: a workspace that is too small; EFCP_ETOOBIG: more than 2^31 - 1 thread blocks.
+ */
+#define EFCP_E4M3 0
+#define EFCP_INT8 1
+typedef struct efcp_rms_norm {
+  int64_t rows, d;
+  int32_t dtype, param_dtype;
+  double p;
+  uint64_t seed, offset;
+  const uint64_t* rng;
+  float eps;
+} efcp_rms_norm;
+int efcp_rms_norm_forward(const efcp_rms_norm* desc, const void* x, int64_t x_row,
+                          const void* residual, int64_t residual_row, const void* weight, void* y,
+                          void* h, float* rstd, void* stream);
+int efcp_rms_norm_quantize(const efcp_rms_norm* desc, int32_t format, int32_t block, const void* x,
+                           int64_t x_row, const void* residual, int64_t residual_row,
+                           const void* weight, void* q, float* scales, void* h, float* rstd,
+                           void* stream);
+int64_t efcp_rms_norm_workspace_bytes(const efcp_rms_norm* desc);
+int efcp_rms_norm_backward(const efcp_rms_norm* desc, const void* dy, int64_t dy_row, const void* h,
+                           int64_t h_row, const void* dh, int64_t dh_row, const float* rstd,
+                           const void* weight, void* dx, void* dresidual, void* dweight,
+                           void* workspace, int64_t workspace_bytes, void* stream);
+/* y = dropout(x) (+ residual, NULL: none); eps and param_dtype are not used. */
+int efcp_dropout(const efcp_rms_norm* desc, const void* x, int64_t x_row, const void* residual,
+                 int64_t residual_row, void* y, void* stream);
+
 /* Static description of an EFCP_* code. */
 const char* efcp_strerror(int code);
 

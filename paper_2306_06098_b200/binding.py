@@ -24,6 +24,7 @@ F32, BF16, F16 = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 ACTS = ("none", "relu", "silu")
+E4M3, INT8 = 0, 1
 MAX_RANK = 8
 
 for _path in (LIB_PATH, MARSHAL_PATH):
@@ -55,6 +56,12 @@ class GroupNormDesc(C.Structure):
                 ("param_dtype", _i32), ("act", _i32), ("x_batch", _i64), ("x_row", _i64),
                 ("y_batch", _i64), ("y_row", _i64), ("dy_batch", _i64), ("dy_row", _i64),
                 ("eps", _f32)]
+
+
+class RmsNormDesc(C.Structure):
+    """efcp_rms_norm."""
+    _fields_ = [("rows", _i64), ("d", _i64), ("dtype", _i32), ("param_dtype", _i32), ("p", C.c_double),
+                ("seed", C.c_uint64), ("offset", C.c_uint64), ("rng", _vp), ("eps", _f32)]
 
 
 EXPORTS = {
@@ -104,12 +111,72 @@ EXPORTS = {
     "efcp_group_norm_workspace_bytes": ([C.POINTER(GroupNormDesc), _i32], _i64),
     "efcp_group_norm_forward": ([C.POINTER(GroupNormDesc)] + [_vp] * 7 + [_i64, _vp], C.c_int),
     "efcp_group_norm_backward": ([C.POINTER(GroupNormDesc)] + [_vp] * 10 + [_i64, _vp], C.c_int),
+    "efcp_rms_norm_forward": ([C.POINTER(RmsNormDesc), _vp, _i64, _vp, _i64] + [_vp] * 5, C.c_int),
+    "efcp_rms_norm_quantize": ([C.POINTER(RmsNormDesc), _i32, _i32, _vp, _i64, _vp, _i64] + [_vp] * 6,
+                               C.c_int),
+    "efcp_rms_norm_workspace_bytes": ([C.POINTER(RmsNormDesc)], _i64),
+    "efcp_rms_norm_backward": ([C.POINTER(RmsNormDesc)] + [_vp, _i64] * 3 + [_vp] * 6 + [_i64, _vp],
+                               C.c_int),
+    "efcp_dropout": ([C.POINTER(RmsNormDesc), _vp, _i64, _vp, _i64, _vp, _vp], C.c_int),
     "efcp_strerror": ([C.c_int], C.c_char_p),
 }
 for _name, (_args, _res) in EXPORTS.items():
     _fn = getattr(_lib, _name)  # AttributeError here = header and library out of sync
     _fn.argtypes = _args
     _fn.restype = _res
+
+
+# ---------------------------------------------------------------------------------------
+# Rows of a residual stream: RMS norm, dropout.  rng: (seed, offset) as two ints, or an int64 tensor of
+# them on the device, which the kernels read when they run (a captured graph then takes what is in it at
+# each replay).  It is not looked at when p is 0.
+
+def rms_norm_forward(x: torch.Tensor, weight: torch.Tensor = None, eps: float = 1e-6,
+                     residual: torch.Tensor = None, p: float = 0.0, rng=None, stream=None):
+    """efcp_rms_norm_forward on x (..., d), rows of any distance (other layouts are copied first):
+    h = dropout(x) + residual, y = h / sqrt(mean(h^2) + eps) * weight.  Returns (y, h, 1 / sqrt(...));
+    h is x itself without a residual and with p == 0.  Asynchronous."""
+    if stream is not None:
+        with _on(stream, (x,)):
+            return rms_norm_forward(x, weight, eps, residual, p, rng)
+    return _done(_marshal.rms_norm_forward(x, weight, eps, residual, p, rng),
+                 "efcp_rms_norm_forward")
+
+
+def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor,
+                      weight: torch.Tensor = None, dh: torch.Tensor = None, p: float = 0.0,
+                      rng=None, want=(True, True, True), stream=None):
+    """efcp_rms_norm_backward: (dx, dresidual, dweight) for the gradients dy and dh (None: zeros) of
+    rms_norm_forward's y and h, with the h and the statistics that call returned and its p and rng.
+    Without dropout dx and dresidual are one tensor.  want: which of the three; the others are None.
+    Asynchronous."""
+    if stream is not None:
+        with _on(stream, (dy,)):
+            return rms_norm_backward(dy, h, rstd, weight, dh, p, rng, want)
+    return _done(_marshal.rms_norm_backward(dy, h, rstd, weight, dh, p, rng, *want),
+                 "efcp_rms_norm_backward")
+
+
+def rms_norm_quantize(x: torch.Tensor, weight: torch.Tensor = None, eps: float = 1e-6,
+                      residual: torch.Tensor = None, block: int = 0, format: str = "e4m3",
+                      stream=None):
+    """efcp_rms_norm_quantize: (q, scales, h) with q * scales the norm of h = x + residual, q in
+    8 bits ("e4m3" or "int8"), one scale for `block` columns (32, 64, 128) or a whole row (0).
+    Asynchronous."""
+    if stream is not None:
+        with _on(stream, (x,)):
+            return rms_norm_quantize(x, weight, eps, residual, block, format)
+    return _done(_marshal.rms_norm_quantize(x, weight, eps, residual, block, format),
+                 "efcp_rms_norm_quantize")
+
+
+def dropout(x: torch.Tensor, p: float, rng, residual: torch.Tensor = None, stream=None):
+    """efcp_dropout: dropout(x) (+ residual).  No mask is kept: the gradient of x is the same call on
+    the gradient of the result, without the residual.  Asynchronous."""
+    if stream is not None:
+        with _on(stream, (x,)):
+            return dropout(x, p, rng, residual)
+    return _done(_marshal.dropout(x, p, rng, residual), "efcp_dropout")
 
 
 class EfcpError(RuntimeError):

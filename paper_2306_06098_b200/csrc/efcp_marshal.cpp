@@ -457,6 +457,216 @@ PyObject* group_norm_backward(PyObject*, PyObject* args) {
   });
 }
 
+// ------------------------------------------------------------------ rows: RMS norm, dropout
+// t itself, or a contiguous copy, as rows of its last dimension `row` elements apart.
+at::Tensor as_rows(const at::Tensor& t, int64_t* row) {
+  const int64_t d = t.size(-1);
+  *row = d;
+  if (t.is_contiguous()) return t;
+  bool ok = t.numel() > 0 && (d == 1 || t.stride(-1) == 1);
+  int64_t count = 1;  // the merged dimensions so far, from the last but one on
+  for (int64_t k = t.dim() - 2; ok && k >= 0; --k) {
+    if (t.size(k) == 1) continue;
+    if (count == 1) *row = t.stride(k);
+    else ok = t.stride(k) == *row * count;
+    count *= t.size(k);
+  }
+  if (ok) return t;
+  *row = d;
+  return t.clone(at::MemoryFormat::Contiguous);
+}
+
+void require_like(const at::Tensor& t, const at::Tensor& x, const char* what) {
+  require(t.layout() == at::kStrided && t.sizes() == x.sizes() &&
+              t.scalar_type() == x.scalar_type() && t.device() == x.device() && !t.is_neg(),
+          what);
+}
+
+efcp_rms_norm rms_desc(const at::Tensor& x, const char* name) {
+  if (!(x.layout() == at::kStrided && x.dim() >= 1 && dtype_of(x) >= 0 && !x.is_neg()))
+    refuse(PyExc_ValueError, std::string(name) + ": (..., d) in fp32, bfloat16 or fp16 expected");
+  if (!x.is_cuda()) refuse(PyExc_ValueError, std::string(name) + ": a CUDA tensor expected");
+  efcp_rms_norm d{};
+  d.d = x.size(-1);
+  d.rows = 1;
+  for (int64_t k = 0; k + 1 < x.dim(); ++k) d.rows *= x.size(k);
+  d.dtype = dtype_of(x);
+  d.param_dtype = EFCP_F32;
+  return d;
+}
+
+void rms_weight(const std::optional<at::Tensor>& weight, const at::Tensor& x, efcp_rms_norm* d) {
+  if (!weight) return;
+  const int dt = dtype_of(*weight);
+  require(weight->layout() == at::kStrided && weight->device() == x.device() && dt >= 0 &&
+              weight->numel() == d->d && weight->is_contiguous() && !weight->is_neg(),
+          "weight: contiguous, one value per column, fp32, bfloat16 or fp16, on x's device");
+  d->param_dtype = dt;
+}
+
+// (seed, offset): two numbers, or an int64 tensor of them on x's device.  Not looked at without dropout.
+void rms_drop(double p, PyObject* rng, const at::Tensor& x, efcp_rms_norm* d) {
+  d->p = p;
+  if (!(p > 0)) return;
+  if (THPVariable_Check(rng)) {
+    const at::Tensor& t = THPVariable_Unpack(rng);
+    require(t.layout() == at::kStrided && t.scalar_type() == at::kLong && t.numel() == 2 &&
+                t.is_contiguous() && t.device() == x.device(),
+            "rng: an int64 tensor of (seed, offset) on x's device expected");
+    d->rng = reinterpret_cast<const uint64_t*>(t.const_data_ptr());
+    return;
+  }
+  if (!PyTuple_Check(rng) || PyTuple_GET_SIZE(rng) != 2 || !PyLong_Check(PyTuple_GET_ITEM(rng, 0)) ||
+      !PyLong_Check(PyTuple_GET_ITEM(rng, 1)))
+    refuse(PyExc_TypeError, "rng: two ints (seed, offset) or an int64 tensor of them expected");
+  d->seed = PyLong_AsUnsignedLongLongMask(PyTuple_GET_ITEM(rng, 0));
+  d->offset = PyLong_AsUnsignedLongLongMask(PyTuple_GET_ITEM(rng, 1));
+}
+
+PyObject* rms_norm_forward(PyObject*, PyObject* args) {
+  PyObject *x_, *w_, *r_, *rng;
+  float eps;
+  double p;
+  if (!PyArg_ParseTuple(args, "OOfOdO", &x_, &w_, &eps, &r_, &p, &rng)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const at::Tensor& given = tensor_of(x_, "x");
+    const auto weight = maybe_tensor(w_, "weight"), residual = maybe_tensor(r_, "residual");
+    efcp_rms_norm d = rms_desc(given, "x");
+    d.eps = eps;
+    rms_weight(weight, given, &d);
+    rms_drop(p, rng, given, &d);
+    if (residual) require_like(*residual, given, "residual: x's shape, type and device expected");
+    const Place place(given.device());
+    int64_t x_row = 0, r_row = 0;
+    const at::Tensor x = as_rows(given, &x_row);
+    const at::Tensor r = residual ? as_rows(*residual, &r_row) : at::Tensor();
+    const at::Tensor y = place.empty(x.sizes(), x.scalar_type());
+    const bool summed = residual || p > 0;
+    const at::Tensor h = summed ? place.empty(x.sizes(), x.scalar_type()) : x;
+    const at::Tensor rstd = place.empty(x.sizes().slice(0, size_t(x.dim() - 1)));
+    const int rc = efcp_rms_norm_forward(
+        &d, x.const_data_ptr(), x_row, residual ? r.const_data_ptr() : nullptr, r_row,
+        data_of(weight), y.mutable_data_ptr(), summed ? h.mutable_data_ptr() : nullptr,
+        rstd.mutable_data_ptr<float>(), place.stream.stream());
+    return triple(rc, y, h, rstd);
+  });
+}
+
+PyObject* rms_norm_quantize(PyObject*, PyObject* args) {
+  PyObject *x_, *w_, *r_;
+  float eps;
+  int block;
+  const char* format;
+  if (!PyArg_ParseTuple(args, "OOfOis", &x_, &w_, &eps, &r_, &block, &format)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const at::Tensor& given = tensor_of(x_, "x");
+    const auto weight = maybe_tensor(w_, "weight"), residual = maybe_tensor(r_, "residual");
+    efcp_rms_norm d = rms_desc(given, "x");
+    d.eps = eps;
+    rms_weight(weight, given, &d);
+    if (residual) require_like(*residual, given, "residual: x's shape, type and device expected");
+    const bool e4m3 = !std::strcmp(format, "e4m3");
+    require(e4m3 || !std::strcmp(format, "int8"), "format: one of e4m3, int8 expected");
+    require(block == 0 || block == 32 || block == 64 || block == 128,
+            "block: 0 (a row), 32, 64 or 128 expected");
+    const Place place(given.device());
+    int64_t x_row = 0, r_row = 0;
+    const at::Tensor x = as_rows(given, &x_row);
+    const at::Tensor r = residual ? as_rows(*residual, &r_row) : at::Tensor();
+    const at::Tensor q = place.empty(x.sizes(), e4m3 ? at::kFloat8_e4m3fn : at::kChar);
+    const at::Tensor h = residual ? place.empty(x.sizes(), x.scalar_type()) : x;
+    std::vector<int64_t> shape(x.sizes().begin(), x.sizes().end());
+    shape.back() = block ? (d.d + block - 1) / block : 1;
+    const at::Tensor scales = place.empty(shape);
+    const int rc = efcp_rms_norm_quantize(
+        &d, e4m3 ? EFCP_E4M3 : EFCP_INT8, block, x.const_data_ptr(), x_row,
+        residual ? r.const_data_ptr() : nullptr, r_row, data_of(weight), q.mutable_data_ptr(),
+        scales.mutable_data_ptr<float>(), residual ? h.mutable_data_ptr() : nullptr, nullptr,
+        place.stream.stream());
+    return triple(rc, q, scales, h);
+  });
+}
+
+PyObject* rms_norm_backward(PyObject*, PyObject* args) {
+  PyObject *dy_, *h_, *r_, *w_, *dh_, *rng;
+  double p;
+  int want_x, want_residual, want_weight;
+  if (!PyArg_ParseTuple(args, "OOOOOdOppp", &dy_, &h_, &r_, &w_, &dh_, &p, &rng, &want_x,
+                        &want_residual, &want_weight))
+    return nullptr;
+  return guarded([&]() -> PyObject* {
+    const at::Tensor &given = tensor_of(h_, "h"), &given_dy = tensor_of(dy_, "dy");
+    const at::Tensor& rstd = tensor_of(r_, "rstd");
+    const auto weight = maybe_tensor(w_, "weight"), given_dh = maybe_tensor(dh_, "dh");
+    efcp_rms_norm d = rms_desc(given, "h");
+    rms_weight(weight, given, &d);
+    rms_drop(p, rng, given, &d);
+    require_like(given_dy, given, "dy: h's shape, type and device expected");
+    if (given_dh) require_like(*given_dh, given, "dh: h's shape, type and device expected");
+    require(rstd.scalar_type() == at::kFloat && rstd.numel() == d.rows && rstd.is_contiguous() &&
+                rstd.device() == given.device(),
+            "rstd: as rms_norm_forward returned it");
+    const Place place(given.device());
+    const bool both = p > 0 && want_x && want_residual, gradient = want_x || want_residual;
+    want_weight = want_weight && weight;
+    c10::DataPtr ws;
+    int64_t bytes = 0;
+    if (want_weight) {
+      bytes = efcp_rms_norm_workspace_bytes(&d);
+      if (bytes < 0) return PyLong_FromLong(EFCP_EINVAL);
+      ws = place.scratch(bytes);
+    }
+    int64_t dy_row = 0, h_row = 0, dh_row = 0;
+    const at::Tensor dy = as_rows(given_dy, &dy_row), h = as_rows(given, &h_row);
+    const at::Tensor dh = given_dh ? as_rows(*given_dh, &dh_row) : at::Tensor();
+    const at::Tensor dx = gradient ? place.empty(h.sizes(), h.scalar_type()) : at::Tensor();
+    const at::Tensor dres = both ? place.empty(h.sizes(), h.scalar_type()) : dx;
+    const at::Tensor dw =
+        want_weight ? place.empty(weight->sizes(), weight->scalar_type()) : at::Tensor();
+    const bool dropped = p > 0 && want_x;
+    const int rc = efcp_rms_norm_backward(
+        &d, dy.const_data_ptr(), dy_row, h.const_data_ptr(), h_row,
+        given_dh ? dh.const_data_ptr() : nullptr, dh_row, rstd.const_data_ptr<float>(),
+        data_of(weight), gradient && (dropped || p <= 0) ? dx.mutable_data_ptr() : nullptr,
+        gradient && p > 0 && want_residual ? dres.mutable_data_ptr() : nullptr,
+        dw.defined() ? dw.mutable_data_ptr() : nullptr, ws.get(), bytes, place.stream.stream());
+    return triple(rc, want_x ? dx : at::Tensor(), want_residual ? dres : at::Tensor(), dw);
+  });
+}
+
+PyObject* dropout(PyObject*, PyObject* args) {
+  PyObject *x_, *rng, *r_;
+  double p;
+  if (!PyArg_ParseTuple(args, "OdOO", &x_, &p, &rng, &r_)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    at::Tensor given = tensor_of(x_, "x");
+    auto residual = maybe_tensor(r_, "residual");
+    rms_desc(given, "x");
+    if (residual) require_like(*residual, given, "residual: x's shape, type and device expected");
+    // what lies in one piece is one row: the mask goes by the logical order alone
+    if (given.is_contiguous() && (!residual || residual->is_contiguous())) {
+      int64_t row = 1;
+      while (row < 4096 && given.numel() % (2 * row) == 0) row *= 2;
+      if (row < 256 && given.numel() < (1ll << 30)) row = given.numel();
+      if (row >= 256) {
+        given = given.view({-1, row});
+        if (residual) residual = residual->view({-1, row});
+      }
+    }
+    efcp_rms_norm d = rms_desc(given, "x");
+    rms_drop(p, rng, given, &d);
+    const Place place(given.device());
+    int64_t x_row = 0, r_row = 0;
+    const at::Tensor x = as_rows(given, &x_row);
+    const at::Tensor r = residual ? as_rows(*residual, &r_row) : at::Tensor();
+    const at::Tensor y = place.empty(tensor_of(x_, "x").sizes(), x.scalar_type());
+    const int rc = efcp_dropout(&d, x.const_data_ptr(), x_row,
+                                residual ? r.const_data_ptr() : nullptr, r_row,
+                                y.mutable_data_ptr(), place.stream.stream());
+    return result(rc, y);
+  });
+}
+
 // rows_layout(x): (elements between samples, between positions), or None when a copy would be made;
 // as_channels_last(x): x or that copy; like_channels_last(x): an empty output for x.  What the calls
 // above do to layouts, on tensors of any device.
@@ -486,6 +696,10 @@ PyMethodDef methods[] = {
     {"grads_gather", grads_gather, METH_VARARGS, "efcp_grads_gather"},
     {"group_norm_forward", group_norm_forward, METH_VARARGS, "efcp_group_norm_forward"},
     {"group_norm_backward", group_norm_backward, METH_VARARGS, "efcp_group_norm_backward"},
+    {"rms_norm_forward", rms_norm_forward, METH_VARARGS, "efcp_rms_norm_forward"},
+    {"rms_norm_backward", rms_norm_backward, METH_VARARGS, "efcp_rms_norm_backward"},
+    {"rms_norm_quantize", rms_norm_quantize, METH_VARARGS, "efcp_rms_norm_quantize"},
+    {"dropout", dropout, METH_VARARGS, "efcp_dropout"},
     {"rows_layout", rows_layout, METH_O, "strides of samples and positions, or None"},
     {"as_channels_last", as_channels_last, METH_O, "the tensor, or a channels-last copy"},
     {"like_channels_last", like_channels_last, METH_O, "an empty channels-last tensor"},

@@ -1,0 +1,45 @@
+// Between the host side of the RMS-norm and dropout calls (efcp_rms_norm.cu) and their kernels (efcp_rms.cuh),
+// which are compiled once per element type.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include "efcp_philox.cuh"
+
+namespace efcp {
+
+struct Rms {
+  long long rows;
+  int d;
+  int warps, groups;  // warps that share a row, rows that a block takes at a time
+  int param_dtype;
+  float eps, inv_d;
+  Drop drop;
+  const void *x, *residual, *weight;  // x: h in the backward call
+  const void *dy, *dh;
+  long long x_row, residual_row, dy_row, dh_row;  // elements between rows; outputs lie row after row
+  void *y, *h;                                    // h null: it is x
+  float* rstd;
+  void *dx, *dresidual, *dweight;  // null: not wanted
+  float* part;                     // sums of dweight, a row of d for each slot
+  float* scales;
+  int block, blocks;  // columns that share a scale (0: a row), scales of a row
+  float most;         // largest value of the 8-bit type
+};
+
+enum RmsOp { kRmsForward, kRmsE4M3, kRmsInt8, kRmsBackward, kDropout };
+
+struct RmsLaunch {
+  RmsOp op;
+  bool vec;         // rows start on 16 bytes, and on multiples of eight elements of the logical order
+  int kept;         // chunks that a warp keeps in registers: 1, 2, 4, or 0 (rows walked twice)
+  unsigned blocks;
+  long long parts;  // rows of `part`
+  cudaStream_t st;
+};
+
+cudaError_t rms_launch_f32(const Rms& p, const RmsLaunch& l);
+cudaError_t rms_launch_bf16(const Rms& p, const RmsLaunch& l);
+cudaError_t rms_launch_f16(const Rms& p, const RmsLaunch& l);
+
+}  // namespace efcp

@@ -1,0 +1,120 @@
+// Rows of d elements, cut into chunks of 256 that a warp takes eight to a lane: side by side in one or two
+// 16-byte accesses where every row starts on 16 bytes (VEC), else 32 apart, so that a warp's accesses still
+// touch neighbouring elements.
+#pragma once
+
+#include "efcp_num.cuh"
+#include "efcp_philox.cuh"
+
+namespace efcp {
+
+constexpr int kChunk = 256;
+constexpr unsigned kAll = 0xFFFFFFFFu;
+
+// column of a lane's element j in the chunk that starts at c0
+template <bool VEC>
+__device__ __forceinline__ int col_of(int c0, int lane, int j) {
+  return VEC ? c0 + lane * 8 + j : c0 + j * 32 + lane;
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T* row, int c0, int lane, int d, float (&v)[8]) {
+  if constexpr (VEC) {
+    const int col = c0 + lane * 8;
+    if (col < d) {
+      Pack<T, 8> a;
+      const uint4* from = reinterpret_cast<const uint4*>(row + col);
+#pragma unroll
+      for (int i = 0; i < int(sizeof(a) / 16); ++i) reinterpret_cast<uint4*>(&a)[i] = from[i];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = to_f32(a.v[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int col = c0 + j * 32 + lane;
+      v[j] = col < d ? to_f32(row[col]) : 0.f;
+    }
+  }
+}
+
+// the same from an array whose type is known at run time
+template <bool VEC>
+__device__ __forceinline__ void load8_param(const void* p, int dtype, int c0, int lane, int d,
+                                            float (&v)[8]) {
+  if (dtype == 0) load8<float, VEC>(static_cast<const float*>(p), c0, lane, d, v);
+  else if (dtype == 1)
+    load8<__nv_bfloat16, VEC>(static_cast<const __nv_bfloat16*>(p), c0, lane, d, v);
+  else load8<__half, VEC>(static_cast<const __half*>(p), c0, lane, d, v);
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void store8(T* row, int c0, int lane, int d, const float (&v)[8]) {
+  if constexpr (VEC) {
+    const int col = c0 + lane * 8;
+    if (col < d) {
+      Pack<T, 8> a;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) a.v[j] = from_f32<T>(v[j]);
+      uint4* to = reinterpret_cast<uint4*>(row + col);
+#pragma unroll
+      for (int i = 0; i < int(sizeof(a) / 16); ++i) to[i] = reinterpret_cast<const uint4*>(&a)[i];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int col = c0 + j * 32 + lane;
+      if (col < d) row[col] = from_f32<T>(v[j]);
+    }
+  }
+}
+
+// Bit j: the lane's element j of the chunk whose first element is `first` in the logical order stays.
+// Where rows do not start on a multiple of eight, the 32 groups that begin in the chunk are spread over the lanes,
+// with one more behind them.
+template <bool VEC>
+__device__ __forceinline__ uint32_t keep8(unsigned long long first, int lane, const DropKey& key,
+                                          uint32_t threshold) {
+  if constexpr (VEC) {
+    return drop_keep8((first >> 3) + lane, key, threshold);  // d is a multiple of 8
+  } else {
+    const int s = int(first & 7);
+    const uint32_t mine = drop_keep8((first >> 3) + lane, key, threshold);
+    const uint32_t last = s ? drop_keep8((first >> 3) + 32, key, threshold) : 0;
+    uint32_t keep = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int q = j * 32 + lane + s;
+      const uint32_t other = __shfl_sync(kAll, mine, (q >> 3) & 31);
+      keep |= (((q >= 256 ? last : other) >> (q & 7)) & 1u) << j;
+    }
+    return keep;
+  }
+}
+
+__device__ __forceinline__ void drop8(float (&v)[8], uint32_t keep, float scale) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = (keep >> j) & 1u ? v[j] * scale : 0.f;
+}
+
+template <typename T>
+__device__ __forceinline__ float rounded(float v) {
+  return to_f32(from_f32<T>(v));
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
+  return v;
+}
+// maximum over the lanes whose numbers agree above bit log2(width); a NaN wins
+__device__ __forceinline__ float max_nan(float a, float b) { return !(a <= b) && !(b != b) ? a : b; }
+__device__ __forceinline__ float lanes_max(float v, int width) {
+  for (int o = width / 2; o; o >>= 1) v = max_nan(v, __shfl_xor_sync(kAll, v, o));
+  return v;
+}
+
+}  // namespace efcp
