@@ -586,6 +586,58 @@ int efcp_rms_norm_backward(const efcp_rms_norm* desc, const void* dy, int64_t dy
 int efcp_dropout(const efcp_rms_norm* desc, const void* x, int64_t x_row, const void* residual,
                  int64_t residual_row, void* y, void* stream);
 
+/*
+ * Softmax cross entropy of a linear layer over a vocabulary, with its gradient, without keeping the logits.  For
+ * tokens i with hidden states h_i and targets t_i, and rows w_v of the layer,
+ *     l_iv = <h_i, w_v>,   lse_i = log sum_v exp l_iv,   loss_i = lse_i - l_i,t(i),
+ * and, given the factors g_i on the losses,
+ *     G_iv = g_i (exp(l_iv - lse_i) - [v = t_i]),   dH = G W,   dW = G^T H.
+ * Tokens whose target is ignore_index count for nothing and cost nothing: their loss and gradient are 0, whatever
+ * their hidden state holds.  A target outside 0 .. vocab - 1 otherwise makes the loss and the gradients NaN.
+ *
+ *   dtype            of hidden, weight, dhidden, dweight: EFCP_F32, EFCP_BF16 or EFCP_F16.
+ *   reduction        EFCP_LOSS_NONE: losses holds one value a token; EFCP_LOSS_MEAN: one value, the mean over
+ *                    the tokens that count (NaN when there is none); EFCP_LOSS_SUM: their sum.
+ *   hidden_row, weight_row   elements between rows; values of a row lie side by side.  dhidden and dweight
+ *                    lie row after row.
+ *   lse              device, `tokens` floats, for the backward call (0 for tokens that do not count).
+ *   grad             device: the factor on each token's loss, grad_step elements apart (0: the same for
+ *                    all), or with a reduction the one on its value.
+ *   dhidden, dweight NULL: not wanted.
+ *   workspace        device, efcp_cross_entropy_workspace_bytes(desc, weight, backward) bytes, 256-byte
+ *                    aligned, undefined afterwards.  The backward call holds the gradient of as many columns of the
+ *                    logits as fit in 256 MB (256 at least); operands that the tensor copies cannot read
+ *                    where they lie, fp32 among them, are laid out there.
+ * Products are exact and added up in fp32; fp32 operands are multiplied in three parts each, to about 2^-22.
+ * The logits' gradient is rounded to bf16 or fp16 (with a common factor that keeps it in range) before the two
+ * products that read it; it has all of fp32 where the operands do.  All sums have a fixed order, so results repeat bit
+ * for bit.  Outputs overlap no input.  Work runs on the current device and on `stream`, asynchronously,
+ * and can be captured in a graph.
+ * EFCP_EINVAL (nothing enqueued): null or misaligned pointers, tokens outside 0 .. 2^30 - 1, vocab
+ * outside 1 .. 2^30 - 1, d outside 1 .. 2^24 - 1, matrices above 2^40 elements, strides that are negative or above 2^32,
+ * unknown types or reductions; EFCP_ENOMEM: a workspace that is too small.
+ *   efcp_cross_entropy_status : waits for the device's work on the default stream; EFCP_ETIMEOUT when a wait
+ *                    inside a kernel of these calls ran out (2 s; the results of that call are undefined), else EFCP_OK.
+ */
+#define EFCP_LOSS_NONE 0
+#define EFCP_LOSS_MEAN 1
+#define EFCP_LOSS_SUM 2
+typedef struct efcp_cross_entropy {
+  int64_t tokens, vocab, d;
+  int64_t hidden_row, weight_row, ignore_index;
+  int32_t dtype, reduction;
+} efcp_cross_entropy;
+int64_t efcp_cross_entropy_workspace_bytes(const efcp_cross_entropy* desc, const void* weight,
+                                           int32_t backward);
+int efcp_cross_entropy_forward(const efcp_cross_entropy* desc, const void* hidden, const void* weight,
+                               const int64_t* targets, float* losses, float* lse, void* workspace,
+                               int64_t workspace_bytes, void* stream);
+int efcp_cross_entropy_backward(const efcp_cross_entropy* desc, const float* grad, int64_t grad_step,
+                                const void* hidden, const void* weight, const int64_t* targets,
+                                const float* lse, void* dhidden, void* dweight, void* workspace,
+                                int64_t workspace_bytes, void* stream);
+int efcp_cross_entropy_status(void);
+
 /* Static description of an EFCP_* code. */
 const char* efcp_strerror(int code);
 

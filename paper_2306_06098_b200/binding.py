@@ -1,5 +1,5 @@
 """Thin binding over libefcp.so (argument marshalling only): ctypes, and _marshal.so for the
-calls on lists of gradients and on activations.
+calls on lists of gradients, on activations and on losses.
 
 The names mirror include/efcp.h.  PyTorch is used for device memory and streams; every
 step of the method runs inside the CUDA library.  Importing this module fails loudly
@@ -25,6 +25,7 @@ ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 ACTS = ("none", "relu", "silu")
 E4M3, INT8 = 0, 1
+LOSS_NONE, LOSS_MEAN, LOSS_SUM = 0, 1, 2
 MAX_RANK = 8
 
 for _path in (LIB_PATH, MARSHAL_PATH):
@@ -62,6 +63,12 @@ class RmsNormDesc(C.Structure):
     """efcp_rms_norm."""
     _fields_ = [("rows", _i64), ("d", _i64), ("dtype", _i32), ("param_dtype", _i32), ("p", C.c_double),
                 ("seed", C.c_uint64), ("offset", C.c_uint64), ("rng", _vp), ("eps", _f32)]
+
+
+class CrossEntropyDesc(C.Structure):
+    """efcp_cross_entropy."""
+    _fields_ = [("tokens", _i64), ("vocab", _i64), ("d", _i64), ("hidden_row", _i64),
+                ("weight_row", _i64), ("ignore_index", _i64), ("dtype", _i32), ("reduction", _i32)]
 
 
 EXPORTS = {
@@ -118,6 +125,11 @@ EXPORTS = {
     "efcp_rms_norm_backward": ([C.POINTER(RmsNormDesc)] + [_vp, _i64] * 3 + [_vp] * 6 + [_i64, _vp],
                                C.c_int),
     "efcp_dropout": ([C.POINTER(RmsNormDesc), _vp, _i64, _vp, _i64, _vp, _vp], C.c_int),
+    "efcp_cross_entropy_workspace_bytes": ([C.POINTER(CrossEntropyDesc), _vp, _i32], _i64),
+    "efcp_cross_entropy_forward": ([C.POINTER(CrossEntropyDesc)] + [_vp] * 6 + [_i64, _vp], C.c_int),
+    "efcp_cross_entropy_backward": ([C.POINTER(CrossEntropyDesc), _vp, _i64] + [_vp] * 7 + [_i64, _vp],
+                                    C.c_int),
+    "efcp_cross_entropy_status": ([], C.c_int),
     "efcp_strerror": ([C.c_int], C.c_char_p),
 }
 for _name, (_args, _res) in EXPORTS.items():
@@ -177,6 +189,44 @@ def dropout(x: torch.Tensor, p: float, rng, residual: torch.Tensor = None, strea
         with _on(stream, (x,)):
             return dropout(x, p, rng, residual)
     return _done(_marshal.dropout(x, p, rng, residual), "efcp_dropout")
+
+
+# ---------------------------------------------------------------------------------------
+# Softmax cross entropy of a linear layer
+
+def cross_entropy_forward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
+                          ignore_index: int = -100, reduction: str = "mean", stream=None):
+    """efcp_cross_entropy_forward: (losses, lse) of the logits hidden @ weight.t(), which are never
+    kept; hidden (..., d), weight (vocabulary, d), targets (...) int64.  losses in fp32, one a token
+    with reduction "none", else the "mean" or "sum" of those whose target is not ignore_index.
+    Asynchronous."""
+    if stream is not None:
+        with _on(stream, (hidden,)):
+            return cross_entropy_forward(hidden, weight, targets, ignore_index, reduction)
+    return _done(_marshal.cross_entropy_forward(hidden, weight, targets, ignore_index, reduction),
+                 "efcp_cross_entropy_forward")
+
+
+def cross_entropy_backward(grad: torch.Tensor, hidden: torch.Tensor, weight: torch.Tensor,
+                           targets: torch.Tensor, lse: torch.Tensor, ignore_index: int = -100,
+                           reduction: str = "mean", want=(True, True), stream=None):
+    """efcp_cross_entropy_backward: (dhidden, dweight) for the gradient of cross_entropy_forward's
+    losses (fp32, of their shape), with the lse that call returned.  want: which of the two; the other
+    is None.  Asynchronous."""
+    if stream is not None:
+        with _on(stream, (hidden,)):
+            return cross_entropy_backward(grad, hidden, weight, targets, lse, ignore_index, reduction,
+                                          want)
+    return _done(_marshal.cross_entropy_backward(grad, hidden, weight, targets, lse, ignore_index,
+                                                 reduction, *want), "efcp_cross_entropy_backward")
+
+
+def cross_entropy_status():
+    """Waits for the default stream's work; raises when a wait inside a kernel of the two calls above
+    ran out (their results are undefined then)."""
+    rc = _lib.efcp_cross_entropy_status()
+    if rc != OK:
+        raise EfcpError(rc, "efcp_cross_entropy_status")
 
 
 class EfcpError(RuntimeError):

@@ -1,4 +1,4 @@
-"""Argument checks of the RMS-norm and dropout calls, without a GPU: through the C ABI a call with valid arguments gets
+"""Argument checks of the RMS-norm, dropout and cross-entropy calls, without a GPU: through the C ABI a call with valid arguments gets
 as far as asking for the device, an invalid one does not; in Python the wrong tensors are refused."""
 import ctypes as C
 import math
@@ -144,3 +144,90 @@ def test_arguments_that_are_refused():
                  lambda: B.rms_norm_forward(torch.ones(4, 0, device="cuda")), lambda: B.rms_norm_forward(x, p=float("nan"))):
         with pytest.raises(B.EfcpError):
             call()
+
+
+# ------------------------------------------------------------------ linear cross entropy
+def loss_desc(tokens=5, vocab=100, d=64, hidden_row=64, weight_row=64, ignore=-100, dtype=1, reduction=0):
+    return C.byref(B.CrossEntropyDesc(tokens, vocab, d, hidden_row, weight_row, ignore, dtype, reduction))
+
+
+def loss_forward(de, h=FAKE, w=FAKE, t=FAKE, out=FAKE, lse=FAKE, ws=FAKE, size=EMPTY):
+    return B._lib.efcp_cross_entropy_forward(de, h, w, t, out, lse, ws, size, None)
+
+
+def loss_backward(de, g=FAKE, step=1, h=FAKE, w=FAKE, t=FAKE, lse=FAKE, dh=FAKE, dw=FAKE, ws=FAKE, size=EMPTY):
+    return B._lib.efcp_cross_entropy_backward(de, g, step, h, w, t, lse, dh, dw, ws, size, None)
+
+
+@no_gpu
+def test_cross_entropy_calls():
+    assert C.sizeof(B.CrossEntropyDesc) == 6 * 8 + 2 * 4
+    for call in (loss_forward, loss_backward):
+        for de in (loss_desc(), loss_desc(dtype=0), loss_desc(dtype=2, reduction=1), loss_desc(d=1), loss_desc(vocab=1),
+                   loss_desc(hidden_row=0), loss_desc(weight_row=63), loss_desc(ignore=2 ** 62)):
+            assert call(de) == B.ECUDA
+        for de in (loss_desc(tokens=-1), loss_desc(tokens=1 << 30), loss_desc(vocab=0), loss_desc(vocab=1 << 30), loss_desc(d=0),
+                   loss_desc(d=1 << 24), loss_desc(hidden_row=-1), loss_desc(weight_row=-1), loss_desc(weight_row=1 << 33),
+                   loss_desc(dtype=3), loss_desc(dtype=-1), loss_desc(reduction=3), loss_desc(reduction=-1),
+                   loss_desc(tokens=1 << 29, d=1 << 20), None):
+            assert call(de) == B.EINVAL
+            if de is not None:
+                assert B._lib.efcp_cross_entropy_workspace_bytes(de, FAKE, 0) == -1
+        for more in (dict(h=None), dict(h=FAKE + 1), dict(w=None), dict(w=FAKE + 1), dict(t=None), dict(t=FAKE + 4),
+                     dict(lse=None), dict(lse=FAKE + 2), dict(ws=None), dict(ws=FAKE + 128)):
+            assert call(loss_desc(), **more) == B.EINVAL
+        assert call(loss_desc(), size=1000) == B.ENOMEM
+    assert loss_forward(loss_desc(), out=None) == loss_forward(loss_desc(), out=FAKE + 2) == B.EINVAL
+    assert loss_forward(loss_desc(tokens=0), h=None, t=None, out=None, lse=None) == B.OK
+    assert loss_forward(loss_desc(tokens=0, reduction=1), out=None) == B.EINVAL
+    for more in (dict(g=None), dict(g=FAKE + 2), dict(step=-1), dict(dh=FAKE + 1), dict(dw=FAKE + 1)):
+        assert loss_backward(loss_desc(), **more) == B.EINVAL
+    assert loss_backward(loss_desc(), dh=None) == loss_backward(loss_desc(), dw=None) == B.ECUDA
+    assert loss_backward(loss_desc(), dh=None, dw=None) == B.OK
+
+
+def test_the_cross_entropy_workspace():
+    size = lambda back, w=FAKE, **k: B._lib.efcp_cross_entropy_workspace_bytes(loss_desc(**k), w, back)  # noqa: E731
+    logits = 16384 * 64000 * 2
+    for back in (0, 1):
+        assert 0 < size(back, tokens=16384, vocab=64000) < logits / 4  # the logits are not kept
+        weight = 64000 * 64 * 2
+        for more in (dict(w=FAKE + 2), dict(weight_row=67)):  # a copy of the weight that can be read by tiles
+            assert size(back, tokens=1, vocab=64000, **more) - size(back, tokens=1, vocab=64000) >= weight
+    assert size(1, tokens=1 << 20, vocab=64000) - (1 << 20) * 64 * 6 < 2 * (1 << 20) * 256 + (64 << 20)
+
+
+@no_gpu
+def test_cross_entropy_tensors_that_are_refused():
+    h, w, t = torch.ones(4, 8), torch.ones(5, 8), torch.zeros(4, dtype=torch.int64)
+    good = (h, w, t)
+    with pytest.raises(ValueError, match="CUDA"):
+        B.cross_entropy_forward(*good)
+    for bad in ((h.double(), w.double(), t), (h, w.half(), t), (h, w[:, :7], t), (h, w[0], t), (h, w, t[:3]), (h, w, t.int()),
+                (torch.tensor(1.0), w, t), (h, w, t[None])):
+        with pytest.raises(ValueError):
+            B.cross_entropy_forward(*bad)
+    for bad in ((None, w, t), (h, 3, t), (h, w, [1, 2, 3, 4])):
+        with pytest.raises(TypeError):
+            B.cross_entropy_forward(*bad)
+    for call in (lambda s: B.cross_entropy_forward(*good, stream=s),
+                 lambda s: B.cross_entropy_backward(torch.ones(()), *good, torch.ones(4), stream=s)):
+        with pytest.raises(ValueError, match="stream"):
+            call(OtherStream())
+
+
+@pytest.mark.gpu
+def test_cross_entropy_arguments_that_are_refused():
+    h, w, t = torch.ones(4, 8, device="cuda"), torch.ones(5, 8, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    one, lse = torch.ones((), device="cuda"), torch.ones(4, device="cuda")
+    for call in (lambda: B.cross_entropy_forward(h, w, t, -100, "average"), lambda: B.cross_entropy_forward(h, w.cpu(), t),
+                 lambda: B.cross_entropy_forward(h, w, t.cpu()), lambda: B.cross_entropy_backward(one, h, w, t, lse[:3]),
+                 lambda: B.cross_entropy_backward(one, h, w, t, lse.double()), lambda: B.cross_entropy_backward(lse, h, w, t, lse),
+                 lambda: B.cross_entropy_backward(one, h, w, t, lse, -100, "none"),
+                 lambda: B.cross_entropy_backward(one.double(), h, w, t, lse)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(B.EfcpError):
+        B.cross_entropy_forward(h, w[:0], t)
+    with pytest.raises(B.EfcpError):
+        B.cross_entropy_forward(h[:, :0], w[:, :0], t)
