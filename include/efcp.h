@@ -616,8 +616,6 @@ int efcp_dropout(const efcp_rms_norm* desc, const void* x, int64_t x_row, const 
  * EFCP_EINVAL (nothing enqueued): null or misaligned pointers, tokens outside 0 .. 2^30 - 1, vocab
  * outside 1 .. 2^30 - 1, d outside 1 .. 2^24 - 1, matrices above 2^40 elements, strides that are negative or above 2^32,
  * unknown types or reductions; EFCP_ENOMEM: a workspace that is too small.
- *   efcp_cross_entropy_status : waits for the device's work on the default stream; EFCP_ETIMEOUT when a wait
- *                    inside a kernel of these calls ran out (2 s; the results of that call are undefined), else EFCP_OK.
  */
 #define EFCP_LOSS_NONE 0
 #define EFCP_LOSS_MEAN 1
@@ -636,7 +634,13 @@ int efcp_cross_entropy_backward(const efcp_cross_entropy* desc, const float* gra
                                 const void* hidden, const void* weight, const int64_t* targets,
                                 const float* lse, void* dhidden, void* dweight, void* workspace,
                                 int64_t workspace_bytes, void* stream);
-int efcp_cross_entropy_status(void);
+
+/*
+ * Whether a wait inside a kernel of the RMS-norm or cross-entropy calls has run out (2 s) on the current device since
+ * the library was loaded: EFCP_ETIMEOUT, and the results of that call are undefined; else EFCP_OK.  Waits for
+ * the work of the default stream only: synchronise others first.
+ */
+int efcp_operators_status(void);
 
 /* Static description of an EFCP_* code. */
 const char* efcp_strerror(int code);

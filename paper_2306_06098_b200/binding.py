@@ -129,7 +129,7 @@ EXPORTS = {
     "efcp_cross_entropy_forward": ([C.POINTER(CrossEntropyDesc)] + [_vp] * 6 + [_i64, _vp], C.c_int),
     "efcp_cross_entropy_backward": ([C.POINTER(CrossEntropyDesc), _vp, _i64] + [_vp] * 7 + [_i64, _vp],
                                     C.c_int),
-    "efcp_cross_entropy_status": ([], C.c_int),
+    "efcp_operators_status": ([], C.c_int),
     "efcp_strerror": ([C.c_int], C.c_char_p),
 }
 for _name, (_args, _res) in EXPORTS.items():
@@ -221,12 +221,13 @@ def cross_entropy_backward(grad: torch.Tensor, hidden: torch.Tensor, weight: tor
                                                  reduction, *want), "efcp_cross_entropy_backward")
 
 
-def cross_entropy_status():
-    """Waits for the default stream's work; raises when a wait inside a kernel of the two calls above
-    ran out (their results are undefined then)."""
-    rc = _lib.efcp_cross_entropy_status()
+def operators_status():
+    """efcp_operators_status after the device's work: raises when a wait inside a kernel of the RMS-norm or
+    cross-entropy calls has run out (the results of that call are undefined)."""
+    torch.cuda.synchronize()
+    rc = _lib.efcp_operators_status()
     if rc != OK:
-        raise EfcpError(rc, "efcp_cross_entropy_status")
+        raise EfcpError(rc, "efcp_operators_status")
 
 
 class EfcpError(RuntimeError):

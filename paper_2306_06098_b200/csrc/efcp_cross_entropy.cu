@@ -11,6 +11,7 @@
 
 #include "efcp_device.h"
 #include "efcp_launch.cuh"
+#include "efcp_status.h"
 #include "efcp_xent.h"
 
 namespace efcp {
@@ -18,9 +19,8 @@ namespace {
 
 constexpr unsigned kAllLanes = 0xFFFFFFFFu;
 
-__device__ int xent_status;
-
-// lse and loss of a token from the statistics of its logits' parts; a warp takes a token.
+// lse and loss of a token from the statistics of its logits' parts (their largest values are in units of log2(e)); a
+// warp takes a token.  The last steps are in 64 bits: lse is several times as large as the loss.
 __global__ void __launch_bounds__(256) k_xent_join(const XentPrep p) {
   take_turn();
   const int lane = threadIdx.x & 31, count = *p.count;
@@ -31,13 +31,14 @@ __global__ void __launch_bounds__(256) k_xent_join(const XentPrep p) {
     for (int k = lane; k < p.parts; k += 32) top = fmaxf(top, part[k].x);
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kAllLanes, top, o));
-    for (int k = lane; k < p.parts; k += 32) sum += part[k].y * expf(part[k].x - top);
+    for (int k = lane; k < p.parts; k += 32) sum += part[k].y * exp2f(part[k].x - top);
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAllLanes, sum, o);
     if (lane) continue;
-    const float lse = top + logf(sum);
-    const float loss = p.target[i] < 0 ? __int_as_float(0x7FC00000) : lse - p.target_logit[i];
-    p.lse_out[p.order[i]] = lse;
+    const double lse = (double(top) + log2(double(sum))) * 0.69314718055994530942;
+    const float loss =
+        p.target[i] < 0 ? __int_as_float(0x7FC00000) : float(lse - double(p.target_logit[i]));
+    p.lse_out[p.order[i]] = float(lse);
     if (p.reduction) p.each[i] = loss;
     else p.losses[p.order[i]] = loss;
   }
@@ -87,19 +88,16 @@ struct Plan {
   bool in_place;
   int64_t padded;      // tokens up to whole tiles
   int64_t packed_row;  // elements of a packed row
-  int col_tiles, col_tile, parts;
   int64_t piece;       // columns of the vocabulary at a time
   int pieces;
+  int col_tiles, col_tile;  // of the logits: all of them forward, a piece's backward
+  int parts;
   int d_tiles, d_tile;
-  int64_t sum_row;
+  int pairs;
+  int64_t sum_row, sum_rows;
   // offsets
-  int64_t count, scale, order, target, lse, coef, logit, each, part, hidden, weight, g, sum, bytes;
+  int64_t count, scale, order, target, lse, coef, place, logit, each, part, hidden, weight, g[2], sum, bytes;
 };
-
-int tile_of(int64_t n, int* tiles) {
-  *tiles = int(ceil_div(n, kXentCols));
-  return int(round_up(ceil_div(n, *tiles), 64));
-}
 
 // Whether the tensor copies can read the weight where it lies.
 bool in_place(const efcp_cross_entropy& d, const void* weight) {
@@ -107,19 +105,26 @@ bool in_place(const efcp_cross_entropy& d, const void* weight) {
          d.weight_row >= d.d;
 }
 
-Plan make_plan(const efcp_cross_entropy& d, const void* weight, bool backward) {
+// Tiles of equal width, a multiple of 128.
+int tile_of(int64_t n, int* tiles) {
+  *tiles = int(ceil_div(n, kXentCols));
+  return int(round_up(ceil_div(n, *tiles), 128));
+}
+
+Plan make_plan(const efcp_cross_entropy& d, const void* weight, bool backward, int sms) {
   Plan p{};
   p.planes = d.dtype == EFCP_F32 ? 3 : 1;
   p.padded = round_up(std::max<int64_t>(1, d.tokens), kXentRows);
   p.packed_row = round_up(d.d, 8);
-  p.col_tile = tile_of(d.vocab, &p.col_tiles);
-  p.parts = 2 * p.col_tiles;
+  p.pairs = std::max(1, sms / 2);
   p.d_tile = tile_of(d.d, &p.d_tiles);
   p.sum_row = round_up(d.d, 32);
-  const int64_t most = std::max<int64_t>(1, kGradBytes / (2 * p.planes * p.padded * kXentCols));  // tiles
+  const int64_t most = std::max<int64_t>(1, kGradBytes / 2 / (2 * p.planes * p.padded * kXentCols));  // tiles
   p.pieces = int(ceil_div(ceil_div(d.vocab, kXentCols), most));
   p.piece = p.pieces == 1 ? round_up(d.vocab, 64) : round_up(ceil_div(d.vocab, p.pieces), kXentCols);
   p.pieces = int(ceil_div(d.vocab, p.piece));
+  p.col_tile = tile_of(backward ? p.piece : d.vocab, &p.col_tiles);
+  p.parts = 2 * p.col_tiles;
   int64_t at = 0;
   const auto take = [&](int64_t bytes) {
     const int64_t here = at;
@@ -137,8 +142,15 @@ Plan make_plan(const efcp_cross_entropy& d, const void* weight, bool backward) {
   if (backward) {
     p.lse = take(4 * p.padded);
     p.coef = take(4 * p.padded);
-    p.g = take(2 * p.planes * p.padded * p.piece);
-    if (p.pieces > 1) p.sum = take(4 * p.padded * p.sum_row);
+    p.place = take(4 * p.padded);
+    for (int i = 0; i < std::min(2, p.pieces); ++i) p.g[i] = take(2 * p.planes * p.padded * p.piece);
+    // how many rows count is not known here: the most that any number of them takes with its parts
+    const int64_t rows = p.padded / kXentRows;
+    int64_t parts = 0;
+    for (int64_t r = 1; r <= std::min<int64_t>(rows, 2 * p.pairs + 1); ++r)
+      parts = std::max<int64_t>(parts, r * xent_splits(int(r), p.d_tiles, int(p.piece), p.pairs));
+    p.sum_rows = std::max(rows, parts) * kXentRows;
+    p.sum = take(4 * p.sum_rows * p.sum_row);
   } else {
     p.each = take(4 * p.padded);
     p.part = take(8 * p.padded * p.parts);
@@ -166,17 +178,21 @@ EncodeTiled encoder() {
   return f;
 }
 
-// Planes of rows of `cols` elements of 2 bytes, copied in boxes of 64 x 64.
+// Planes of rows of `cols` elements, `row` elements apart, copied in boxes of `box_rows` rows of 128 (or 64) bytes.
 bool make_map(CUtensorMap* map, int dtype, const void* base, int64_t cols, int64_t rows, int64_t row,
-              int planes, int64_t plane) {
+              int planes, int64_t plane, int box_rows, int box_bytes = 128) {
   const EncodeTiled f = encoder();
   if (!f) return false;
-  const cuuint64_t size[3] = {cuuint64_t(cols), cuuint64_t(rows), cuuint64_t(planes)};
-  const cuuint64_t stride[2] = {cuuint64_t(row) * 2, cuuint64_t(planes > 1 ? plane : row) * 2};
-  const cuuint32_t box[3] = {64, 64, 1}, step[3] = {1, 1, 1};
-  return f(map, dtype == EFCP_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
-           const_cast<void*>(base), size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+  const int size = kTypeBytes[dtype];
+  const cuuint64_t sizes[3] = {cuuint64_t(cols), cuuint64_t(rows), cuuint64_t(planes)};
+  const cuuint64_t stride[2] = {cuuint64_t(row) * size, cuuint64_t(planes > 1 ? plane : row) * size};
+  const cuuint32_t box[3] = {cuuint32_t(box_bytes / size), cuuint32_t(box_rows), 1}, step[3] = {1, 1, 1};
+  const CUtensorMapDataType type = dtype == EFCP_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == EFCP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                        : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  return f(map, type, 3, const_cast<void*>(base), sizes, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+           box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+           CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -187,12 +203,14 @@ struct Call {
   cudaStream_t st;
   XentPrep prep{};
   XentGemm gemm{};
-  CUtensorMap hidden, weight, g;
 
   template <class T>
   T* at(void* ws, int64_t off) const {
     return reinterpret_cast<T*>(static_cast<char*>(ws) + off);
   }
+
+  // (fp32 operands are held as three bfloat16 ones)
+  int operand_type() const { return d.dtype == EFCP_F16 ? EFCP_F16 : EFCP_BF16; }
 
   bool begin(const void* h, const void* w, const int64_t* targets, void* ws) {
     const Plan& p = plan;
@@ -217,22 +235,34 @@ struct Call {
     prep.target_logit = at<float>(ws, p.logit);
     prep.parts = p.parts;
     prep.reduction = d.reduction;
+    prep.d_tiles = p.d_tiles;
+    prep.piece = int(p.piece);
+    prep.pairs = p.pairs;
     gemm.count = prep.count;
-    gemm.order = prep.order;
     gemm.target = prep.target;
     gemm.scale = prep.scale;
     gemm.target_logit = prep.target_logit;
     gemm.parts = p.parts;
     gemm.vocab = prep.vocab;
     gemm.d = prep.d;
-    gemm.planes = p.planes;
-    void* status = nullptr;
-    if (cudaGetSymbolAddress(&status, xent_status) != cudaSuccess) return false;
-    gemm.status = static_cast<int*>(status);
-    return make_map(&hidden, d.dtype, prep.hidden_packed, d.d, p.padded, p.packed_row, p.planes,
-                    prep.hidden_plane) &&
-           make_map(&weight, d.dtype, p.in_place ? w : prep.weight_packed, d.d, d.vocab,
-                    p.in_place ? d.weight_row : p.packed_row, p.planes, prep.weight_plane);
+    gemm.d_tiles = p.d_tiles;
+    gemm.d_tile = p.d_tile;
+    gemm.col_tiles = p.col_tiles;
+    gemm.col_tile = p.col_tile;
+    gemm.piece = int(p.piece);
+    gemm.status = device_status();
+    if (!gemm.status) return false;
+    const void* weight = p.in_place ? w : prep.weight_packed;
+    const int64_t weight_row = p.in_place ? d.weight_row : p.packed_row;
+    const int type = operand_type();
+    const auto hidden_map = [&](CUtensorMap* m, int box) {
+      return make_map(m, type, prep.hidden_packed, d.d, p.padded, p.packed_row, p.planes, prep.hidden_plane, box);
+    };
+    const auto weight_map = [&](CUtensorMap* m, int box) {
+      return make_map(m, type, weight, d.d, d.vocab, weight_row, p.planes, prep.weight_plane, box);
+    };
+    return hidden_map(&gemm.hidden_rows, kXentRows / 2) && hidden_map(&gemm.hidden_cols, 64) &&
+           weight_map(&gemm.weight_rows, p.col_tile / 2) && weight_map(&gemm.weight_cols, 64);
   }
 
   bool prepare(bool backward) {
@@ -242,20 +272,19 @@ struct Call {
     return e == cudaSuccess;
   }
 
-  bool multiply(XentMode mode, int64_t tiles) {
-    const unsigned blocks = unsigned(std::max<int64_t>(1, std::min<int64_t>(tiles, sms)));
-    const cudaError_t e = d.dtype == EFCP_F32    ? xent_gemm_f32(mode, gemm, blocks, st)
-                          : d.dtype == EFCP_BF16 ? xent_gemm_bf16(mode, gemm, blocks, st)
-                                                 : xent_gemm_f16(mode, gemm, blocks, st);
+  bool multiply(bool backward) {
+    const unsigned pairs = unsigned(plan.pairs);
+    const cudaError_t e = d.dtype == EFCP_F32    ? xent_gemm_f32(backward, gemm, pairs, st)
+                          : d.dtype == EFCP_BF16 ? xent_gemm_bf16(backward, gemm, pairs, st)
+                                                 : xent_gemm_f16(backward, gemm, pairs, st);
     return e == cudaSuccess;
   }
 
-  bool logits(XentMode mode) {
-    gemm.a = hidden;
-    gemm.b = weight;
-    gemm.row_tiles = -1;
-    gemm.depth = gemm.d;
-    return multiply(mode, plan.padded / kXentRows * gemm.col_tiles);
+  bool finish() {
+    const cudaError_t e = d.dtype == EFCP_F32    ? xent_finish_f32(prep, sms, st)
+                          : d.dtype == EFCP_BF16 ? xent_finish_bf16(prep, sms, st)
+                                                 : xent_finish_f16(prep, sms, st);
+    return e == cudaSuccess;
   }
 };
 
@@ -274,7 +303,8 @@ extern "C" {
 int64_t efcp_cross_entropy_workspace_bytes(const efcp_cross_entropy* desc, const void* weight,
                                            int32_t backward) {
   if (!valid(desc)) return -1;
-  return make_plan(*desc, weight, backward != 0).bytes;
+  const int sms = device_sms();
+  return make_plan(*desc, weight, backward != 0, sms < 1 ? 148 : sms).bytes;  // (no device: a B200's)
 }
 
 int efcp_cross_entropy_forward(const efcp_cross_entropy* desc, const void* hidden, const void* weight,
@@ -285,20 +315,19 @@ int efcp_cross_entropy_forward(const efcp_cross_entropy* desc, const void* hidde
   if (desc->reduction && misaligned(losses, 4)) return EFCP_EINVAL;
   if (desc->tokens && (misaligned(hidden, size) || misaligned(targets, 8))) return EFCP_EINVAL;
   if (misaligned(weight, size) || misaligned(workspace, 256)) return EFCP_EINVAL;
-  Call c{*desc, make_plan(*desc, weight, false)};
+  const int sms = device_sms();
+  Call c{*desc, make_plan(*desc, weight, false, sms < 1 ? 148 : sms), sms};
   if (workspace_bytes < c.plan.bytes) return EFCP_ENOMEM;
   if (desc->tokens == 0 && !desc->reduction) return EFCP_OK;
-  c.sms = device_sms();
-  if (c.sms < 1) return EFCP_ECUDA;
+  if (sms < 1) return EFCP_ECUDA;
   c.st = static_cast<cudaStream_t>(stream);
   if (!c.begin(hidden, weight, targets, workspace)) return failed();
   c.prep.losses = losses;
   c.prep.lse_out = lse;
   c.prep.each = c.at<float>(workspace, c.plan.each);
   c.prep.part = c.gemm.part = c.at<float2>(workspace, c.plan.part);
-  c.gemm.col_tiles = c.plan.col_tiles;
-  c.gemm.col_tile = c.plan.col_tile;
-  if (!c.prepare(false) || !c.logits(kXentStats) || xent_join(c.prep, c.sms, c.st) != cudaSuccess)
+  c.gemm.logits = 1;
+  if (!c.prepare(false) || !c.multiply(false) || xent_join(c.prep, c.sms, c.st) != cudaSuccess)
     return failed();
   return EFCP_OK;
 }
@@ -314,12 +343,12 @@ int efcp_cross_entropy_backward(const efcp_cross_entropy* desc, const float* gra
     return EFCP_EINVAL;
   if (misaligned(weight, size) || (dweight && misaligned(dweight, size)) || misaligned(workspace, 256))
     return EFCP_EINVAL;
-  Call c{*desc, make_plan(*desc, weight, true)};
+  const int sms = device_sms();
+  Call c{*desc, make_plan(*desc, weight, true, sms < 1 ? 148 : sms), sms};
   if (workspace_bytes < c.plan.bytes) return EFCP_ENOMEM;
   c.st = static_cast<cudaStream_t>(stream);
   if (!dhidden && !dweight) return EFCP_OK;
-  c.sms = device_sms();
-  if (c.sms < 1) return EFCP_ECUDA;
+  if (sms < 1) return EFCP_ECUDA;
   if (desc->tokens == 0) {
     if (dweight && cudaMemsetAsync(dweight, 0, size_t(desc->vocab * desc->d) * size, c.st) != cudaSuccess)
       return failed();
@@ -333,53 +362,43 @@ int efcp_cross_entropy_backward(const efcp_cross_entropy* desc, const float* gra
   c.prep.lse_in = lse;
   c.prep.lse = c.at<float>(workspace, p.lse);
   c.prep.coef = c.at<float>(workspace, p.coef);
+  c.prep.place = c.at<int>(workspace, p.place);
+  float* sum = c.at<float>(workspace, p.sum);
+  c.prep.sum = sum;
+  c.prep.sum_row = p.sum_row;
   c.prep.dhidden = dhidden;
   m.lse = c.prep.lse;
   m.coef = c.prep.coef;
-  m.g = c.at<void>(workspace, p.g);
-  m.g_row = p.piece;
-  m.g_plane = p.padded * p.piece;
-  m.sum = c.at<float>(workspace, p.sum);
-  m.sum_row = p.sum_row;
-  m.out_row = desc->d;
-  m.piece = int(p.piece);
-  if (!make_map(&c.g, desc->dtype, m.g, p.piece, p.padded, p.piece, p.planes, m.g_plane) ||
-      !c.prepare(true))
-    return failed();
-  for (int k = 0; k < p.pieces; ++k) {
-    m.v0 = int(k * p.piece);
-    m.first = k == 0;
-    m.last = k == p.pieces - 1;
-    m.col_tile = tile_of(p.piece, &m.col_tiles);
-    if (!c.logits(kXentGrad)) return failed();
-    m.col_tiles = p.d_tiles;
-    m.col_tile = p.d_tile;
-    if (dhidden) {
-      m.a = c.g;
-      m.b = c.weight;
-      m.row_tiles = -1;
-      m.depth = m.piece;
-      m.out = dhidden;
-      m.vec_out = reinterpret_cast<uintptr_t>(dhidden) % 16 == 0 && desc->d * size % 16 == 0;
-      if (!c.multiply(kXentHidden, p.padded / kXentRows * p.d_tiles)) return failed();
-    }
-    if (dweight) {
-      m.a = c.g;
-      m.b = c.hidden;
-      m.row_tiles = int(ceil_div(std::min<int64_t>(p.piece, desc->vocab - m.v0), kXentRows));
-      m.depth = -1;
-      m.out = dweight;
-      m.vec_out = reinterpret_cast<uintptr_t>(dweight) % 16 == 0 && desc->d * size % 16 == 0;
-      if (!c.multiply(kXentWeight, int64_t(m.row_tiles) * p.d_tiles)) return failed();
-    }
+  m.dweight = dweight;
+  m.box_dweight = dweight && reinterpret_cast<uintptr_t>(dweight) % 16 == 0 && desc->d * size % 16 == 0;
+  const int type = c.operand_type();
+  const int64_t plane = p.padded * p.piece;
+  for (int i = 0; i < 2; ++i) {
+    const void* g = c.at<void>(workspace, p.g[p.pieces > 1 ? i : 0]);
+    if (!make_map(&m.g_rows[i], type, g, p.piece, p.padded, p.piece, p.planes, plane, kXentRows / 2) ||
+        !make_map(&m.g_cols[i], type, g, p.piece, p.padded, p.piece, p.planes, plane, 64) ||
+        !make_map(&m.g_out[i], type, g, p.piece, p.padded, p.piece, p.planes, plane, 32, p.planes == 1 ? 128 : 64))
+      return failed();
   }
+  if (!make_map(&m.sum_out, EFCP_F32, sum, p.sum_row, p.sum_rows, p.sum_row, 1, 0, 32) ||
+      (m.box_dweight &&
+       !make_map(&m.dweight_out, desc->dtype, dweight, desc->d, desc->vocab, desc->d, 1, 0, 32)))
+    return failed();
+  if (!c.prepare(true)) return failed();
+  // launch k: the products of piece k - 1, the logits of piece k
+  for (int k = 0; k <= p.pieces; ++k) {
+    m.logits = k < p.pieces;
+    m.next_v0 = int(k * p.piece);
+    m.next_buffer = k & 1;
+    m.hidden = k > 0 && dhidden;
+    m.weight = k > 0 && dweight;
+    m.first = k == 1;
+    m.v0 = k > 0 ? int((k - 1) * p.piece) : 0;
+    m.buffer = (k + 1) & 1;
+    if (!c.multiply(true)) return failed();
+  }
+  if (dhidden && !c.finish()) return failed();
   return EFCP_OK;
-}
-
-int efcp_cross_entropy_status(void) {
-  int s = 0;
-  if (cudaMemcpyFromSymbol(&s, xent_status, sizeof s) != cudaSuccess) return failed();
-  return s;
 }
 
 }  // extern "C"

@@ -32,9 +32,9 @@ __device__ __forceinline__ DropKey drop_key(const Drop& d) {
   return {uint32_t(s), uint32_t(s >> 32), uint32_t(o), uint32_t(o >> 32)};
 }
 
-// Bit j: element 8 * group + j stays.
-__device__ __forceinline__ uint32_t drop_keep8(unsigned long long group, const DropKey& key,
-                                               uint32_t threshold) {
+// The four words of a group of eight elements.
+__device__ __forceinline__ void drop_words(unsigned long long group, const DropKey& key,
+                                           uint32_t (&word)[4]) {
   uint32_t a = uint32_t(group), b = uint32_t(group >> 32), c = key.o0, d = key.o1;
   uint32_t k0 = key.k0, k1 = key.k1;
 #pragma unroll
@@ -47,14 +47,34 @@ __device__ __forceinline__ uint32_t drop_keep8(unsigned long long group, const D
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
   }
-  uint32_t keep = 0;
-  const uint32_t word[4] = {a, b, c, d};
+  word[0] = a; word[1] = b; word[2] = c; word[3] = d;
+}
+
+// Bit j: element 8 * group + j stays.
+__device__ __forceinline__ uint32_t drop_keep8(unsigned long long group, const DropKey& key,
+                                               uint32_t threshold) {
+  uint32_t keep = 0, word[4];
+  drop_words(group, key, word);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     keep |= uint32_t((word[i] & 0xFFFFu) >= threshold) << (2 * i);
     keep |= uint32_t((word[i] >> 16) >= threshold) << (2 * i + 1);
   }
   return keep;
+}
+
+// Dropout of the eight elements of a group.  (A half-word in the upper half of a register is compared there, next to
+// whatever the lower half holds: one instruction less.)
+__device__ __forceinline__ void drop_group(float (&v)[8], unsigned long long group, const DropKey& key,
+                                           uint32_t threshold, float scale) {
+  uint32_t word[4];
+  drop_words(group, key, word);
+  const uint32_t below = (threshold << 16) - 1;  // (threshold > 0; 65536 drops all)
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = (word[i] << 16) > below ? v[2 * i] * scale : 0.f;
+    v[2 * i + 1] = word[i] > below ? v[2 * i + 1] * scale : 0.f;
+  }
 }
 
 }  // namespace efcp

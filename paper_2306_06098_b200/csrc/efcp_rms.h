@@ -25,6 +25,16 @@ struct Rms {
   float* scales;
   int block, blocks;  // columns that share a scale (0: a row), scales of a row
   float most;         // largest value of the 8-bit type
+  int* status;
+};
+
+// Rows that arrive in shared memory by bulk copies, some ahead of their use.  A group of warps has a ring of `stages`
+// places of its own; a place holds a unit: one row, or several short ones that share a warp.
+struct RmsRing {
+  int stages, inputs;
+  int rows, lanes;     // rows of a unit, lanes that share a row (32 unless rows > 1)
+  int row_bytes, unit_bytes;
+  int weight_at, data_at;  // in shared memory: the weight in fp32, the rings
 };
 
 enum RmsOp { kRmsForward, kRmsE4M3, kRmsInt8, kRmsBackward, kDropout };
@@ -35,6 +45,9 @@ struct RmsLaunch {
   int kept;         // chunks that a warp keeps in registers: 1, 2, 4, or 0 (rows walked twice)
   unsigned blocks;
   long long parts;  // rows of `part`
+  bool ringed;      // see RmsRing
+  RmsRing ring;
+  size_t smem;
   cudaStream_t st;
 };
 

@@ -9,12 +9,24 @@
 
 #include "efcp_device.h"
 #include "efcp_rms.h"
+#include "efcp_status.h"
 
 namespace efcp {
+
+__device__ int operators_status;
+
+int* device_status() {
+  void* p = nullptr;
+  if (cudaGetSymbolAddress(&p, operators_status) == cudaSuccess) return static_cast<int*>(p);
+  (void)cudaGetLastError();
+  return nullptr;
+}
+
 namespace {
 
 constexpr int kTypeBytes[3] = {4, 2, 2};
 constexpr int kColumns = 256;  // of a chunk: see efcp_rows.cuh
+constexpr int64_t kMostSmem = 115400;  // leaves an SM room for two blocks, with what is not dynamic
 constexpr int64_t kMostBlocks = (1ll << 31) - 1;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -77,6 +89,37 @@ void share(const efcp_rms_norm* d, int sms, Rms* p, RmsLaunch* l) {
   p->groups = l->kept && p->warps < 8 ? 8 / p->warps : 1;
 }
 
+// Rows through shared memory, where a group of warps has two places at least: whether that is so, and how.  Units of
+// several rows for rows of up to 128 elements; a warp takes rows of up to 1024 alone.  With fewer rows than places to
+// work on them the plain kernels are as fast or faster: there is nothing to fetch ahead.
+bool plan_ring(const efcp_rms_norm* d, bool vec, int inputs, bool weight, int sms, Rms* p, RmsLaunch* l) {
+  if (!vec || d->rows < 2 * sms || d->d > 8192) return false;
+  const int64_t chunks = ceil_div(d->d, kColumns), row_bytes = d->d * kTypeBytes[d->dtype];
+  RmsRing& q = l->ring;
+  q = RmsRing{};
+  q.inputs = inputs;
+  q.lanes = 32;
+  while (q.lanes > 1 && d->d <= q.lanes * 4) q.lanes /= 2;
+  q.rows = 32 / q.lanes;
+  q.row_bytes = int(row_bytes);
+  q.unit_bytes = int(row_bytes * q.rows);
+  p->warps = chunks <= 4 ? 1 : int(std::min<int64_t>(8, ceil_div(chunks, 2)));
+  p->groups = 8 / p->warps;
+  const int64_t kept = ceil_div(chunks, p->warps);
+  l->kept = kept <= 2 ? int(kept) : 4;
+  q.weight_at = 512;  // behind the barriers
+  q.data_at = int(ceil_div(q.weight_at + (weight ? d->d * 4 : 0), 128) * 128);
+  const int64_t stage = int64_t(p->groups) * inputs * q.unit_bytes;
+  q.stages = int(std::min<int64_t>(4, (kMostSmem - q.data_at) / stage));
+  if (q.stages < 2) return false;
+  l->ringed = true;
+  l->smem = size_t(q.data_at + q.stages * stage);
+  const int64_t units = ceil_div(d->rows, q.rows);
+  l->blocks = unsigned(std::min<int64_t>(2 * sms, ceil_div(units, p->groups)));
+  l->parts = int64_t(l->blocks) * p->groups;
+  return true;
+}
+
 struct Backward {
   unsigned blocks;
   int64_t parts;
@@ -91,8 +134,10 @@ Backward backward_blocks(const efcp_rms_norm* d, int sms, const Rms& p, const Rm
   return {unsigned(blocks), 8 * y};
 }
 
-int run(const Rms& p, RmsLaunch& l, int dtype, cudaStream_t st) {
+int run(Rms& p, RmsLaunch& l, int dtype, cudaStream_t st) {
   l.st = st;
+  p.status = device_status();
+  if (!p.status) return EFCP_ECUDA;
   const cudaError_t e = dtype == EFCP_F32    ? rms_launch_f32(p, l)
                         : dtype == EFCP_BF16 ? rms_launch_bf16(p, l)
                                              : rms_launch_f16(p, l);
@@ -120,10 +165,13 @@ int forward(const efcp_rms_norm* d, RmsOp op, const void* x, int64_t x_row, cons
   l.op = op;
   l.vec = d->d % 8 == 0 && wide(d, x, x_row) && wide(d, residual, residual_row) && wide(d, weight, 0) &&
           (!summed || wide(d, h, 0)) && reinterpret_cast<uintptr_t>(y) % 16 == 0;
-  share(d, sms, &p, &l);
-  const int64_t blocks = ceil_div(d->rows, p.groups);
-  if (blocks > kMostBlocks) return EFCP_ETOOBIG;
-  l.blocks = unsigned(blocks);
+  const bool ring = op == kRmsForward || d->p == 0.;
+  if (!plan_ring(d, l.vec && ring, residual ? 2 : 1, weight, sms, &p, &l)) {
+    share(d, sms, &p, &l);
+    const int64_t blocks = ceil_div(d->rows, p.groups);
+    if (blocks > kMostBlocks) return EFCP_ETOOBIG;
+    l.blocks = unsigned(blocks);
+  }
   p.x = x; p.x_row = x_row; p.residual = residual; p.residual_row = residual_row;
   p.weight = weight; p.y = y; p.h = summed ? h : nullptr; p.rstd = rstd;
   p.scales = scales; p.block = block;
@@ -164,8 +212,13 @@ int64_t efcp_rms_norm_workspace_bytes(const efcp_rms_norm* desc) {
   if (sms < 1) sms = 148;  // no device: the SM count of a B200
   Rms p = common(desc);
   RmsLaunch l{};
+  // (whether the rows go through shared memory hangs on their alignment, which is not known here)
+  int64_t parts = 0;
+  for (int inputs : {2, 3})
+    if (plan_ring(desc, desc->d % 8 == 0, inputs, false, sms, &p, &l)) parts = std::max<int64_t>(parts, l.parts);
   share(desc, sms, &p, &l);
-  return std::max<int64_t>(16, backward_blocks(desc, sms, p, l).parts * desc->d * 4);
+  parts = std::max(parts, backward_blocks(desc, sms, p, l).parts);
+  return std::max<int64_t>(16, parts * desc->d * 4);
 }
 
 int efcp_rms_norm_backward(const efcp_rms_norm* desc, const void* dy, int64_t dy_row, const void* h,
@@ -195,11 +248,13 @@ int efcp_rms_norm_backward(const efcp_rms_norm* desc, const void* dy, int64_t dy
   l.op = kRmsBackward;
   l.vec = desc->d % 8 == 0 && wide(desc, dy, dy_row) && wide(desc, h, h_row) && wide(desc, dh, dh_row) &&
           wide(desc, weight, 0) && wide(desc, dx, 0) && wide(desc, dresidual, 0);
-  share(desc, sms, &p, &l);
-  const Backward b = backward_blocks(desc, sms, p, l);
-  l.blocks = b.blocks;
-  l.parts = b.parts;
-  if (dweight && workspace_bytes < b.parts * desc->d * 4) return EFCP_ENOMEM;
+  if (!plan_ring(desc, l.vec, dh ? 3 : 2, weight, sms, &p, &l)) {
+    share(desc, sms, &p, &l);
+    const Backward b = backward_blocks(desc, sms, p, l);
+    l.blocks = b.blocks;
+    l.parts = b.parts;
+  }
+  if (dweight && workspace_bytes < l.parts * desc->d * 4) return EFCP_ENOMEM;
   p.dy = dy; p.dy_row = dy_row; p.x = h; p.x_row = h_row; p.dh = dh; p.dh_row = dh_row;
   p.rstd = const_cast<float*>(rstd); p.weight = weight;
   p.dx = dx; p.dresidual = dresidual; p.dweight = dweight;
@@ -226,6 +281,13 @@ int efcp_dropout(const efcp_rms_norm* desc, const void* x, int64_t x_row, const 
   l.blocks = unsigned(std::min<int64_t>(ceil_div(chunks, 8), 8ll * sms));
   p.x = x; p.x_row = x_row; p.residual = residual; p.residual_row = residual_row; p.y = y;
   return run(p, l, desc->dtype, static_cast<cudaStream_t>(stream));
+}
+
+int efcp_operators_status(void) {
+  int s = 0;
+  if (cudaMemcpyFromSymbol(&s, operators_status, sizeof s) == cudaSuccess) return s;
+  (void)cudaGetLastError();
+  return EFCP_ECUDA;
 }
 
 }  // extern "C"

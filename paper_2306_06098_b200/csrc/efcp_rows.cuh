@@ -72,32 +72,35 @@ __device__ __forceinline__ void store8(T* row, int c0, int lane, int d, const fl
   }
 }
 
-// Bit j: the lane's element j of the chunk whose first element is `first` in the logical order stays.
-// Where rows do not start on a multiple of eight, the 32 groups that begin in the chunk are spread over the lanes,
-// with one more behind them.
-template <bool VEC>
+// Bit j: element j * 32 + lane of the chunk whose first element is `first` in the logical order stays.  Rows need not
+// start on a multiple of eight: the 32 groups that begin in the chunk are spread over the lanes, with one more behind
+// them.
 __device__ __forceinline__ uint32_t keep8(unsigned long long first, int lane, const DropKey& key,
                                           uint32_t threshold) {
-  if constexpr (VEC) {
-    return drop_keep8((first >> 3) + lane, key, threshold);  // d is a multiple of 8
-  } else {
-    const int s = int(first & 7);
-    const uint32_t mine = drop_keep8((first >> 3) + lane, key, threshold);
-    const uint32_t last = s ? drop_keep8((first >> 3) + 32, key, threshold) : 0;
-    uint32_t keep = 0;
+  const int s = int(first & 7);
+  const uint32_t mine = drop_keep8((first >> 3) + lane, key, threshold);
+  const uint32_t last = s ? drop_keep8((first >> 3) + 32, key, threshold) : 0;
+  uint32_t keep = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int q = j * 32 + lane + s;
-      const uint32_t other = __shfl_sync(kAll, mine, (q >> 3) & 31);
-      keep |= (((q >= 256 ? last : other) >> (q & 7)) & 1u) << j;
-    }
-    return keep;
+  for (int j = 0; j < 8; ++j) {
+    const int q = j * 32 + lane + s;
+    const uint32_t other = __shfl_sync(kAll, mine, (q >> 3) & 31);
+    keep |= (((q >= 256 ? last : other) >> (q & 7)) & 1u) << j;
   }
+  return keep;
 }
 
-__device__ __forceinline__ void drop8(float (&v)[8], uint32_t keep, float scale) {
+// Dropout of a lane's eight elements of that chunk.
+template <bool VEC>
+__device__ __forceinline__ void drop8(float (&v)[8], unsigned long long first, int lane, const DropKey& key,
+                                      const Drop& drop) {
+  if constexpr (VEC) {
+    drop_group(v, (first >> 3) + lane, key, drop.threshold, drop.scale);
+  } else {
+    const uint32_t keep = keep8(first, lane, key, drop.threshold);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = (keep >> j) & 1u ? v[j] * scale : 0.f;
+    for (int j = 0; j < 8; ++j) v[j] = (keep >> j) & 1u ? v[j] * drop.scale : 0.f;
+  }
 }
 
 template <typename T>
@@ -110,10 +113,14 @@ __device__ __forceinline__ float warp_sum(float v) {
   for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
   return v;
 }
-// maximum over the lanes whose numbers agree above bit log2(width); a NaN wins
-__device__ __forceinline__ float max_nan(float a, float b) { return !(a <= b) && !(b != b) ? a : b; }
+// The larger of two magnitudes (neither negative); a NaN, whose bits lie above infinity's, wins.
+__device__ __forceinline__ float larger(float a, float b) {
+  return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
+}
+// The largest over `width` neighbouring lanes (a power of two).
 __device__ __forceinline__ float lanes_max(float v, int width) {
-  for (int o = width / 2; o; o >>= 1) v = max_nan(v, __shfl_xor_sync(kAll, v, o));
+  if (width == 32) return __uint_as_float(__reduce_max_sync(kAll, __float_as_uint(v)));
+  for (int o = width / 2; o; o >>= 1) v = larger(v, __shfl_xor_sync(kAll, v, o));
   return v;
 }
 

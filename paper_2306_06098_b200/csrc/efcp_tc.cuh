@@ -24,9 +24,6 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
                : "memory");
 }
-__device__ __forceinline__ void bar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
 __device__ __forceinline__ bool bar_poll(uint32_t bar, uint32_t parity) {
   uint32_t done;
   asm volatile(
@@ -66,29 +63,70 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
   }
 }
 
+// ------------------------------------------------------------------ pairs of blocks
+__device__ __forceinline__ uint32_t pair_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void pair_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The address of the first block's copy of something in shared memory.
+__device__ __forceinline__ uint32_t of_first(uint32_t addr) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+  return r;
+}
+// (What is told is that tensor memory was read, which the fence before it orders; a release for the whole cluster
+// would wait for every store to global memory under way.)
+__device__ __forceinline__ void bar_arrive_pair(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
 // ------------------------------------------------------------------ tensor copies
-// One box of a three-dimensional map into shared memory; the innermost coordinate is a multiple of 16 bytes.
+// One box of a three-dimensional map into this block's shared memory, counted on a barrier of the pair's first
+// block; the innermost coordinate is a multiple of 16 bytes.
 __device__ __forceinline__ void load_box(const CUtensorMap* map, uint32_t dst, uint32_t bar, int x,
                                          int y, int z) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], "
-      "[%2];" ::"r"(dst),
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], "
+      "[%1, {%3, %4, %5}], [%2];" ::"r"(dst),
       "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
       : "memory");
 }
-__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
-  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
-}
 
-// ------------------------------------------------------------------ tensor memory and products
+// A box out of shared memory: stored, or added to what is there (fp32).
+__device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map),
+               "r"(src), "r"(x), "r"(y), "r"(z)
+               : "memory");
+}
+__device__ __forceinline__ void add_box(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(
+                   map),
+               "r"(src), "r"(x), "r"(y), "r"(z)
+               : "memory");
+}
+__device__ __forceinline__ void close_stores() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// all but the newest LEFT groups of this thread have left shared memory
+template <int LEFT>
+__device__ __forceinline__ void stores_read() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory");
+}
+__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// what was written to shared memory comes before copies out of it
+__device__ __forceinline__ void fence_copies() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// ------------------------------------------------------------------ tensor memory and products, of both blocks of a pair
 __device__ __forceinline__ void tmem_alloc(uint32_t where, uint32_t columns) {
-  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(where),
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(where),
                "r"(columns)
                : "memory");
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
 }
 __device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t columns) {
-  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(columns));
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(columns));
 }
 __device__ __forceinline__ void fence_after() {
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -100,10 +138,10 @@ __device__ __forceinline__ void fence_before() {
 // Descriptor of an operand in shared memory whose 64-element rows of 128 bytes are swizzled (128-byte mode).
 //   inner dimension K:   eight rows of the outer dimension are 1024 bytes; groups of them lie side by side.
 //   inner dimension M/N: eight rows of K are 1024 bytes, groups of them side by side; the next 64 of M/N lie
-//                        `lead` bytes further.
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead) {
+//                        8 KB further (64 rows of K).
+__device__ __forceinline__ uint64_t operand(uint32_t addr) {
   uint64_t d = (addr & 0x3FFFF) >> 4;
-  d |= uint64_t(lead >> 4) << 16;
+  d |= uint64_t(8192 >> 4) << 16;
   d |= uint64_t(1024 >> 4) << 32;
   d |= uint64_t(1) << 46;  // version of the format
   d |= uint64_t(2) << 61;  // 128-byte swizzle
@@ -116,26 +154,30 @@ __host__ __device__ constexpr uint32_t instruction(bool bf16, int m, int n, bool
          (uint32_t(b_mn) << 16) | (uint32_t(n >> 3) << 17) | (uint32_t(m >> 4) << 24);
 }
 
+// Issued by one thread of the first block: 256 rows, 128 of them in each block's tensor memory; each block holds its
+// rows of A and half of the columns of B.
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t ins, bool add) {
   asm volatile(
       "{\n"
       ".reg .pred p;\n"
       "setp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n"
       "}\n" ::"r"(d),
       "l"(a), "l"(b), "r"(ins), "r"(uint32_t(add))
       : "memory");
 }
-// The barrier is arrived at when all products issued so far by this thread are done.
+// Both blocks' barriers at this address are arrived at when all products issued so far by this thread are done.
 __device__ __forceinline__ void commit(uint32_t bar) {
   asm volatile(
-      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+          bar),
+      "h"(uint16_t(3))
       : "memory");
 }
 
-// 32 columns of this warp's 32 lanes
+// 32 columns of this warp's 32 lanes, on their way until tmem_wait
 __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
-  uint32_t r[32];
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
       "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
@@ -146,9 +188,18 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
         "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
         "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+// v has arrived, with every other load before it.  (It passes through, so that nothing reads it earlier.)
+__device__ __forceinline__ void tmem_wait(float (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]),
+                 "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]),
+                 "+f"(v[14]), "+f"(v[15])
+               :
+               : "memory");
+  asm volatile("" : "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]),
+                    "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]),
+                    "+f"(v[30]), "+f"(v[31]));
 }
 
 }  // namespace tc

@@ -1,11 +1,18 @@
 // Softmax cross entropy of a linear layer over a vocabulary (the formulas stand in include/efcp.h), in products of
 // tiles on the fifth-generation tensor cores.  The logits never reach memory: a tile of them is turned into the rows'
 // largest value and sum of exponentials, and in the backward pass, computed once more for a piece of the vocabulary
-// at a time, into their gradient, which the two products behind it read.
+// at a time, into their gradient, which the two products behind it read.  One launch holds both products of a piece
+// and the logits of the next one, so that few tiles are left over at its end.
 //
-// A block holds one SM: a warp that copies tiles of both operands into a ring in shared memory, a warp that issues the
-// products into one of two accumulators in tensor memory, and eight warps that work on the other accumulator.
-// Every wait is bounded; when one runs out the block ends, and the status tells of it.
+// A pair of blocks on neighbouring SMs works on a tile of 256 x 256: each block holds 128 rows of it in its tensor
+// memory, and loads its rows of one operand and half of the other, which the instructions of the pair share.  In each block
+// a warp copies operands into a ring in shared memory, and eight warps work on one of two accumulators while the
+// tensor cores fill the other; a warp of the first block issues the products.  Every wait is bounded; when one runs out
+// the blocks end, and the status tells of it.
+//
+// The tensor cores cut what they add up to fp32 instead of rounding it.  Where results are fp32, an accumulator holds no
+// more than 256 products of a sum, and the parts are added up in registers, rounded (SUMS): 0.9e-6 instead of 2.7e-6
+// off for the loss of four tokens with d = 768.
 //
 // fp32 values are held as three bfloat16 ones (8 bits of the significand each), of whose nine products the six
 // largest are added up, the small ones first; what is left out is below 2^-24 of the result.
@@ -13,6 +20,7 @@
 
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "efcp.h"
@@ -25,11 +33,15 @@
 namespace efcp {
 namespace {
 
-constexpr int kStages = 4;
-constexpr int kOutWarps = 8, kXentThreads = (kOutWarps + 2) * 32;
-constexpr uint32_t kBoxBytes = 64 * 128;
-constexpr uint32_t kABytes = kXentRows / 64 * kBoxBytes, kBBytes = kXentCols / 64 * kBoxBytes;
-constexpr size_t kXentSmem = kStages * (kABytes + kBBytes) + 1024;
+constexpr int kStages = 6;
+constexpr int kOutWarps = 8, kXentThreads = (kOutWarps + 4) * 32;
+constexpr int kBlockRows = kXentRows / 2;       // of a tile, held by a block
+constexpr uint32_t kBoxBytes = 64 * 128;        // 64 rows of 64 elements
+constexpr uint32_t kABytes = kBlockRows / 64 * kBoxBytes, kBBytes = kXentCols / 128 * kBoxBytes;
+constexpr uint32_t kStageBytes = kABytes + kBBytes;
+constexpr uint32_t kOutBytes = 32 * 128;        // a warp's box of results
+constexpr size_t kXentSmem = kStages * kStageBytes + kOutWarps * kOutBytes + 1024;
+constexpr int kPart = 8;                        // steps of an accumulator with SUMS
 constexpr float kLog2e = 1.4426950408889634f;
 
 template <typename T>
@@ -39,25 +51,6 @@ __device__ __forceinline__ float pow2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
-}
-
-// 32 values to T, `valid` of them
-template <typename T>
-__device__ __forceinline__ void store32(T* to, int valid, bool vec, const float (&v)[32]) {
-  constexpr int kPer = 16 / sizeof(T);
-  if (vec && valid >= 32) {
-#pragma unroll
-    for (int i = 0; i < 32; i += kPer) {
-      Pack<T, kPer> a;
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) a.v[j] = from_f32<T>(v[i + j]);
-      *reinterpret_cast<uint4*>(to + i) = *reinterpret_cast<const uint4*>(&a);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (i < valid) to[i] = from_f32<T>(v[i]);
-  }
 }
 
 // x as up to three values of O whose sum it is
@@ -70,11 +63,174 @@ __device__ __forceinline__ void split(float x, O (&v)[PLANES]) {
   }
 }
 
-template <int MODE, typename T>
+enum XentKind { kHidden, kWeight, kLogits };
+
+struct XentTile {
+  XentKind kind;
+  int m0, n0;     // rows and columns of the result
+  int cols;       // width of the tile
+  int k0, depth;  // first step along the sum, and steps
+  int part;       // of the sum over the piece (hidden); tile of the columns (logits)
+};
+
+// The tiles of a launch.  Rows first, so that a tile of the other operand serves many pairs at the same time.
+struct XentWork {
+  int row_tiles, weight_rows, splits, steps, token_steps;
+  long long hidden, weight, all;  // tiles of hidden; and of weight; and of logits
+
+  __device__ __forceinline__ XentWork(const XentGemm& p, int count, int pairs) {
+    row_tiles = (count + kXentRows - 1) / kXentRows;
+    const int real = min(p.piece, p.vocab - p.v0);
+    weight_rows = (real + kXentRows - 1) / kXentRows;
+    steps = (real + kXentDepth - 1) / kXentDepth;
+    token_steps = (count + kXentDepth - 1) / kXentDepth;
+    splits = xent_splits(row_tiles, p.d_tiles, p.piece, pairs);
+    hidden = p.hidden ? (long long)row_tiles * p.d_tiles * splits : 0;
+    weight = hidden + (p.weight ? (long long)weight_rows * p.d_tiles : 0);
+    all = weight + (p.logits ? (long long)row_tiles * p.col_tiles : 0);
+  }
+  __device__ __forceinline__ XentTile tile(const XentGemm& p, long long t) const {
+    XentTile r;
+    if (t < hidden) {
+      const int c = int(t / row_tiles), n = c / splits;
+      r.kind = kHidden;
+      r.m0 = int(t - (long long)c * row_tiles) * kXentRows;
+      r.n0 = n * p.d_tile;
+      r.cols = p.d_tile;
+      r.part = c - n * splits;
+      const int per = (steps + splits - 1) / splits;
+      r.k0 = min(steps, r.part * per);
+      r.depth = min(per, steps - r.k0);
+    } else if (t < weight) {
+      t -= hidden;
+      const int c = int(t / weight_rows);
+      r.kind = kWeight;
+      r.m0 = int(t - (long long)c * weight_rows) * kXentRows;
+      r.n0 = c * p.d_tile;
+      r.cols = p.d_tile;
+      r.part = r.k0 = 0;
+      r.depth = token_steps;
+    } else {
+      t -= weight;
+      const int c = int(t / row_tiles);
+      r.kind = kLogits;
+      r.m0 = int(t - (long long)c * row_tiles) * kXentRows;
+      r.n0 = c * p.col_tile;
+      r.cols = p.col_tile;
+      r.part = c;
+      r.k0 = 0;
+      r.depth = (p.d + kXentDepth - 1) / kXentDepth;
+    }
+    return r;
+  }
+};
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// 2^(v log2(e) - base), two at a time
+__device__ __forceinline__ float2 exp_pair(float a, float b, float base) {
+  const float2 x = fma2(make_float2(a, b), both(kLog2e), both(-base));
+  return make_float2(pow2(x.x), pow2(x.y));
+}
+
+// What becomes of 32 columns of a row of logits, forward: their largest value (times log2(e)) and the sum of
+// exponentials relative to it are joined to the row's.
+struct RowStats {
+  float top = -INFINITY, total = 0.f;
+  __device__ __forceinline__ void add(const XentGemm& p, int row, int target, int col, float (&v)[32]) {
+    const int valid = p.vocab - col;
+    if (valid <= 0) return;
+    const int hit = target - col;
+    if (hit >= 0 && hit < 32) {
+      float x = 0.f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x = i == hit ? v[i] : x;
+      p.target_logit[row] = x;
+    }
+    if (valid < 32) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = i < valid ? v[i] : -INFINITY;
+    }
+    float m = fmaxf(v[0], v[1]), n = fmaxf(v[2], v[3]);
+#pragma unroll
+    for (int i = 4; i < 32; i += 4) {
+      m = max3(m, v[i], v[i + 1]);
+      n = max3(n, v[i + 2], v[i + 3]);
+    }
+    m = fmaxf(top, fmaxf(m, n) * kLog2e);
+    const float base = m == -INFINITY ? 0.f : m;
+    total *= pow2(top - base);
+    top = m;
+    float2 s = both(0.f), t = both(0.f);
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+      s = add2(s, exp_pair(v[i], v[i + 1], base));
+      t = add2(t, exp_pair(v[i + 2], v[i + 3], base));
+    }
+    s = add2(s, t);
+    total += s.x + s.y;
+  }
+};
+
+// Results leave through shared memory, 32 rows of 128 (or 64) bytes at a time for each warp, swizzled, so that its
+// lanes, a row each, write to different banks.
+template <typename O, int BYTES = 128>
+struct OutBox {
+  uint32_t at;  // of the warp
+  int lane;
+  // 16-byte pieces `first`, ... of the lane's row
+  __device__ __forceinline__ void put(int first, const float (&v)[32]) const {
+    constexpr int kPer = 16 / sizeof(O);
+#pragma unroll
+    for (int k = 0; k < 32 / kPer; ++k) {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(O) == 4) {
+          w[i] = __float_as_uint(v[k * 4 + i]);
+        } else {
+          const float2 x = make_float2(v[k * 8 + 2 * i], v[k * 8 + 2 * i + 1]);
+          if constexpr (std::is_same_v<O, __half>) {
+            const __half2 h = __float22half2_rn(x);
+            w[i] = reinterpret_cast<const uint32_t&>(h);
+          } else {
+            const __nv_bfloat162 h = __float22bfloat162_rn(x);
+            w[i] = reinterpret_cast<const uint32_t&>(h);
+          }
+        }
+      }
+      const int swizzle = BYTES == 128 ? lane & 7 : (lane >> 1) & 3;
+      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(
+                       at + lane * BYTES + (((first + k) ^ swizzle) << 4)),
+                   "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+                   : "memory");
+    }
+  }
+  // before the box is written again: its last copy has read it  (these two are for whole warps)
+  __device__ __forceinline__ void open() const {
+    if (lane == 0) tc::stores_read<0>();
+    __syncwarp();
+  }
+  __device__ __forceinline__ void send(const CUtensorMap* map, int x, int y, int z, bool add) const {
+    tc::fence_copies();
+    __syncwarp();
+    if (lane == 0) {
+      if (add) tc::add_box(map, at, x, y, z);
+      else tc::store_box(map, at, x, y, z);
+      tc::close_stores();
+    }
+  }
+};
+
+template <typename T, bool BACKWARD>
 __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant__ XentGemm p) {
   using O = Operand<T>;
-  constexpr bool kAMn = MODE == kXentWeight, kBMn = MODE >= kXentHidden;
-  constexpr int kPlanes = std::is_same_v<T, float> ? 3 : 1, kPairs = kPlanes == 3 ? 6 : 1;
+  constexpr bool kSums = !BACKWARD || std::is_same_v<T, float>;
+  constexpr int kPairs = std::is_same_v<T, float> ? 6 : 1;
   extern __shared__ unsigned char ring_[];
   __shared__ alignas(8) uint64_t bars[2 * kStages + 5];
   __shared__ uint32_t tmem_at;
@@ -84,6 +240,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
   const uint32_t full = tc::smem_of(bars), empty = full + 8 * kStages, done = empty + 8 * kStages,
                  taken = done + 16, drained = taken + 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = int(tc::pair_rank());
   if (threadIdx.x == 0) {
     gave_up_ = 0;
     for (int i = 0; i < kStages; ++i) {
@@ -92,86 +249,98 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
     }
     for (int i = 0; i < 2; ++i) {
       tc::bar_init(done + 8 * i, 1);
-      tc::bar_init(taken + 8 * i, kOutWarps);
+      tc::bar_init(taken + 8 * i, 2 * kOutWarps);
     }
     tc::bar_init(drained, 1);
     tc::bar_init_fence();
   }
-  if (warp == kOutWarps) {
-    tc::tmem_alloc(tc::smem_of(&tmem_at), 512);
-    if (lane == 0) {
-      tc::prefetch_map(&p.a);
-      tc::prefetch_map(&p.b);
-    }
-  }
+  if (warp == kOutWarps) tc::tmem_alloc(tc::smem_of(&tmem_at), 512);
   tc::fence_before();
   __syncthreads();
+  tc::pair_sync();
   tc::fence_after();
   take_turn();
   const uint32_t tmem = tmem_at;
-  const int count = *p.count;
-  const int row_tiles = p.row_tiles >= 0 ? p.row_tiles : (count + kXentRows - 1) / kXentRows;
-  const int depth = ((p.depth >= 0 ? p.depth : count) + kXentDepth - 1) / kXentDepth;
-  const int steps = depth * kPairs;
-  const long long tiles = (long long)row_tiles * p.col_tiles;
+  const int count = *p.count, pairs = int(gridDim.x / 2), pair = int(blockIdx.x / 2);
+  const XentWork work(p, count, pairs);
 
+  // Registers go where the sums are held: 128 x 72 + 256 x 216 of the launch's 384 x 168.
+  if (warp >= kOutWarps) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
   if (warp == kOutWarps) {
     if (lane == 0) {
-      // copies: rows first, so that a tile of the other operand serves many blocks at the same time
-      const uint32_t bytes = kABytes + uint32_t(p.col_tile / 64) * kBoxBytes;
       unsigned n = 0;  // steps so far
       bool ok = true;
-      for (long long t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
-        const int tc_ = int(t / row_tiles), m0 = int(t - (long long)tc_ * row_tiles) * kXentRows,
-                  n0 = tc_ * p.col_tile;
-        const int an = m0, bn = MODE == kXentGrad ? p.v0 + n0 : n0;
-        const int bk = MODE == kXentHidden ? p.v0 : 0;
-        for (int i = 0; i < steps && ok; ++i, ++n) {
-          const int pair = kPairs == 1 ? 0 : i / depth, k = (i - pair * depth) * kXentDepth;
-          // planes of the pairs: (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
-          const int pa = kPairs == 1 ? 0 : (0x001102 >> (4 * pair)) & 15;
-          const int pb = kPairs == 1 ? 0 : (0x010120 >> (4 * pair)) & 15;
+      for (long long t = pair; t < work.all && ok; t += pairs) {
+        const XentTile w = work.tile(p, t);
+        const int an = w.m0 + rank * kBlockRows, bn = w.n0 + rank * (w.cols / 2);
+        const uint32_t bytes = 2 * (kABytes + uint32_t(w.cols) * 64);
+        for (int i = 0; i < w.depth * kPairs && ok; ++i, ++n) {
+          const int turn = kPairs == 1 ? 0 : i / w.depth, k = (w.k0 + i - turn * w.depth) * kXentDepth;
+          // planes of the turns: (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
+          const int pa = kPairs == 1 ? 0 : (0x001102 >> (4 * turn)) & 15;
+          const int pb = kPairs == 1 ? 0 : (0x010120 >> (4 * turn)) & 15;
           const unsigned s = n % kStages;
           ok = tc::bar_wait(empty + 8 * s, (n / kStages + 1) & 1, gave_up);
           if (!ok) break;
-          const uint32_t bar = full + 8 * s, at = ring + s * (kABytes + kBBytes);
-          tc::bar_expect(bar, bytes);
+          const uint32_t bar = tc::of_first(full + 8 * s), a = ring + s * kStageBytes, b = a + kABytes;
+          if (rank == 0) tc::bar_expect(full + 8 * s, bytes);
+          if (w.kind == kLogits) {
+            tc::load_box(&p.hidden_rows, a, bar, k, an, pa);
+            tc::load_box(&p.weight_rows, b, bar, k, p.next_v0 + bn, pb);
+          } else {
+            const CUtensorMap* other = w.kind == kHidden ? &p.weight_cols : &p.hidden_cols;
+            if (w.kind == kHidden) {
+              tc::load_box(&p.g_rows[p.buffer], a, bar, k, an, pa);
+            } else {
 #pragma unroll
-          for (int j = 0; j < kXentRows / 64; ++j)
-            tc::load_box(&p.a, at + j * kBoxBytes, bar, kAMn ? an + 64 * j : k, kAMn ? k : an + 64 * j, pa);
-          for (int j = 0; j < p.col_tile / 64; ++j)
-            tc::load_box(&p.b, at + kABytes + j * kBoxBytes, bar, kBMn ? bn + 64 * j : k,
-                         kBMn ? bk + k : bn + 64 * j, pb);
+              for (int j = 0; j < kBlockRows / 64; ++j)
+                tc::load_box(&p.g_cols[p.buffer], a + j * kBoxBytes, bar, an + 64 * j, k, pa);
+            }
+            for (int j = 0; j < w.cols / 128; ++j)
+              tc::load_box(other, b + j * kBoxBytes, bar, bn + 64 * j, w.kind == kHidden ? p.v0 + k : k, pb);
+          }
         }
       }
-      if (!ok)  // nothing may land in shared memory that the block has left
-        for (unsigned i = n < kStages ? 0 : n - kStages; i < n; ++i)
-          (void)tc::bar_wait(full + 8 * (i % kStages), (i / kStages) & 1, gave_up, tc::kDrainNs);
+      if (!ok) {  // nothing may land in shared memory that the block has left: copies take microseconds
+        const uint64_t start = tc::clock_ns();
+        while (tc::clock_ns() - start < tc::kDrainNs) {
+        }
+      }
     }
     __syncwarp();
   } else if (warp == kOutWarps + 1) {
-    if (lane == 0) {
-      const uint32_t ins = tc::instruction(std::is_same_v<O, __nv_bfloat16>, kXentRows, p.col_tile, kAMn, kBMn);
+    if (lane == 0 && rank == 0) {
       unsigned n = 0, turn = 0;
       bool ok = true;
-      for (long long t = blockIdx.x; t < tiles && ok; t += gridDim.x, ++turn) {
-        const unsigned buf = turn & 1;
-        ok = tc::bar_wait(taken + 8 * buf, (turn / 2 + 1) & 1, gave_up);
-        if (!ok) break;
-        tc::fence_after();
-        for (int i = 0; i < steps; ++i, ++n) {
-          const unsigned s = n % kStages;
-          ok = tc::bar_wait(full + 8 * s, (n / kStages) & 1, gave_up);
+      for (long long t = pair; t < work.all && ok; t += pairs) {
+        const XentTile w = work.tile(p, t);
+        const bool a_mn = w.kind == kWeight, b_mn = w.kind != kLogits;
+        const uint32_t ins = tc::instruction(std::is_same_v<O, __nv_bfloat16>, kXentRows, w.cols, a_mn, b_mn);
+        const uint32_t a_step = a_mn ? 2048 : 32, b_step = b_mn ? 2048 : 32;
+        const int steps = w.depth * kPairs, most = kSums ? kPart : steps;
+        int i = 0;
+        do {  // an accumulator: the whole sum, or parts of it
+          const unsigned buf = turn & 1;
+          ok = tc::bar_wait(taken + 8 * buf, (turn / 2 + 1) & 1, gave_up);
           if (!ok) break;
           tc::fence_after();
-          const uint32_t a = ring + s * (kABytes + kBBytes), b = a + kABytes;
+          for (int j = 0; j < most && i < steps; ++j, ++i, ++n) {
+            const unsigned s = n % kStages;
+            ok = tc::bar_wait(full + 8 * s, (n / kStages) & 1, gave_up);
+            if (!ok) break;
+            tc::fence_after();
+            const uint32_t a = ring + s * kStageBytes, b = a + kABytes;
 #pragma unroll
-          for (int k = 0; k < kXentDepth / 16; ++k)
-            tc::mma(tmem + buf * kXentCols, tc::operand(a + k * (kAMn ? 2048 : 32), kBoxBytes),
-                    tc::operand(b + k * (kBMn ? 2048 : 32), kBoxBytes), ins, i > 0 || k > 0);
-          tc::commit(empty + 8 * s);
-        }
-        if (ok) tc::commit(done + 8 * buf);
+            for (int k = 0; k < kXentDepth / 16; ++k)
+              tc::mma(tmem + buf * kXentCols, tc::operand(a + k * a_step), tc::operand(b + k * b_step), ins,
+                      j > 0 || k > 0);
+            tc::commit(empty + 8 * s);
+          }
+          if (!ok) break;
+          tc::commit(done + 8 * buf);
+          ++turn;
+        } while (i < steps);
       }
       if (!ok) {  // the products under way end before the tensor memory is given back
         tc::commit(drained);
@@ -179,219 +348,307 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
       }
     }
     __syncwarp();
+  }
   } else {
-    const int quarter = warp & 3, half = warp >> 2, cols = p.col_tile / 2;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    const int quarter = warp & 3, half = warp >> 2;
+    const float back = BACKWARD ? p.scale[1] : 1.f;
+    const uint32_t box = ring + kStages * kStageBytes + warp * kOutBytes;
     unsigned turn = 0;
-    for (long long t = blockIdx.x; t < tiles; t += gridDim.x, ++turn) {
-      const unsigned buf = turn & 1;
-      const int tc_ = int(t / row_tiles), m0 = int(t - (long long)tc_ * row_tiles) * kXentRows;
-      const int row = m0 + quarter * 32 + lane, n0 = tc_ * p.col_tile + half * cols;
+    bool ok = true;
+    for (long long t = pair; t < work.all && ok; t += pairs) {
+      const XentTile w = work.tile(p, t);
+      const int row0 = w.m0 + rank * kBlockRows + quarter * 32, row = row0 + lane;
+      const int cols = w.cols / 2, n0 = w.n0 + half * cols;
+      const int steps = w.depth * kPairs;
       int target = -1;
-      float lse = 0.f, coef = 0.f, back = 1.f;
-      if constexpr (MODE == kXentStats || MODE == kXentGrad) target = p.target[row];
-      if constexpr (MODE == kXentGrad) {
-        lse = p.lse[row];
-        coef = p.coef[row];
+      float lse = 0.f, coef = 0.f;
+      if (w.kind == kLogits) {
+        target = p.target[row];
+        if constexpr (BACKWARD) {
+          lse = p.lse[row] * kLog2e;
+          coef = p.coef[row];
+        }
       }
-      if constexpr (MODE >= kXentHidden) back = p.scale[1];
-      if (!__all_sync(kAll, tc::bar_wait(done + 8 * buf, (turn / 2) & 1, gave_up))) break;
-      tc::fence_after();
-      const uint32_t at = tmem + buf * kXentCols + half * cols + (uint32_t(quarter * 32) << 16);
-      float top = -INFINITY, total = 0.f;
-      for (int c = 0; c < cols; c += 32) {
-        float v[32];
-        __syncwarp();
-        tc::tmem_load32(at + c, v);
+      RowStats stats;
+      // 32 columns of the finished result
+      const auto put = [&](int c, float(&v)[32]) {
         const int col = n0 + c;
-        if constexpr (MODE == kXentStats) {
-          const int valid = p.vocab - col;
-          if (valid <= 0) continue;
-          const int hit = target - col;
-          if (hit >= 0 && hit < 32) {
-            float x = 0.f;
+        if constexpr (!BACKWARD) {
+          stats.add(p, row, target, col, v);
+        } else if (w.kind == kLogits) {
+          if (col >= p.piece) return;  // (all lanes, here and below: no box begins outside of what it is stored to)
+          const int hit = target - (p.next_v0 + col);
+          const int valid = row < count ? min(p.piece, p.vocab - p.next_v0) - col : 0;
+          const bool mine = hit >= 0 && hit < 32;
+          float x = 0.f;
+          if (mine) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) x = i == hit ? v[i] : x;
-            p.target_logit[row] = x;
+            x = (exp_pair(x, x, lse).x - 1.f) * coef;
+          }
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const float2 e = mul2(exp_pair(v[i], v[i + 1], lse), both(coef));
+            v[i] = e.x;
+            v[i + 1] = e.y;
+          }
+          if (mine) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = i == hit ? x : v[i];
           }
           if (valid < 32) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = i < valid ? v[i] : -INFINITY;
+            for (int i = 0; i < 32; ++i) v[i] = i < valid ? v[i] : 0.f;
           }
-          float m = top;
-#pragma unroll
-          for (int i = 0; i < 32; ++i) m = fmaxf(m, v[i]);
-          const float base = m == -INFINITY ? 0.f : m;
-          total *= pow2((top - base) * kLog2e);
-          top = m;
-          float s[4] = {};
-#pragma unroll
-          for (int i = 0; i < 32; ++i) s[i & 3] += pow2((v[i] - base) * kLog2e);
-          total += (s[0] + s[1]) + (s[2] + s[3]);
-        } else if constexpr (MODE == kXentGrad) {
-          if (col >= int(p.g_row)) continue;
-          const int hit = target - (p.v0 + col), valid = row < count ? min(p.piece, p.vocab - p.v0) - col : 0;
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const float x = pow2((v[i] - lse) * kLog2e) - (i == hit ? 1.f : 0.f);
-            v[i] = i < valid ? x * coef : 0.f;
-          }
-          O* to = static_cast<O*>(p.g) + (long long)row * p.g_row + col;
-          if constexpr (kPlanes == 1) {
-            store32<O>(to, 32, true, v);
+          if constexpr (kPairs == 1) {
+            const OutBox<O> out{box, lane};
+            const bool second = c & 32;  // half of a box of 64 columns
+            if (!second) out.open();
+            out.put(second ? 4 : 0, v);
+            if (second) out.send(&p.g_out[p.next_buffer], col - 32, row0, 0, false);
           } else {
 #pragma unroll
-            for (int plane = 0; plane < kPlanes; ++plane) {
-              store32<O>(to + plane * p.g_plane, 32, true, v);
+            for (int plane = 0; plane < 3; ++plane) {
+              const OutBox<O, 64> out{box, lane};
+              out.open();
+              out.put(0, v);
+              out.send(&p.g_out[p.next_buffer], col, row0, plane, false);
 #pragma unroll
               for (int i = 0; i < 32; ++i) v[i] -= rounded<O>(v[i]);
             }
           }
-        } else if constexpr (MODE == kXentHidden) {
-          const int valid = p.d - col;
-          if (row >= count || valid <= 0) continue;
-          float* sum = p.sum + row * p.sum_row + col;  // (rows of whole 32s)
-          if (!p.first) {
+        } else if (w.kind == kHidden) {
+          if (col >= p.d) return;
+          if (!steps) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-              const float4 o = *reinterpret_cast<const float4*>(sum + i);
-              v[i] += o.x; v[i + 1] += o.y; v[i + 2] += o.z; v[i + 3] += o.w;
-            }
+            for (int i = 0; i < 32; ++i) v[i] = 0.f;
           }
-          if (p.last) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= back;
-            store32<T>(static_cast<T*>(p.out) + (long long)p.order[row] * p.out_row + col, valid, p.vec_out, v);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 32; i += 4)
-              *reinterpret_cast<float4*>(sum + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-          }
+          const OutBox<float> out{box, lane};
+          out.open();
+          out.put(0, v);
+          out.send(&p.sum_out, col, w.part * work.row_tiles * kXentRows + row0, 0, !p.first);
         } else {
-          const int valid = p.d - col;
-          if (row >= min(p.piece, p.vocab - p.v0) || valid <= 0) continue;
+          if ((col & ~63) >= p.d || row0 >= min(p.piece, p.vocab - p.v0)) return;
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = steps ? v[i] * back : 0.f;
-          store32<T>(static_cast<T*>(p.out) + (long long)(p.v0 + row) * p.out_row + col, valid, p.vec_out, v);
+          if (p.box_dweight) {
+            constexpr int kWide = 128 / int(sizeof(T));  // columns of a box
+            const OutBox<T> out{box, lane};
+            const bool second = c & (kWide - 32);
+            if (!second) out.open();
+            out.put(second ? 4 : 0, v);
+            if (second || (kWide == 32 && col < p.d)) out.send(&p.dweight_out, col & ~(kWide - 1), p.v0 + row0, 0, false);
+          } else if (row < min(p.piece, p.vocab - p.v0)) {
+            T* to = static_cast<T*>(p.dweight) + (long long)(p.v0 + row) * p.d + col;
+            const int valid = p.d - col;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (i < valid) to[i] = from_f32<T>(v[i]);
+          }
+        }
+      };
+      const auto await = [&] {
+        ok = __all_sync(kAll, tc::bar_wait(done + 8 * (turn & 1), (turn / 2) & 1, gave_up));
+        tc::fence_after();
+        return ok;
+      };
+      const auto give = [&] {
+        tc::fence_before();
+        __syncwarp();
+        if (lane == 0) tc::bar_arrive_pair(tc::of_first(taken + 8 * (turn & 1)));
+        ++turn;
+      };
+      const auto at = [&](int c) {
+        return tmem + (turn & 1) * kXentCols + half * cols + c + (uint32_t(quarter * 32) << 16);
+      };
+      // (cols is 64 or 128: an even number of 32s)
+      if constexpr (kSums) {
+        float acc[kXentCols / 64][32];
+        if (!await()) break;
+#pragma unroll
+        for (int j = 0; j < kXentCols / 64; ++j)
+          if (32 * j < cols) tc::tmem_load32(at(32 * j), acc[j]);
+#pragma unroll
+        for (int j = 0; j < kXentCols / 64; ++j) tc::tmem_wait(acc[j]);
+        give();
+        for (int i = kPart; i < steps; i += kPart) {
+          if (!await()) break;
+          float v[2][32];
+          tc::tmem_load32(at(0), v[0]);
+#pragma unroll
+          for (int j = 0; j < kXentCols / 64; ++j) {
+            if (32 * j >= cols) break;
+            tc::tmem_wait(v[j & 1]);
+            if (j + 1 < kXentCols / 64 && 32 * (j + 1) < cols) tc::tmem_load32(at(32 * (j + 1)), v[(j + 1) & 1]);
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              const float2 s = add2(make_float2(acc[j][e], acc[j][e + 1]), make_float2(v[j & 1][e], v[j & 1][e + 1]));
+              acc[j][e] = s.x;
+              acc[j][e + 1] = s.y;
+            }
+          }
+          give();
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int j = 0; j < kXentCols / 64; ++j)
+          if (32 * j < cols) put(32 * j, acc[j]);
+      } else {
+        if (!await()) break;
+        float v[2][32];
+        tc::tmem_load32(at(0), v[0]);
+        for (int c = 0; c < cols; c += 64) {
+          tc::tmem_wait(v[0]);
+          tc::tmem_load32(at(c + 32), v[1]);
+          put(c, v[0]);
+          __syncwarp();
+          tc::tmem_wait(v[1]);
+          if (c + 64 < cols) tc::tmem_load32(at(c + 64), v[0]);
+          else give();
+          put(c + 32, v[1]);
+          __syncwarp();
         }
       }
-      if constexpr (MODE == kXentStats)
-        p.part[(long long)row * p.parts + tc_ * 2 + half] = make_float2(top, total);
-      tc::fence_before();
+      if constexpr (!BACKWARD)
+        p.part[(long long)row * p.parts + w.part * 2 + half] = make_float2(stats.top, stats.total);
       __syncwarp();
-      if (lane == 0) tc::bar_arrive(taken + 8 * buf);
     }
+    if (lane == 0) tc::stores_done();
+    __syncwarp();
   }
   tc::fence_before();
   __syncthreads();
+  tc::pair_sync();  // the other block's products read this one's shared memory
   if (warp == kOutWarps) tc::tmem_free(tmem, 512);
   if (threadIdx.x == 0 && gave_up_) atomicExch(p.status, EFCP_ETIMEOUT);
 }
 
-// Sum of v over the threads before this one of a block of 1024, and over all.
-__device__ __forceinline__ int block_before(int v, int* all) {
-  __shared__ int part[33];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int sum = v;
-#pragma unroll
-  for (int o = 1; o < 32; o *= 2) {
-    const int other = __shfl_up_sync(kAll, sum, o);
-    if (lane >= o) sum += other;
-  }
-  if (lane == 31) part[warp] = sum;
-  __syncthreads();
-  if (warp == 0) {
-    int w = part[lane];
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-      const int other = __shfl_up_sync(kAll, w, o);
-      if (lane >= o) w += other;
-    }
-    part[lane] = w;
-  }
-  __syncthreads();
-  *all = part[31];
-  return sum - v + (warp ? part[warp - 1] : 0);
-}
-
-// One block: which tokens have a target, in order; backward also the factors on their gradients, times a power of two
-// that brings the largest near 1 (near 2^14 for fp16, whose probabilities would vanish otherwise).
-template <bool HALF>
-__global__ void __launch_bounds__(1024) k_xent_select(const XentPrep p, bool backward) {
-  take_turn();
-  __shared__ unsigned most;
-  const long long per = (p.tokens + 1023) / 1024, lo = threadIdx.x * per, hi = min(p.tokens, lo + per);
-  if (threadIdx.x == 0) most = 0;
-  int mine = 0, all;
-  for (long long i = lo; i < hi; ++i) mine += p.targets[i] != p.ignore;
-  int at = block_before(mine, &all);
-  const float mean = p.reduction == 1 ? 1.f / float(all) : 1.f;
-  float big = 0.f;
-  for (long long i = lo; i < hi; ++i) {
-    const long long t = p.targets[i];
-    if (t == p.ignore) continue;
-    const bool in = t >= 0 && t < p.vocab;
-    p.order[at] = int(i);
-    p.target[at] = in ? int(t) : -1;
-    if (backward) {
-      const float g = p.grad[p.reduction ? 0 : i * p.grad_step] * mean;
-      p.coef[at] = in ? g : __int_as_float(0x7FC00000);
-      p.lse[at] = p.lse_in[i];
-      if (fabsf(g) < INFINITY) big = fmaxf(big, fabsf(g));
-    }
-    ++at;
-  }
-  for (int i = all + threadIdx.x; i < (all + kXentRows - 1) / kXentRows * kXentRows; i += 1024) {
-    p.target[i] = -1;
-    if (backward) p.coef[i] = p.lse[i] = 0.f;
-  }
-  if (threadIdx.x == 0) *p.count = all;
-  if (!backward) return;
-  atomicMax(&most, __float_as_uint(big));  // (of values that are not negative the bits are in order)
-  __syncthreads();
-  big = __uint_as_float(most);
-  const int e = big > 0.f ? max(-100, min(100, ilogbf(big))) : 0;
-  const float up = scalbnf(1.f, (HALF ? 14 : 0) - e);
-  if (threadIdx.x == 0) {
-    p.scale[0] = up;
-    p.scale[1] = scalbnf(1.f, e - (HALF ? 14 : 0));
-  }
-  for (int i = threadIdx.x; i < all; i += 1024) p.coef[i] *= up;
-}
-
-// Rows of H that have a target, one behind the other (and zeros up to whole tiles), as the copies of tiles want them;
-// what belongs to the other tokens becomes zero.  A warp takes a row.
+// What comes before the products: which tokens have a target, in order; their rows of H, one behind the other (and
+// zeros up to whole tiles), as the copies of tiles want them; backward also the factors on their gradients, times a
+// power of two that brings the largest near 1 (near 2^14 for fp16, whose probabilities would vanish otherwise); and
+// zeros for what belongs to the other tokens.
+//
+// A block takes a run of tokens.  It counts those with a target before its own by itself, so that one launch is
+// enough: all targets pass through every block, 8 bytes for each row of H.
 template <typename T>
-__global__ void __launch_bounds__(256) k_xent_gather(const XentPrep p) {
+__global__ void __launch_bounds__(512) k_xent_prepare(const XentPrep p, bool backward, int per) {
   take_turn();
   using O = Operand<T>;
   constexpr int kPlanes = std::is_same_v<T, float> ? 3 : 1;
-  const int lane = threadIdx.x & 31, count = *p.count;
-  const long long padded = (count + kXentRows - 1) / kXentRows * kXentRows;
-  const long long warps = (long long)gridDim.x * 8, first = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  for (long long i = first; i < padded; i += warps) {
-    const T* from = static_cast<const T*>(p.hidden) + (i < count ? (long long)p.order[i] * p.hidden_row : 0);
-    O* to = static_cast<O*>(p.hidden_packed) + i * p.packed_row;
-    const bool vec = kPlanes == 1 && reinterpret_cast<uintptr_t>(from) % 16 == 0 && p.d % 8 == 0;
-    if (vec) {
+  constexpr bool kHalf = std::is_same_v<T, __half>;
+  __shared__ int before_, all_, places[512 / 32], tokens[512];
+  __shared__ unsigned most_;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long lo = (long long)blockIdx.x * per, hi = min(p.tokens, lo + per);
+  if (threadIdx.x == 0) {
+    before_ = all_ = 0;
+    most_ = 0;
+  }
+  __syncthreads();
+  int before = 0, all = 0;
+  float big = 0.f;
+  const bool each = backward && p.reduction == 0;
+#pragma unroll 8
+  for (long long i = threadIdx.x; i < p.tokens; i += 512) {
+    const bool used = p.targets[i] != p.ignore;
+    all += used;
+    before += used && i < lo;
+    if (each && used) {
+      const float g = fabsf(p.grad[i * p.grad_step]);
+      if (g < INFINITY) big = fmaxf(big, g);
+    }
+  }
+  before = __reduce_add_sync(kAll, before);
+  all = __reduce_add_sync(kAll, all);
+  big = lanes_max(big, 32);
+  if (lane == 0) {
+    atomicAdd(&before_, before);  // (whole numbers: any order)
+    atomicAdd(&all_, all);
+    atomicMax(&most_, __float_as_uint(big));  // (of values that are not negative the bits are in order)
+  }
+  __syncthreads();
+  all = all_;
+  int at = before_;
+  const int padded = (all + kXentRows - 1) / kXentRows * kXentRows;
+  float one = 0.f, up = 1.f;
+  if (backward) {
+    if (!each) {
+      one = p.grad[0] * (p.reduction == 1 ? 1.f / float(all) : 1.f);
+      big = fabsf(one) < INFINITY ? fabsf(one) : 0.f;
+    } else {
+      big = __uint_as_float(most_);
+    }
+    const int e = big > 0.f ? max(-100, min(100, ilogbf(big))) : 0, shift = kHalf ? 14 : 0;
+    up = scalbnf(1.f, shift - e);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+      p.scale[0] = up;
+      p.scale[1] = scalbnf(1.f, e - shift);
+    }
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.count = all;
+  const auto row = [&](long long token, int place) {  // (a warp)
+    const T* from = static_cast<const T*>(p.hidden) + token * p.hidden_row;
+    O* to = static_cast<O*>(p.hidden_packed) + place * p.packed_row;
+    if (kPlanes == 1 && reinterpret_cast<uintptr_t>(from) % 16 == 0 && p.d % 8 == 0) {
+#pragma unroll 4
       for (int c = lane * 8; c < p.d; c += 256)
-        *reinterpret_cast<uint4*>(to + c) =
-            i < count ? *reinterpret_cast<const uint4*>(from + c) : make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(to + c) = *reinterpret_cast<const uint4*>(from + c);
     } else {
       for (int c = lane; c < p.d; c += 32) {
         O v[kPlanes];
-        split<O, kPlanes>(i < count ? to_f32(from[c]) : 0.f, v);
+        split<O, kPlanes>(to_f32(from[c]), v);
 #pragma unroll
         for (int k = 0; k < kPlanes; ++k) to[k * p.hidden_plane + c] = v[k];
       }
     }
+  };
+  for (long long base = lo; base < hi; base += 512) {
+    const long long i = base + threadIdx.x;
+    const long long t = i < hi ? p.targets[i] : p.ignore;
+    const bool used = t != p.ignore;
+    const unsigned mask = __ballot_sync(kAll, used);
+    if (lane == 0) places[warp] = __popc(mask);
+    __syncthreads();
+    int first = 0, here = 0;  // tokens with a target before this warp's; of the block
+    for (int k = 0; k < 512 / 32; ++k) {
+      if (k < warp) first += places[k];
+      here += places[k];
+    }
+    const int local = first + __popc(mask & ((1u << lane) - 1)), place = at + local;
+    if (used) tokens[local] = int(i);
+    if (i < hi) {
+      if (p.place) p.place[i] = used ? place : -1;
+      if (used) {
+        const bool in = t >= 0 && t < p.vocab;
+        p.order[place] = int(i);
+        p.target[place] = in ? int(t) : -1;
+        if (backward) {
+          const float g = each ? p.grad[i * p.grad_step] : one;
+          p.coef[place] = in ? g * up : __int_as_float(0x7FC00000);
+          p.lse[place] = p.lse_in[i];
+        }
+      } else {
+        if (p.losses && !p.reduction) p.losses[i] = 0.f;
+        if (p.lse_out) p.lse_out[i] = 0.f;
+      }
+    }
+    __syncthreads();
+    for (int k = warp; k < here; k += 512 / 32) row(tokens[k], at + k);
+    at += here;
+    __syncthreads();
   }
-  for (long long i = first; i < p.tokens; i += warps) {
-    if (p.targets[i] != p.ignore) continue;
-    if (lane == 0 && p.losses && !p.reduction) p.losses[i] = 0.f;
-    if (lane == 0 && p.lse_out) p.lse_out[i] = 0.f;
-    if (p.dhidden)
-      for (int c = lane; c < p.d; c += 32) static_cast<T*>(p.dhidden)[i * p.d + c] = from_f32<T>(0.f);
+  if (blockIdx.x == gridDim.x - 1) {
+    for (int i = all + threadIdx.x; i < padded; i += 512) {
+      p.target[i] = -1;
+      if (backward) p.coef[i] = p.lse[i] = 0.f;
+    }
   }
+  for (int i = all + int(blockIdx.x) * 16 + warp; i < padded; i += int(gridDim.x) * 16)
+    for (int k = 0; k < kPlanes; ++k) {
+      O* to = static_cast<O*>(p.hidden_packed) + k * p.hidden_plane + (long long)i * p.packed_row;
+      for (int c = lane; c < p.d; c += 32) to[c] = from_f32<O>(0.f);
+    }
 }
 
 // W as the copies of tiles want it, where it does not lie so.
@@ -405,6 +662,7 @@ __global__ void __launch_bounds__(256) k_xent_pack(const XentPrep p) {
   for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < p.vocab; i += warps) {
     const T* from = static_cast<const T*>(p.weight) + i * p.weight_row;
     O* to = static_cast<O*>(p.weight_packed) + i * p.packed_row;
+#pragma unroll 4
     for (int c = lane; c < p.d; c += 32) {
       O v[kPlanes];
       split<O, kPlanes>(to_f32(from[c]), v);
@@ -414,45 +672,83 @@ __global__ void __launch_bounds__(256) k_xent_pack(const XentPrep p) {
   }
 }
 
-template <int MODE, typename T>
-cudaError_t xent_launch(const XentGemm& p, unsigned blocks, cudaStream_t st) {
-  const auto kern = k_xent<MODE, T>;
+// The gradient of H from its parts; zeros for tokens without a target.  A warp takes a row.
+template <typename T>
+__global__ void __launch_bounds__(256) k_xent_finish(const XentPrep p) {
+  take_turn();
+  const int lane = threadIdx.x & 31;
+  const int row_tiles = (*p.count + kXentRows - 1) / kXentRows;
+  const int splits = xent_splits(row_tiles, p.d_tiles, p.piece, p.pairs);
+  const long long part = (long long)row_tiles * kXentRows * p.sum_row;
+  const float back = p.scale[1];
+  const bool vec = reinterpret_cast<uintptr_t>(p.dhidden) % 16 == 0 && p.d % 8 == 0;
+  for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < p.tokens; i += (long long)gridDim.x * 8) {
+    const int place = p.place[i];
+    T* to = static_cast<T*>(p.dhidden) + i * p.d;
+    const float* from = p.sum + place * p.sum_row;  // (not read where there is none)
+    if (vec) {
+      for (int c = lane * 4; c < p.d; c += 128) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (place >= 0) {
+          for (int k = 0; k < splits; ++k) {
+            const float4 o = *reinterpret_cast<const float4*>(from + k * part + c);
+            v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+          }
+        }
+        Pack<T, 4> a;
+        a.v[0] = from_f32<T>(v.x * back); a.v[1] = from_f32<T>(v.y * back);
+        a.v[2] = from_f32<T>(v.z * back); a.v[3] = from_f32<T>(v.w * back);
+        if constexpr (sizeof(a) == 16) *reinterpret_cast<uint4*>(to + c) = *reinterpret_cast<const uint4*>(&a);
+        else *reinterpret_cast<uint2*>(to + c) = *reinterpret_cast<const uint2*>(&a);
+      }
+    } else {
+      for (int c = lane; c < p.d; c += 32) {
+        float v = 0.f;
+        if (place >= 0)
+          for (int k = 0; k < splits; ++k) v += from[k * part + c];
+        to[c] = from_f32<T>(v * back);
+      }
+    }
+  }
+}
+
+template <typename T, bool BACKWARD>
+cudaError_t xent_launch(const XentGemm& p, unsigned pairs, cudaStream_t st) {
+  const auto kern = k_xent<T, BACKWARD>;
   // (the same value every time: a kernel's limit belongs to the device, not to this launch)
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kXentSmem));
   if (e != cudaSuccess) return e;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(blocks);
+  cfg.gridDim = dim3(2 * pairs);
   cfg.blockDim = dim3(kXentThreads);
   cfg.dynamicSmemBytes = kXentSmem;
   cfg.stream = st;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
 template <typename T>
-cudaError_t xent_gemm(XentMode mode, const XentGemm& p, unsigned blocks, cudaStream_t st) {
-  switch (mode) {
-    case kXentStats: return xent_launch<kXentStats, T>(p, blocks, st);
-    case kXentGrad: return xent_launch<kXentGrad, T>(p, blocks, st);
-    case kXentHidden: return xent_launch<kXentHidden, T>(p, blocks, st);
-    default: return xent_launch<kXentWeight, T>(p, blocks, st);
-  }
+cudaError_t xent_prepare(const XentPrep& p, bool backward, int sms, cudaStream_t st) {
+  // runs of tokens for each SM, at least one for each warp of a block
+  const long long per = std::max<long long>(16, (p.tokens + sms - 1) / sms);
+  const unsigned blocks = unsigned(std::max<long long>(1, (p.tokens + per - 1) / per));
+  cudaError_t e = launch(k_xent_prepare<T>, Shape{blocks, 512, 0, 0}, st, p, backward, int(per));
+  if (e != cudaSuccess || !p.weight) return e;
+  return launch(k_xent_pack<T>, Shape{unsigned(std::min(p.vocab / 8 + 1, 8 * sms)), 256, 0, 0}, st, p);
 }
 
 template <typename T>
-cudaError_t xent_prepare(const XentPrep& p, bool backward, int sms, cudaStream_t st) {
-  cudaError_t e = launch(k_xent_select<std::is_same_v<T, __half>>, Shape{1, 1024, 0, 0}, st, p, backward);
-  if (e != cudaSuccess) return e;
-  const auto blocks = [&](long long rows) {
-    return unsigned(rows / 8 + 1 < 8ll * sms ? rows / 8 + 1 : 8ll * sms);
-  };
-  e = launch(k_xent_gather<T>, Shape{blocks(p.tokens + kXentRows), 256, 0, 0}, st, p);
-  if (e != cudaSuccess || !p.weight) return e;
-  return launch(k_xent_pack<T>, Shape{blocks(p.vocab), 256, 0, 0}, st, p);
+cudaError_t xent_finish(const XentPrep& p, int sms, cudaStream_t st) {
+  const long long rows = p.tokens / 8 + 1;
+  return launch(k_xent_finish<T>, Shape{unsigned(std::min<long long>(rows, 8ll * sms)), 256, 0, 0}, st, p);
 }
 
 }  // namespace

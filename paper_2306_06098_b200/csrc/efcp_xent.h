@@ -8,42 +8,39 @@
 
 namespace efcp {
 
-// Products of tiles: what is multiplied, and what becomes of the sums.
-enum XentMode {
-  kXentStats,    // logits = H W^T: largest value and sum of exponentials of a row's part, the target's logit
-  kXentGrad,     // logits once more: gradient of the logits of a piece of the vocabulary
-  kXentHidden,   // gradient of H, added up over the pieces
-  kXentWeight,   // gradient of the piece's rows of W
-};
+// A tile of a product (256 x up to 256, of a pair of blocks), and a step along the sum.
+constexpr int kXentRows = 256, kXentCols = 256, kXentDepth = 64;
+constexpr int kXentSplits = 8;  // parts of the sum over a piece that are added up apart, at most
 
-constexpr int kXentRows = 128, kXentCols = 256, kXentDepth = 64;  // a tile, and a step along the sum
-
+// The products of tiles that a launch works on, in this order:
+//   hidden   gradient of H from a piece's gradient of the logits, in parts, added to those of the pieces before
+//   weight   gradient of the piece's rows of W
+//   logits   forward: largest value and sum of exponentials of a row's part, and the target's logit;
+//            backward: the gradient of the logits of the next piece
 struct XentGemm {
-  CUtensorMap a, b;
+  // operands whose inner dimension is that of the sum (rows of 64 in boxes of a block's share of a tile), and the
+  // others (boxes of 64 x 64)
+  CUtensorMap hidden_rows, weight_rows, g_rows[2], hidden_cols, weight_cols, g_cols[2];
+  // results, stored in boxes of 32 rows of 128 bytes
+  CUtensorMap g_out[2], sum_out, dweight_out;
   const int* count;    // tokens that have a target
-  const int* order;    // their places in the batch
   const int* target;   // their targets, -1: out of range
   const float* lse;    // logarithm of the sum of exponentials (by the tokens' order here)
   const float* coef;   // factor on a token's gradient
   const float* scale;  // [0]: the factor that coef holds, [1]: its inverse
   float2* part;        // statistics, a row of `parts` for each token
   float* target_logit;
-  void* g;                        // gradient of the logits: planes of rows of the piece's columns
-  long long g_row, g_plane;       // in elements
-  float* sum;                     // of the pieces before, fp32, sum_row elements a row
-  long long sum_row;
-  void* out;                      // gradient of H or W
-  long long out_row;
+  void* dweight;
   int* status;
   int vocab, d;
-  int v0, piece;     // columns v0 .. v0 + piece of the vocabulary (padded with zeros to g's width)
   int parts;
-  int row_tiles;     // -1: of the tokens that have a target
-  int col_tiles, col_tile;
-  int depth;         // length of the sum, -1: the tokens
-  int planes;        // 1, or 3 for fp32 values held as three bfloat16 ones
-  int first, last;   // piece
-  int vec_out;       // rows of out start on 16 bytes
+  int d_tiles, d_tile;
+  int hidden, weight, logits;          // which products
+  int v0, buffer, first;               // of the piece that hidden and weight read
+  int next_v0, next_buffer;            // of the piece that logits writes (or 0)
+  int col_tiles, col_tile;             // of logits
+  int piece;                           // columns of a piece
+  int box_dweight;                     // rows of dweight start on 16 bytes: it can be stored in boxes
 };
 
 struct XentPrep {
@@ -65,15 +62,31 @@ struct XentPrep {
   long long grad_step;
   const float* lse_in;
   float *losses, *lse_out, *each;  // each: losses by order, to be added up
-  void* dhidden;       // rows without a target become zeros
+  int* place;                      // a token's place in the order, -1: none
+  const float* sum;                // gradient of H: parts of the whole tiles' rows, sum_row elements each
+  long long sum_row;
+  int d_tiles, piece, pairs;
+  void* dhidden;
 };
 
-cudaError_t xent_gemm_f32(XentMode mode, const XentGemm& p, unsigned blocks, cudaStream_t st);
-cudaError_t xent_gemm_bf16(XentMode mode, const XentGemm& p, unsigned blocks, cudaStream_t st);
-cudaError_t xent_gemm_f16(XentMode mode, const XentGemm& p, unsigned blocks, cudaStream_t st);
+// How many parts the sum over a piece is cut into for the gradient of H: as many as give every pair of blocks two
+// tiles, none shorter than 16 steps.
+__host__ __device__ inline int xent_splits(int row_tiles, int d_tiles, int piece, int pairs) {
+  const int tiles = row_tiles * d_tiles, deepest = (piece + kXentDepth * 16 - 1) / (kXentDepth * 16);
+  int s = tiles > 0 ? (2 * pairs + tiles - 1) / tiles : 1;
+  s = s < deepest ? s : deepest;
+  return s < 1 ? 1 : s < kXentSplits ? s : kXentSplits;
+}
+
+cudaError_t xent_gemm_f32(bool backward, const XentGemm& p, unsigned pairs, cudaStream_t st);
+cudaError_t xent_gemm_bf16(bool backward, const XentGemm& p, unsigned pairs, cudaStream_t st);
+cudaError_t xent_gemm_f16(bool backward, const XentGemm& p, unsigned pairs, cudaStream_t st);
 cudaError_t xent_prepare_f32(const XentPrep& p, bool backward, int sms, cudaStream_t st);
 cudaError_t xent_prepare_bf16(const XentPrep& p, bool backward, int sms, cudaStream_t st);
 cudaError_t xent_prepare_f16(const XentPrep& p, bool backward, int sms, cudaStream_t st);
+cudaError_t xent_finish_f32(const XentPrep& p, int sms, cudaStream_t st);
+cudaError_t xent_finish_bf16(const XentPrep& p, int sms, cudaStream_t st);
+cudaError_t xent_finish_f16(const XentPrep& p, int sms, cudaStream_t st);
 cudaError_t xent_join(const XentPrep& p, int sms, cudaStream_t st);
 
 }  // namespace efcp

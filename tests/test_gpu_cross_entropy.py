@@ -60,7 +60,7 @@ def check_forward(hidden, weight, targets, ignore=-100):
             assert one.isnan()
     again = B().cross_entropy_forward(hidden, weight, targets, ignore, "none")
     assert torch.equal(again[0], losses) and torch.equal(again[1], lse)
-    B().cross_entropy_status()
+    B().operators_status()
     return losses, lse
 
 
@@ -96,7 +96,7 @@ def check_backward(hidden, weight, targets, grad, ignore=-100, reduction="none")
         part = B().cross_entropy_backward(grad, hidden, weight, targets, lse, ignore, reduction, want)
         assert (part[0] is not None, part[1] is not None) == want
         assert torch.equal(part[0], dh) if want[0] else torch.equal(part[1], dw)
-    B().cross_entropy_status()
+    B().operators_status()
     return dh, dw
 
 
@@ -325,4 +325,4 @@ def test_captured_and_on_other_streams():
     lone = B().cross_entropy_forward(hidden, weight, targets, stream=streams[0])
     streams[0].synchronize()
     assert torch.equal(lone[0], want[0])
-    B().cross_entropy_status()
+    B().operators_status()

@@ -194,7 +194,8 @@ def test_the_cross_entropy_workspace():
         weight = 64000 * 64 * 2
         for more in (dict(w=FAKE + 2), dict(weight_row=67)):  # a copy of the weight that can be read by tiles
             assert size(back, tokens=1, vocab=64000, **more) - size(back, tokens=1, vocab=64000) >= weight
-    assert size(1, tokens=1 << 20, vocab=64000) - (1 << 20) * 64 * 6 < 2 * (1 << 20) * 256 + (64 << 20)
+    # two pieces of 256 columns at least, rows of both kinds
+    assert size(1, tokens=1 << 20, vocab=64000) - (1 << 20) * 64 * 6 < 2 * 2 * (1 << 20) * 256 + (64 << 20)
 
 
 @no_gpu
