@@ -8,7 +8,6 @@
 // added up in a fixed order by a second kernel.
 #pragma once
 
-#include <cuda_fp8.h>
 #include <cuda_runtime.h>
 
 #include <type_traits>
@@ -16,8 +15,8 @@
 #include "efcp.h"
 #include "efcp_launch.cuh"
 #include "efcp_rms.h"
+#include "efcp_rms_ring.cuh"
 #include "efcp_rows.cuh"
-#include "efcp_tc.cuh"
 
 namespace efcp {
 namespace {
@@ -87,34 +86,6 @@ __device__ __forceinline__ float max8(const float (&v)[8]) {
   return m;
 }
 
-// The scale of a block whose largest magnitude is `top`: 1 for zeros, NaN where a value is not finite.
-__device__ __forceinline__ float scale_of(float top, float most) {
-  if (!(top < __int_as_float(0x7F800000))) return __int_as_float(0x7FC00000);
-  const float s = top / most;
-  return s > 0.f ? s : 1.f;
-}
-
-// 1 / s, and 0 for a scale of NaN
-__device__ __forceinline__ float inverse_of(float s) { return s == s ? 1.f / s : 0.f; }
-
-// z / s as 8 bits, given 1 / s: the quotient is off by up to two roundings of fp32, so a value that close to the
-// border between two 8-bit ones may go either way; 0 in a block whose scale is NaN.
-template <bool E4M3>
-__device__ __forceinline__ unsigned quantized(float z, float inv) {
-  const float q = inv > 0.f ? z * inv : 0.f;
-  if constexpr (E4M3) return __nv_cvt_float_to_fp8(q, __NV_SATFINITE, __NV_E4M3);
-  else return unsigned(max(-127, min(127, __float2int_rn(q)))) & 0xFFu;
-}
-template <bool E4M3>
-__device__ __forceinline__ unsigned quantized2(float2 z, float inv) {
-  if constexpr (E4M3) {
-    const float2 q = inv > 0.f ? make_float2(z.x * inv, z.y * inv) : make_float2(0.f, 0.f);
-    return __nv_cvt_float2_to_fp8x2(q, __NV_SATFINITE, __NV_E4M3);
-  } else {
-    return quantized<false>(z.x, inv) | quantized<false>(z.y, inv) << 8;
-  }
-}
-
 template <bool VEC, bool E4M3>
 __device__ __forceinline__ void store_q8(unsigned char* row, int c0, int lane, int d,
                                          const float (&v)[8], const float (&s)[8]) {
@@ -124,8 +95,8 @@ __device__ __forceinline__ void store_q8(unsigned char* row, int c0, int lane, i
       uint2 q = {0, 0};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        q.x |= quantized<E4M3>(v[j], inverse_of(s[j])) << (8 * j);
-        q.y |= quantized<E4M3>(v[4 + j], inverse_of(s[4 + j])) << (8 * j);
+        q.x |= quantized<E4M3>(v[j], s[j], inverse_of(s[j])) << (8 * j);
+        q.y |= quantized<E4M3>(v[4 + j], s[4 + j], inverse_of(s[4 + j])) << (8 * j);
       }
       *reinterpret_cast<uint2*>(row + col) = q;
     }
@@ -133,7 +104,7 @@ __device__ __forceinline__ void store_q8(unsigned char* row, int c0, int lane, i
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int col = c0 + j * 32 + lane;
-      if (col < d) row[col] = (unsigned char)quantized<E4M3>(v[j], inverse_of(s[j]));
+      if (col < d) row[col] = (unsigned char)quantized<E4M3>(v[j], s[j], inverse_of(s[j]));
     }
   }
 }
@@ -147,7 +118,7 @@ __device__ __forceinline__ void block_scales(const Rms& p, float* scales, int c0
     const float one = scale_of(lanes_max(max8(v), lanes), p.most);
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[j] = one;
-    if (lane % lanes == 0 && col < p.d) scales[col / p.block] = one;
+    if (lane % lanes == 0 && col < p.d) scales[col >> p.block_shift] = one;
   } else {
     const int strips = p.block / 32;
     float top[8];
@@ -167,7 +138,7 @@ __device__ __forceinline__ void block_scales(const Rms& p, float* scales, int c0
     for (int j = 0; j < 8; ++j) {
       s[j] = scale_of(top[j], p.most);
       const int col = c0 + j * 32;
-      if (lane == 0 && j % strips == 0 && col < p.d) scales[col / p.block] = s[j];
+      if (lane == 0 && j % strips == 0 && col < p.d) scales[col >> p.block_shift] = s[j];
     }
   }
 }
@@ -391,6 +362,7 @@ __global__ void __launch_bounds__(1024) k_rms_dweight_join(const float* part, lo
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, col = int(blockIdx.x) * 32 + tx;
   float s = 0.f;
   if (col < d)
+#pragma unroll 8
     for (long long i = ty; i < count; i += 32) s += part[i * d + col];
   sum[ty][tx] = s;
   __syncthreads();
@@ -423,472 +395,7 @@ __global__ void __launch_bounds__(256) k_dropout(const Rms p) {
   }
 }
 
-// ------------------------------------------------------------------ rows through shared memory
-// Bulk copies bring whole rows into shared memory while earlier ones are worked on, so that enough bytes are on
-// their way without a register being held for them.  Two blocks of eight warps share an SM.  A group of warps
-// asks for the next unit of a place when a barrier has told that all of them are done with the one there.
-
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-      "l"(src), "r"(bytes), "r"(bar)
-      : "memory");
-}
-
-struct RingInput {
-  const void* data;
-  long long row;  // bytes between rows
-};
-
-// A group's view of its ring.
-template <int INPUTS>
-struct Ring {
-  const Rms& p;
-  const RmsRing& q;
-  unsigned char* data;  // of this group
-  uint32_t bars;
-  int* gave_up;
-  long long first, step, units;  // units of the group: first, first + step, ...
-  int group, warp, lane;
-  RingInput in[INPUTS];
-
-  __device__ __forceinline__ unsigned char* place(int s, int i) const {
-    return data + (s * q.inputs + i) * q.unit_bytes;
-  }
-  // the warps of the group meet
-  __device__ __forceinline__ void meet() const {
-    if (p.warps == 1) __syncwarp();
-    else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(p.warps * 32) : "memory");
-  }
-  // (one thread) the group's unit number n into its place
-  __device__ __forceinline__ void ask(long long n) const {
-    const long long u = first + n * step;
-    if (u >= units) return;
-    const int s = int(n % q.stages);
-    const long long row = u * q.rows;
-    const int rows = int(min((long long)q.rows, p.rows - row));
-    const uint32_t bar = bars + 8 * s;
-    tc::bar_expect(bar, uint32_t(rows * q.row_bytes * q.inputs));
-#pragma unroll
-    for (int i = 0; i < INPUTS; ++i) {
-      if (i >= q.inputs) break;
-      const char* from = static_cast<const char*>(in[i].data) + row * in[i].row;
-      const uint32_t to = tc::smem_of(place(s, i));
-      if (in[i].row == q.row_bytes) bulk_copy(to, from, uint32_t(rows * q.row_bytes), bar);
-      else
-        for (int r = 0; r < rows; ++r) bulk_copy(to + r * q.row_bytes, from + r * in[i].row, uint32_t(q.row_bytes), bar);
-    }
-  }
-  // Unit number n has arrived.  When the limit passes the work goes on with whatever lies there (the warps of a
-  // group keep meeting), no further wait is long, and the status tells.
-  __device__ __forceinline__ void await(long long n) const {
-    (void)tc::bar_wait(bars + 8 * int(n % q.stages), uint32_t(n / q.stages) & 1, gave_up);
-  }
-  // Nothing may land in shared memory that the block has left.
-  __device__ __forceinline__ void end(long long asked) const {
-    if (!*(volatile int*)gave_up) return;
-    for (long long n = asked < q.stages ? 0 : asked - q.stages; n < asked; ++n)
-      if (first + n * step < units)
-        (void)tc::bar_wait(bars + 8 * int(n % q.stages), uint32_t(n / q.stages) & 1, gave_up, tc::kDrainNs);
-  }
-};
-
-// Barriers, the weight in fp32, and the group that a warp belongs to.  (Up to 8 groups of up to 4 places.)
-template <int INPUTS>
-__device__ __forceinline__ Ring<INPUTS> ring_begin(const Rms& p, const RmsRing& q, unsigned char* smem,
-                                                   int* gave_up) {
-  const int warp = threadIdx.x >> 5;
-  const uint32_t bars = tc::smem_of(smem);
-  if (threadIdx.x == 0) {
-    *gave_up = 0;
-    for (int i = 0; i < p.groups * q.stages; ++i) tc::bar_init(bars + 8 * i, 1);
-    tc::bar_init_fence();
-  }
-  take_turn();
-  float* weight = reinterpret_cast<float*>(smem + q.weight_at);
-  if (p.weight)
-    for (int c = threadIdx.x; c < p.d; c += blockDim.x) weight[c] = load_as_f32(p.weight, p.param_dtype, c);
-  __syncthreads();
-  const int g = warp / p.warps;
-  return Ring<INPUTS>{p, q, smem + q.data_at + (size_t)g * q.stages * q.inputs * q.unit_bytes,
-                      bars + 8 * g * q.stages, gave_up,
-                      (long long)blockIdx.x * p.groups + g, (long long)gridDim.x * p.groups,
-                      (p.rows + q.rows - 1) / q.rows, g, warp - g * p.warps, int(threadIdx.x) & 31, {}};
-}
-
-// Eight elements as they lie in memory.
-template <typename T>
-struct Eight {
-  uint4 raw[sizeof(T) / 2];
-
-  __device__ __forceinline__ void load_shared(uint32_t at) {
-#pragma unroll
-    for (int i = 0; i < int(sizeof(T) / 2); ++i)
-      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                   : "=r"(raw[i].x), "=r"(raw[i].y), "=r"(raw[i].z), "=r"(raw[i].w)
-                   : "r"(at + 16 * i)
-                   : "memory");
-  }
-  __device__ __forceinline__ void store_shared(uint32_t at) const {
-#pragma unroll
-    for (int i = 0; i < int(sizeof(T) / 2); ++i)
-      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + 16 * i), "r"(raw[i].x),
-                   "r"(raw[i].y), "r"(raw[i].z), "r"(raw[i].w)
-                   : "memory");
-  }
-  __device__ __forceinline__ void store(T* to) const {
-#pragma unroll
-    for (int i = 0; i < int(sizeof(T) / 2); ++i) reinterpret_cast<uint4*>(to)[i] = raw[i];
-  }
-  __device__ __forceinline__ void get(float2 (&v)[4]) const {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(raw);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (std::is_same_v<T, float>) {
-        v[i] = make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
-      } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
-        v[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
-      } else {
-        v[i] = __half22float2(reinterpret_cast<const __half2*>(w)[i]);
-      }
-    }
-  }
-  __device__ __forceinline__ void set(const float2 (&v)[4]) {
-    uint32_t* w = reinterpret_cast<uint32_t*>(raw);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (std::is_same_v<T, float>) {
-        w[2 * i] = __float_as_uint(v[i].x);
-        w[2 * i + 1] = __float_as_uint(v[i].y);
-      } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
-        reinterpret_cast<__nv_bfloat162*>(w)[i] = __float22bfloat162_rn(v[i]);
-      } else {
-        reinterpret_cast<__half2*>(w)[i] = __float22half2_rn(v[i]);
-      }
-    }
-  }
-};
-
-__device__ __forceinline__ void drop_pairs(float2 (&v)[4], unsigned long long group, const DropKey& key,
-                                           const Drop& drop) {
-  float w[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { w[2 * i] = v[i].x; w[2 * i + 1] = v[i].y; }
-  drop_group(w, group, key, drop.threshold, drop.scale);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = make_float2(w[2 * i], w[2 * i + 1]);
-}
-
-// Sum (or maximum) over the lanes and warps that share a row; `slot` as in row_join.
-template <bool MAX, int INPUTS>
-__device__ __forceinline__ float ring_join(const Ring<INPUTS>& r, float v, int slot) {
-  __shared__ float part[4][8];
-  for (int o = r.q.lanes / 2; o; o >>= 1) {
-    const float other = __shfl_xor_sync(kAll, v, o);
-    if constexpr (MAX) v = larger(v, other);
-    else v += other;
-  }
-  if (r.p.warps == 1) {
-    __syncwarp();
-    return v;
-  }
-  float* mine = part[slot] + r.group * r.p.warps;
-  if (r.lane == 0) mine[r.warp] = v;
-  r.meet();
-  float all = mine[0];
-  for (int i = 1; i < r.p.warps; ++i) {
-    if constexpr (MAX) all = larger(all, mine[i]);
-    else all += mine[i];
-  }
-  return all;
-}
-
-// K: chunks of a warp; h and z stay in registers.  SUM: h is not x; DROP: with dropout.
-template <typename T, int K, int QUANT, bool SUM, bool DROP>
-__global__ void __launch_bounds__(256, 2) k_rms_forward_ring(const Rms p, const RmsRing q) {
-  extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ int gave_up;
-  constexpr int kInputs = SUM ? 2 : 1;
-  Ring<kInputs> r = ring_begin<kInputs>(p, q, smem, &gave_up);
-  r.in[0] = {p.x, p.x_row * (long long)sizeof(T)};
-  if constexpr (SUM) r.in[1] = {p.residual, p.residual_row * (long long)sizeof(T)};
-  const bool asks = r.warp == 0 && r.lane == 0;
-  if (asks)
-    for (int n = 0; n < q.stages; ++n) r.ask(n);
-  DropKey key{};
-  if constexpr (DROP) key = drop_key(p.drop);
-  const uint32_t weight = tc::smem_of(smem + q.weight_at);
-  const int sub = r.lane / q.lanes, first_col = (r.lane - sub * q.lanes) * 8 + r.warp * kChunk;
-  const int step = p.warps * kChunk;
-  const bool two = SUM && p.residual;
-  unsigned s = 0;
-  long long n = 0;
-  for (long long u = r.first; u < r.units; u += r.step, ++n) {
-    const long long row = u * q.rows + sub;
-    const bool on = row < p.rows && sub < q.rows;
-    const uint32_t x = tc::smem_of(r.place(int(s), 0)) + sub * q.row_bytes, res = x + q.unit_bytes;
-    const unsigned long long at = (unsigned long long)row * p.d;
-    r.await(n);
-    Eight<T> h[K];
-    float2 sq = both(0.f);
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int c = first_col + k * step;
-      if (!on || c >= p.d) continue;
-      h[k].load_shared(x + c * sizeof(T));
-      float2 v[4];
-      h[k].get(v);
-      if constexpr (SUM) {
-        if constexpr (DROP) drop_pairs(v, (at + c) >> 3, key, p.drop);
-        if (two) {
-          Eight<T> a;
-          a.load_shared(res + c * sizeof(T));
-          float2 w[4];
-          a.get(w);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = add2(v[i], w[i]);
-        }
-        h[k].set(v);
-        h[k].store(static_cast<T*>(p.h) + at + c);
-        h[k].get(v);
-      }
-      float2 t = mul2(v[0], v[0]);
-#pragma unroll
-      for (int i = 1; i < 4; ++i) t = fma2(v[i], v[i], t);
-      sq = fma2(t, both(p.inv_d), sq);
-    }
-    const float rstd = rsqrtf(ring_join<false>(r, sq.x + sq.y, int(n & 1)) + p.eps);
-    // every warp of the group is done with the places up to this one's
-    if (asks) r.ask(n + q.stages);
-    if (on && first_col == 0 && p.rstd) p.rstd[row] = rstd;
-    const auto norm8 = [&](int k, int c, float2(&v)[4]) {
-      h[k].get(v);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], both(rstd));
-      if (p.weight) {
-        Eight<float> w;
-        w.load_shared(weight + c * 4);
-        float2 f[4];
-        w.get(f);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], f[i]);
-      }
-    };
-    if constexpr (QUANT == 0) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int c = first_col + k * step;
-        if (!on || c >= p.d) continue;
-        float2 v[4];
-        norm8(k, c, v);
-        Eight<T> y;
-        y.set(v);
-        y.store(static_cast<T*>(p.y) + at + c);
-      }
-    } else {
-      float* scales = p.scales + row * p.blocks;
-      float2 z[K][4];
-      float top = 0.f, one = 1.f;
-      const auto max_of = [](const float2(&v)[4]) {  // of the bits of magnitudes: NaN lies above infinity
-        unsigned m = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          m = max(m, max(__float_as_uint(v[i].x) & 0x7FFFFFFFu, __float_as_uint(v[i].y) & 0x7FFFFFFFu));
-        return __uint_as_float(m);
-      };
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int c = first_col + k * step;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z[k][i] = both(0.f);
-        if (on && c < p.d) norm8(k, c, z[k]);
-        if (p.block == 0) top = larger(top, max_of(z[k]));
-      }
-      if (p.block == 0) {
-        one = scale_of(ring_join<true>(r, top, 2 + int(n & 1)), p.most);
-        if (on && first_col == 0) scales[0] = one;
-      }
-      const int lanes = min(p.block / 8, q.lanes);
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int c = first_col + k * step;
-        float scale = one;
-        if (p.block) {  // (all lanes: the maximum of a block is exchanged between them)
-          scale = scale_of(lanes_max(max_of(z[k]), lanes), p.most);
-          if (on && c < p.d && c % p.block == 0) scales[c / p.block] = scale;
-        }
-        if (!on || c >= p.d) continue;
-        const float inv = inverse_of(scale);
-        uint2 o = {0, 0};
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          o.x |= quantized2<QUANT == 1>(z[k][j], inv) << (16 * j);
-          o.y |= quantized2<QUANT == 1>(z[k][2 + j], inv) << (16 * j);
-        }
-        *reinterpret_cast<uint2*>(static_cast<unsigned char*>(p.y) + at + c) = o;
-      }
-    }
-    s = s + 1 == unsigned(q.stages) ? 0 : s + 1;
-  }
-  if (asks) r.end(n + q.stages);
-  if (threadIdx.x == 0 && *(volatile int*)&gave_up) atomicExch(p.status, EFCP_ETIMEOUT);
-}
-
-// K: chunks of a warp; it holds their sums of the weight's gradient in registers.
-template <typename T, int K, bool DROP>
-__global__ void __launch_bounds__(256, 2) k_rms_backward_ring(const Rms p, const RmsRing q) {
-  extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ int gave_up;
-  Ring<3> r = ring_begin<3>(p, q, smem, &gave_up);
-  r.in[0] = {p.dy, p.dy_row * (long long)sizeof(T)};
-  r.in[1] = {p.x, p.x_row * (long long)sizeof(T)};
-  r.in[2] = {p.dh, p.dh_row * (long long)sizeof(T)};
-  const bool asks = r.warp == 0 && r.lane == 0;
-  if (asks)
-    for (int n = 0; n < q.stages; ++n) r.ask(n);
-  DropKey key{};
-  if constexpr (DROP) key = drop_key(p.drop);
-  const uint32_t weight = tc::smem_of(smem + q.weight_at);
-  const int sub = r.lane / q.lanes, first_col = (r.lane - sub * q.lanes) * 8 + r.warp * kChunk;
-  const int step = p.warps * kChunk;
-  float2 dw[K][4];
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) dw[k][i] = both(0.f);
-  const auto rstd_of = [&](long long u) {
-    const long long row = u * q.rows + sub;
-    return row < p.rows ? p.rstd[row] : 0.f;
-  };
-  const auto weight8 = [&](int c, float2(&w)[4]) {
-    Eight<float> a;
-    a.load_shared(weight + c * 4);
-    a.get(w);
-  };
-  unsigned s = 0;
-  long long n = 0;
-  float next = rstd_of(r.first);
-  for (long long u = r.first; u < r.units; u += r.step, ++n) {
-    const long long row = u * q.rows + sub;
-    const bool on = row < p.rows && sub < q.rows;
-    const uint32_t dy = tc::smem_of(r.place(int(s), 0)) + sub * q.row_bytes, h = dy + q.unit_bytes,
-                   dh = h + q.unit_bytes;
-    const unsigned long long at = (unsigned long long)row * p.d;
-    const float rs = next;
-    next = rstd_of(u + r.step);
-    r.await(n);
-    Eight<T> a8[K], b8[K];
-    float2 sum = both(0.f);
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int c = first_col + k * step;
-      if (!on || c >= p.d) continue;
-      a8[k].load_shared(dy + c * sizeof(T));
-      b8[k].load_shared(h + c * sizeof(T));
-      float2 a[4], b[4];
-      a8[k].get(a);
-      b8[k].get(b);
-      if (p.weight) {
-        float2 w[4];
-        weight8(c, w);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = mul2(a[i], w[i]);
-      }
-      float2 t = mul2(a[0], b[0]);
-#pragma unroll
-      for (int i = 1; i < 4; ++i) t = fma2(a[i], b[i], t);
-      sum = add2(sum, t);
-    }
-    const float m = -ring_join<false>(r, sum.x + sum.y, int(n & 1)) * p.inv_d * rs * rs;
-    // every warp of the group is done with the place before this one (its last input is read below)
-    if (asks && n > 0) r.ask(n - 1 + q.stages);
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int c = first_col + k * step;
-      if (!on || c >= p.d) continue;
-      float2 a[4], b[4];
-      a8[k].get(a);
-      b8[k].get(b);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) dw[k][i] = fma2(a[i], mul2(b[i], both(rs)), dw[k][i]);
-      if (p.weight) {
-        float2 w[4];
-        weight8(c, w);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = mul2(a[i], w[i]);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = mul2(fma2(b[i], both(m), a[i]), both(rs));
-      if (p.dh) {
-        Eight<T> e8;
-        e8.load_shared(dh + c * sizeof(T));
-        float2 e[4];
-        e8.get(e);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = add2(a[i], e[i]);
-      }
-      Eight<T> out;
-      if (p.dresidual) {
-        out.set(a);
-        out.store(static_cast<T*>(p.dresidual) + at + c);
-      }
-      if (p.dx) {
-        if constexpr (DROP) drop_pairs(a, (at + c) >> 3, key, p.drop);
-        out.set(a);
-        out.store(static_cast<T*>(p.dx) + at + c);
-      }
-    }
-    s = s + 1 == unsigned(q.stages) ? 0 : s + 1;
-  }
-  if (p.part) {
-    if (q.lanes < 32) {  // the rows of a unit, one warp
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        for (int o = q.lanes; o < 32; o *= 2) {
-          dw[0][i].x += __shfl_xor_sync(kAll, dw[0][i].x, o);
-          dw[0][i].y += __shfl_xor_sync(kAll, dw[0][i].y, o);
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int c = first_col + k * step;
-      if (sub || c >= p.d) continue;
-      Eight<float> out;
-      out.set(dw[k]);
-      out.store(p.part + r.first * p.d + c);
-    }
-  }
-  if (asks) r.end(n - 1 + q.stages);
-  if (threadIdx.x == 0 && *(volatile int*)&gave_up) atomicExch(p.status, EFCP_ETIMEOUT);
-}
-
-template <typename T, int K>
-cudaError_t rms_launch_ring_k(const Rms& p, const RmsLaunch& l) {
-  const Shape s{l.blocks, unsigned(p.groups * p.warps * 32), l.smem, 0};
-  const bool sum = p.h, drop = p.drop.threshold;
-  switch (l.op) {
-    case kRmsE4M3:
-      return sum ? launch(k_rms_forward_ring<T, K, 1, true, false>, s, l.st, p, l.ring)
-                 : launch(k_rms_forward_ring<T, K, 1, false, false>, s, l.st, p, l.ring);
-    case kRmsInt8:
-      return sum ? launch(k_rms_forward_ring<T, K, 2, true, false>, s, l.st, p, l.ring)
-                 : launch(k_rms_forward_ring<T, K, 2, false, false>, s, l.st, p, l.ring);
-    case kRmsForward:
-      return drop  ? launch(k_rms_forward_ring<T, K, 0, true, true>, s, l.st, p, l.ring)
-             : sum ? launch(k_rms_forward_ring<T, K, 0, true, false>, s, l.st, p, l.ring)
-                   : launch(k_rms_forward_ring<T, K, 0, false, false>, s, l.st, p, l.ring);
-    default:
-      return drop ? launch(k_rms_backward_ring<T, K, true>, s, l.st, p, l.ring)
-                  : launch(k_rms_backward_ring<T, K, false>, s, l.st, p, l.ring);
-  }
-}
-
-template <typename T>
-cudaError_t rms_launch_ring(const Rms& p, const RmsLaunch& l) {
-  const cudaError_t e = l.kept == 1   ? rms_launch_ring_k<T, 1>(p, l)
-                        : l.kept == 2 ? rms_launch_ring_k<T, 2>(p, l)
-                                      : rms_launch_ring_k<T, 4>(p, l);
-  if (e != cudaSuccess || !p.part) return e;
+inline cudaError_t rms_join(const Rms& p, const RmsLaunch& l) {
   return launch(k_rms_dweight_join, Shape{unsigned((p.d + 31) / 32), 1024, 0, 0}, l.st,
                 static_cast<const float*>(p.part), l.parts, p.d, p.dweight, p.param_dtype);
 }
@@ -916,13 +423,16 @@ cudaError_t rms_launch_vec(const Rms& p, const RmsLaunch& l) {
     e = launch(k_rms_dweight<T, VEC>, Shape{tiles * unsigned(l.parts / 8), 256, 0, 0}, l.st, p);
     if (e != cudaSuccess) return e;
   }
-  return launch(k_rms_dweight_join, Shape{unsigned((p.d + 31) / 32), 1024, 0, 0}, l.st,
-                static_cast<const float*>(p.part), l.parts, p.d, p.dweight, p.param_dtype);
+  return rms_join(p, l);
 }
 
 template <typename T>
 cudaError_t rms_launch(const Rms& p, const RmsLaunch& l) {
-  if (l.ringed) return rms_launch_ring<T>(p, l);
+  if (l.ringed) {
+    const cudaError_t e = l.vec ? rms_launch_ring<T, false>(p, l) : rms_launch_ring<T, true>(p, l);
+    if (e != cudaSuccess || !p.part) return e;
+    return rms_join(p, l);
+  }
   return l.vec ? rms_launch_vec<T, true>(p, l) : rms_launch_vec<T, false>(p, l);
 }
 

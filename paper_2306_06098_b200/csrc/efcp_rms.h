@@ -24,6 +24,7 @@ struct Rms {
   float* part;                     // sums of dweight, a row of d for each slot
   float* scales;
   int block, blocks;  // columns that share a scale (0: a row), scales of a row
+  int block_shift;    // log2(block)
   float most;         // largest value of the 8-bit type
   int* status;
 };
@@ -32,8 +33,10 @@ struct Rms {
 // places of its own; a place holds a unit: one row, or several short ones that share a warp.
 struct RmsRing {
   int stages, inputs;
-  int rows, lanes;     // rows of a unit, lanes that share a row (32 unless rows > 1)
+  int rows, lanes;  // rows that a warp takes at once, lanes that share one (32 unless rows > 1)
+  int reps;         // such sets of rows in a unit
   int row_bytes, unit_bytes;
+  int pitch;               // bytes between rows of a unit in a place, where an input's rows are not side by side
   int weight_at, data_at;  // in shared memory: the weight in fp32, the rings
 };
 
@@ -41,7 +44,8 @@ enum RmsOp { kRmsForward, kRmsE4M3, kRmsInt8, kRmsBackward, kDropout };
 
 struct RmsLaunch {
   RmsOp op;
-  bool vec;         // rows start on 16 bytes, and on multiples of eight elements of the logical order
+  bool vec;         // rows start on 16 bytes, and on multiples of eight elements of the logical order  (not so, but
+                    // ringed: outputs start on 16 bytes)
   int kept;         // chunks that a warp keeps in registers: 1, 2, 4, or 0 (rows walked twice)
   unsigned blocks;
   long long parts;  // rows of `part`

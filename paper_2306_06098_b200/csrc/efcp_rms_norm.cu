@@ -26,7 +26,7 @@ namespace {
 
 constexpr int kTypeBytes[3] = {4, 2, 2};
 constexpr int kColumns = 256;  // of a chunk: see efcp_rows.cuh
-constexpr int64_t kMostSmem = 115400;  // leaves an SM room for two blocks, with what is not dynamic
+constexpr int64_t kMostSmem = 114600;  // leaves an SM room for two blocks, with what is not dynamic
 constexpr int64_t kMostBlocks = (1ll << 31) - 1;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -90,33 +90,45 @@ void share(const efcp_rms_norm* d, int sms, Rms* p, RmsLaunch* l) {
 }
 
 // Rows through shared memory, where a group of warps has two places at least: whether that is so, and how.  Units of
-// several rows for rows of up to 128 elements; a warp takes rows of up to 1024 alone.  With fewer rows than places to
-// work on them the plain kernels are as fast or faster: there is nothing to fetch ahead.
+// several rows for short ones, up to 2 KB where that is possible; a warp takes rows of up to 1024 alone.  With fewer
+// rows than places to work on them the plain kernels are as fast or faster: there is nothing to fetch ahead.
 bool plan_ring(const efcp_rms_norm* d, bool vec, int inputs, bool weight, int sms, Rms* p, RmsLaunch* l) {
-  if (!vec || d->rows < 2 * sms || d->d > 8192) return false;
-  const int64_t chunks = ceil_div(d->d, kColumns), row_bytes = d->d * kTypeBytes[d->dtype];
+  if (d->rows < 2 * sms || d->d > 8192) return false;
+  // groups of eight that a row touches, wherever it begins
+  const int64_t eights = vec ? d->d / 8 : (d->d + 14) / 8;
+  const int64_t chunks = ceil_div(eights, 32), row_bytes = d->d * kTypeBytes[d->dtype];
+  if (chunks > 32) return false;
   RmsRing& q = l->ring;
   q = RmsRing{};
   q.inputs = inputs;
   q.lanes = 32;
-  while (q.lanes > 1 && d->d <= q.lanes * 4) q.lanes /= 2;
+  while (q.lanes > 1 && eights <= q.lanes / 2) q.lanes /= 2;
   q.rows = 32 / q.lanes;
+  q.reps = 1;
+  while (vec && chunks == 1 && q.reps < 8 && row_bytes * q.rows * q.reps < 1024) q.reps *= 2;
   q.row_bytes = int(row_bytes);
-  q.unit_bytes = int(row_bytes * q.rows);
+  q.pitch = int(ceil_div(row_bytes, 16) * 16 + 16);
+  // (not vec: room for the pieces of 16 bytes that rows begin and end in: see efcp_rms_ring.cuh)
+  q.unit_bytes = int(vec ? row_bytes * q.rows * q.reps : 48 + q.pitch * q.rows + 64);
   p->warps = chunks <= 4 ? 1 : int(std::min<int64_t>(8, ceil_div(chunks, 2)));
   p->groups = 8 / p->warps;
   const int64_t kept = ceil_div(chunks, p->warps);
   l->kept = kept <= 2 ? int(kept) : 4;
   q.weight_at = 512;  // behind the barriers
-  q.data_at = int(ceil_div(q.weight_at + (weight ? d->d * 4 : 0), 128) * 128);
+  const int64_t weights = vec ? d->d : p->groups * p->warps * l->kept * kColumns;  // (not vec: as each lane reads it)
+  q.data_at = int(ceil_div(q.weight_at + (weight ? weights * 4 : 0), 128) * 128);
   const int64_t stage = int64_t(p->groups) * inputs * q.unit_bytes;
   q.stages = int(std::min<int64_t>(4, (kMostSmem - q.data_at) / stage));
   if (q.stages < 2) return false;
   l->ringed = true;
-  l->smem = size_t(q.data_at + q.stages * stage);
-  const int64_t units = ceil_div(d->rows, q.rows);
+  // (above 48 KB by itself, so that a launch raises the kernel's limit: what is not dynamic counts too)
+  l->smem = size_t(std::max<int64_t>(q.data_at + q.stages * stage, 48 * 1024 + 16));
+  const int64_t units = ceil_div(d->rows, q.rows * q.reps);
   l->blocks = unsigned(std::min<int64_t>(2 * sms, ceil_div(units, p->groups)));
-  l->parts = int64_t(l->blocks) * p->groups;
+  // the rows of a group are a multiple of eight apart
+  if (!vec)
+    while (int64_t(l->blocks) * p->groups * q.rows % 8) ++l->blocks;
+  l->parts = int64_t(l->blocks) * p->groups * (vec ? 1 : q.rows);
   return true;
 }
 
@@ -165,8 +177,10 @@ int forward(const efcp_rms_norm* d, RmsOp op, const void* x, int64_t x_row, cons
   l.op = op;
   l.vec = d->d % 8 == 0 && wide(d, x, x_row) && wide(d, residual, residual_row) && wide(d, weight, 0) &&
           (!summed || wide(d, h, 0)) && reinterpret_cast<uintptr_t>(y) % 16 == 0;
-  const bool ring = op == kRmsForward || d->p == 0.;
-  if (!plan_ring(d, l.vec && ring, residual ? 2 : 1, weight, sms, &p, &l)) {
+  // (the 8-bit outputs take no dropout; columns that share a scale have to lie on multiples of eight)
+  const bool ring = (op == kRmsForward || d->p == 0.) && (l.vec || !block) && reinterpret_cast<uintptr_t>(y) % 16 == 0 &&
+                    (!summed || wide(d, h, 0));
+  if (!ring || !plan_ring(d, l.vec, residual ? 2 : 1, weight, sms, &p, &l)) {
     share(d, sms, &p, &l);
     const int64_t blocks = ceil_div(d->rows, p.groups);
     if (blocks > kMostBlocks) return EFCP_ETOOBIG;
@@ -176,6 +190,7 @@ int forward(const efcp_rms_norm* d, RmsOp op, const void* x, int64_t x_row, cons
   p.weight = weight; p.y = y; p.h = summed ? h : nullptr; p.rstd = rstd;
   p.scales = scales; p.block = block;
   p.blocks = block ? int(ceil_div(d->d, block)) : 1;
+  p.block_shift = block == 128 ? 7 : block == 64 ? 6 : 5;
   p.most = op == kRmsInt8 ? 127.f : 448.f;
   return run(p, l, d->dtype, static_cast<cudaStream_t>(stream));
 }
@@ -215,7 +230,9 @@ int64_t efcp_rms_norm_workspace_bytes(const efcp_rms_norm* desc) {
   // (whether the rows go through shared memory hangs on their alignment, which is not known here)
   int64_t parts = 0;
   for (int inputs : {2, 3})
-    if (plan_ring(desc, desc->d % 8 == 0, inputs, false, sms, &p, &l)) parts = std::max<int64_t>(parts, l.parts);
+    for (bool vec : {false, true})
+      if ((!vec || desc->d % 8 == 0) && plan_ring(desc, vec, inputs, false, sms, &p, &l))
+        parts = std::max<int64_t>(parts, l.parts);
   share(desc, sms, &p, &l);
   parts = std::max(parts, backward_blocks(desc, sms, p, l).parts);
   return std::max<int64_t>(16, parts * desc->d * 4);
@@ -248,7 +265,8 @@ int efcp_rms_norm_backward(const efcp_rms_norm* desc, const void* dy, int64_t dy
   l.op = kRmsBackward;
   l.vec = desc->d % 8 == 0 && wide(desc, dy, dy_row) && wide(desc, h, h_row) && wide(desc, dh, dh_row) &&
           wide(desc, weight, 0) && wide(desc, dx, 0) && wide(desc, dresidual, 0);
-  if (!plan_ring(desc, l.vec, dh ? 3 : 2, weight, sms, &p, &l)) {
+  const bool ring = wide(desc, dx, 0) && wide(desc, dresidual, 0);
+  if (!ring || !plan_ring(desc, l.vec, dh ? 3 : 2, weight, sms, &p, &l)) {
     share(desc, sms, &p, &l);
     const Backward b = backward_blocks(desc, sms, p, l);
     l.blocks = b.blocks;

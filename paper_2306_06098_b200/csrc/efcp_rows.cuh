@@ -3,6 +3,8 @@
 // touch neighbouring elements.
 #pragma once
 
+#include <cuda_fp8.h>
+
 #include "efcp_num.cuh"
 #include "efcp_philox.cuh"
 
@@ -122,6 +124,48 @@ __device__ __forceinline__ float lanes_max(float v, int width) {
   if (width == 32) return __uint_as_float(__reduce_max_sync(kAll, __float_as_uint(v)));
   for (int o = width / 2; o; o >>= 1) v = larger(v, __shfl_xor_sync(kAll, v, o));
   return v;
+}
+
+// ------------------------------------------------------------------ 8 bits
+// The scale of a block whose largest magnitude is `top`: 1 for zeros, NaN where a value is not finite.
+__device__ __forceinline__ float scale_of(float top, float most) {
+  if (!(top < __int_as_float(0x7F800000))) return __int_as_float(0x7FC00000);
+  const float s = top / most;
+  return s > 0.f ? s : 1.f;
+}
+
+// 1 / s; 0 for a scale of NaN, or one so small that the inverse would leave fp32's range.
+__device__ __forceinline__ float inverse_of(float s) { return s >= 0x1p-100f ? __fdividef(1.f, s) : 0.f; }
+
+// z / s as 8 bits, given inverse_of(s): the quotient is off by a few roundings of fp32, so a value that close to the
+// border between two 8-bit ones may go either way; 0 in a block whose scale is NaN.
+template <bool E4M3>
+__device__ __forceinline__ unsigned quantized(float z, float s, float inv) {
+  const float q = inv > 0.f ? z * inv : s > 0.f ? z / s : 0.f;
+  if constexpr (E4M3) return __nv_cvt_float_to_fp8(q, __NV_SATFINITE, __NV_E4M3);
+  else return unsigned(max(-127, min(127, __float2int_rn(q)))) & 0xFFu;
+}
+template <bool E4M3>
+__device__ __forceinline__ uint2 quantized8(const float2 (&z)[4], float s, float inv) {
+  uint2 o = {0, 0};
+  if (inv > 0.f) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 q = mul2(z[j], both(inv));
+      unsigned w;
+      if constexpr (E4M3) {
+        w = __nv_cvt_float2_to_fp8x2(q, __NV_SATFINITE, __NV_E4M3);
+      } else {  // (|q| is at most 127 and a few roundings)
+        w = (unsigned(__float2int_rn(q.x)) & 0xFFu) | (unsigned(__float2int_rn(q.y)) & 0xFFu) << 8;
+      }
+      (j < 2 ? o.x : o.y) |= w << (16 * (j & 1));
+    }
+  } else if (s > 0.f) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      (j < 2 ? o.x : o.y) |= (quantized<E4M3>(z[j].x, s, 0.f) | quantized<E4M3>(z[j].y, s, 0.f) << 8) << (16 * (j & 1));
+  }
+  return o;
 }
 
 }  // namespace efcp

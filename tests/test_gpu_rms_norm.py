@@ -313,3 +313,55 @@ def test_offsets_beyond_32_bits():
     x = torch.as_strided(big, (rows, d), (2 ** 30, 1))
     x.copy_(rand((rows, d), 1, torch.bfloat16))
     check_forward(x, rand((rows, d), 2, torch.bfloat16), rand((d,), 3), 0.1)
+
+
+# ------------------------------------------------------------------ many rows, begun anywhere
+ODD = [(300, 1), (299, 7), (1000, 33), (301, 127), (600, 250), (1531, 1111), (297, 2051), (310, 4099), (298, 8179)]
+
+
+@pytest.mark.parametrize("rows,d", ODD)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_odd_rows(rows, d, dtype):
+    x, r, w = rand((rows, d), 1, dtype), rand((rows, d), 2, dtype), rand((d,), 3)
+    check_forward(x, r, w, 0.1)
+    check_forward(x, None, w)
+    check_backward(rows, d, dtype, w)
+    check_backward(rows, d, dtype, rand((d,), 9, dtype), with_dh=False, p=0.3, pad=1)
+
+
+@pytest.mark.parametrize("pad,shift", [(1, 0), (8, 3), (2, 1), (5, 8)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_odd_rows_of_wider_tensors(pad, shift, dtype):
+    for rows, d in ((299, 45), (320, 1001), (300, 264)):
+        x, r = rand((rows, d), 1, dtype, pad, shift), rand((rows, d), 2, dtype, shift)
+        check_forward(x, r, rand((d,), 3, torch.bfloat16), 0.25)
+        check_forward(r, x, None)
+        check_backward(rows, d, dtype, rand((d,), 9), pad=pad)
+    check_forward(rand((1, 1001), 7, dtype).expand(400, 1001), rand((400, 1001), 8, dtype), None)
+
+
+@pytest.mark.parametrize("format", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_quantize_many_rows(format, dtype):
+    for rows, d, block in ((300, 1111, 0), (297, 77, 0), (400, 40, 32), (300, 1000, 64), (350, 4104, 128), (300, 96, 0)):
+        test_quantize(rows, d, block, format, dtype)
+
+
+@pytest.mark.parametrize("rows", [3, 400])
+@pytest.mark.parametrize("format", ["e4m3", "int8"])
+def test_quantize_values_whose_scale_is_tiny(rows, format):
+    # the inverse of such a scale is beyond fp32
+    w = torch.full((64,), 2.0 ** -126, device="cuda")
+    x = rand((rows, 64), 1)
+    q, s, _ = B().rms_norm_quantize(x, w, EPS, None, 0, format)
+    z = x.double() / (x.double().square().mean(-1, keepdim=True) + EPS).sqrt() * w.double()
+    most = 448.0 if format == "e4m3" else 127.0
+    tiny, s = 2.0 ** -149, s.double()
+    assert s.shape == (rows, 1)
+    # subnormal products and scales: half a step of 2^-149 each; the norm's own error as in test_quantize
+    rel = (0.5 * (8 + 64 / 256 + 5 + 32 + 3) + 8) * U
+    top = z.abs().amax(1, keepdim=True)
+    assert ((s - top / most).abs() <= rel * top / most + 2 * tiny).all()
+    value = q.double() * s
+    step = (z.abs() * 2.0 ** -4).maximum(s * 2.0 ** -10) if format == "e4m3" else 0.5 * s
+    assert ((value - z).abs() <= step * (1 + 2.0 ** -10) + 4 * rel * z.abs() + 2 * tiny).all()
