@@ -145,7 +145,7 @@ __device__ __forceinline__ void block_scales(const Rms& p, float* scales, int c0
 
 // QUANT 0: y in T; 1: e4m3; 2: int8
 template <typename T, bool VEC, int K, int QUANT>
-__global__ void __launch_bounds__(K == 0 ? 1024 : 512) k_rms_forward(const Rms p) {
+__global__ void __launch_bounds__(K == 0 ? 1024 : 512, K == 0 ? 1 : 2) k_rms_forward(const Rms p) {
   take_turn();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int group = warp / p.warps, w = warp - group * p.warps;
@@ -395,6 +395,50 @@ __global__ void __launch_bounds__(256) k_dropout(const Rms p) {
   }
 }
 
+// The same of rows that lie one behind the other: one row of eights, two to a thread at a time.
+template <typename T>
+__global__ void __launch_bounds__(256) k_dropout_flat(const Rms p) {
+  take_turn();
+  const T* const x = static_cast<const T*>(p.x);
+  const T* const residual = static_cast<const T*>(p.residual);
+  T* const y = static_cast<T*>(p.y);
+  const DropKey key = drop_key(p.drop);
+  const long long n = p.rows * p.d, eights = n / 8, step = (long long)gridDim.x * 256;
+  const auto one = [&](long long g, Eight<T>& a, const Eight<T>& b) {
+    float2 v[4], r[4];
+    a.get(v);
+    if (p.drop.threshold) drop_pairs(v, (unsigned long long)g, key, p.drop);
+    if (residual) {
+      b.get(r);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = add2(v[i], r[i]);
+    }
+    a.set(v);
+    a.store(y + g * 8);
+  };
+  for (long long g = (long long)blockIdx.x * 256 + threadIdx.x; g < eights; g += 2 * step) {
+    const long long h = g + step;
+    const bool both_ = h < eights;
+    Eight<T> a[2], b[2];
+    a[0].load(x + g * 8);
+    if (residual) b[0].load(residual + g * 8);
+    if (both_) {
+      a[1].load(x + h * 8);
+      if (residual) b[1].load(residual + h * 8);
+    }
+    one(g, a[0], b[0]);
+    if (both_) one(h, a[1], b[1]);
+  }
+  if (blockIdx.x == 0 && threadIdx.x < n - eights * 8) {
+    const long long e = eights * 8 + threadIdx.x;
+    float v = to_f32(x[e]);
+    if (p.drop.threshold)
+      v = (drop_keep8((unsigned long long)eights, key, p.drop.threshold) >> threadIdx.x) & 1u ? v * p.drop.scale : 0.f;
+    if (residual) v += to_f32(residual[e]);
+    y[e] = from_f32<T>(v);
+  }
+}
+
 inline cudaError_t rms_join(const Rms& p, const RmsLaunch& l) {
   return launch(k_rms_dweight_join, Shape{unsigned((p.d + 31) / 32), 1024, 0, 0}, l.st,
                 static_cast<const float*>(p.part), l.parts, p.d, p.dweight, p.param_dtype);
@@ -412,7 +456,8 @@ cudaError_t rms_launch_k(const Rms& p, const RmsLaunch& l) {
 template <typename T, bool VEC>
 cudaError_t rms_launch_vec(const Rms& p, const RmsLaunch& l) {
   if (l.op == kDropout)
-    return launch(k_dropout<T, VEC>, Shape{l.blocks, 256, 0, 0}, l.st, p);
+    return l.flat ? launch(k_dropout_flat<T>, Shape{l.blocks, 256, 0, 0}, l.st, p)
+                  : launch(k_dropout<T, VEC>, Shape{l.blocks, 256, 0, 0}, l.st, p);
   cudaError_t e = l.kept == 1   ? rms_launch_k<T, VEC, 1>(p, l)
                   : l.kept == 2 ? rms_launch_k<T, VEC, 2>(p, l)
                   : l.kept == 4 ? rms_launch_k<T, VEC, 4>(p, l)

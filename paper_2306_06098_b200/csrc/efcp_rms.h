@@ -49,6 +49,7 @@ struct RmsLaunch {
   int kept;         // chunks that a warp keeps in registers: 1, 2, 4, or 0 (rows walked twice)
   unsigned blocks;
   long long parts;  // rows of `part`
+  bool flat;        // dropout of rows that lie one behind the other
   bool ringed;      // see RmsRing
   RmsRing ring;
   size_t smem;

@@ -75,29 +75,33 @@ Rms common(const efcp_rms_norm* d) {
   return p;
 }
 
-// Chunks that a warp keeps, warps of a row, rows of a block.
-void share(const efcp_rms_norm* d, int sms, Rms* p, RmsLaunch* l) {
+// Chunks that a warp keeps, warps of a row, rows of a block.  (One chunk a warp: what it holds is little, and many
+// warps hide each other's waits.  Backward 1531 x 1111 fp32 13.0 us, 17.1 with four chunks a warp; forward 8.1 and 5.9.)
+void share(const efcp_rms_norm* d, Rms* p, RmsLaunch* l) {
   const int64_t chunks = ceil_div(d->d, kColumns);
   if (chunks > 64) {
     l->kept = 0;
     p->warps = int(std::min<int64_t>(32, chunks));
   } else {
-    const bool few = d->rows * ceil_div(chunks, 4) < 16 * sms;
-    l->kept = few ? (chunks <= 16 ? 1 : chunks <= 32 ? 2 : 4) : (chunks >= 3 ? 4 : int(chunks));
+    l->kept = chunks <= 16 ? 1 : chunks <= 32 ? 2 : 4;
     p->warps = int(ceil_div(chunks, l->kept));
   }
   p->groups = l->kept && p->warps < 8 ? 8 / p->warps : 1;
 }
 
 // Rows through shared memory, where a group of warps has two places at least: whether that is so, and how.  Units of
-// several rows for short ones, up to 2 KB where that is possible; a warp takes rows of up to 1024 alone.  With fewer
-// rows than places to work on them the plain kernels are as fast or faster: there is nothing to fetch ahead.
-bool plan_ring(const efcp_rms_norm* d, bool vec, int inputs, bool weight, int sms, Rms* p, RmsLaunch* l) {
+// several rows for short ones.  Two places: with more bytes on their way the memory gets slower (forward 16384 x 4096
+// bf16: 90 us with two, 104 with three or four).  The plain kernels take what is little (there is nothing to fetch ahead),
+// and fp32 rows that begin anywhere, forward: their loads of 4 bytes are as good as any (5000 x 1111: 22.5 us, 27.9 here;
+// bf16, 20000 x 1111: 61 and 53).
+bool plan_ring(const efcp_rms_norm* d, RmsOp op, bool vec, int inputs, bool weight, int sms, Rms* p, RmsLaunch* l) {
   if (d->rows < 2 * sms || d->d > 8192) return false;
+  const bool backward = op == kRmsBackward;
+  if (!vec && !backward && d->dtype == EFCP_F32) return false;
   // groups of eight that a row touches, wherever it begins
   const int64_t eights = vec ? d->d / 8 : (d->d + 14) / 8;
   const int64_t chunks = ceil_div(eights, 32), row_bytes = d->d * kTypeBytes[d->dtype];
-  if (chunks > 32) return false;
+  if (chunks > 32 || d->rows * chunks < (vec && backward ? 16 : 64) * sms) return false;
   RmsRing& q = l->ring;
   q = RmsRing{};
   q.inputs = inputs;
@@ -110,25 +114,37 @@ bool plan_ring(const efcp_rms_norm* d, bool vec, int inputs, bool weight, int sm
   q.pitch = int(ceil_div(row_bytes, 16) * 16 + 16);
   // (not vec: room for the pieces of 16 bytes that rows begin and end in: see efcp_rms_ring.cuh)
   q.unit_bytes = int(vec ? row_bytes * q.rows * q.reps : 48 + q.pitch * q.rows + 64);
-  p->warps = chunks <= 4 ? 1 : int(std::min<int64_t>(8, ceil_div(chunks, 2)));
-  p->groups = 8 / p->warps;
-  const int64_t kept = ceil_div(chunks, p->warps);
-  l->kept = kept <= 2 ? int(kept) : 4;
+  const auto share = [&](int64_t kept) {
+    p->warps = int(std::min<int64_t>(8, ceil_div(chunks, kept)));
+    p->groups = 8 / p->warps;
+    const int64_t k = ceil_div(chunks, p->warps);
+    l->kept = k <= 2 ? int(k) : 4;
+  };
+  const bool few = d->rows * chunks < 64 * sms, quantized = op == kRmsE4M3 || op == kRmsInt8;
+  share(few ? 1 : backward || d->dtype == EFCP_F32 ? 2 : 4);
+  if (l->kept == 4 && !quantized && 4 * p->groups * inputs * int64_t(q.unit_bytes) > 98304) share(2);
   q.weight_at = 512;  // behind the barriers
-  const int64_t weights = vec ? d->d : p->groups * p->warps * l->kept * kColumns;  // (not vec: as each lane reads it)
-  q.data_at = int(ceil_div(q.weight_at + (weight ? weights * 4 : 0), 128) * 128);
-  const int64_t stage = int64_t(p->groups) * inputs * q.unit_bytes;
-  q.stages = int(std::min<int64_t>(4, (kMostSmem - q.data_at) / stage));
-  if (q.stages < 2) return false;
+  // two places for each group, as many groups as fit; 16 warps on an SM
+  q.stages = 2;
+  int64_t stage, per_sm;
+  while (true) {
+    const int64_t weights = vec ? d->d : p->groups * p->warps * l->kept * kColumns;  // (not vec: as each lane reads it)
+    q.data_at = int(ceil_div(q.weight_at + (weight ? weights * 4 : 0), 128) * 128);
+    stage = int64_t(p->groups) * inputs * q.unit_bytes;
+    per_sm = std::max(2, 16 / (p->warps * p->groups));
+    if (q.data_at + 2 * stage <= 2 * kMostSmem / per_sm) break;
+    if (--p->groups < 1) return false;
+  }
   l->ringed = true;
-  // (above 48 KB by itself, so that a launch raises the kernel's limit: what is not dynamic counts too)
-  l->smem = size_t(std::max<int64_t>(q.data_at + q.stages * stage, 48 * 1024 + 16));
+  // (above 48 KB by itself where it is near, so that a launch raises the kernel's limit: what is not dynamic counts too)
+  l->smem = size_t(q.data_at + q.stages * stage);
+  if (l->smem > 40 * 1024) l->smem = std::max<size_t>(l->smem, 48 * 1024 + 16);
   const int64_t units = ceil_div(d->rows, q.rows * q.reps);
-  l->blocks = unsigned(std::min<int64_t>(2 * sms, ceil_div(units, p->groups)));
+  l->blocks = unsigned(std::min<int64_t>(per_sm * sms, ceil_div(units, p->groups)));
   // the rows of a group are a multiple of eight apart
   if (!vec)
     while (int64_t(l->blocks) * p->groups * q.rows % 8) ++l->blocks;
-  l->parts = int64_t(l->blocks) * p->groups * (vec ? 1 : q.rows);
+  l->parts = l->blocks;
   return true;
 }
 
@@ -180,8 +196,8 @@ int forward(const efcp_rms_norm* d, RmsOp op, const void* x, int64_t x_row, cons
   // (the 8-bit outputs take no dropout; columns that share a scale have to lie on multiples of eight)
   const bool ring = (op == kRmsForward || d->p == 0.) && (l.vec || !block) && reinterpret_cast<uintptr_t>(y) % 16 == 0 &&
                     (!summed || wide(d, h, 0));
-  if (!ring || !plan_ring(d, l.vec, residual ? 2 : 1, weight, sms, &p, &l)) {
-    share(d, sms, &p, &l);
+  if (!ring || !plan_ring(d, op, l.vec, residual ? 2 : 1, weight, sms, &p, &l)) {
+    share(d, &p, &l);
     const int64_t blocks = ceil_div(d->rows, p.groups);
     if (blocks > kMostBlocks) return EFCP_ETOOBIG;
     l.blocks = unsigned(blocks);
@@ -231,9 +247,9 @@ int64_t efcp_rms_norm_workspace_bytes(const efcp_rms_norm* desc) {
   int64_t parts = 0;
   for (int inputs : {2, 3})
     for (bool vec : {false, true})
-      if ((!vec || desc->d % 8 == 0) && plan_ring(desc, vec, inputs, false, sms, &p, &l))
+      if ((!vec || desc->d % 8 == 0) && plan_ring(desc, kRmsBackward, vec, inputs, false, sms, &p, &l))
         parts = std::max<int64_t>(parts, l.parts);
-  share(desc, sms, &p, &l);
+  share(desc, &p, &l);
   parts = std::max(parts, backward_blocks(desc, sms, p, l).parts);
   return std::max<int64_t>(16, parts * desc->d * 4);
 }
@@ -266,8 +282,8 @@ int efcp_rms_norm_backward(const efcp_rms_norm* desc, const void* dy, int64_t dy
   l.vec = desc->d % 8 == 0 && wide(desc, dy, dy_row) && wide(desc, h, h_row) && wide(desc, dh, dh_row) &&
           wide(desc, weight, 0) && wide(desc, dx, 0) && wide(desc, dresidual, 0);
   const bool ring = wide(desc, dx, 0) && wide(desc, dresidual, 0);
-  if (!ring || !plan_ring(desc, l.vec, dh ? 3 : 2, weight, sms, &p, &l)) {
-    share(desc, sms, &p, &l);
+  if (!ring || !plan_ring(desc, kRmsBackward, l.vec, dh ? 3 : 2, weight, sms, &p, &l)) {
+    share(desc, &p, &l);
     const Backward b = backward_blocks(desc, sms, p, l);
     l.blocks = b.blocks;
     l.parts = b.parts;
@@ -293,10 +309,13 @@ int efcp_dropout(const efcp_rms_norm* desc, const void* x, int64_t x_row, const 
   Rms p = common(desc);
   RmsLaunch l{};
   l.op = kDropout;
+  // one row behind the other: no matter where rows begin
+  l.flat = x_row == desc->d && (!residual || residual_row == desc->d) && wide(desc, x, 0) && wide(desc, residual, 0) &&
+           wide(desc, y, 0);
   l.vec = desc->d % 8 == 0 && wide(desc, x, x_row) && wide(desc, residual, residual_row) && wide(desc, y, 0);
   p.warps = p.groups = 1;
   const int64_t chunks = desc->rows * ceil_div(desc->d, kColumns);
-  l.blocks = unsigned(std::min<int64_t>(ceil_div(chunks, 8), 8ll * sms));
+  l.blocks = unsigned(std::min<int64_t>(ceil_div(l.flat ? ceil_div(desc->rows * desc->d, kColumns) : chunks, 8), 8ll * sms));
   p.x = x; p.x_row = x_row; p.residual = residual; p.residual_row = residual_row; p.y = y;
   return run(p, l, desc->dtype, static_cast<cudaStream_t>(stream));
 }

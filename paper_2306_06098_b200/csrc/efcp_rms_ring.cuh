@@ -52,9 +52,9 @@ struct Ring {
   RingInput in[INPUTS];
   int at = 0;  // place of the running unit, and the phase of its barrier
   uint32_t phase = 0;
+  uint32_t plain = 0;  // see prepare()
 
   __device__ __forceinline__ uint32_t place(int s) const { return data + uint32_t(s * q.inputs * q.unit_bytes); }
-  __device__ __forceinline__ int before() const { return (at ? at : q.stages) - 1; }
   __device__ __forceinline__ void next() {
     if (++at == q.stages) {
       at = 0;
@@ -93,6 +93,25 @@ struct Ring {
     return uint32_t(b - a);
   }
 
+  // ODD: what the copies of a unit bring in all, where one each does and a unit has others before and behind it; 0: not so.
+  __device__ __forceinline__ uint32_t covered(uint32_t off, int i) const {
+    return (off + uint32_t(in[i].row == q.row_bytes ? q.rows : 1) * q.row_bytes + 15) & ~15u;
+  }
+  __device__ __forceinline__ void prepare() {
+    if constexpr (ODD) {
+      plain = 0;
+#pragma unroll
+      for (int i = 0; i < INPUTS; ++i) {
+        if (i >= q.inputs) break;
+        if ((in[i].row != q.row_bytes && q.rows > 1) || in[i].row < 16) {
+          plain = 0;
+          return;
+        }
+        plain += covered(uint32_t(reinterpret_cast<uintptr_t>(in[i].data + first * q.rows * in[i].row) & 15), i);
+      }
+    }
+  }
+
   // (one thread) unit u into place s
   __device__ __forceinline__ void ask(long long u, int s) const {
     if (u >= units) return;
@@ -110,6 +129,15 @@ struct Ring {
         else
           for (int r = 0; r < rows; ++r)
             bulk_copy(to + i * q.unit_bytes + r * q.row_bytes, from + r * in[i].row, uint32_t(q.row_bytes), bar);
+      }
+    } else if (u > 0 && u < units - 1 && plain) {
+      tc::bar_expect(bar, plain);
+#pragma unroll
+      for (int i = 0; i < INPUTS; ++i) {
+        if (i >= q.inputs) break;
+        const char* lo = in[i].data + row * in[i].row;
+        const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(lo) & 15);
+        bulk_copy(to + i * q.unit_bytes + kRingFront, lo - off, covered(off, i), bar);
       }
     } else {
       const auto each = [&](bool issue) {
@@ -195,12 +223,20 @@ __device__ __forceinline__ RingCols ring_cols(const R& r, unsigned char* smem) {
     a.c -= int(((r.first * q.rows + a.sub) * p.d) & 7);
     // each lane's own, as it reads them
     float* mine = weight + (int(threadIdx.x >> 5) * K * 32 + r.lane) * 8;
-    if (p.weight)
+    const auto copy = [&](const auto* w) {
+#pragma unroll 1
       for (int k = 0; k < K; ++k)
+#pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int c = a.c + k * a.step + j;
-          mine[k * kChunk + j] = c >= 0 && c < p.d ? load_as_f32(p.weight, p.param_dtype, c) : 0.f;
+          mine[k * kChunk + j] = c >= 0 && c < p.d ? to_f32(w[c]) : 0.f;
         }
+    };
+    if (p.weight) {
+      if (p.param_dtype == EFCP_F32) copy(static_cast<const float*>(p.weight));
+      else if (p.param_dtype == EFCP_BF16) copy(static_cast<const __nv_bfloat16*>(p.weight));
+      else copy(static_cast<const __half*>(p.weight));
+    }
     a.weight = tc::smem_of(mine);
     a.weight_step = kChunk * 4;
   } else {
@@ -252,6 +288,13 @@ struct Eight {
       }
 #pragma unroll
       for (int i = 0; i < kWords; ++i) w[i] = a[i];
+    }
+  }
+  __device__ __forceinline__ void load(const T* from) {
+#pragma unroll
+    for (int i = 0; i < kWords; i += 4) {
+      const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(from) + i);
+      w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
     }
   }
   __device__ __forceinline__ void store(T* to) const {
@@ -378,6 +421,7 @@ __global__ void __launch_bounds__(256, 2) k_rms_forward_ring(const Rms p, const 
   auto r = ring_begin<T, kInputs, ODD>(p, q, smem, &gave_up);
   r.in[0] = {static_cast<const char*>(p.x), p.x_row * (long long)sizeof(T)};
   if constexpr (SUM) r.in[1] = {static_cast<const char*>(p.residual), p.residual_row * (long long)sizeof(T)};
+  r.prepare();
   take_turn();
   __syncthreads();
   const bool asks = r.warp == 0 && r.lane == 0;
@@ -520,6 +564,7 @@ __global__ void __launch_bounds__(256, 2) k_rms_backward_ring(const Rms p, const
   r.in[0] = {static_cast<const char*>(p.dy), p.dy_row * (long long)sizeof(T)};
   r.in[1] = {static_cast<const char*>(p.x), p.x_row * (long long)sizeof(T)};
   r.in[2] = {static_cast<const char*>(p.dh), p.dh_row * (long long)sizeof(T)};
+  r.prepare();
   take_turn();
   __syncthreads();
   const bool asks = r.warp == 0 && r.lane == 0;
@@ -558,7 +603,7 @@ __global__ void __launch_bounds__(256, 2) k_rms_backward_ring(const Rms p, const
       const long long at = row * p.d;
       const float rs = next;
       next = rep + 1 < q.reps ? rstd_of(u, rep + 1) : rstd_of(u + r.step, 0);
-      Eight<T> a8[K], b8[K];
+      Eight<T> a8[K], b8[K], e8[K];
       float2 sum = both(0.f);
 #pragma unroll
       for (int k = 0; k < K; ++k) {
@@ -566,6 +611,7 @@ __global__ void __launch_bounds__(256, 2) k_rms_backward_ring(const Rms p, const
         if (!on || c >= p.d) continue;
         a8[k].template load_shared<ODD>(dy + k * me.step * sizeof(T));
         b8[k].template load_shared<ODD>(h + k * me.step * sizeof(T));
+        if (p.dh) e8[k].template load_shared<ODD>(dh + k * me.step * sizeof(T));
         float2 a[4], b[4];
         if constexpr (ODD) {
           if (c < 0 || c + 8 > p.d) {
@@ -591,8 +637,8 @@ __global__ void __launch_bounds__(256, 2) k_rms_backward_ring(const Rms p, const
         sum = add2(sum, t);
       }
       const float m = -ring_join<false>(r, sum.x + sum.y, int(odd)) * p.inv_d * rs * rs;
-      // every warp of the group is done with the place before this one (its last input is read below)
-      if (asks && rep == 0 && n > 0) r.ask(u + (q.stages - 1) * r.step, r.before());
+      // every warp of the group is done with this place
+      if (asks && rep == q.reps - 1) r.ask(u + q.stages * r.step, r.at);
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const int c = me.c + k * me.step;
@@ -611,10 +657,8 @@ __global__ void __launch_bounds__(256, 2) k_rms_backward_ring(const Rms p, const
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = mul2(fma2(b[i], both(m), a[i]), both(rs));
         if (p.dh) {
-          Eight<T> e8;
-          e8.template load_shared<ODD>(dh + k * me.step * sizeof(T));
           float2 e[4];
-          e8.get(e);
+          e8[k].get(e);
 #pragma unroll
           for (int i = 0; i < 4; ++i) a[i] = add2(a[i], e[i]);
         }
@@ -632,36 +676,37 @@ __global__ void __launch_bounds__(256, 2) k_rms_backward_ring(const Rms p, const
     }
     r.next();
   }
+  if (asks) r.end(n + q.stages);
+  __syncthreads();
+  if (threadIdx.x == 0 && gave_up) atomicExch(p.status, EFCP_ETIMEOUT);
   if (p.part) {
-    if (!ODD && q.lanes < 32) {  // the rows of a unit, one warp
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        for (int o = q.lanes; o < 32; o *= 2) {
-          dw[0][i].x += __shfl_xor_sync(kAll, dw[0][i].x, o);
-          dw[0][i].y += __shfl_xor_sync(kAll, dw[0][i].y, o);
-        }
-    }
-    // (ODD: the rows of a unit begin differently, and their sums stay apart)
-    float* to = p.part + (ODD ? r.first * q.rows + me.sub : r.first) * p.d;
+    // The rows of a block's warps, each in its place of shared memory (the rings are done with), are added up in order.
+    float* sums = reinterpret_cast<float*>(smem + q.data_at);
+    float* const out = p.part + (long long)blockIdx.x * p.d;
+    const bool alone = p.groups * q.rows == 1;
+    float* mine = alone ? out : sums + (r.group * q.rows + me.sub) * p.d;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c = me.c + k * me.step;
-      if ((!ODD && me.sub) || c >= p.d) continue;
+      if (c >= p.d) continue;
+      Eight<float> a;
+      a.set(dw[k]);
       if constexpr (!ODD) {
-        Eight<float> out;
-        out.set(dw[k]);
-        out.store(to + c);
+        a.store(mine + c);
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (unsigned(c + 2 * i) < unsigned(p.d)) to[c + 2 * i] = dw[k][i].x;
-          if (unsigned(c + 2 * i + 1) < unsigned(p.d)) to[c + 2 * i + 1] = dw[k][i].y;
-        }
+        for (int j = 0; j < 8; ++j)
+          if (unsigned(c + j) < unsigned(p.d)) mine[c + j] = __uint_as_float(a.w[j]);
       }
     }
+    if (alone) return;
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.d; c += blockDim.x) {
+      float v = sums[c];
+      for (int i = 1; i < p.groups * q.rows; ++i) v += sums[i * p.d + c];
+      out[c] = v;
+    }
   }
-  if (asks) r.end(n - 1 + q.stages);
-  if (threadIdx.x == 0 && *(volatile int*)&gave_up) atomicExch(p.status, EFCP_ETIMEOUT);
 }
 
 template <typename T, int K, bool ODD>

@@ -141,3 +141,19 @@ def test_module():
         Dropout(1.5)
     s = new_rng(2 ** 64 - 1, "cuda")
     assert s.tolist() == [-1, 0] and take(s).tolist() == [-1, 0] and s.tolist() == [-1, 1]
+
+
+@pytest.mark.parametrize("rows,d", [(1, 1), (3, 5), (1, 8), (7, 31), (513, 1001), (9001, 301), (3, 100003)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_rows_one_behind_the_other(rows, d, dtype):
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, r = (torch.randn(rows, d, device="cuda", generator=g).to(dtype) for _ in range(2))
+    for p in (0.0, 0.25, 1.0):
+        for residual in (None, r):
+            got = B().dropout(x, p, (9, 10), residual)
+            # the same rows, further apart
+            wide = [t if t is None else torch.nn.functional.pad(t, (0, 3))[:, :d] for t in (x, residual)]
+            assert torch.equal(got, B().dropout(wide[0], p, (9, 10), wide[1]))
+            keep = kept((rows, d), p, 9, 10).cuda() if p else torch.ones_like(x, dtype=torch.bool)
+            want = torch.where(keep, x.float() * (65536 / (65536 - threshold(p)) if p < 1 else 0.0), 0.0)
+            assert torch.equal(got, (want if residual is None else want + r.float()).to(dtype))
