@@ -41,6 +41,7 @@ constexpr uint32_t kABytes = kBlockRows / 64 * kBoxBytes, kBBytes = kXentCols / 
 constexpr uint32_t kStageBytes = kABytes + kBBytes;
 constexpr uint32_t kOutBytes = 32 * 128;        // a warp's box of results
 constexpr size_t kXentSmem = kStages * kStageBytes + kOutWarps * kOutBytes + 1024;
+constexpr int kSquare = 8;                      // rows of tiles that pairs work on side by side
 constexpr int kPart = 8;                        // steps of an accumulator with SUMS
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -73,7 +74,8 @@ struct XentTile {
   int part;       // of the sum over the piece (hidden); tile of the columns (logits)
 };
 
-// The tiles of a launch.  Rows first, so that a tile of the other operand serves many pairs at the same time.
+// The tiles of a launch, eight rows of tiles by as many columns as there are pairs at a time for the products of G, which
+// does not stay in the cache (8192 x 8192 bf16: read twice instead of seven times); all rows first for the logits: H does.
 struct XentWork {
   int row_tiles, weight_rows, splits, steps, token_steps;
   long long hidden, weight, all;  // tiles of hidden; and of weight; and of logits
@@ -89,24 +91,30 @@ struct XentWork {
     weight = hidden + (p.weight ? (long long)weight_rows * p.d_tiles : 0);
     all = weight + (p.logits ? (long long)row_tiles * p.col_tiles : 0);
   }
+  static __device__ __forceinline__ int2 square(int t, int rows, int cols) {
+    const int g = t / (kSquare * cols), first = g * kSquare, here = min(kSquare, rows - first);
+    t -= first * cols;
+    const int c = t / here;
+    return make_int2(first + t - c * here, c);
+  }
   __device__ __forceinline__ XentTile tile(const XentGemm& p, long long t) const {
     XentTile r;
     if (t < hidden) {
-      const int c = int(t / row_tiles), n = c / splits;
+      const int2 mn = square(int(t), row_tiles, p.d_tiles * splits);
+      const int n = mn.y / splits;
       r.kind = kHidden;
-      r.m0 = int(t - (long long)c * row_tiles) * kXentRows;
+      r.m0 = mn.x * kXentRows;
       r.n0 = n * p.d_tile;
       r.cols = p.d_tile;
-      r.part = c - n * splits;
+      r.part = mn.y - n * splits;
       const int per = (steps + splits - 1) / splits;
       r.k0 = min(steps, r.part * per);
       r.depth = min(per, steps - r.k0);
     } else if (t < weight) {
-      t -= hidden;
-      const int c = int(t / weight_rows);
+      const int2 mn = square(int(t - hidden), weight_rows, p.d_tiles);
       r.kind = kWeight;
-      r.m0 = int(t - (long long)c * weight_rows) * kXentRows;
-      r.n0 = c * p.d_tile;
+      r.m0 = mn.x * kXentRows;
+      r.n0 = mn.y * p.d_tile;
       r.cols = p.d_tile;
       r.part = r.k0 = 0;
       r.depth = token_steps;
@@ -671,63 +679,79 @@ __global__ void __launch_bounds__(512) k_xent_prepare(const XentPrep p, bool bac
     }
 }
 
-// W as the copies of tiles want it, where it does not lie so.
+// W as the copies of tiles want it, where it does not lie so.  A warp takes 256 columns of a row, a lane pairs of them.
 template <typename T>
 __global__ void __launch_bounds__(256) k_xent_pack(const XentPrep p) {
   take_turn();
   using O = Operand<T>;
   constexpr int kPlanes = std::is_same_v<T, float> ? 3 : 1;
-  const int lane = threadIdx.x & 31;
-  const long long warps = (long long)gridDim.x * 8;
-  for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < p.vocab; i += warps) {
-    const T* from = static_cast<const T*>(p.weight) + i * p.weight_row;
-    O* to = static_cast<O*>(p.weight_packed) + i * p.packed_row;
-#pragma unroll 4
-    for (int c = lane; c < p.d; c += 32) {
-      O v[kPlanes];
-      split<O, kPlanes>(to_f32(from[c]), v);
+  const int lane = threadIdx.x & 31, chunks = (p.d + 255) / 256;
+  const long long warps = (long long)gridDim.x * 8, all = (long long)p.vocab * chunks;
+  for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < all; i += warps) {
+    const long long row = i / chunks;
+    const int c0 = int(i - row * chunks) * 256 + 2 * lane;
+    const T* from = static_cast<const T*>(p.weight) + row * p.weight_row;
+    O* to = static_cast<O*>(p.weight_packed) + row * p.packed_row;
+    float v[4][2];
 #pragma unroll
-      for (int k = 0; k < kPlanes; ++k) to[k * p.weight_plane + c] = v[k];
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) v[k][j] = c0 + 64 * k + j < p.d ? to_f32(from[c0 + 64 * k + j]) : 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int c = c0 + 64 * k;
+      if (c >= p.d) continue;  // (rows are a multiple of eight long: the second of a pair has its place)
+      O a[kPlanes], b[kPlanes];
+      split<O, kPlanes>(v[k][0], a);
+      split<O, kPlanes>(v[k][1], b);
+#pragma unroll
+      for (int j = 0; j < kPlanes; ++j) {
+        Pack<O, 2> two;
+        two.v[0] = a[j];
+        two.v[1] = b[j];
+        *reinterpret_cast<Pack<O, 2>*>(to + j * p.weight_plane + c) = two;
+      }
     }
   }
 }
 
-// The gradient of H from its parts; zeros for tokens without a target.  A warp takes a row.
+// The gradient of H from its parts; zeros for tokens without a target.  A warp takes 128 columns of a row.
 template <typename T>
 __global__ void __launch_bounds__(256) k_xent_finish(const XentPrep p) {
   take_turn();
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, chunks = (p.d + 127) / 128;
   const int row_tiles = (*p.count + kXentRows - 1) / kXentRows;
   const int splits = xent_splits(row_tiles, p.d_tiles, p.piece, p.pairs);
-  const long long part = (long long)row_tiles * kXentRows * p.sum_row;
+  const long long part = (long long)row_tiles * kXentRows * p.sum_row, all = p.tokens * chunks;
   const float back = p.scale[1];
-  const bool vec = reinterpret_cast<uintptr_t>(p.dhidden) % 16 == 0 && p.d % 8 == 0;
-  for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < p.tokens; i += (long long)gridDim.x * 8) {
-    const int place = p.place[i];
-    T* to = static_cast<T*>(p.dhidden) + i * p.d;
-    const float* from = p.sum + place * p.sum_row;  // (not read where there is none)
+  const bool vec = reinterpret_cast<uintptr_t>(p.dhidden) % 16 == 0 && p.d % 4 == 0;
+  for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < all; i += (long long)gridDim.x * 8) {
+    const long long token = i / chunks;
+    const int c = int(i - token * chunks) * 128 + lane * 4;
+    if (c >= p.d) continue;
+    const int place = p.place[token];
+    T* to = static_cast<T*>(p.dhidden) + token * p.d;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (place >= 0) {
+      const float* from = p.sum + place * p.sum_row + c;  // (rows are a multiple of 32 long)
+      float4 o[kXentSplits];
+#pragma unroll
+      for (int k = 0; k < kXentSplits; ++k)
+        o[k] = k < splits ? *reinterpret_cast<const float4*>(from + k * part) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kXentSplits; ++k) {
+        v.x += o[k].x; v.y += o[k].y; v.z += o[k].z; v.w += o[k].w;
+      }
+    }
+    Pack<T, 4> a;
+    a.v[0] = from_f32<T>(v.x * back); a.v[1] = from_f32<T>(v.y * back);
+    a.v[2] = from_f32<T>(v.z * back); a.v[3] = from_f32<T>(v.w * back);
     if (vec) {
-      for (int c = lane * 4; c < p.d; c += 128) {
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (place >= 0) {
-          for (int k = 0; k < splits; ++k) {
-            const float4 o = *reinterpret_cast<const float4*>(from + k * part + c);
-            v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
-          }
-        }
-        Pack<T, 4> a;
-        a.v[0] = from_f32<T>(v.x * back); a.v[1] = from_f32<T>(v.y * back);
-        a.v[2] = from_f32<T>(v.z * back); a.v[3] = from_f32<T>(v.w * back);
-        if constexpr (sizeof(a) == 16) *reinterpret_cast<uint4*>(to + c) = *reinterpret_cast<const uint4*>(&a);
-        else *reinterpret_cast<uint2*>(to + c) = *reinterpret_cast<const uint2*>(&a);
-      }
+      *reinterpret_cast<Pack<T, 4>*>(to + c) = a;
     } else {
-      for (int c = lane; c < p.d; c += 32) {
-        float v = 0.f;
-        if (place >= 0)
-          for (int k = 0; k < splits; ++k) v += from[k * part + c];
-        to[c] = from_f32<T>(v * back);
-      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (c + j < p.d) to[c + j] = a.v[j];
     }
   }
 }
@@ -762,13 +786,14 @@ cudaError_t xent_prepare(const XentPrep& p, bool backward, int sms, cudaStream_t
   const unsigned blocks = unsigned(std::max<long long>(1, (p.tokens + per - 1) / per));
   cudaError_t e = launch(k_xent_prepare<T>, Shape{blocks, 512, 0, 0}, st, p, backward, int(per));
   if (e != cudaSuccess || !p.weight) return e;
-  return launch(k_xent_pack<T>, Shape{unsigned(std::min(p.vocab / 8 + 1, 8 * sms)), 256, 0, 0}, st, p);
+  const long long warps = (long long)p.vocab * ((p.d + 255) / 256);
+  return launch(k_xent_pack<T>, Shape{unsigned(std::min<long long>(warps / 8 + 1, 8ll * sms)), 256, 0, 0}, st, p);
 }
 
 template <typename T>
 cudaError_t xent_finish(const XentPrep& p, int sms, cudaStream_t st) {
-  const long long rows = p.tokens / 8 + 1;
-  return launch(k_xent_finish<T>, Shape{unsigned(std::min<long long>(rows, 8ll * sms)), 256, 0, 0}, st, p);
+  const long long warps = p.tokens * ((p.d + 127) / 128);
+  return launch(k_xent_finish<T>, Shape{unsigned(std::min<long long>(warps / 8 + 1, 8ll * sms)), 256, 0, 0}, st, p);
 }
 
 }  // namespace
