@@ -159,6 +159,56 @@ Plan make_plan(const efcp_cross_entropy& d, const void* weight, bool backward, i
   return p;
 }
 
+// Up to eight tokens have kernels of their own, which hold the hidden states in shared memory (two blocks on an SM), and
+// backward their gradient in registers: loss of four tokens, 768 x 30522 bf16, see efcp_xent_few.cuh.
+bool few(const efcp_cross_entropy& d, bool backward) {
+  if (d.tokens < 1 || d.tokens > kFewTokens) return false;
+  const int64_t n = d.tokens <= 4 ? 4 : 8;
+  return backward ? d.d <= 512 * (32 / n) : n * round_up(d.d, 256) * 4 <= 110 * 1024;
+}
+
+struct FewPlan {
+  int64_t logit, bytes;
+  int blocks;
+};
+FewPlan few_plan(const efcp_cross_entropy& d, bool backward, int sms) {
+  FewPlan p{};
+  const int64_t n = d.tokens <= 4 ? 4 : 8;
+  p.blocks = int(std::min<int64_t>(2 * sms, ceil_div(d.vocab, 32)));
+  p.logit = 256 * ceil_div(8 * n * p.blocks, 256);
+  p.bytes = backward ? 4 * n * p.blocks * round_up(d.d, 256) : p.logit + 256;
+  return p;
+}
+
+XentFew few_call(const efcp_cross_entropy& d, const FewPlan& plan, const void* hidden, const void* weight,
+                 const int64_t* targets) {
+  XentFew p{};
+  p.targets = reinterpret_cast<const long long*>(targets);
+  p.ignore = d.ignore_index;
+  p.tokens = int(d.tokens);
+  p.vocab = int(d.vocab);
+  p.d = int(d.d);
+  p.padded = int(round_up(d.d, 256));
+  p.blocks = plan.blocks;
+  p.reduction = d.reduction;
+  p.hidden = hidden;
+  p.hidden_row = d.hidden_row;
+  p.weight = weight;
+  p.weight_row = d.weight_row;
+  return p;
+}
+
+int few_run(const efcp_cross_entropy& d, const XentFew& p, bool backward, cudaStream_t st) {
+  const bool vec = d.d % 8 == 0 && reinterpret_cast<uintptr_t>(p.weight) % 16 == 0 &&
+                   d.weight_row * kTypeBytes[d.dtype] % 16 == 0 && reinterpret_cast<uintptr_t>(p.dweight) % 16 == 0;
+  const cudaError_t e = d.dtype == EFCP_F32    ? few_launch_f32(p, vec, backward, st)
+                        : d.dtype == EFCP_BF16 ? few_launch_bf16(p, vec, backward, st)
+                                               : few_launch_f16(p, vec, backward, st);
+  if (e == cudaSuccess) return EFCP_OK;
+  (void)cudaGetLastError();
+  return EFCP_ECUDA;
+}
+
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
@@ -303,8 +353,10 @@ extern "C" {
 int64_t efcp_cross_entropy_workspace_bytes(const efcp_cross_entropy* desc, const void* weight,
                                            int32_t backward) {
   if (!valid(desc)) return -1;
-  const int sms = device_sms();
-  return make_plan(*desc, weight, backward != 0, sms < 1 ? 148 : sms).bytes;  // (no device: a B200's)
+  int sms = device_sms();
+  if (sms < 1) sms = 148;  // (no device: a B200's)
+  return few(*desc, backward != 0) ? few_plan(*desc, backward != 0, sms).bytes
+                                   : make_plan(*desc, weight, backward != 0, sms).bytes;
 }
 
 int efcp_cross_entropy_forward(const efcp_cross_entropy* desc, const void* hidden, const void* weight,
@@ -316,6 +368,17 @@ int efcp_cross_entropy_forward(const efcp_cross_entropy* desc, const void* hidde
   if (desc->tokens && (misaligned(hidden, size) || misaligned(targets, 8))) return EFCP_EINVAL;
   if (misaligned(weight, size) || misaligned(workspace, 256)) return EFCP_EINVAL;
   const int sms = device_sms();
+  if (few(*desc, false)) {
+    const FewPlan plan = few_plan(*desc, false, sms < 1 ? 148 : sms);
+    if (workspace_bytes < plan.bytes) return EFCP_ENOMEM;
+    if (sms < 1) return EFCP_ECUDA;
+    XentFew p = few_call(*desc, plan, hidden, weight, targets);
+    p.part = static_cast<float2*>(workspace);
+    p.target_logit = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.logit);
+    p.losses = losses;
+    p.lse_out = lse;
+    return few_run(*desc, p, false, static_cast<cudaStream_t>(stream));
+  }
   Call c{*desc, make_plan(*desc, weight, false, sms < 1 ? 148 : sms), sms};
   if (workspace_bytes < c.plan.bytes) return EFCP_ENOMEM;
   if (desc->tokens == 0 && !desc->reduction) return EFCP_OK;
@@ -344,6 +407,20 @@ int efcp_cross_entropy_backward(const efcp_cross_entropy* desc, const float* gra
   if (misaligned(weight, size) || (dweight && misaligned(dweight, size)) || misaligned(workspace, 256))
     return EFCP_EINVAL;
   const int sms = device_sms();
+  if (few(*desc, true)) {
+    const FewPlan plan = few_plan(*desc, true, sms < 1 ? 148 : sms);
+    if (workspace_bytes < plan.bytes) return EFCP_ENOMEM;
+    if (!dhidden && !dweight) return EFCP_OK;
+    if (sms < 1) return EFCP_ECUDA;
+    XentFew p = few_call(*desc, plan, hidden, weight, targets);
+    p.grad = grad;
+    p.grad_step = grad_step;
+    p.lse_in = lse;
+    p.sums = dhidden ? static_cast<float*>(workspace) : nullptr;
+    p.dhidden = dhidden;
+    p.dweight = dweight;
+    return few_run(*desc, p, true, static_cast<cudaStream_t>(stream));
+  }
   Call c{*desc, make_plan(*desc, weight, true, sms < 1 ? 148 : sms), sms};
   if (workspace_bytes < c.plan.bytes) return EFCP_ENOMEM;
   c.st = static_cast<cudaStream_t>(stream);

@@ -69,6 +69,31 @@ struct XentPrep {
   void* dhidden;
 };
 
+// The calls for up to eight tokens (efcp_xent_few.cuh).
+constexpr int kFewTokens = 8;
+struct XentFew {
+  const long long* targets;
+  long long ignore;
+  int tokens, vocab, d;
+  int padded;  // d up to a multiple of 256
+  int blocks;
+  int reduction;
+  const void* hidden;
+  long long hidden_row;
+  const void* weight;
+  long long weight_row;
+  // forward
+  float2* part;  // a token's statistics, one a block
+  float* target_logit;
+  float *losses, *lse_out;
+  // backward
+  const float* grad;
+  long long grad_step;
+  const float* lse_in;
+  float* sums;  // of the gradient of H: for each token a row of `padded` for each block
+  void *dhidden, *dweight;
+};
+
 // How many parts the sum over a piece is cut into for the gradient of H: as many as give every pair of blocks two
 // tiles, none shorter than 16 steps.
 __host__ __device__ inline int xent_splits(int row_tiles, int d_tiles, int piece, int pairs) {
@@ -87,6 +112,9 @@ cudaError_t xent_prepare_f16(const XentPrep& p, bool backward, int sms, cudaStre
 cudaError_t xent_finish_f32(const XentPrep& p, int sms, cudaStream_t st);
 cudaError_t xent_finish_bf16(const XentPrep& p, int sms, cudaStream_t st);
 cudaError_t xent_finish_f16(const XentPrep& p, int sms, cudaStream_t st);
+cudaError_t few_launch_f32(const XentFew& p, bool vec, bool backward, cudaStream_t st);
+cudaError_t few_launch_bf16(const XentFew& p, bool vec, bool backward, cudaStream_t st);
+cudaError_t few_launch_f16(const XentFew& p, bool vec, bool backward, cudaStream_t st);
 cudaError_t xent_join(const XentPrep& p, int sms, cudaStream_t st);
 
 }  // namespace efcp

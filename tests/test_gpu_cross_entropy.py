@@ -326,3 +326,40 @@ def test_captured_and_on_other_streams():
     streams[0].synchronize()
     assert torch.equal(lone[0], want[0])
     B().operators_status()
+
+
+# ------------------------------------------------------------------ a few tokens
+@pytest.mark.parametrize("n", [1, 3, 4, 5, 8, 9])
+@pytest.mark.parametrize("d,v", [(24, 1), (100, 31), (129, 33), (768, 2000), (1300, 513), (2048, 700), (2056, 100), (4096, 300),
+                                 (4100, 65), (8000, 40)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_few_tokens(n, d, v, dtype):
+    hidden, weight, targets = inputs(n, d, v, dtype, 4)
+    check_forward(hidden, weight, targets)
+    check_backward(hidden, weight, targets, grads(n))
+    if n > 1:  # rows of wider tensors, and a token that does not count, whatever it holds
+        targets[1] = -100
+        hidden, weight = (torch.nn.functional.pad(x, (1, 2))[:, 1:-2] for x in (hidden, weight))
+        hidden[1] = float("nan")
+        losses, _ = check_forward(hidden, weight, targets)
+        assert not losses.isnan().any()
+        dh, dw = B().cross_entropy_backward(torch.tensor(2.0, device="cuda"), hidden, weight, targets,
+                                            B().cross_entropy_forward(hidden, weight, targets)[1])
+        assert not dh.isnan().any() and not dw.isnan().any() and (dh[1] == 0).all()
+
+
+@pytest.mark.parametrize("n", [2, 7])
+def test_few_tokens_that_have_no_target_or_a_wrong_one(n):
+    hidden, weight, targets = inputs(n, 72, 300, torch.bfloat16, 5)
+    one = torch.ones((), device="cuda")
+    targets[0] = 300
+    losses, lse = B().cross_entropy_forward(hidden, weight, targets, -100, "none")
+    assert losses[0].isnan() and not losses[1:].isnan().any() and not lse.isnan().any()
+    dh, dw = B().cross_entropy_backward(one, hidden, weight, targets, lse, -100, "sum")
+    assert dh[0].isnan().all() and dw.isnan().all() and not dh[1:].isnan().any()
+    targets[:] = 0  # a class that does not count
+    for how in ("none", "sum", "mean"):
+        got, lse = B().cross_entropy_forward(hidden, weight, targets, 0, how)
+        assert got.isnan() if how == "mean" else (got == 0).all()
+        dh, dw = B().cross_entropy_backward(torch.ones_like(got), hidden, weight, targets, lse, 0, how)
+        assert (dh == 0).all() and (lse == 0).all() and (dw == 0).all()

@@ -176,7 +176,9 @@ def test_cross_entropy_calls():
         for more in (dict(h=None), dict(h=FAKE + 1), dict(w=None), dict(w=FAKE + 1), dict(t=None), dict(t=FAKE + 4),
                      dict(lse=None), dict(lse=FAKE + 2), dict(ws=None), dict(ws=FAKE + 128)):
             assert call(loss_desc(), **more) == B.EINVAL
-        assert call(loss_desc(), size=1000) == B.ENOMEM
+        for tokens in (5, 500):
+            need = B._lib.efcp_cross_entropy_workspace_bytes(loss_desc(tokens=tokens), FAKE, call is loss_backward)
+            assert call(loss_desc(tokens=tokens), size=need - 1) == B.ENOMEM
     assert loss_forward(loss_desc(), out=None) == loss_forward(loss_desc(), out=FAKE + 2) == B.EINVAL
     assert loss_forward(loss_desc(tokens=0), h=None, t=None, out=None, lse=None) == B.OK
     assert loss_forward(loss_desc(tokens=0, reduction=1), out=None) == B.EINVAL
@@ -193,7 +195,8 @@ def test_the_cross_entropy_workspace():
         assert 0 < size(back, tokens=16384, vocab=64000) < logits / 4  # the logits are not kept
         weight = 64000 * 64 * 2
         for more in (dict(w=FAKE + 2), dict(weight_row=67)):  # a copy of the weight that can be read by tiles
-            assert size(back, tokens=1, vocab=64000, **more) - size(back, tokens=1, vocab=64000) >= weight
+            assert size(back, tokens=9, vocab=64000, **more) - size(back, tokens=9, vocab=64000) >= weight
+            assert size(back, tokens=8, vocab=64000, **more) == size(back, tokens=8, vocab=64000) < weight  # read where it lies
     # two pieces of 256 columns at least, rows of both kinds
     assert size(1, tokens=1 << 20, vocab=64000) - (1 << 20) * 64 * 6 < 2 * 2 * (1 << 20) * 256 + (64 << 20)
 
