@@ -159,24 +159,24 @@ Plan make_plan(const efcp_cross_entropy& d, const void* weight, bool backward, i
   return p;
 }
 
-// Up to eight tokens have kernels of their own, which hold the hidden states in shared memory (two blocks on an SM), and
-// backward their gradient in registers: loss of four tokens, 768 x 30522 bf16, see efcp_xent_few.cuh.
-bool few(const efcp_cross_entropy& d, bool backward) {
-  if (d.tokens < 1 || d.tokens > kFewTokens) return false;
-  const int64_t n = d.tokens <= 4 ? 4 : 8;
-  return backward ? d.d <= 512 * (32 / n) : n * round_up(d.d, 256) * 4 <= 110 * 1024;
+// Up to eight tokens have kernels of their own, which hold the hidden states in shared memory (two blocks on an SM): see
+// efcp_xent_few.cuh.
+bool few(const efcp_cross_entropy& d) {
+  return d.tokens >= 1 && d.tokens <= kFewTokens && (d.tokens <= 4 ? 4 : 8) * round_up(d.d, 256) * 4 <= 110 * 1024;
 }
 
 struct FewPlan {
-  int64_t logit, bytes;
-  int blocks;
+  int64_t logit, sums, bytes;
+  int blocks, ranges;
 };
 FewPlan few_plan(const efcp_cross_entropy& d, bool backward, int sms) {
   FewPlan p{};
   const int64_t n = d.tokens <= 4 ? 4 : 8;
   p.blocks = int(std::min<int64_t>(2 * sms, ceil_div(d.vocab, 32)));
-  p.logit = 256 * ceil_div(8 * n * p.blocks, 256);
-  p.bytes = backward ? 4 * n * p.blocks * round_up(d.d, 256) : p.logit + 256;
+  p.ranges = int(std::max<int64_t>(1, std::min(2 * sms / ceil_div(d.d, 1024 / n), ceil_div(d.vocab, 32))));
+  p.logit = round_up(8 * n * p.blocks, 256);
+  p.sums = round_up(4 * n * d.vocab, 256);
+  p.bytes = backward ? p.sums + 4 * n * p.ranges * round_up(d.d, 256) : p.logit + 256;
   return p;
 }
 
@@ -190,6 +190,7 @@ XentFew few_call(const efcp_cross_entropy& d, const FewPlan& plan, const void* h
   p.d = int(d.d);
   p.padded = int(round_up(d.d, 256));
   p.blocks = plan.blocks;
+  p.ranges = plan.ranges;
   p.reduction = d.reduction;
   p.hidden = hidden;
   p.hidden_row = d.hidden_row;
@@ -355,7 +356,7 @@ int64_t efcp_cross_entropy_workspace_bytes(const efcp_cross_entropy* desc, const
   if (!valid(desc)) return -1;
   int sms = device_sms();
   if (sms < 1) sms = 148;  // (no device: a B200's)
-  return few(*desc, backward != 0) ? few_plan(*desc, backward != 0, sms).bytes
+  return few(*desc) ? few_plan(*desc, backward != 0, sms).bytes
                                    : make_plan(*desc, weight, backward != 0, sms).bytes;
 }
 
@@ -368,7 +369,7 @@ int efcp_cross_entropy_forward(const efcp_cross_entropy* desc, const void* hidde
   if (desc->tokens && (misaligned(hidden, size) || misaligned(targets, 8))) return EFCP_EINVAL;
   if (misaligned(weight, size) || misaligned(workspace, 256)) return EFCP_EINVAL;
   const int sms = device_sms();
-  if (few(*desc, false)) {
+  if (few(*desc)) {
     const FewPlan plan = few_plan(*desc, false, sms < 1 ? 148 : sms);
     if (workspace_bytes < plan.bytes) return EFCP_ENOMEM;
     if (sms < 1) return EFCP_ECUDA;
@@ -407,7 +408,7 @@ int efcp_cross_entropy_backward(const efcp_cross_entropy* desc, const float* gra
   if (misaligned(weight, size) || (dweight && misaligned(dweight, size)) || misaligned(workspace, 256))
     return EFCP_EINVAL;
   const int sms = device_sms();
-  if (few(*desc, true)) {
+  if (few(*desc)) {
     const FewPlan plan = few_plan(*desc, true, sms < 1 ? 148 : sms);
     if (workspace_bytes < plan.bytes) return EFCP_ENOMEM;
     if (!dhidden && !dweight) return EFCP_OK;
@@ -416,7 +417,8 @@ int efcp_cross_entropy_backward(const efcp_cross_entropy* desc, const float* gra
     p.grad = grad;
     p.grad_step = grad_step;
     p.lse_in = lse;
-    p.sums = dhidden ? static_cast<float*>(workspace) : nullptr;
+    p.g = static_cast<float*>(workspace);
+    p.sums = dhidden ? reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.sums) : nullptr;
     p.dhidden = dhidden;
     p.dweight = dweight;
     return few_run(*desc, p, true, static_cast<cudaStream_t>(stream));

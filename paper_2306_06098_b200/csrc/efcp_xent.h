@@ -90,7 +90,9 @@ struct XentFew {
   const float* grad;
   long long grad_step;
   const float* lse_in;
-  float* sums;  // of the gradient of H: for each token a row of `padded` for each block
+  float* g;     // the logits' gradient, 4 or 8 tokens of a row of the weight side by side
+  float* sums;  // of the gradient of H: for each token `ranges` rows of `padded`  (null: not wanted)
+  int ranges;   // blocks that share a set of columns
   void *dhidden, *dweight;
 };
 

@@ -3,9 +3,9 @@
 //
 // The hidden states lie in shared memory in fp32.  A warp takes four rows of the weight, multiplies them with all
 // tokens in fp32 (two products to an instruction), and adds up its lanes' parts so that each lane ends up with one logit.
-// Backward a block does that for 32 rows, turns the logits into their gradient in shared memory, and then its warps, on
-// columns of their own, read the rows once more out of the cache: they hold the gradient of the hidden states in registers
-// and write the gradient of the weight.  The blocks' sums are added up in order.
+// Backward the logits' gradient is written, a few values a row; then warps on columns of their own walk down the rows,
+// out of the cache where they fit there: they hold the hidden states and their gradient in registers, and write the gradient
+// of the weight.  The blocks' sums are added up in order.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -36,7 +36,7 @@ __device__ __forceinline__ void few_hidden(const XentFew& p, float* h) {
   }
 }
 
-// 8 (or fewer) values of a token, at the columns that load8 gives a lane
+// Eight values of a token, at the columns that load8 gives a lane.
 template <bool VEC, int W>
 __device__ __forceinline__ void few_values(const float* h, int lane, float2 (&v)[W / 2]) {
   if constexpr (VEC) {
@@ -52,9 +52,36 @@ __device__ __forceinline__ void few_values(const float* h, int lane, float2 (&v)
   }
 }
 
+// 256 columns of four rows of the weight (zeros outside), on their way.
+template <typename T, bool VEC>
+struct FewRows {
+  Pack<T, 8> w[kFewRows];
+  __device__ __forceinline__ void fetch(const XentFew& p, long long row0, int c0, int lane) {
+#pragma unroll
+    for (int r = 0; r < kFewRows; ++r) {
+      const T* row = static_cast<const T*>(p.weight) + (row0 + r) * p.weight_row;
+      const int d = row0 + r < p.vocab ? p.d : 0;
+      if constexpr (VEC) {
+        const int c = c0 + lane * 8;
+#pragma unroll
+        for (int i = 0; i < int(sizeof(w[r]) / 16); ++i)
+          reinterpret_cast<uint4*>(&w[r])[i] = c < d ? reinterpret_cast<const uint4*>(row + c)[i] : make_uint4(0, 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int c = c0 + j * 32 + lane;
+          w[r].v[j] = c < d ? row[c] : from_f32<T>(0.f);
+        }
+      }
+    }
+  }
+};
+
 // The logits of rows row0 .. row0 + 3: a lane's is that of row lane / N and token lane % N.  (N == 4: of the lanes below 16.)
+// `ahead` holds the rows' first columns; then those of the rows from `next` on.
 template <typename T, bool VEC, int N>
-__device__ __forceinline__ float few_logits(const XentFew& p, const float* h, long long row0, int lane) {
+__device__ __forceinline__ float few_logits(const XentFew& p, const float* h, long long row0, long long next, int lane,
+                                            FewRows<T, VEC>& ahead) {
   constexpr int kAll32 = kFewRows * N;
   float2 acc[kFewRows][N];
 #pragma unroll
@@ -65,8 +92,10 @@ __device__ __forceinline__ float few_logits(const XentFew& p, const float* h, lo
     float w[kFewRows][8];
 #pragma unroll
     for (int r = 0; r < kFewRows; ++r)
-      load8<T, VEC>(static_cast<const T*>(p.weight) + (row0 + r) * p.weight_row, c0, lane, row0 + r < p.vocab ? p.d : 0,
-                    w[r]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[r][j] = to_f32(ahead.w[r].v[j]);
+    const bool last = c0 + kChunk >= p.d;
+    ahead.fetch(p, last ? next : row0, last ? 0 : c0 + kChunk, lane);
 #pragma unroll
     for (int t = 0; t < N; ++t) {
       float2 v[4];
@@ -101,35 +130,56 @@ __device__ __forceinline__ void few_join(float& top, float& sum, float top2, flo
   top = m;
 }
 
-template <typename T, bool VEC, int N>
-__global__ void __launch_bounds__(256, 2) k_few_forward(const XentFew p) {
+// Forward: the statistics of the block's rows for each token, and the targets' logits.  Backward: the logits' gradient.
+template <typename T, bool VEC, int N, bool BACKWARD>
+__global__ void __launch_bounds__(256, 2) k_few_logits(const XentFew p) {
   extern __shared__ __align__(16) float h[];
   __shared__ float2 each[8][N];
   take_turn();
-  few_hidden<T, N>(p, h);
-  __syncthreads();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = lane % N, r = lane / N;
   const bool mine = r < kFewRows;
+  const long long first = ((long long)blockIdx.x * 8 + warp) * kFewRows, step = (long long)gridDim.x * kFewTile;
+  FewRows<T, VEC> ahead;
+  ahead.fetch(p, first, 0, lane);
+  few_hidden<T, N>(p, h);
   const long long target = t < p.tokens && mine ? p.targets[t] : -1;  // (one that is ignored meets no reader)
+  float coef = 0.f, lse = 0.f;
+  if constexpr (BACKWARD) {
+    int count = 0;
+    for (int i = 0; i < p.tokens; ++i) count += p.targets[i] != p.ignore;
+    if (t < p.tokens && p.targets[t] != p.ignore) {
+      coef = p.reduction == 0 ? p.grad[t * p.grad_step] : p.reduction == 1 ? p.grad[0] / float(count) : p.grad[0];
+      if (p.targets[t] < 0 || p.targets[t] >= p.vocab) coef = __int_as_float(0x7FC00000);
+      lse = p.lse_in[t];
+    } else {
+      lse = INFINITY;  // (no token: whatever a row holds, exp gives 0)
+    }
+  }
+  __syncthreads();
   float top = -INFINITY, sum = 0.f;
-  for (long long row0 = ((long long)blockIdx.x * 8 + warp) * kFewRows; row0 < p.vocab;
-       row0 += (long long)gridDim.x * kFewTile) {
-    const float v = few_logits<T, VEC, N>(p, h, row0, lane);
+  for (long long row0 = first; row0 < p.vocab; row0 += step) {
+    const float v = few_logits<T, VEC, N>(p, h, row0, row0 + step, lane, ahead);
     const long long row = row0 + r;
     if (!mine || row >= p.vocab) continue;
-    if (row == target) p.target_logit[t] = v;
-    few_join(top, sum, v, 1.f);
+    if constexpr (BACKWARD) {
+      p.g[row * N + t] = lse == INFINITY && coef == 0.f ? 0.f : coef * (few_exp(v - lse) - (row == target ? 1.f : 0.f));
+    } else {
+      if (row == target) p.target_logit[t] = v;
+      few_join(top, sum, v, 1.f);
+    }
   }
+  if constexpr (!BACKWARD) {
 #pragma unroll
-  for (int o = N; o < 32; o *= 2)
-    few_join(top, sum, __shfl_xor_sync(kAll, top, o), __shfl_xor_sync(kAll, sum, o));
-  if (lane < N) each[warp][lane] = make_float2(top, sum);
-  __syncthreads();
-  if (threadIdx.x >= N) return;
-  top = each[0][t].x;
-  sum = each[0][t].y;
-  for (int w = 1; w < 8; ++w) few_join(top, sum, each[w][t].x, each[w][t].y);
-  p.part[t * gridDim.x + blockIdx.x] = make_float2(top, sum);
+    for (int o = N; o < 32; o *= 2)
+      few_join(top, sum, __shfl_xor_sync(kAll, top, o), __shfl_xor_sync(kAll, sum, o));
+    if (lane < N) each[warp][lane] = make_float2(top, sum);
+    __syncthreads();
+    if (threadIdx.x >= N) return;
+    top = each[0][t].x;
+    sum = each[0][t].y;
+    for (int w = 1; w < 8; ++w) few_join(top, sum, each[w][t].x, each[w][t].y);
+    p.part[t * gridDim.x + blockIdx.x] = make_float2(top, sum);
+  }
 }
 
 // The losses, a warp for each token, and their sum or mean.  The last steps are in 64 bits: lse is several times as large as
@@ -217,118 +267,75 @@ __device__ __forceinline__ void few_store(T* row, int c0, int lane, int d, const
   }
 }
 
-// K: sets of columns of a warp
-template <typename T, bool VEC, int N, int K>
-__global__ void __launch_bounds__(256, 2) k_few_backward(const XentFew p) {
+// Both products of the logits' gradient.  A block takes a set of columns (kWide) and its warps four rows of the weight in
+// turn; p.ranges blocks share a set.
+template <typename T, bool VEC, int N>
+__global__ void __launch_bounds__(256, 2) k_few_products(const XentFew p) {
   constexpr int kCols = 32 / N, kWide = 32 * kCols;  // columns of a lane, of a warp
-  extern __shared__ __align__(16) float h[];
-  __shared__ __align__(16) float g[2][kFewTile][N];
+  __shared__ float part[8][32][32];
   take_turn();
-  few_hidden<T, N>(p, h);
-  __syncthreads();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = lane % N, r = lane / N;
-  // the factor on the token's gradient
-  float coef = 0.f, lse = 0.f;
-  long long target = -1;
-  {
-    int count = 0;
-    for (int i = 0; i < p.tokens; ++i) count += p.targets[i] != p.ignore;
-    if (t < p.tokens && p.targets[t] != p.ignore) {
-      target = p.targets[t];
-      coef = p.reduction == 0 ? p.grad[t * p.grad_step] : p.reduction == 1 ? p.grad[0] / float(count) : p.grad[0];
-      if (target < 0 || target >= p.vocab) coef = __int_as_float(0x7FC00000);
-      lse = p.lse_in[t];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int set = int(blockIdx.x) / p.ranges, range = int(blockIdx.x) - set * p.ranges, c0 = set * kWide;
+  const auto col = [&](int j) { return VEC ? lane * kCols + j : 32 * j + lane; };
+  float2 x[N][kCols / 2], acc[N][kCols / 2];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const bool used = n < p.tokens && p.targets[n] != p.ignore;
+    const T* from = static_cast<const T*>(p.hidden) + n * p.hidden_row + c0;
+    float v[kCols];
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) v[j] = used && c0 + col(j) < p.d ? to_f32(from[col(j)]) : 0.f;
+#pragma unroll
+    for (int j = 0; j < kCols / 2; ++j) {
+      x[n][j] = make_float2(v[2 * j], v[2 * j + 1]);
+      acc[n][j] = both(0.f);
     }
   }
-  // sets of columns: several for each warp, or rows shared out to the warps of one
-  const int sets = (p.d + kWide - 1) / kWide, shares = sets >= 8 ? 1 : 8 / sets;
-  const int set = sets >= 8 ? warp : warp % sets, share = sets >= 8 ? 0 : warp / sets;
-  float2 acc[K][N][kCols / 2];
+  for (long long row0 = (range * 8ll + warp) * kFewRows; row0 < p.vocab; row0 += p.ranges * (8ll * kFewRows)) {
+    float2 w[kFewRows][kCols / 2];
+    float4 f[kFewRows][N / 4];
 #pragma unroll
-  for (int k = 0; k < K; ++k)
+    for (int b = 0; b < kFewRows; ++b) {
+      const bool on = row0 + b < p.vocab;
+      if (p.sums)
+        few_load<T, VEC, kCols>(static_cast<const T*>(p.weight) + (row0 + b) * p.weight_row, c0, lane, on ? p.d : 0, w[b]);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+      for (int n = 0; n < N / 4; ++n)
+        f[b][n] = on ? reinterpret_cast<const float4*>(p.g + (row0 + b) * N)[n] : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
 #pragma unroll
-      for (int j = 0; j < kCols / 2; ++j) acc[k][i][j] = both(0.f);
-  int turn = 0;
-  for (long long tile = (long long)blockIdx.x * kFewTile; tile < p.vocab; tile += (long long)gridDim.x * kFewTile, turn ^= 1) {
-    const long long row = tile + warp * kFewRows + r;
-    const float v = few_logits<T, VEC, N>(p, h, tile + warp * kFewRows, lane);
-    if (r < kFewRows)
-      g[turn][warp * kFewRows + r][t] =
-          row < p.vocab && t < p.tokens ? coef * (few_exp(v - lse) - (row == target ? 1.f : 0.f)) : 0.f;
-    __syncthreads();  // (the other half of g is free by the time that it is written again)
-    if (share >= shares) continue;
+    for (int b = 0; b < kFewRows; ++b) {
+      float2 dw[kCols / 2];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int c0 = (set + 8 * k) * kWide;
-      if (c0 >= p.d) continue;
-      for (int i = share; i < kFewTile && tile + i < p.vocab; i += 2 * shares) {
-        // two rows at a time, for one read of the hidden states
-        float2 w[2][kCols / 2], dw[2][kCols / 2];
-        float f[2][N];
+      for (int j = 0; j < kCols / 2; ++j) dw[j] = both(0.f);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const int at = i + b * shares;
-          const bool on = at < kFewTile && tile + at < p.vocab;
+      for (int n = 0; n < N; ++n) {
+        const float4 q = f[b][n / 4];
+        const float g = n % 4 == 0 ? q.x : n % 4 == 1 ? q.y : n % 4 == 2 ? q.z : q.w;
 #pragma unroll
-          for (int j = 0; j < kCols / 2; ++j) dw[b][j] = w[b][j] = both(0.f);
-          if (on && p.sums)
-            few_load<T, VEC, kCols>(static_cast<const T*>(p.weight) + (tile + at) * p.weight_row, c0, lane, p.d, w[b]);
-#pragma unroll
-          for (int n = 0; n < N; n += 4)
-            *reinterpret_cast<float4*>(&f[b][n]) =
-                on ? *reinterpret_cast<const float4*>(&g[turn][at][n]) : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-          float2 x[kCols / 2];
-          few_values<VEC, kCols>(h + n * p.padded + c0, lane, x);
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int j = 0; j < kCols / 2; ++j) {
-              dw[b][j] = fma2(both(f[b][n]), x[j], dw[b][j]);
-              acc[k][n][j] = fma2(both(f[b][n]), w[b][j], acc[k][n][j]);
-            }
-        }
-        if (p.dweight) {
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const int at = i + b * shares;
-            if (at < kFewTile && tile + at < p.vocab)
-              few_store<T, VEC, kCols>(static_cast<T*>(p.dweight) + (tile + at) * p.d, c0, lane, p.d, dw[b]);
-          }
+        for (int j = 0; j < kCols / 2; ++j) {
+          dw[j] = fma2(both(g), x[n][j], dw[j]);
+          if (p.sums) acc[n][j] = fma2(both(g), w[b][j], acc[n][j]);
         }
       }
+      if (p.dweight && row0 + b < p.vocab)
+        few_store<T, VEC, kCols>(static_cast<T*>(p.dweight) + (row0 + b) * p.d, c0, lane, p.d, dw);
     }
   }
   if (!p.sums) return;
-  // the shares of a set are added up in order, in the place of the hidden states
-  for (int s = 1; s < shares; ++s) {
-    __syncthreads();
-    const int c0 = set * kWide;
-    if (share == s)
 #pragma unroll
-      for (int n = 0; n < N; ++n) few_store<float, VEC, kCols>(h + n * p.padded, c0, lane, p.padded, acc[0][n]);
-    __syncthreads();
-    if (share == 0)
+  for (int n = 0; n < N; ++n)
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        float2 x[kCols / 2];
-        few_values<VEC, kCols>(h + n * p.padded + c0, lane, x);
-#pragma unroll
-        for (int j = 0; j < kCols / 2; ++j) acc[0][n][j] = add2(acc[0][n][j], x[j]);
-      }
-  }
-  if (share) return;
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int c0 = (set + 8 * k) * kWide;
-    if (c0 >= p.d) continue;
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-      few_store<float, VEC, kCols>(p.sums + ((long long)n * gridDim.x + blockIdx.x) * p.padded, c0, lane, p.padded, acc[k][n]);
+    for (int j = 0; j < kCols / 2; ++j) {
+      part[warp][n * kCols + 2 * j][lane] = acc[n][j].x;
+      part[warp][n * kCols + 2 * j + 1][lane] = acc[n][j].y;
+    }
+  __syncthreads();
+  for (int i = warp; i < 32; i += 8) {
+    float v = part[0][i][lane];
+    for (int k = 1; k < 8; ++k) v += part[k][i][lane];
+    const int n = i / kCols, j = i % kCols;
+    if (n < p.tokens && c0 + col(j) < p.d) p.sums[((long long)n * p.ranges + range) * p.padded + c0 + col(j)] = v;
   }
 }
 
@@ -339,10 +346,11 @@ __global__ void __launch_bounds__(1024) k_few_finish(const XentFew p) {
   __shared__ float part[32][33];
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, strips = (p.d + 31) / 32;
   const int t = blockIdx.x / strips, c0 = (blockIdx.x - t * strips) * 32;
-  const float* from = p.sums + (long long)t * p.blocks * p.padded + c0 + tx;
+  const float* from = p.sums + (long long)t * p.ranges * p.padded + c0 + tx;
   float s = 0.f;
-#pragma unroll 8
-  for (int i = ty; i < p.blocks; i += 32) s += from[(long long)i * p.padded];
+  if (c0 + tx < p.d)
+#pragma unroll 4
+    for (int i = ty; i < p.ranges; i += 32) s += from[(long long)i * p.padded];
   part[ty][tx] = s;
   __syncthreads();
   const float all = warp_sum(part[tx][ty]);
@@ -357,11 +365,13 @@ cudaError_t few_launch_n(const XentFew& p, bool backward, cudaStream_t st) {
   if (smem > 40 * 1024) smem = std::max<size_t>(smem, 48 * 1024 + 16);
   const Shape s{unsigned(p.blocks), 256, smem, 0};
   if (!backward) {
-    const cudaError_t e = launch(k_few_forward<T, VEC, N>, s, st, p);
+    const cudaError_t e = launch(k_few_logits<T, VEC, N, false>, s, st, p);
     return e != cudaSuccess ? e : launch(k_few_join, Shape{1, 256, 0, 0}, st, p);
   }
-  const cudaError_t e = p.d <= 256 * (32 / N) ? launch(k_few_backward<T, VEC, N, 1>, s, st, p)
-                                              : launch(k_few_backward<T, VEC, N, 2>, s, st, p);
+  cudaError_t e = launch(k_few_logits<T, VEC, N, true>, s, st, p);
+  if (e != cudaSuccess) return e;
+  constexpr int kWide = 32 * (32 / N);
+  e = launch(k_few_products<T, VEC, N>, Shape{unsigned((p.d + kWide - 1) / kWide * p.ranges), 256, 0, 0}, st, p);
   if (e != cudaSuccess || !p.dhidden) return e;
   return launch(k_few_finish<T>, Shape{unsigned((p.d + 31) / 32 * p.tokens), 1024, 0, 0}, st, p);
 }
