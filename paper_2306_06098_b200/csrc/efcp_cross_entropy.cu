@@ -90,6 +90,7 @@ struct Plan {
   int64_t packed_row;  // elements of a packed row
   int64_t piece;       // columns of the vocabulary at a time
   int pieces;
+  int shifts;  // how often a piece may be doubled, when few tokens count
   int col_tiles, col_tile;  // of the logits: all of them forward, a piece's backward
   int parts;
   int d_tiles, d_tile;
@@ -146,9 +147,11 @@ Plan make_plan(const efcp_cross_entropy& d, const void* weight, bool backward, i
     for (int i = 0; i < std::min(2, p.pieces); ++i) p.g[i] = take(2 * p.planes * p.padded * p.piece);
     // how many rows count is not known here: the most that any number of them takes with its parts
     const int64_t rows = p.padded / kXentRows;
+    while (p.shifts < kXentShifts && (p.piece << p.shifts) < d.vocab && (rows >> (p.shifts + 1)) > 0) ++p.shifts;
     int64_t parts = 0;
     for (int64_t r = 1; r <= std::min<int64_t>(rows, 2 * p.pairs + 1); ++r)
-      parts = std::max<int64_t>(parts, r * xent_splits(int(r), p.d_tiles, int(p.piece), p.pairs));
+      parts = std::max<int64_t>(parts, r * xent_splits(int(r), p.d_tiles, int(p.piece << xent_shift(int(r), int(rows), p.shifts)),
+                                                       p.pairs));
     p.sum_rows = std::max(rows, parts) * kXentRows;
     p.sum = take(4 * p.sum_rows * p.sum_row);
   } else {
@@ -287,7 +290,9 @@ struct Call {
     prep.parts = p.parts;
     prep.reduction = d.reduction;
     prep.d_tiles = p.d_tiles;
-    prep.piece = int(p.piece);
+    prep.piece = gemm.piece = int(p.piece);
+    prep.tiles = gemm.tiles = int(p.padded / kXentRows);
+    prep.shifts = gemm.shifts = p.shifts;
     prep.pairs = p.pairs;
     gemm.count = prep.count;
     gemm.target = prep.target;
@@ -300,7 +305,6 @@ struct Call {
     gemm.d_tile = p.d_tile;
     gemm.col_tiles = p.col_tiles;
     gemm.col_tile = p.col_tile;
-    gemm.piece = int(p.piece);
     gemm.status = device_status();
     if (!gemm.status) return false;
     const void* weight = p.in_place ? w : prep.weight_packed;
@@ -390,7 +394,6 @@ int efcp_cross_entropy_forward(const efcp_cross_entropy* desc, const void* hidde
   c.prep.lse_out = lse;
   c.prep.each = c.at<float>(workspace, c.plan.each);
   c.prep.part = c.gemm.part = c.at<float2>(workspace, c.plan.part);
-  c.gemm.logits = 1;
   if (!c.prepare(false) || !c.multiply(false) || xent_join(c.prep, c.sms, c.st) != cudaSuccess)
     return failed();
   return EFCP_OK;
@@ -452,30 +455,26 @@ int efcp_cross_entropy_backward(const efcp_cross_entropy* desc, const float* gra
   m.box_dweight = dweight && reinterpret_cast<uintptr_t>(dweight) % 16 == 0 && desc->d * size % 16 == 0;
   const int type = c.operand_type();
   const int64_t plane = p.padded * p.piece;
-  for (int i = 0; i < 2; ++i) {
-    const void* g = c.at<void>(workspace, p.g[p.pieces > 1 ? i : 0]);
-    if (!make_map(&m.g_rows[i], type, g, p.piece, p.padded, p.piece, p.planes, plane, kXentRows / 2) ||
-        !make_map(&m.g_cols[i], type, g, p.piece, p.padded, p.piece, p.planes, plane, 64) ||
-        !make_map(&m.g_out[i], type, g, p.piece, p.padded, p.piece, p.planes, plane, 32, p.planes == 1 ? 128 : 64))
-      return failed();
-  }
+  for (int s = 0; s <= p.shifts; ++s)
+    for (int i = 0; i < 2; ++i) {
+      const void* g = c.at<void>(workspace, p.g[p.pieces > 1 ? i : 0]);
+      const int64_t wide = p.piece << s, rows = (p.padded / kXentRows >> s) * kXentRows;
+      auto& map = m.g[s][i];
+      if (!make_map(&map.rows, type, g, wide, rows, wide, p.planes, plane, kXentRows / 2) ||
+          !make_map(&map.cols, type, g, wide, rows, wide, p.planes, plane, 64) ||
+          !make_map(&map.out, type, g, wide, rows, wide, p.planes, plane, 32, p.planes == 1 ? 128 : 64))
+        return failed();
+    }
   if (!make_map(&m.sum_out, EFCP_F32, sum, p.sum_row, p.sum_rows, p.sum_row, 1, 0, 32) ||
       (m.box_dweight &&
        !make_map(&m.dweight_out, desc->dtype, dweight, desc->d, desc->vocab, desc->d, 1, 0, 32)))
     return failed();
   if (!c.prepare(true)) return failed();
-  // launch k: the products of piece k - 1, the logits of piece k
-  for (int k = 0; k <= p.pieces; ++k) {
-    m.logits = k < p.pieces;
-    m.next_v0 = int(k * p.piece);
-    m.next_buffer = k & 1;
-    m.hidden = k > 0 && dhidden;
-    m.weight = k > 0 && dweight;
-    m.first = k == 1;
-    m.v0 = k > 0 ? int((k - 1) * p.piece) : 0;
-    m.buffer = (k + 1) & 1;
+  m.hidden = dhidden != nullptr;
+  m.weight = dweight != nullptr;
+  // (where pieces are wider than they might be, the last launches find nothing to do)
+  for (m.turn = 0; m.turn <= p.pieces; ++m.turn)
     if (!c.multiply(true)) return failed();
-  }
   if (dhidden && !c.finish()) return failed();
   return EFCP_OK;
 }

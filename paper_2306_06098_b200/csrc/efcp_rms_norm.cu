@@ -243,12 +243,13 @@ int64_t efcp_rms_norm_workspace_bytes(const efcp_rms_norm* desc) {
   if (sms < 1) sms = 148;  // no device: the SM count of a B200
   Rms p = common(desc);
   RmsLaunch l{};
-  // (whether the rows go through shared memory hangs on their alignment, which is not known here)
+  // (whether and how the rows go through shared memory hangs on pointers that are not known here)
   int64_t parts = 0;
   for (int inputs : {2, 3})
     for (bool vec : {false, true})
-      if ((!vec || desc->d % 8 == 0) && plan_ring(desc, kRmsBackward, vec, inputs, false, sms, &p, &l))
-        parts = std::max<int64_t>(parts, l.parts);
+      for (bool weight : {false, true})
+        if ((!vec || desc->d % 8 == 0) && plan_ring(desc, kRmsBackward, vec, inputs, weight, sms, &p, &l))
+          parts = std::max<int64_t>(parts, l.parts);
   share(desc, &p, &l);
   parts = std::max(parts, backward_blocks(desc, sms, p, l).parts);
   return std::max<int64_t>(16, parts * desc->d * 4);

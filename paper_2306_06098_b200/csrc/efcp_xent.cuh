@@ -78,18 +78,31 @@ struct XentTile {
 // does not stay in the cache (8192 x 8192 bf16: read twice instead of seven times); all rows first for the logits: H does.
 struct XentWork {
   int row_tiles, weight_rows, splits, steps, token_steps;
-  long long hidden, weight, all;  // tiles of hidden; and of weight; and of logits
+  int shift, piece, v0, next_v0, col_tiles;  // pieces: the one that hidden and weight read, the one that logits writes
+  int rows, next_cols;                       // of them: rows of W, columns
+  long long hidden, weight, all;             // tiles of hidden; and of weight; and of logits
 
-  __device__ __forceinline__ XentWork(const XentGemm& p, int count, int pairs) {
+  __device__ __forceinline__ XentWork(const XentGemm& p, int count, int pairs, bool backward) {
     row_tiles = (count + kXentRows - 1) / kXentRows;
-    const int real = min(p.piece, p.vocab - p.v0);
-    weight_rows = (real + kXentRows - 1) / kXentRows;
-    steps = (real + kXentDepth - 1) / kXentDepth;
+    shift = backward ? xent_shift(row_tiles, p.tiles, p.shifts) : 0;
+    piece = p.piece << shift;
+    col_tiles = p.col_tiles << shift;
+    // (what begins behind the vocabulary is not worked on)
+    const long long begin = backward ? (p.turn - 1ll) * piece : 0, next = backward ? (long long)p.turn * piece : 0;
+    const bool products = begin >= 0 && begin < p.vocab && backward, logits = next < p.vocab;
+    v0 = products ? int(begin) : 0;
+    next_v0 = logits ? int(next) : 0;
+    rows = min(piece, p.vocab - v0);
+    next_cols = min(piece, p.vocab - next_v0);
+    // (the last piece's tiles end with the vocabulary: pieces are whole tiles, or there is one)
+    if (backward) col_tiles = min(col_tiles, (next_cols + p.col_tile - 1) / p.col_tile);
+    weight_rows = (rows + kXentRows - 1) / kXentRows;
+    steps = (rows + kXentDepth - 1) / kXentDepth;
     token_steps = (count + kXentDepth - 1) / kXentDepth;
-    splits = xent_splits(row_tiles, p.d_tiles, p.piece, pairs);
-    hidden = p.hidden ? (long long)row_tiles * p.d_tiles * splits : 0;
-    weight = hidden + (p.weight ? (long long)weight_rows * p.d_tiles : 0);
-    all = weight + (p.logits ? (long long)row_tiles * p.col_tiles : 0);
+    splits = xent_splits(row_tiles, p.d_tiles, piece, pairs);
+    hidden = products && p.hidden ? (long long)row_tiles * p.d_tiles * splits : 0;
+    weight = hidden + (products && p.weight ? (long long)weight_rows * p.d_tiles : 0);
+    all = weight + (logits ? (long long)row_tiles * col_tiles : 0);
   }
   static __device__ __forceinline__ int2 square(int t, int rows, int cols) {
     const int g = t / (kSquare * cols), first = g * kSquare, here = min(kSquare, rows - first);
@@ -243,14 +256,15 @@ struct Ring {
 // A block's copies of a tile's operands.  (One thread issues them; what a step needs beside them counts, so that a kind
 // has its own loop: with one loop for all, 1130 cycles a step of 520 on the tensor cores.)
 template <XentKind KIND, int PAIRS>
-__device__ __forceinline__ bool load_tile(const XentGemm& p, const XentTile& w, const Ring& r, int rank, unsigned& n,
-                                          volatile int* gave_up) {
+__device__ __forceinline__ bool load_tile(const XentGemm& p, const XentWork& work, const XentTile& w, const Ring& r,
+                                          int rank, unsigned& n, volatile int* gave_up) {
+  const auto& g = p.g[work.shift][(p.turn + 1) & 1];
   const int an = w.m0 + rank * kBlockRows, bn = w.n0 + rank * (w.cols / 2);
   const uint32_t bytes = 2 * (kABytes + uint32_t(w.cols) * 64);
   const bool wide = w.cols > 128;
-  const CUtensorMap* const ma = KIND == kLogits ? &p.hidden_rows : KIND == kHidden ? &p.g_rows[p.buffer] : &p.g_cols[p.buffer];
+  const CUtensorMap* const ma = KIND == kLogits ? &p.hidden_rows : KIND == kHidden ? &g.rows : &g.cols;
   const CUtensorMap* const mb = KIND == kLogits ? &p.weight_rows : KIND == kHidden ? &p.weight_cols : &p.hidden_cols;
-  const int b0 = KIND == kLogits ? p.next_v0 + bn : KIND == kHidden ? p.v0 : 0;
+  const int b0 = KIND == kLogits ? work.next_v0 + bn : KIND == kHidden ? work.v0 : 0;
   for (int turn = 0; turn < PAIRS; ++turn) {
     // planes of the turns: (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
     const int pa = PAIRS == 1 ? 0 : (0x001102 >> (4 * turn)) & 15;
@@ -314,7 +328,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
   take_turn();
   const uint32_t tmem = tmem_at;
   const int count = *p.count, pairs = int(gridDim.x / 2), pair = int(blockIdx.x / 2);
-  const XentWork work(p, count, pairs);
+  const XentWork work(p, count, pairs, BACKWARD);
 
   // Registers go where the sums are held: 128 x 72 + 256 x 216 of the launch's 384 x 168.
   if (warp >= kOutWarps) {
@@ -326,9 +340,9 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
       bool ok = true;
       for (long long t = pair; t < work.all && ok; t += pairs) {
         const XentTile w = work.tile(p, t);
-        if (w.kind == kLogits) ok = load_tile<kLogits, kPairs>(p, w, ring_of, rank, n, gave_up);
-        else if (w.kind == kHidden) ok = load_tile<kHidden, kPairs>(p, w, ring_of, rank, n, gave_up);
-        else ok = load_tile<kWeight, kPairs>(p, w, ring_of, rank, n, gave_up);
+        if (w.kind == kLogits) ok = load_tile<kLogits, kPairs>(p, work, w, ring_of, rank, n, gave_up);
+        else if (w.kind == kHidden) ok = load_tile<kHidden, kPairs>(p, work, w, ring_of, rank, n, gave_up);
+        else ok = load_tile<kWeight, kPairs>(p, work, w, ring_of, rank, n, gave_up);
       }
       if (!ok) {  // nothing may land in shared memory that the block has left: copies take microseconds
         const uint64_t start = tc::clock_ns();
@@ -382,6 +396,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
     const int quarter = warp & 3, half = warp >> 2;
     const float back = BACKWARD ? p.scale[1] : 1.f;
     const uint32_t box = ring + kStages * kStageBytes + warp * kOutBytes;
+    const CUtensorMap* const g_out = &p.g[work.shift][p.turn & 1].out;
     unsigned turn = 0;
     bool ok = true;
     for (long long t = pair; t < work.all && ok; t += pairs) {
@@ -405,9 +420,9 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
         if constexpr (!BACKWARD) {
           stats.add(p, row, target, col, v);
         } else if (w.kind == kLogits) {
-          if (col >= p.piece) return;  // (all lanes, here and below: no box begins outside of what it is stored to)
-          const int hit = target - (p.next_v0 + col);
-          const int valid = row < count ? min(p.piece, p.vocab - p.next_v0) - col : 0;
+          if (col >= work.piece) return;  // (all lanes, here and below: no box begins outside of what it is stored to)
+          const int hit = target - (work.next_v0 + col);
+          const int valid = row < count ? work.next_cols - col : 0;
           const bool mine = hit >= 0 && hit < 32;
           float x = 0.f;
           if (mine) {
@@ -434,14 +449,14 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
             const bool second = c & 32;  // half of a box of 64 columns
             if (!second) out.open();
             out.put(second ? 4 : 0, v);
-            if (second) out.send(&p.g_out[p.next_buffer], col - 32, row0, 0, false);
+            if (second) out.send(g_out, col - 32, row0, 0, false);
           } else {
 #pragma unroll
             for (int plane = 0; plane < 3; ++plane) {
               const OutBox<O, 64> out{box, lane};
               out.open();
               out.put(0, v);
-              out.send(&p.g_out[p.next_buffer], col, row0, plane, false);
+              out.send(g_out, col, row0, plane, false);
 #pragma unroll
               for (int i = 0; i < 32; ++i) v[i] -= rounded<O>(v[i]);
             }
@@ -455,9 +470,9 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
           const OutBox<float> out{box, lane};
           out.open();
           out.put(0, v);
-          out.send(&p.sum_out, col, w.part * work.row_tiles * kXentRows + row0, 0, !p.first);
+          out.send(&p.sum_out, col, w.part * work.row_tiles * kXentRows + row0, 0, p.turn > 1);
         } else {
-          if ((col & ~63) >= p.d || row0 >= min(p.piece, p.vocab - p.v0)) return;
+          if ((col & ~63) >= p.d || row0 >= work.rows) return;
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = steps ? v[i] * back : 0.f;
           if (p.box_dweight) {
@@ -466,9 +481,9 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
             const bool second = c & (kWide - 32);
             if (!second) out.open();
             out.put(second ? 4 : 0, v);
-            if (second || (kWide == 32 && col < p.d)) out.send(&p.dweight_out, col & ~(kWide - 1), p.v0 + row0, 0, false);
-          } else if (row < min(p.piece, p.vocab - p.v0)) {
-            T* to = static_cast<T*>(p.dweight) + (long long)(p.v0 + row) * p.d + col;
+            if (second || (kWide == 32 && col < p.d)) out.send(&p.dweight_out, col & ~(kWide - 1), work.v0 + row0, 0, false);
+          } else if (row < work.rows) {
+            T* to = static_cast<T*>(p.dweight) + (long long)(work.v0 + row) * p.d + col;
             const int valid = p.d - col;
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -721,7 +736,8 @@ __global__ void __launch_bounds__(256) k_xent_finish(const XentPrep p) {
   take_turn();
   const int lane = threadIdx.x & 31, chunks = (p.d + 127) / 128;
   const int row_tiles = (*p.count + kXentRows - 1) / kXentRows;
-  const int splits = xent_splits(row_tiles, p.d_tiles, p.piece, p.pairs);
+  const int splits =
+      xent_splits(row_tiles, p.d_tiles, p.piece << xent_shift(row_tiles, p.tiles, p.shifts), p.pairs);
   const long long part = (long long)row_tiles * kXentRows * p.sum_row, all = p.tokens * chunks;
   const float back = p.scale[1];
   const bool vec = reinterpret_cast<uintptr_t>(p.dhidden) % 16 == 0 && p.d % 4 == 0;

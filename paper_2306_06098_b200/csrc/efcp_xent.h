@@ -10,6 +10,7 @@ namespace efcp {
 
 // A tile of a product (256 x up to 256, of a pair of blocks), and a step along the sum.
 constexpr int kXentRows = 256, kXentCols = 256, kXentDepth = 64;
+constexpr int kXentShifts = 3;
 constexpr int kXentSplits = 8;  // parts of the sum over a piece that are added up apart, at most
 
 // The products of tiles that a launch works on, in this order:
@@ -20,9 +21,12 @@ constexpr int kXentSplits = 8;  // parts of the sum over a piece that are added 
 struct XentGemm {
   // operands whose inner dimension is that of the sum (rows of 64 in boxes of a block's share of a tile), and the
   // others (boxes of 64 x 64)
-  CUtensorMap hidden_rows, weight_rows, g_rows[2], hidden_cols, weight_cols, g_cols[2];
+  CUtensorMap hidden_rows, weight_rows, hidden_cols, weight_cols;
   // results, stored in boxes of 32 rows of 128 bytes
-  CUtensorMap g_out[2], sum_out, dweight_out;
+  CUtensorMap sum_out, dweight_out;
+  struct {
+    CUtensorMap rows, cols, out;
+  } g[kXentShifts + 1][2];  // the gradient of the logits, by the width of a piece
   const int* count;    // tokens that have a target
   const int* target;   // their targets, -1: out of range
   const float* lse;    // logarithm of the sum of exponentials (by the tokens' order here)
@@ -35,11 +39,10 @@ struct XentGemm {
   int vocab, d;
   int parts;
   int d_tiles, d_tile;
-  int hidden, weight, logits;          // which products
-  int v0, buffer, first;               // of the piece that hidden and weight read
-  int next_v0, next_buffer;            // of the piece that logits writes (or 0)
-  int col_tiles, col_tile;             // of logits
-  int piece;                           // columns of a piece
+  int hidden, weight;                  // which of the products of a piece are wanted
+  int turn;                            // the launch works on piece turn - 1 and the logits of piece turn
+  int col_tiles, col_tile;             // of logits (forward; of a piece not widened)
+  int piece, tiles, shifts;            // see xent_shift
   int box_dweight;                     // rows of dweight start on 16 bytes: it can be stored in boxes
 };
 
@@ -65,7 +68,7 @@ struct XentPrep {
   int* place;                      // a token's place in the order, -1: none
   const float* sum;                // gradient of H: parts of the whole tiles' rows, sum_row elements each
   long long sum_row;
-  int d_tiles, piece, pairs;
+  int d_tiles, piece, tiles, shifts, pairs;
   void* dhidden;
 };
 
@@ -95,6 +98,14 @@ struct XentFew {
   int ranges;   // blocks that share a set of columns
   void *dhidden, *dweight;
 };
+
+// How often a piece's columns are doubled.  The buffers hold `piece` columns for all tokens, `tiles` tiles of rows; how many
+// of them have a target is known on the device alone, and with fewer rows a piece is wider: fewer launches do something.
+__host__ __device__ inline int xent_shift(int row_tiles, int tiles, int shifts) {
+  int s = 0;
+  while (s < shifts && row_tiles <= (tiles >> (s + 1))) ++s;
+  return s;
+}
 
 // How many parts the sum over a piece is cut into for the gradient of H: as many as give every pair of blocks two
 // tiles, none shorter than 16 steps.

@@ -363,3 +363,13 @@ def test_few_tokens_that_have_no_target_or_a_wrong_one(n):
         assert got.isnan() if how == "mean" else (got == 0).all()
         dh, dw = B().cross_entropy_backward(torch.ones_like(got), hidden, weight, targets, lse, 0, how)
         assert (dh == 0).all() and (lse == 0).all() and (dw == 0).all()
+
+
+# ------------------------------------------------------------------ wider pieces where few tokens count
+@pytest.mark.parametrize("labelled", [0.0, 0.0001, 0.1, 0.2, 0.45, 0.9])
+@pytest.mark.parametrize("dtype,v", [(torch.float32, 5003), (torch.bfloat16, 9001), (torch.float16, 8192)])
+def test_pieces_of_every_width(labelled, dtype, v):
+    n, d = 16300, 40  # pieces of 1280 columns for fp32, 4096 for 16 bits, when all tokens count
+    hidden, weight, targets = inputs(n, d, v, dtype, 6, labelled)
+    check_backward(hidden, weight, targets, grads(n))
+    check_backward(hidden, weight, targets, torch.tensor(0.5, device="cuda"), reduction="sum")
