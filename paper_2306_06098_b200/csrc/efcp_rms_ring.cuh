@@ -535,8 +535,8 @@ __global__ void __launch_bounds__(256, 2) k_rms_forward_ring(const Rms p, const 
           if (!ODD && p.block) {  // (all lanes: the maximum of a block is exchanged between them)
             float top = most_of(z);
             const int lanes = min(p.block / 8, q.lanes);
-            top = larger(top, __shfl_xor_sync(kAll, top, 1));
-            top = larger(top, __shfl_xor_sync(kAll, top, 2));
+            if (lanes > 1) top = larger(top, __shfl_xor_sync(kAll, top, 1));
+            if (lanes > 2) top = larger(top, __shfl_xor_sync(kAll, top, 2));
             if (lanes > 4) top = larger(top, __shfl_xor_sync(kAll, top, 4));
             if (lanes > 8) top = larger(top, __shfl_xor_sync(kAll, top, 8));
             one = scale_of(top, p.most);

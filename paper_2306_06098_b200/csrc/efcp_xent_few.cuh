@@ -123,6 +123,11 @@ __device__ __forceinline__ float few_logits(const XentFew& p, const float* h, lo
   return v[0];
 }
 
+// Tokens that count.  (a warp)
+__device__ __forceinline__ int few_count(const XentFew& p, int lane) {
+  return __popc(__ballot_sync(kAll, lane < p.tokens && p.targets[lane] != p.ignore));
+}
+
 // Largest logit and sum of exponentials relative to it, of two sets.
 __device__ __forceinline__ void few_join(float& top, float& sum, float top2, float sum2) {
   const float m = fmaxf(top, top2), base = m == -INFINITY ? 0.f : m;
@@ -145,8 +150,7 @@ __global__ void __launch_bounds__(256, 2) k_few_logits(const XentFew p) {
   const long long target = t < p.tokens && mine ? p.targets[t] : -1;  // (one that is ignored meets no reader)
   float coef = 0.f, lse = 0.f;
   if constexpr (BACKWARD) {
-    int count = 0;
-    for (int i = 0; i < p.tokens; ++i) count += p.targets[i] != p.ignore;
+    const int count = few_count(p, lane);
     if (t < p.tokens && p.targets[t] != p.ignore) {
       coef = p.reduction == 0 ? p.grad[t * p.grad_step] : p.reduction == 1 ? p.grad[0] / float(count) : p.grad[0];
       if (p.targets[t] < 0 || p.targets[t] >= p.vocab) coef = __int_as_float(0x7FC00000);
@@ -188,14 +192,18 @@ __global__ void __launch_bounds__(256) k_few_join(const XentFew p) {
   take_turn();
   __shared__ double each[8];
   const int lane = threadIdx.x & 31, t = threadIdx.x >> 5;
-  int count = 0;
-  for (int i = 0; i < p.tokens; ++i) count += p.targets[i] != p.ignore;
+  const int count = few_count(p, lane);
   if (t < p.tokens) {
     const long long target = p.targets[t];
     float top = -INFINITY, sum = 0.f;
-    for (int i = lane; i < p.blocks; i += 32) {
-      const float2 o = p.part[t * p.blocks + i];
-      few_join(top, sum, o.x, o.y);
+    constexpr int kAhead = 5;  // loads on their way
+    for (int i = lane; i < p.blocks; i += 32 * kAhead) {
+      float2 o[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        o[k] = i + 32 * k < p.blocks ? p.part[t * p.blocks + i + 32 * k] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) few_join(top, sum, o[k].x, o[k].y);
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1)

@@ -343,7 +343,8 @@ def test_many_odd_rows_of_wider_tensors(pad, shift, dtype):
 @pytest.mark.parametrize("format", ["e4m3", "int8"])
 @pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
 def test_quantize_many_rows(format, dtype):
-    for rows, d, block in ((300, 1111, 0), (297, 77, 0), (400, 40, 32), (300, 1000, 64), (350, 4104, 128), (300, 96, 0)):
+    for rows, d, block in ((300, 1111, 0), (297, 77, 0), (400, 40, 32), (300, 1000, 64), (350, 4104, 128), (300, 96, 0), (9600, 8, 32),
+                          (9600, 16, 64), (9600, 24, 128), (9600, 104, 64), (9600, 128, 128), (9600, 200, 32)):
         test_quantize(rows, d, block, format, dtype)
 
 
