@@ -12,8 +12,8 @@
 // those pieces' elements are copied one by one.
 //
 // The memory bounds rows that begin on 16 bytes without dropout, forward and backward: 16384 x 4096 bf16 with a residual
-// 90 us (5.96 TB/s) and 108 us (4.97 TB/s); 16384 x 768, 17 us.  Instructions bound the rest, with 16 warps on an SM, which
-// is what the registers allow: dropout's ten rounds for eight elements (16384 x 768, 25 us), the maxima and conversions of 8-bit
+// 90 us (5.96 TB/s) and 108 us (4.97 TB/s); 16384 x 768, 16 us.  Instructions bound the rest, with 16 warps on an SM, which
+// is what the registers allow: dropout's ten rounds for eight elements (16384 x 768, 24 us), the maxima and conversions of 8-bit
 // outputs (8192 x 4096: 58 us, blocks of 128), the shifts and the rows' ends of rows that begin anywhere (20000 x 1111 bf16:
 // 53 us forward, 79 us backward; 117 and 153 with loads of single elements).
 #pragma once
@@ -33,10 +33,13 @@ namespace {
 
 constexpr int kRingFront = 48, kRingBack = 64;  // room around a place's rows (ODD): shifted pieces reach there
 
+// (An input is read once; the cache is for the outputs, which are read next: 16384 x 768 bf16 forward 16.9 -> 15.7 us.)
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  uint64_t first_out;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(first_out));
   asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-      "l"(src), "r"(bytes), "r"(bar)
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
+      "l"(src), "r"(bytes), "r"(bar), "l"(first_out)
       : "memory");
 }
 
