@@ -28,10 +28,26 @@ __global__ void __launch_bounds__(256) k_xent_join(const XentPrep p) {
   for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < count; i += warps) {
     const float2* part = p.part + i * p.parts;
     float top = -INFINITY, sum = 0.f;
-    for (int k = lane; k < p.parts; k += 32) top = fmaxf(top, part[k].x);
+    constexpr int kAhead = 4;  // loads on their way
+    for (int k = lane; k < p.parts; k += 32 * kAhead) {
+      float2 o[kAhead];
+      float m = top;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kAllLanes, top, o));
-    for (int k = lane; k < p.parts; k += 32) sum += part[k].y * exp2f(part[k].x - top);
+      for (int j = 0; j < kAhead; ++j) {
+        o[j] = k + 32 * j < p.parts ? part[k + 32 * j] : make_float2(-INFINITY, 0.f);
+        m = fmaxf(m, o[j].x);
+      }
+      const float base = m == -INFINITY ? 0.f : m;
+      sum *= exp2f(top - base);
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) sum += o[j].y * exp2f(o[j].x - base);
+      top = m;
+    }
+    float m = top;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAllLanes, m, o));
+    sum *= exp2f(top - (m == -INFINITY ? 0.f : m));
+    top = m;
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAllLanes, sum, o);
     if (lane) continue;

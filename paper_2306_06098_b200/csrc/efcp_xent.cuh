@@ -630,17 +630,23 @@ __global__ void __launch_bounds__(512) k_xent_prepare(const XentPrep p, bool bac
     }
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.count = all;
-  const auto row = [&](long long token, int place) {  // (a warp)
+  const int chunks = (p.d + 255) / 256;
+  const auto copy = [&](long long token, int place, int c0) {  // 256 columns of a row  (a warp)
     const T* from = static_cast<const T*>(p.hidden) + token * p.hidden_row;
     O* to = static_cast<O*>(p.hidden_packed) + place * p.packed_row;
     if (kPlanes == 1 && reinterpret_cast<uintptr_t>(from) % 16 == 0 && p.d % 8 == 0) {
-#pragma unroll 4
-      for (int c = lane * 8; c < p.d; c += 256)
-        *reinterpret_cast<uint4*>(to + c) = *reinterpret_cast<const uint4*>(from + c);
+      const int c = c0 + lane * 8;
+      if (c < p.d) *reinterpret_cast<uint4*>(to + c) = *reinterpret_cast<const uint4*>(from + c);
     } else {
-      for (int c = lane; c < p.d; c += 32) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = c0 + 32 * j + lane < p.d ? to_f32(from[c0 + 32 * j + lane]) : 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int c = c0 + 32 * j + lane;
+        if (c >= p.d) continue;
         O v[kPlanes];
-        split<O, kPlanes>(to_f32(from[c]), v);
+        split<O, kPlanes>(x[j], v);
 #pragma unroll
         for (int k = 0; k < kPlanes; ++k) to[k * p.hidden_plane + c] = v[k];
       }
@@ -677,7 +683,11 @@ __global__ void __launch_bounds__(512) k_xent_prepare(const XentPrep p, bool bac
       }
     }
     __syncthreads();
-    for (int k = warp; k < here; k += 512 / 32) row(tokens[k], at + k);
+#pragma unroll 2
+    for (int k = warp; k < here * chunks; k += 512 / 32) {
+      const int token = k / chunks;
+      copy(tokens[token], at + token, (k - token * chunks) * 256);
+    }
     at += here;
     __syncthreads();
   }
@@ -690,7 +700,7 @@ __global__ void __launch_bounds__(512) k_xent_prepare(const XentPrep p, bool bac
   for (int i = all + int(blockIdx.x) * 16 + warp; i < padded; i += int(gridDim.x) * 16)
     for (int k = 0; k < kPlanes; ++k) {
       O* to = static_cast<O*>(p.hidden_packed) + k * p.hidden_plane + (long long)i * p.packed_row;
-      for (int c = lane; c < p.d; c += 32) to[c] = from_f32<O>(0.f);
+      for (int c = lane * 8; c < p.packed_row; c += 256) *reinterpret_cast<uint4*>(to + c) = make_uint4(0, 0, 0, 0);
     }
 }
 
@@ -797,8 +807,8 @@ cudaError_t xent_launch(const XentGemm& p, unsigned pairs, cudaStream_t st) {
 
 template <typename T>
 cudaError_t xent_prepare(const XentPrep& p, bool backward, int sms, cudaStream_t st) {
-  // runs of tokens for each SM, at least one for each warp of a block
-  const long long per = std::max<long long>(16, (p.tokens + sms - 1) / sms);
+  // runs of tokens for two blocks on each SM
+  const long long per = std::max<long long>(4, (p.tokens + 2 * sms - 1) / (2 * sms));
   const unsigned blocks = unsigned(std::max<long long>(1, (p.tokens + per - 1) / per));
   cudaError_t e = launch(k_xent_prepare<T>, Shape{blocks, 512, 0, 0}, st, p, backward, int(per));
   if (e != cudaSuccess || !p.weight) return e;
