@@ -167,7 +167,7 @@ Plan make_plan(const efcp_cross_entropy& d, const void* weight, bool backward, i
     int64_t parts = 0;
     for (int64_t r = 1; r <= std::min<int64_t>(rows, 2 * p.pairs + 1); ++r)
       parts = std::max<int64_t>(parts, r * xent_splits(int(r), p.d_tiles, int(p.piece << xent_shift(int(r), int(rows), p.shifts)),
-                                                       p.pairs));
+                                                       p.pairs, p.planes > 1));
     p.sum_rows = std::max(rows, parts) * kXentRows;
     p.sum = take(4 * p.sum_rows * p.sum_row);
   } else {

@@ -82,7 +82,7 @@ struct XentWork {
   int rows, next_cols;                       // of them: rows of W, columns
   long long hidden, weight, all;             // tiles of hidden; and of weight; and of logits
 
-  __device__ __forceinline__ XentWork(const XentGemm& p, int count, int pairs, bool backward) {
+  __device__ __forceinline__ XentWork(const XentGemm& p, int count, int pairs, bool backward, bool six) {
     row_tiles = (count + kXentRows - 1) / kXentRows;
     shift = backward ? xent_shift(row_tiles, p.tiles, p.shifts) : 0;
     piece = p.piece << shift;
@@ -99,7 +99,7 @@ struct XentWork {
     weight_rows = (rows + kXentRows - 1) / kXentRows;
     steps = (rows + kXentDepth - 1) / kXentDepth;
     token_steps = (count + kXentDepth - 1) / kXentDepth;
-    splits = xent_splits(row_tiles, p.d_tiles, piece, pairs);
+    splits = xent_splits(row_tiles, p.d_tiles, piece, pairs, six);
     hidden = products && p.hidden ? (long long)row_tiles * p.d_tiles * splits : 0;
     weight = hidden + (products && p.weight ? (long long)weight_rows * p.d_tiles : 0);
     all = weight + (logits ? (long long)row_tiles * col_tiles : 0);
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
   take_turn();
   const uint32_t tmem = tmem_at;
   const int count = *p.count, pairs = int(gridDim.x / 2), pair = int(blockIdx.x / 2);
-  const XentWork work(p, count, pairs, BACKWARD);
+  const XentWork work(p, count, pairs, BACKWARD, kPairs > 1);
 
   // Registers go where the sums are held: 128 x 72 + 256 x 216 of the launch's 384 x 168.
   if (warp >= kOutWarps) {
@@ -747,7 +747,7 @@ __global__ void __launch_bounds__(256) k_xent_finish(const XentPrep p) {
   const int lane = threadIdx.x & 31, chunks = (p.d + 127) / 128;
   const int row_tiles = (*p.count + kXentRows - 1) / kXentRows;
   const int splits =
-      xent_splits(row_tiles, p.d_tiles, p.piece << xent_shift(row_tiles, p.tiles, p.shifts), p.pairs);
+      xent_splits(row_tiles, p.d_tiles, p.piece << xent_shift(row_tiles, p.tiles, p.shifts), p.pairs, std::is_same_v<T, float>);
   const long long part = (long long)row_tiles * kXentRows * p.sum_row, all = p.tokens * chunks;
   const float back = p.scale[1];
   const bool vec = reinterpret_cast<uintptr_t>(p.dhidden) % 16 == 0 && p.d % 4 == 0;
@@ -760,13 +760,15 @@ __global__ void __launch_bounds__(256) k_xent_finish(const XentPrep p) {
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (place >= 0) {
       const float* from = p.sum + place * p.sum_row + c;  // (rows are a multiple of 32 long)
-      float4 o[kXentSplits];
+      for (int k0 = 0; k0 < splits; k0 += 8) {
+        float4 o[8];
 #pragma unroll
-      for (int k = 0; k < kXentSplits; ++k)
-        o[k] = k < splits ? *reinterpret_cast<const float4*>(from + k * part) : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < 8; ++k)
+          o[k] = k0 + k < splits ? *reinterpret_cast<const float4*>(from + (k0 + k) * part) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int k = 0; k < kXentSplits; ++k) {
-        v.x += o[k].x; v.y += o[k].y; v.z += o[k].z; v.w += o[k].w;
+        for (int k = 0; k < 8; ++k) {
+          v.x += o[k].x; v.y += o[k].y; v.z += o[k].z; v.w += o[k].w;
+        }
       }
     }
     Pack<T, 4> a;

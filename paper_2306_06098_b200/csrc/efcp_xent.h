@@ -11,7 +11,7 @@ namespace efcp {
 // A tile of a product (256 x up to 256, of a pair of blocks), and a step along the sum.
 constexpr int kXentRows = 256, kXentCols = 256, kXentDepth = 64;
 constexpr int kXentShifts = 3;
-constexpr int kXentSplits = 8;  // parts of the sum over a piece that are added up apart, at most
+constexpr int kXentSplits = 32;  // parts of the sum over a piece that are added up apart, at most
 
 // The products of tiles that a launch works on, in this order:
 //   hidden   gradient of H from a piece's gradient of the logits, in parts, added to those of the pieces before
@@ -108,12 +108,18 @@ __host__ __device__ inline int xent_shift(int row_tiles, int tiles, int shifts) 
 }
 
 // How many parts the sum over a piece is cut into for the gradient of H: as many as give every pair of blocks two
-// tiles, none shorter than 16 steps.
-__host__ __device__ inline int xent_splits(int row_tiles, int d_tiles, int piece, int pairs) {
-  const int tiles = row_tiles * d_tiles, deepest = (piece + kXentDepth * 16 - 1) / (kXentDepth * 16);
-  int s = tiles > 0 ? (2 * pairs + tiles - 1) / tiles : 1;
+// tiles, up to eight, none shorter than 16 steps.  With a few tiles of H only (up to four on a B200), as many as give every
+// pair one, and shorter ones where a step is six products.  (17 tokens x 64 x 933 fp32, gradients: 39 us, 60 with eight at
+// most; but 1003 x 509 x 10007 with more than eight 275 us, and 239.)
+__host__ __device__ inline int xent_splits(int row_tiles, int d_tiles, int piece, int pairs, bool six) {
+  const int tiles = row_tiles * d_tiles;
+  if (tiles == 0) return 1;
+  const bool lone = 16 * tiles <= pairs;
+  const int least = kXentDepth * (lone && six ? 4 : 16), deepest = (piece + least - 1) / least;
+  int s = ((lone ? 1 : 2) * pairs + tiles - 1) / tiles;
   s = s < deepest ? s : deepest;
-  return s < 1 ? 1 : s < kXentSplits ? s : kXentSplits;
+  const int most = lone ? kXentSplits : 8;
+  return s < 1 ? 1 : s < most ? s : most;
 }
 
 cudaError_t xent_gemm_f32(bool backward, const XentGemm& p, unsigned pairs, cudaStream_t st);
