@@ -231,6 +231,15 @@ struct OutBox {
                    : "memory");
     }
   }
+  // (fp32) the lane's column of a row that another lane has put
+  __device__ __forceinline__ float get(int r) const {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];"
+                 : "=f"(v)
+                 : "r"(at + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4)
+                 : "memory");
+    return v;
+  }
   // before the box is written again: its last copy has read it  (these two are for whole warps)
   __device__ __forceinline__ void open() const {
     if (lane == 0) tc::stores_read<0>();
@@ -482,12 +491,16 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
             if (!second) out.open();
             out.put(second ? 4 : 0, v);
             if (second || (kWide == 32 && col < p.d)) out.send(&p.dweight_out, col & ~(kWide - 1), work.v0 + row0, 0, false);
-          } else if (row < work.rows) {
-            T* to = static_cast<T*>(p.dweight) + (long long)(work.v0 + row) * p.d + col;
-            const int valid = p.d - col;
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (i < valid) to[i] = from_f32<T>(v[i]);
+          } else {  // rows that begin anywhere: turned in shared memory, so that a warp's accesses lie together
+            const OutBox<float> turned{box, lane};
+            turned.open();
+            turned.put(0, v);
+            __syncwarp();
+            T* to = static_cast<T*>(p.dweight) + (long long)(work.v0 + row0) * p.d + col + lane;
+            const int valid = col + lane < p.d ? min(32, work.rows - row0) : 0;
+#pragma unroll 8
+            for (int r = 0; r < valid; ++r, to += p.d) *to = from_f32<T>(turned.get(r));
+            __syncwarp();
           }
         }
       };
