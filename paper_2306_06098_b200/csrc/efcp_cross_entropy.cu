@@ -113,7 +113,7 @@ struct Plan {
   int pairs;
   int64_t sum_row, sum_rows;
   // offsets
-  int64_t count, scale, order, target, lse, coef, place, logit, each, part, hidden, weight, g[2], sum, bytes;
+  int64_t count, scale, order, target, lse, coef, rest, place, logit, each, part, hidden, weight, g[2], sum, bytes;
 };
 
 // Whether the tensor copies can read the weight where it lies.
@@ -159,6 +159,7 @@ Plan make_plan(const efcp_cross_entropy& d, const void* weight, bool backward, i
   if (backward) {
     p.lse = take(4 * p.padded);
     p.coef = take(4 * p.padded);
+    p.rest = take(4 * p.padded);
     p.place = take(4 * p.padded);
     for (int i = 0; i < std::min(2, p.pieces); ++i) p.g[i] = take(2 * p.planes * p.padded * p.piece);
     // how many rows count is not known here: the most that any number of them takes with its parts
@@ -460,6 +461,8 @@ int efcp_cross_entropy_backward(const efcp_cross_entropy* desc, const float* gra
   c.prep.lse_in = lse;
   c.prep.lse = c.at<float>(workspace, p.lse);
   c.prep.coef = c.at<float>(workspace, p.coef);
+  c.prep.rest = m.rest = p.planes == 1 ? c.at<float>(workspace, p.rest) : nullptr;
+  c.prep.layer = weight;
   c.prep.place = c.at<int>(workspace, p.place);
   float* sum = c.at<float>(workspace, p.sum);
   c.prep.sum = sum;

@@ -438,6 +438,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
 #pragma unroll
             for (int i = 0; i < 32; ++i) x = i == hit ? v[i] : x;
             x = (exp_pair(x, x, lse).x - 1.f) * coef;
+            if constexpr (kPairs == 1) p.rest[row] = x - rounded<O>(x);
           }
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
@@ -687,6 +688,7 @@ __global__ void __launch_bounds__(512) k_xent_prepare(const XentPrep p, bool bac
         p.target[place] = in ? int(t) : -1;
         if (backward) {
           const float g = each ? p.grad[i * p.grad_step] : one;
+          if (p.rest) p.rest[place] = 0.f;
           p.coef[place] = in ? g * up : __int_as_float(0x7FC00000);
           p.lse[place] = p.lse_in[i];
         }
@@ -753,7 +755,8 @@ __global__ void __launch_bounds__(256) k_xent_pack(const XentPrep p) {
   }
 }
 
-// The gradient of H from its parts; zeros for tokens without a target.  A warp takes 128 columns of a row.
+// The gradient of H from its parts; zeros for tokens without a target.  A warp takes 128 columns of a row.  The target's entry of
+// G is by far a row's largest, and what its rounding to 16 bits left is added here.
 template <typename T>
 __global__ void __launch_bounds__(256) k_xent_finish(const XentPrep p) {
   take_turn();
@@ -782,6 +785,14 @@ __global__ void __launch_bounds__(256) k_xent_finish(const XentPrep p) {
         for (int k = 0; k < 8; ++k) {
           v.x += o[k].x; v.y += o[k].y; v.z += o[k].z; v.w += o[k].w;
         }
+      }
+      const float rest = p.rest ? p.rest[place] : 0.f;
+      if (rest != 0.f) {
+        const T* w = static_cast<const T*>(p.layer) + p.target[place] * p.weight_row + c;
+        v.x += rest * to_f32(w[0]);
+        if (c + 1 < p.d) v.y += rest * to_f32(w[1]);
+        if (c + 2 < p.d) v.z += rest * to_f32(w[2]);
+        if (c + 3 < p.d) v.w += rest * to_f32(w[3]);
       }
     }
     Pack<T, 4> a;

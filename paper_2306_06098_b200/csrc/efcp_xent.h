@@ -32,6 +32,7 @@ struct XentGemm {
   const float* lse;    // logarithm of the sum of exponentials (by the tokens' order here)
   const float* coef;   // factor on a token's gradient
   const float* scale;  // [0]: the factor that coef holds, [1]: its inverse
+  float* rest;         // what the rounding of G left of the targets' entries (16 bits)
   float2* part;        // statistics, a row of `parts` for each token
   float* target_logit;
   void* dweight;
@@ -65,6 +66,8 @@ struct XentPrep {
   long long grad_step;
   const float* lse_in;
   float *losses, *lse_out, *each;  // each: losses by order, to be added up
+  float* rest;                     // see XentGemm
+  const void* layer;               // the weight as it was given
   int* place;                      // a token's place in the order, -1: none
   const float* sum;                // gradient of H: parts of the whole tiles' rows, sum_row elements each
   long long sum_row;
