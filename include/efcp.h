@@ -610,7 +610,8 @@ int efcp_dropout(const efcp_rms_norm* desc, const void* x, int64_t x_row, const 
  *                    where they lie, fp32 among them, are laid out there.
  * Products are exact and added up in fp32; fp32 operands are multiplied in three parts each, to about 2^-22.
  * The logits' gradient is rounded to bf16 or fp16 (with a common factor that keeps it in range) before the two
- * products that read it; it has all of fp32 where the operands do.  All sums have a fixed order, so results repeat bit
+ * products that read it, except for the entries of the targets, which have about twice as many bits; it has all of fp32
+ * where the operands do.  All sums have a fixed order, so results repeat bit
  * for bit.  Outputs overlap no input.  Work runs on the current device and on `stream`, asynchronously,
  * and can be captured in a graph.
  * EFCP_EINVAL (nothing enqueued): null or misaligned pointers, tokens outside 0 .. 2^30 - 1, vocab

@@ -83,6 +83,11 @@ __device__ __forceinline__ uint32_t of_first(uint32_t addr) {
 __device__ __forceinline__ void bar_arrive_pair(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// What this thread wrote to shared memory comes before; the waiting thread fences.
+__device__ __forceinline__ void bar_release_pair(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_pair() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
 
 // ------------------------------------------------------------------ tensor copies
 // One box of a three-dimensional map into this block's shared memory, counted on a barrier of the pair's first

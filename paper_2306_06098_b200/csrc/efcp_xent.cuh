@@ -14,6 +14,11 @@
 // more than 256 products of a sum, and the parts are added up in registers, rounded (SUMS): 0.9e-6 instead of 2.7e-6
 // off for the loss of four tokens with d = 768.
 //
+// With 16-bit operands the logits' gradient is rounded to their type, but for the entries of the targets, by far the largest: without
+// what that rounding leaves of them the gradients are 0.0017 off (2-norm, 2458 x 256 x 30522 bf16), with it below 0.0001, where the
+// results' own rounding is 0.0017.  The gradient of H gets it in k_xent_finish, the gradient of W in steps of its own, with the tokens
+// whose targets are near (XentGemm::hits).
+//
 // fp32 values are held as three bfloat16 ones (8 bits of the significand each), of whose nine products the six
 // largest are added up, the small ones first; what is left out is below 2^-24 of the result.
 #pragma once
@@ -71,6 +76,7 @@ struct XentTile {
   int m0, n0;     // rows and columns of the result
   int cols;       // width of the tile
   int k0, depth;  // first step along the sum, and steps
+  int rests;      // steps more, of what the rounding of G left (weight)
   int part;       // of the sum over the piece (hidden); tile of the columns (logits)
 };
 
@@ -81,8 +87,15 @@ struct XentWork {
   int shift, piece, v0, next_v0, col_tiles;  // pieces: the one that hidden and weight read, the one that logits writes
   int rows, next_cols;                       // of them: rows of W, columns
   long long hidden, weight, all;             // tiles of hidden; and of weight; and of logits
+  bool six;                                  // products for each step
 
-  __device__ __forceinline__ XentWork(const XentGemm& p, int count, int pairs, bool backward, bool six) {
+  // the words that tell of the rests for the piece's rows of W from m0 on
+  __device__ __forceinline__ const unsigned* hits(const XentGemm& p, int m0) const {
+    return p.hits + (long long)((v0 + m0) / kXentRows) * p.hit_words;
+  }
+
+  __device__ __forceinline__ XentWork(const XentGemm& p, int count, int pairs, bool backward, bool six_) {
+    six = six_;
     row_tiles = (count + kXentRows - 1) / kXentRows;
     shift = backward ? xent_shift(row_tiles, p.tiles, p.shifts) : 0;
     piece = p.piece << shift;
@@ -112,6 +125,7 @@ struct XentWork {
   }
   __device__ __forceinline__ XentTile tile(const XentGemm& p, long long t) const {
     XentTile r;
+    r.rests = 0;
     if (t < hidden) {
       const int2 mn = square(int(t), row_tiles, p.d_tiles * splits);
       const int n = mn.y / splits;
@@ -131,6 +145,8 @@ struct XentWork {
       r.cols = p.d_tile;
       r.part = r.k0 = 0;
       r.depth = token_steps;
+      if (!six)
+        for (int i = 0; i < p.hit_words; ++i) r.rests += __popc(hits(p, r.m0)[i]);
     } else {
       t -= weight;
       const int c = int(t / row_tiles);
@@ -284,6 +300,7 @@ __device__ __forceinline__ bool load_tile(const XentGemm& p, const XentWork& wor
       if (!tc::bar_wait(r.empty + 8 * s, (n / kStages + 1) & 1, gave_up)) return false;
       const uint32_t bar = r.full + 8 * s, a = r.stages + s * kStageBytes, b = a + kABytes;
       if (rank == 0) tc::bar_expect(r.full_here + 8 * s, bytes);
+      else tc::bar_arrive_pair(bar);
       if (KIND == kWeight) {
         tc::load_box(ma, a, bar, an, k, pa);
         tc::load_box(ma, a + kBoxBytes, bar, an + 64, k, pa);
@@ -298,6 +315,54 @@ __device__ __forceinline__ bool load_tile(const XentGemm& p, const XentWork& wor
       }
     }
   }
+  return true;
+}
+
+// (a warp) The steps of a tile of the layer's gradient that bring the rests of the targets' entries: of G's part of 64 tokens there is
+// one value a token, which is written to shared memory next to zeros.
+template <typename O>
+__device__ __forceinline__ bool load_rests(const XentGemm& p, const XentWork& work, const XentTile& w, const Ring& r, int count,
+                                           int rank, int lane, unsigned& n, volatile int* gave_up) {
+  const int first = work.v0 + w.m0 + rank * kBlockRows, bn = w.n0 + rank * (w.cols / 2);
+  const unsigned* const hits = work.hits(p, w.m0);
+  const bool wide = w.cols > 128;
+  for (int i = 0, left = w.rests; left; ++i)
+    for (unsigned word = hits[i]; word; word &= word - 1, --left, ++n) {
+      const int k = (i * 32 + __ffs(word) - 1) * kXentDepth;
+      const unsigned s = n % kStages;
+      if (!__all_sync(kAll, tc::bar_wait(r.empty + 8 * s, (n / kStages + 1) & 1, gave_up))) return false;
+      const uint32_t bar = r.full + 8 * s, a = r.stages + s * kStageBytes, b = a + kABytes;
+      int col[2];  // of this lane's two tokens
+      float rest[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int token = k + 32 * j + lane;
+        col[j] = token < count ? p.target[token] - first : -1;
+        rest[j] = col[j] >= 0 && col[j] < kBlockRows ? p.rest[token] : 0.f;
+      }
+#pragma unroll 8
+      for (uint32_t at = lane * 16; at < kABytes; at += 512)
+        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(a + at), "r"(0) : "memory");
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int row = 32 * j + lane, c = col[j];
+        if (c < 0 || c >= kBlockRows) continue;
+        const O v = from_f32<O>(rest[j]);
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(a + (c >> 6) * kBoxBytes + row * 128 +
+                                                     ((((c & 63) >> 3) ^ (row & 7)) << 4) + (c & 7) * 2),
+                     "h"(reinterpret_cast<const uint16_t&>(v))
+                     : "memory");
+      }
+      tc::fence_copies();
+      __syncwarp();
+      if (lane == 0) {
+        if (rank == 0) tc::bar_expect(r.full_here + 8 * s, 2 * uint32_t(w.cols) * 64);
+        else tc::bar_release_pair(bar);
+        tc::load_box(&p.hidden_cols, b, bar, bn, k, 0);
+        if (wide) tc::load_box(&p.hidden_cols, b + kBoxBytes, bar, bn + 64, k, 0);
+      }
+    }
   return true;
 }
 
@@ -319,7 +384,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
   if (threadIdx.x == 0) {
     gave_up_ = 0;
     for (int i = 0; i < kStages; ++i) {
-      tc::bar_init(full + 8 * i, 1);
+      tc::bar_init(full + 8 * i, 2);  // a thread of either block
       tc::bar_init(empty + 8 * i, 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -343,20 +408,25 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
   if (warp >= kOutWarps) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
   if (warp == kOutWarps) {
-    if (lane == 0) {
-      const Ring ring_of{ring, empty, tc::of_first(full), full};
-      unsigned n = 0;  // steps so far
-      bool ok = true;
-      for (long long t = pair; t < work.all && ok; t += pairs) {
-        const XentTile w = work.tile(p, t);
-        if (w.kind == kLogits) ok = load_tile<kLogits, kPairs>(p, work, w, ring_of, rank, n, gave_up);
-        else if (w.kind == kHidden) ok = load_tile<kHidden, kPairs>(p, work, w, ring_of, rank, n, gave_up);
-        else ok = load_tile<kWeight, kPairs>(p, work, w, ring_of, rank, n, gave_up);
+    const Ring ring_of{ring, empty, tc::of_first(full), full};
+    unsigned n = 0;  // steps so far
+    bool ok = true;
+    for (long long t = pair; t < work.all && ok; t += pairs) {
+      const XentTile w = work.tile(p, t);
+      if constexpr (BACKWARD && kPairs == 1)
+        if (w.rests) ok = load_rests<O>(p, work, w, ring_of, count, rank, lane, n, gave_up);
+      if (ok && lane == 0) {
+        unsigned m = n;
+        if (w.kind == kLogits) ok = load_tile<kLogits, kPairs>(p, work, w, ring_of, rank, m, gave_up);
+        else if (w.kind == kHidden) ok = load_tile<kHidden, kPairs>(p, work, w, ring_of, rank, m, gave_up);
+        else ok = load_tile<kWeight, kPairs>(p, work, w, ring_of, rank, m, gave_up);
       }
-      if (!ok) {  // nothing may land in shared memory that the block has left: copies take microseconds
-        const uint64_t start = tc::clock_ns();
-        while (tc::clock_ns() - start < tc::kDrainNs) {
-        }
+      n += unsigned(w.depth * kPairs);
+      ok = __all_sync(kAll, ok);
+    }
+    if (!ok && lane == 0) {  // nothing may land in shared memory that the block has left: copies take microseconds
+      const uint64_t start = tc::clock_ns();
+      while (tc::clock_ns() - start < tc::kDrainNs) {
       }
     }
     __syncwarp();
@@ -369,7 +439,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
         const bool a_mn = w.kind == kWeight, b_mn = w.kind != kLogits;
         const uint32_t ins = tc::instruction(std::is_same_v<O, __nv_bfloat16>, kXentRows, w.cols, a_mn, b_mn);
         const uint32_t a_step = a_mn ? 2048 : 32, b_step = b_mn ? 2048 : 32;
-        const int steps = w.depth * kPairs, most = kSums ? kPart : steps;
+        const int steps = w.depth * kPairs + w.rests, most = kSums ? kPart : steps;
         int i = 0;
         do {  // an accumulator: the whole sum, or parts of it
           const unsigned buf = turn & 1;
@@ -380,6 +450,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
             const unsigned s = n % kStages;
             ok = tc::bar_wait(full + 8 * s, (n / kStages) & 1, gave_up);
             if (!ok) break;
+            if (i < w.rests) tc::fence_pair();  // (operands that threads of both blocks have written)
             tc::fence_after();
             const uint32_t a = ring + s * kStageBytes, b = a + kABytes;
 #pragma unroll
@@ -412,7 +483,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
       const XentTile w = work.tile(p, t);
       const int row0 = w.m0 + rank * kBlockRows + quarter * 32, row = row0 + lane;
       const int cols = w.cols / 2, n0 = w.n0 + half * cols;
-      const int steps = w.depth * kPairs;
+      const int steps = w.depth * kPairs + w.rests;
       int target = -1;
       float lse = 0.f, coef = 0.f;
       if (w.kind == kLogits) {
@@ -581,10 +652,14 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
   if (threadIdx.x == 0 && gave_up_) atomicExch(p.status, EFCP_ETIMEOUT);
 }
 
+constexpr int kBuckets = 1024;  // of targets
+
 // What comes before the products: which tokens have a target, in order; their rows of H, one behind the other (and
 // zeros up to whole tiles), as the copies of tiles want them; backward also the factors on their gradients, times a
 // power of two that brings the largest near 1 (near 2^14 for fp16, whose probabilities would vanish otherwise); and
-// zeros for what belongs to the other tokens.
+// zeros for what belongs to the other tokens.  Where the rests of the targets' entries are asked for (p.hits) the order goes by
+// the targets' tiles first, so that a tile of rows of W meets its targets in few steps (2458 tokens x 30522 classes: in one or two of
+// 39; in the tokens' own order it would be 16).
 //
 // A block takes a run of tokens.  It counts those with a target before its own by itself, so that one launch is
 // enough: all targets pass through every block, 8 bytes for each row of H.
@@ -594,7 +669,8 @@ __global__ void __launch_bounds__(512) k_xent_prepare(const XentPrep p, bool bac
   using O = Operand<T>;
   constexpr int kPlanes = std::is_same_v<T, float> ? 3 : 1;
   constexpr bool kHalf = std::is_same_v<T, __half>;
-  __shared__ int before_, all_, places[512 / 32], tokens[512];
+  __shared__ int before_, all_, places[512 / 32], tokens[512], rows[512];
+  __shared__ int bucket[512], bucket_all[kBuckets], bucket_at[kBuckets];  // (sorted)
   __shared__ unsigned most_;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long lo = (long long)blockIdx.x * per, hi = min(p.tokens, lo + per);
@@ -605,12 +681,25 @@ __global__ void __launch_bounds__(512) k_xent_prepare(const XentPrep p, bool bac
   __syncthreads();
   int before = 0, all = 0;
   float big = 0.f;
-  const bool each = backward && p.reduction == 0;
+  const bool each = backward && p.reduction == 0, sorted = p.hits;
+  const int tiles = (p.vocab - 1) / kXentRows;
+  int wide = 0;  // a bucket's tiles of rows of W: 2^wide
+  while (tiles >> wide >= kBuckets) ++wide;
+  const auto bucket_of = [&](long long t) { return t >= 0 && t < p.vocab ? int(t / kXentRows) >> wide : 0; };
+  if (sorted) {
+    for (int i = threadIdx.x; i < kBuckets; i += 512) bucket_all[i] = bucket_at[i] = 0;
+    __syncthreads();
+  }
 #pragma unroll 8
   for (long long i = threadIdx.x; i < p.tokens; i += 512) {
-    const bool used = p.targets[i] != p.ignore;
+    const long long t = p.targets[i];
+    const bool used = t != p.ignore;
     all += used;
     before += used && i < lo;
+    if (sorted && used) {  // (whole numbers: any order)
+      atomicAdd(&bucket_all[bucket_of(t)], 1);
+      if (i < lo) atomicAdd(&bucket_at[bucket_of(t)], 1);
+    }
     if (each && used) {
       const float g = fabsf(p.grad[i * p.grad_step]);
       if (g < INFINITY) big = fmaxf(big, g);
@@ -625,6 +714,21 @@ __global__ void __launch_bounds__(512) k_xent_prepare(const XentPrep p, bool bac
     atomicMax(&most_, __float_as_uint(big));  // (of values that are not negative the bits are in order)
   }
   __syncthreads();
+  if (sorted) {  // where the block's next token of each bucket goes
+    const int k = 2 * threadIdx.x, two = bucket_all[k] + bucket_all[k + 1];
+    int sum = two;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int other = __shfl_up_sync(kAll, sum, o);
+      if (lane >= o) sum += other;
+    }
+    if (lane == 31) places[warp] = sum;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) sum += places[w];
+    bucket_at[k] += sum - two;
+    bucket_at[k + 1] += sum - two + bucket_all[k];
+    __syncthreads();
+  }
   all = all_;
   int at = before_;
   const int padded = (all + kXentRows - 1) / kXentRows * kXentRows;
@@ -672,14 +776,23 @@ __global__ void __launch_bounds__(512) k_xent_prepare(const XentPrep p, bool bac
     const bool used = t != p.ignore;
     const unsigned mask = __ballot_sync(kAll, used);
     if (lane == 0) places[warp] = __popc(mask);
+    if (sorted) bucket[threadIdx.x] = used ? bucket_of(t) : -1;
     __syncthreads();
     int first = 0, here = 0;  // tokens with a target before this warp's; of the block
     for (int k = 0; k < 512 / 32; ++k) {
       if (k < warp) first += places[k];
       here += places[k];
     }
-    const int local = first + __popc(mask & ((1u << lane) - 1)), place = at + local;
-    if (used) tokens[local] = int(i);
+    const int local = first + __popc(mask & ((1u << lane) - 1));
+    int place = at + local;
+    if (sorted && used) {
+      place = bucket_at[bucket[threadIdx.x]];
+      for (int k = 0; k < threadIdx.x; ++k) place += bucket[k] == bucket[threadIdx.x];
+    }
+    if (used) {
+      tokens[local] = int(i);
+      rows[local] = place;
+    }
     if (i < hi) {
       if (p.place) p.place[i] = used ? place : -1;
       if (used) {
@@ -698,10 +811,11 @@ __global__ void __launch_bounds__(512) k_xent_prepare(const XentPrep p, bool bac
       }
     }
     __syncthreads();
+    if (sorted && used) atomicAdd(&bucket_at[bucket[threadIdx.x]], 1);
 #pragma unroll 2
     for (int k = warp; k < here * chunks; k += 512 / 32) {
       const int token = k / chunks;
-      copy(tokens[token], at + token, (k - token * chunks) * 256);
+      copy(tokens[token], rows[token], (k - token * chunks) * 256);
     }
     at += here;
     __syncthreads();

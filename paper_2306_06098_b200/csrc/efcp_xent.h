@@ -33,6 +33,8 @@ struct XentGemm {
   const float* coef;   // factor on a token's gradient
   const float* scale;  // [0]: the factor that coef holds, [1]: its inverse
   float* rest;         // what the rounding of G left of the targets' entries (16 bits)
+  const unsigned* hits;  // for each tile of rows of W `hit_words` words: the steps of 64 tokens that have a target there (16 bits)
+  int hit_words;
   float2* part;        // statistics, a row of `parts` for each token
   float* target_logit;
   void* dweight;
@@ -69,6 +71,8 @@ struct XentPrep {
   float* rest;                     // see XentGemm
   const void* layer;               // the weight as it was given
   int* place;                      // a token's place in the order, -1: none
+  unsigned* hits;                  // see XentGemm; null: not wanted
+  int hit_words;
   const float* sum;                // gradient of H: parts of the whole tiles' rows, sum_row elements each
   long long sum_row;
   int d_tiles, piece, tiles, shifts, pairs;
@@ -138,5 +142,6 @@ cudaError_t few_launch_f32(const XentFew& p, bool vec, bool backward, cudaStream
 cudaError_t few_launch_bf16(const XentFew& p, bool vec, bool backward, cudaStream_t st);
 cudaError_t few_launch_f16(const XentFew& p, bool vec, bool backward, cudaStream_t st);
 cudaError_t xent_join(const XentPrep& p, int sms, cudaStream_t st);
+cudaError_t xent_hits(const XentPrep& p, int sms, cudaStream_t st);
 
 }  // namespace efcp

@@ -1,0 +1,61 @@
+"""Softmax cross entropy of a linear layer: what its roundings leave, held to bounds that a mistake in one part alone exceeds.
+Such mistakes are planted in the 64-bit results, which then have to lie outside of the bounds."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_cross_entropy import HALF, SUM, TINY, U, B, definition, grads, inputs
+
+pytestmark = pytest.mark.gpu
+
+
+def inside(got, want, bound, dtype):
+    return ((got.double() - want).abs() <= bound + HALF[dtype] * (want.abs() + bound) + TINY[dtype]).all()
+
+
+# few tokens next to the classes, so that the targets' entries make up the gradients; d that is no multiple of a tile; one tile of
+# classes; several pieces of the vocabulary, as they are and widened
+@pytest.mark.parametrize("n,d,v,labelled", [(40, 64, 3000, 1.0), (300, 72, 5003, 1.0), (130, 300, 4096, 0.5), (14, 40, 120, 1.0),
+                                            (16300, 24, 30011, 1.0), (16300, 24, 30011, 0.1), (16300, 40, 9001, 0.01), (2500, 128, 30522, 1.0), (40, 8, 300000, 1.0)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_entries_of_the_targets(n, d, v, labelled, dtype):
+    """Both gradients, where the other entries of the logits' gradient are rounded to the operands' type once, and those of the
+    targets are not."""
+    hidden, weight, targets = inputs(n, d, v, dtype, 7, labelled, size=0.05)
+    grad = grads(n)
+    _, lse = B().cross_entropy_forward(hidden, weight, targets, -100, "none")
+    dh, dw = B().cross_entropy_backward(grad, hidden, weight, targets, lse, -100, "none")
+    assert torch.equal(B().cross_entropy_backward(grad, hidden, weight, targets, lse, -100, "none", (False, True))[1], dw)
+    assert torch.equal(B().cross_entropy_backward(grad, hidden, weight, targets, lse, -100, "none", (True, False))[0], dh)
+    B().operators_status()
+    used, h, w, t, logits, lse64, _, off = definition(hidden, weight, targets)
+    count, g = t.numel(), grad[used].double()[:, None]
+    each = torch.arange(count, device="cuda")
+    p = torch.exp(logits - lse64[:, None])
+    G = g * p
+    G[each, t] -= g[:, 0]
+    # before the rounding: as in test_gpu_cross_entropy.py
+    dG = g.abs() * p * (2 * off + SUM + 2 * U * lse64.abs() + 4 * U)[:, None] + 3 * U * G.abs()
+    dG[each, t] += 2 * U * g[:, 0].abs()
+    del logits, p
+    # a common factor brings the largest near 1 (bf16) or 2^14 (fp16); a value that near a border may go to either side
+    up = 2.0 ** ((14 if dtype == torch.float16 else 0) - math.floor(math.log2(g.abs().max().item())))
+
+    def rounded(x):
+        return (x * up).to(dtype).double() / up
+
+    once, half = rounded(G), HALF[dtype]
+    dG += torch.where(rounded(G - dG) == rounded(G + dG), 0.0, 2 * half * G.abs())
+    dG[each, t] += half * half * G[each, t].abs()  # in two parts
+    exact = once.clone()
+    exact[each, t] = G[each, t]
+    bound_h = dG @ w.abs() + ((v / 8 + 8) + 300) * 2.0 ** -23 * (G.abs() @ w.abs())
+    bound_w = dG.t() @ h.abs() + (count / 8 + 8) * 2.0 ** -23 * (G.abs().t() @ h.abs())
+    want_h, want_w = exact @ w, exact.t() @ h
+    # the targets' entries rounded like the others  (fp32 sums over many classes may be as far off as fp16's half step)
+    assert not inside((once.t() @ h).to(dtype), want_w, bound_w, dtype)
+    if v / 8 * 2.0 ** -23 < half / 4:
+        assert not inside((once @ w).to(dtype), want_h, bound_h, dtype)
+    assert inside(dh[used], want_h, bound_h, dtype)
+    assert inside(dw, want_w, bound_w, dtype)
