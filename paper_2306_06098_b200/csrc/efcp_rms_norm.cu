@@ -37,7 +37,7 @@ bool valid(const efcp_rms_norm* d) {
   if (d->dtype < 0 || d->dtype > 2 || d->param_dtype < 0 || d->param_dtype > 2) return false;
   if (!(d->eps >= 0.f) || !std::isfinite(d->eps)) return false;
   if (!(d->p >= 0. && d->p <= 1.)) return false;
-  return reinterpret_cast<uintptr_t>(d->rng) % 8 == 0;
+  return d->p == 0. || reinterpret_cast<uintptr_t>(d->rng) % 8 == 0;
 }
 
 bool misaligned(const void* p, int bytes) {
@@ -60,7 +60,8 @@ Drop drop_of(const efcp_rms_norm* d) {
   r.scale = r.threshold < 65536 ? 65536.f / float(65536 - r.threshold) : 0.f;
   r.seed = d->seed;
   r.offset = d->offset;
-  r.rng = reinterpret_cast<const unsigned long long*>(d->rng);
+  // (kernels read what this points to, whether anything is dropped or not)
+  r.rng = r.threshold ? reinterpret_cast<const unsigned long long*>(d->rng) : nullptr;
   return r;
 }
 
