@@ -62,6 +62,9 @@ struct Ring {
   int at = 0;  // place of the running unit, and the phase of its barrier
   uint32_t phase = 0;
   uint32_t plain = 0;  // see prepare()
+  bool lost = false;   // a wait of this thread has run out
+  long long asked = 0;  // (the asking thread) units asked for
+  uint64_t limit = tc::kWaitNs;
 
   __device__ __forceinline__ uint32_t place(int s) const { return data + uint32_t(s * q.inputs * q.unit_bytes); }
   __device__ __forceinline__ void next() {
@@ -121,9 +124,11 @@ struct Ring {
     }
   }
 
-  // (one thread) unit u into place s
-  __device__ __forceinline__ void ask(long long u, int s) const {
-    if (u >= units) return;
+  // (one thread) unit u into place s.  Not when the wait for what is there has run out: its copies may still come, and the
+  // barrier is not done with them.
+  __device__ __forceinline__ void ask(long long u, int s) {
+    if (u >= units || lost) return;
+    ++asked;
     const int of_unit = q.rows * q.reps;
     const long long row = u * of_unit;
     const int rows = int(min((long long)of_unit, p.rows - row));
@@ -179,14 +184,15 @@ struct Ring {
            sub * (whole ? q.row_bytes : q.pitch) + col;
   }
   // The running unit has arrived.  When the limit passes the work goes on with whatever lies there (the warps of a
-  // group keep meeting), no further wait is long, and the status tells.
-  __device__ __forceinline__ void await() const { (void)tc::bar_wait(bars + 8 * at, phase, gave_up); }
-  // Nothing may land in shared memory that the block has left.  (Asked for: all units before the `asked`-th.)
-  __device__ __forceinline__ void end(long long asked) const {
+  // group keep meeting) without further waits, and the status tells.
+  __device__ __forceinline__ void await() {
+    if (!lost) lost = !tc::bar_wait(bars + 8 * at, phase, gave_up, limit);
+  }
+  // Nothing may land in shared memory that the block has left.
+  __device__ __forceinline__ void end() const {
     if (!*(volatile int*)gave_up) return;
     for (long long n = asked < q.stages ? 0 : asked - q.stages; n < asked; ++n)
-      if (first + n * step < units)
-        (void)tc::bar_wait(bars + 8 * int(n % q.stages), uint32_t(n / q.stages) & 1, gave_up, tc::kDrainNs);
+      (void)tc::bar_wait(bars + 8 * int(n % q.stages), uint32_t(n / q.stages) & 1, gave_up, tc::kDrainNs);
   }
 };
 
@@ -443,8 +449,7 @@ __global__ void __launch_bounds__(256, 2) k_rms_forward_ring(const Rms p, const 
   const bool two = SUM && p.residual, kept = SUM && p.h;
   const uint32_t x0 = r.offset(0, me.sub, me.c), res0 = two ? r.offset(1, me.sub, me.c) : 0;
   unsigned odd = 0;
-  long long n = 0;
-  for (long long u = r.first; u < r.units; u += r.step, ++n) {
+  for (long long u = r.first; u < r.units; u += r.step) {
     r.await();
     for (int rep = 0; rep < q.reps; ++rep, odd ^= 1) {
       const long long row = (u * q.reps + rep) * q.rows + me.sub;
@@ -560,7 +565,7 @@ __global__ void __launch_bounds__(256, 2) k_rms_forward_ring(const Rms p, const 
     }
     r.next();
   }
-  if (asks) r.end(n + q.stages);
+  if (asks) r.end();
   if (threadIdx.x == 0 && *(volatile int*)&gave_up) atomicExch(p.status, EFCP_ETIMEOUT);
 }
 
@@ -600,9 +605,8 @@ __global__ void __launch_bounds__(256, 2) k_rms_backward_ring(const Rms p, const
     a.get(w);
   };
   unsigned odd = 0;
-  long long n = 0;
   float next = rstd_of(r.first, 0);
-  for (long long u = r.first; u < r.units; u += r.step, ++n) {
+  for (long long u = r.first; u < r.units; u += r.step) {
     r.await();
     for (int rep = 0; rep < q.reps; ++rep, odd ^= 1) {
       const long long row = (u * q.reps + rep) * q.rows + me.sub;
@@ -685,7 +689,7 @@ __global__ void __launch_bounds__(256, 2) k_rms_backward_ring(const Rms p, const
     }
     r.next();
   }
-  if (asks) r.end(n + q.stages);
+  if (asks) r.end();
   __syncthreads();
   if (threadIdx.x == 0 && gave_up) atomicExch(p.status, EFCP_ETIMEOUT);
   if (p.part) {
