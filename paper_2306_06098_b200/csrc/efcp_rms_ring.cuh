@@ -196,6 +196,12 @@ struct Ring {
   }
 };
 
+// (all threads) Tells when a wait of any group has run out.  Groups come here at different times, so the block meets first.
+__device__ __forceinline__ void ring_tell(int* status, volatile int* gave_up) {
+  __syncthreads();
+  if (threadIdx.x == 0 && *gave_up) atomicExch(status, EFCP_ETIMEOUT);
+}
+
 // Barriers, and the group that a warp belongs to.  (Up to 8 groups of up to 4 places.)
 template <typename T, int INPUTS, bool ODD>
 __device__ __forceinline__ Ring<T, INPUTS, ODD> ring_begin(const Rms& p, const RmsRing& q, unsigned char* smem,
@@ -566,7 +572,7 @@ __global__ void __launch_bounds__(256, 2) k_rms_forward_ring(const Rms p, const 
     r.next();
   }
   if (asks) r.end();
-  if (threadIdx.x == 0 && *(volatile int*)&gave_up) atomicExch(p.status, EFCP_ETIMEOUT);
+  ring_tell(p.status, &gave_up);
 }
 
 // K: chunks of a warp; it holds their sums of the weight's gradient in registers.
@@ -690,8 +696,7 @@ __global__ void __launch_bounds__(256, 2) k_rms_backward_ring(const Rms p, const
     r.next();
   }
   if (asks) r.end();
-  __syncthreads();
-  if (threadIdx.x == 0 && gave_up) atomicExch(p.status, EFCP_ETIMEOUT);
+  ring_tell(p.status, &gave_up);
   if (p.part) {
     // The rows of a block's warps, each in its place of shared memory (the rings are done with), are added up in order.
     float* sums = reinterpret_cast<float*>(smem + q.data_at);

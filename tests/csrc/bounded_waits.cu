@@ -44,6 +44,23 @@ __global__ void k_ring(const Rms p, const RmsRing q, int* out) {
   r.end();
 }
 
+// A block of two groups: one comes to its end while the other's wait is still running out.  out: the status; what the first would
+// have told by itself
+__global__ void k_late(int* out) {
+  __shared__ alignas(8) uint64_t bar;
+  __shared__ int gave_up;
+  if (threadIdx.x == 0) {
+    gave_up = 0;
+    tc::bar_init(tc::smem_of(&bar), 1);
+    tc::bar_init_fence();
+    out[0] = 0;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) out[1] = *(volatile int*)&gave_up;
+  if (threadIdx.x >= 32) (void)tc::bar_wait(tc::smem_of(&bar), 0, &gave_up, kLimit);
+  ring_tell(out, &gave_up);
+}
+
 }  // namespace
 }  // namespace efcp
 
@@ -52,6 +69,8 @@ using namespace efcp;
 extern "C" int probe(int which, const float* x, int* out) {
   if (which == 0) {
     k_wait<<<1, 1>>>(out);
+  } else if (which == 1) {
+    k_late<<<1, 64>>>(out);
   } else {
     Rms p{};
     p.rows = 4;

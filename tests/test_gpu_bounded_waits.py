@@ -7,7 +7,7 @@ import subprocess
 import pytest
 import torch
 
-from paper_2306_06098_b200 import build
+from paper_2306_06098_b200 import binding, build
 
 pytestmark = pytest.mark.gpu
 
@@ -36,4 +36,24 @@ def test_a_wait_ends(probe):
 
 def test_a_ring_asks_for_nothing_when_a_wait_has_run_out(probe):
     """The place's copies may still be under way, and its barrier takes one arrival for each phase."""
-    assert probe(1) == [0, 1, 0, 1]
+    assert probe(2) == [0, 1, 0, 1]
+
+
+def test_a_wait_that_runs_out_late_is_told(probe):
+    assert probe(1)[:2] == [binding.ETIMEOUT, 0]
+
+
+def test_the_status_raises(monkeypatch):
+    class Library:
+        code = binding.OK
+
+        def __getattr__(self, name):
+            return (lambda: self.code) if name == "efcp_operators_status" else getattr(library, name)
+
+    library, fake = binding._lib, Library()
+    monkeypatch.setattr(binding, "_lib", fake)
+    binding.operators_status()
+    fake.code = binding.ETIMEOUT
+    with pytest.raises(binding.EfcpError) as raised:
+        binding.operators_status()
+    assert raised.value.code == binding.ETIMEOUT
