@@ -1,6 +1,7 @@
 """Dropout for training with torch.autograd (argument marshalling only): the CUDA library behind `binding`
 computes the mask from a counter in both directions, and nothing but the counter is kept in between.
 """
+import threading
 from typing import Optional
 
 import torch
@@ -19,7 +20,8 @@ class _Dropout(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        rng = ctx.saved_tensors[0] if ctx.saved_tensors else ctx.rng
+        saved = ctx.saved_tensors  # (a checkpointed pass hands them out once)
+        rng = saved[0] if saved else ctx.rng
         dx = binding.dropout(dy, ctx.p, rng) if ctx.needs_input_grad[0] else None
         return dx, dy if ctx.residual else None, None, None
 
@@ -41,15 +43,64 @@ def new_rng(seed: Optional[int] = None, device=None) -> torch.Tensor:
 
 def take(rng: torch.Tensor) -> torch.Tensor:
     """The state to use now, as a copy; `rng` moves on to the next one, on the device: in a captured graph at
-    each replay."""
-    now = rng.clone()
-    rng[1:].add_(1)
+    each replay.  Where torch.utils.checkpoint computes a forward pass again, inside the backward pass, the masks
+    have to be those of the first time: see `checkpoint_contexts`, without which this raises there."""
+    tapes = _tapes()
+    again = max((i for i, t in enumerate(tapes) if t.again), default=-1)
+    if again >= 0:
+        now = tapes[again].next()
+    elif torch._C._current_graph_task_id() != -1:
+        raise RuntimeError("a generator was asked for its next state inside a backward pass, where it would give another mask "
+                           "than in the forward pass: use torch.utils.checkpoint.checkpoint(..., use_reentrant=False, "
+                           "context_fn=dropout.checkpoint_contexts)")
+    else:
+        now = rng.clone()
+        rng[1:].add_(1)
+    for t in tapes[again + 1:]:
+        t.states.append(now)
     return now
 
 
+_local = threading.local()  # (a backward pass has threads of its own)
+
+
+def _tapes() -> list:
+    if not hasattr(_local, "tapes"):
+        _local.tapes = []
+    return _local.tapes
+
+
+class _Tape:
+    """Inside of it states that are taken are written down, or (again) come from what was written."""
+
+    def __init__(self, states: list, again: bool):
+        self.states, self.again, self.at = states, again, 0
+
+    def next(self) -> torch.Tensor:
+        if self.at == len(self.states):
+            raise RuntimeError("a forward pass that was computed again asked for more generator states than the first time")
+        self.at += 1
+        return self.states[self.at - 1]
+
+    def __enter__(self):
+        self.at = 0
+        _tapes().append(self)
+
+    def __exit__(self, *_):
+        _tapes().remove(self)
+
+
+def checkpoint_contexts():
+    """The context_fn for torch.utils.checkpoint.checkpoint(f, ..., use_reentrant=False): modules with a generator of
+    their own take the same states, and so draw the same masks, when f is computed again."""
+    states = []
+    return _Tape(states, False), _Tape(states, True)
+
+
 class Dropout(torch.nn.Module):
-    """torch.nn.Dropout(p) with a generator of its own, in a buffer (so that a checkpoint goes on with the
-    same masks); forward(x, residual) adds the residual in the same pass."""
+    """torch.nn.Dropout(p) with a generator of its own, in a buffer (so that a saved model goes on with the
+    same masks); forward(x, residual) adds the residual in the same pass.  Inside of torch.utils.checkpoint: see
+    `checkpoint_contexts`."""
 
     def __init__(self, p: float = 0.5, seed: Optional[int] = None, device=None):
         super().__init__()

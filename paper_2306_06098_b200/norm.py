@@ -102,7 +102,8 @@ def add_rms_norm(x: torch.Tensor, residual: torch.Tensor, weight: Optional[torch
 class RMSNorm(torch.nn.Module):
     """Root-mean-square norm of the last dimension, of size d.  forward(x) normalises x;
     forward(x, residual) returns the norm of h = dropout(x) + residual, and h.  The dropout of share p is
-    active in training, with a generator of its own in a buffer."""
+    active in training, with a generator of its own in a buffer (inside of torch.utils.checkpoint: see
+    dropout.checkpoint_contexts)."""
 
     def __init__(self, d: int, eps: float = 1e-6, affine: bool = True, p: float = 0.0,
                  seed: Optional[int] = None, device=None, dtype=None):
