@@ -97,9 +97,48 @@ def checkpoint_contexts():
     return _Tape(states, False), _Tape(states, True)
 
 
-class Dropout(torch.nn.Module):
-    """torch.nn.Dropout(p) with a generator of its own, in a buffer (so that a saved model goes on with the
-    same masks); forward(x, residual) adds the residual in the same pass.  Inside of torch.utils.checkpoint: see
+class WithGenerator(torch.nn.Module):
+    """A module with a generator of its own: its state `rng` (None: it has none) is saved, loaded and moved with the module.
+    It is no buffer, since DistributedDataParallel gives all processes the buffers of the first one before each forward
+    pass: they would drop the same elements of their own batches.  (They do when they are given equal seeds.)"""
+    rng: Optional[torch.Tensor] = None
+
+    def _apply(self, fn, *args, **kwargs):
+        super()._apply(fn, *args, **kwargs)
+        if self.rng is not None:
+            self.rng = fn(self.rng)
+        return self
+
+    def _save_to_state_dict(self, destination, prefix, keep_vars):
+        super()._save_to_state_dict(destination, prefix, keep_vars)
+        if self.rng is not None:
+            destination[prefix + "rng"] = self.rng
+
+    def _load_from_state_dict(self, state_dict, prefix, local_metadata, strict, missing_keys, unexpected_keys,
+                              error_msgs):
+        super()._load_from_state_dict(state_dict, prefix, local_metadata, strict, missing_keys, unexpected_keys,
+                                      error_msgs)
+        name = prefix + "rng"
+        if self.rng is None:
+            return
+        if name not in state_dict:
+            if strict:
+                missing_keys.append(name)
+            return
+        if name in unexpected_keys:
+            unexpected_keys.remove(name)
+        given = state_dict[name]
+        if not isinstance(given, torch.Tensor) or given.shape != self.rng.shape or given.dtype != self.rng.dtype:
+            error_msgs.append(f"{name}: an int64 tensor of (seed, offset) expected")
+        elif local_metadata.get("assign_to_params_buffers", False):
+            self.rng = given
+        else:
+            self.rng.copy_(given)
+
+
+class Dropout(WithGenerator):
+    """torch.nn.Dropout(p) with a generator of its own (saved with the model, so that it goes on with the same masks);
+    forward(x, residual) adds the residual in the same pass.  Inside of torch.utils.checkpoint: see
     `checkpoint_contexts`."""
 
     def __init__(self, p: float = 0.5, seed: Optional[int] = None, device=None):
@@ -107,7 +146,7 @@ class Dropout(torch.nn.Module):
         if not 0 <= p <= 1:
             raise ValueError("p: between 0 and 1")
         self.p = p
-        self.register_buffer("rng", new_rng(seed, device))
+        self.rng = new_rng(seed, device)
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
         if not self.training or self.p == 0:

@@ -9,7 +9,7 @@ from typing import Optional, Tuple
 import torch
 
 from . import binding
-from .dropout import new_rng, take
+from .dropout import WithGenerator, new_rng, take
 
 
 class _GroupNormAct(torch.autograd.Function):
@@ -99,10 +99,10 @@ def add_rms_norm(x: torch.Tensor, residual: torch.Tensor, weight: Optional[torch
     return _RmsNorm.apply(x, residual, weight, eps, p, rng)
 
 
-class RMSNorm(torch.nn.Module):
+class RMSNorm(WithGenerator):
     """Root-mean-square norm of the last dimension, of size d.  forward(x) normalises x;
     forward(x, residual) returns the norm of h = dropout(x) + residual, and h.  The dropout of share p is
-    active in training, with a generator of its own in a buffer (inside of torch.utils.checkpoint: see
+    active in training, with a generator of its own (inside of torch.utils.checkpoint: see
     dropout.checkpoint_contexts)."""
 
     def __init__(self, d: int, eps: float = 1e-6, affine: bool = True, p: float = 0.0,
@@ -113,7 +113,7 @@ class RMSNorm(torch.nn.Module):
         if not 0 <= p <= 1:
             raise ValueError("p: between 0 and 1")
         self.d, self.eps, self.p = d, eps, p
-        self.register_buffer("rng", new_rng(seed, device) if p else None)
+        self.rng = new_rng(seed, device) if p else None
         if affine:
             self.weight = torch.nn.Parameter(torch.ones(d, device=device, dtype=dtype))
         else:
