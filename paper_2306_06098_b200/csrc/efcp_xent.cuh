@@ -10,9 +10,8 @@
 // tensor cores fill the other; a warp of the first block issues the products.  Every wait is bounded; when one runs out
 // the blocks end, and the status tells of it.
 //
-// The tensor cores cut what they add up to fp32 instead of rounding it.  Where results are fp32, an accumulator holds no
-// more than 256 products of a sum, and the parts are added up in registers, rounded (SUMS): 0.9e-6 instead of 2.7e-6
-// off for the loss of four tokens with d = 768.
+// The tensor cores cut what they add up to fp32 instead of rounding it, 16 products at a time.  Where results are fp32, an accumulator
+// holds 128 or 256 products of a sum (part_of), and the parts are added up in registers, rounded (SUMS).
 //
 // With 16-bit operands the logits' gradient is rounded to their type, but for the entries of the targets, by far the largest: without
 // what that rounding leaves of them the gradients are 0.0017 off (2-norm, 2458 x 256 x 30522 bf16), with it below 0.0001, where the
@@ -47,7 +46,6 @@ constexpr uint32_t kStageBytes = kABytes + kBBytes;
 constexpr uint32_t kOutBytes = 32 * 128;        // a warp's box of results
 constexpr size_t kXentSmem = kStages * kStageBytes + kOutWarps * kOutBytes + 1024;
 constexpr int kSquare = 8;                      // rows of tiles that pairs work on side by side
-constexpr int kPart = 8;                        // steps of an accumulator with SUMS
 constexpr float kLog2e = 1.4426950408889634f;
 
 template <typename T>
@@ -70,6 +68,19 @@ __device__ __forceinline__ void split(float x, O (&v)[PLANES]) {
 }
 
 enum XentKind { kHidden, kWeight, kLogits };
+
+// Steps of an accumulator, from step i of a tile on.  What the tensor cores cut is of the size of the running sum: of fp32 operands the
+// products of the largest parts come last, and the others may be added up longer.  (Mean error of lse, 1003 x 509 x 10007 fp32:
+// -0.9e-6; with eight steps for all -3.4e-6, and no faster.  2048 x 4096 x 8000 fp16: four steps -2.1e-6, eight -4.0e-6.)
+template <bool F32, bool BACKWARD>
+__device__ __forceinline__ int part_of(int i, int depth, int steps) {
+  if constexpr (F32) {
+    const int small = 5 * depth;
+    return i < small ? min(32, small - i) : min(2, steps - i);
+  } else {
+    return BACKWARD ? steps : min(4, steps - i);
+  }
+}
 
 struct XentTile {
   XentKind kind;
@@ -439,14 +450,15 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
         const bool a_mn = w.kind == kWeight, b_mn = w.kind != kLogits;
         const uint32_t ins = tc::instruction(std::is_same_v<O, __nv_bfloat16>, kXentRows, w.cols, a_mn, b_mn);
         const uint32_t a_step = a_mn ? 2048 : 32, b_step = b_mn ? 2048 : 32;
-        const int steps = w.depth * kPairs + w.rests, most = kSums ? kPart : steps;
+        const int steps = w.depth * kPairs + w.rests;
         int i = 0;
         do {  // an accumulator: the whole sum, or parts of it
           const unsigned buf = turn & 1;
           ok = tc::bar_wait(taken + 8 * buf, (turn / 2 + 1) & 1, gave_up);
           if (!ok) break;
           tc::fence_after();
-          for (int j = 0; j < most && i < steps; ++j, ++i, ++n) {
+          const int end = i + part_of<(kPairs > 1), BACKWARD>(i, w.depth, steps);
+          for (int j = 0; i < end; ++j, ++i, ++n) {
             const unsigned s = n % kStages;
             ok = tc::bar_wait(full + 8 * s, (n / kStages) & 1, gave_up);
             if (!ok) break;
@@ -600,7 +612,8 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
 #pragma unroll
         for (int j = 0; j < kXentCols / 64; ++j) tc::tmem_wait(acc[j]);
         give();
-        for (int i = kPart; i < steps; i += kPart) {
+        for (int i = part_of<(kPairs > 1), BACKWARD>(0, w.depth, steps); i < steps;
+             i += part_of<(kPairs > 1), BACKWARD>(i, w.depth, steps)) {
           if (!await()) break;
           float v[2][32];
           tc::tmem_load32(at(0), v[0]);

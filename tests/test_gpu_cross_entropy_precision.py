@@ -59,3 +59,16 @@ def test_entries_of_the_targets(n, d, v, labelled, dtype):
         assert not inside((once @ w).to(dtype), want_h, bound_h, dtype)
     assert inside(dh[used], want_h, bound_h, dtype)
     assert inside(dw, want_w, bound_w, dtype)
+
+
+# Roundings to nearest average out over many tokens, and their number grows with the depth of a sum only below its size; what is cut off
+# adds up.  The mean loss is a few units off however many tokens there are: four of fp32, and sixteen for operands of 16 bits, whose
+# own rounding is 2^12 to 2^15 units.
+@pytest.mark.parametrize("n,d,v,dtype,most", [(1003, 509, 10007, torch.float32, 4 * U), (700, 2048, 5000, torch.float32, 4 * U),
+                                              (2048, 1024, 20000, torch.bfloat16, 16 * U), (2048, 4096, 8000, torch.float16, 16 * U)])
+def test_the_mean_loss_is_not_biased(n, d, v, dtype, most):
+    hidden, weight, targets = inputs(n, d, v, dtype, 1)
+    hidden = (hidden.float() + 1.5 * weight.float()[targets]).to(dtype)  # losses of about two
+    want = definition(hidden, weight, targets)[6].mean()
+    got = B().cross_entropy_forward(hidden, weight, targets)[0].double()
+    assert abs(got - want) <= most * want
