@@ -10,8 +10,8 @@
 // tensor cores fill the other; a warp of the first block issues the products.  Every wait is bounded; when one runs out
 // the blocks end, and the status tells of it.
 //
-// The tensor cores cut what they add up to fp32 instead of rounding it, 16 products at a time.  Where results are fp32, an accumulator
-// holds 128 or 256 products of a sum (part_of), and the parts are added up in registers, rounded (SUMS).
+// The tensor cores cut what they add up to fp32 instead of rounding it, 16 products at a time.  An accumulator holds no more products
+// than may be added up so (part_of), and the parts are added up in registers, rounded.
 //
 // With 16-bit operands the logits' gradient is rounded to their type, but for the entries of the targets, by far the largest: without
 // what that rounding leaves of them the gradients are 0.0017 off (2-norm, 2458 x 256 x 30522 bf16), with it below 0.0001, where the
@@ -71,14 +71,17 @@ enum XentKind { kHidden, kWeight, kLogits };
 
 // Steps of an accumulator, from step i of a tile on.  What the tensor cores cut is of the size of the running sum: of fp32 operands the
 // products of the largest parts come last, and the others may be added up longer.  (Mean error of lse, 1003 x 509 x 10007 fp32:
-// -0.9e-6; with eight steps for all -3.4e-6, and no faster.  2048 x 4096 x 8000 fp16: four steps -2.1e-6, eight -4.0e-6.)
-template <bool F32, bool BACKWARD>
-__device__ __forceinline__ int part_of(int i, int depth, int steps) {
+// -0.9e-6; with eight steps for all -3.4e-6, and no faster.  2048 x 4096 x 8000 fp16: four steps -2.1e-6, eight -4.0e-6.)  The logits
+// are the same in both directions, so that a row's probabilities add up to one (fp16, 4096 products of one sign: 6e-4 short of it
+// with one accumulator); the products with G, whose results are 16 bits, may be longer (131072 tokens of one sign, fp16: 1e-5 off
+// with 64 steps, 9e-4 with one accumulator; that is 6 % on 8192 x 4096 x 64000).
+template <bool F32>
+__device__ __forceinline__ int part_of(XentKind kind, int i, int depth, int steps) {
   if constexpr (F32) {
     const int small = 5 * depth;
     return i < small ? min(32, small - i) : min(2, steps - i);
   } else {
-    return BACKWARD ? steps : min(4, steps - i);
+    return min(kind == kLogits ? 4 : 64, steps - i);
   }
 }
 
@@ -380,7 +383,6 @@ __device__ __forceinline__ bool load_rests(const XentGemm& p, const XentWork& wo
 template <typename T, bool BACKWARD>
 __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant__ XentGemm p) {
   using O = Operand<T>;
-  constexpr bool kSums = !BACKWARD || std::is_same_v<T, float>;
   constexpr int kPairs = std::is_same_v<T, float> ? 6 : 1;
   extern __shared__ unsigned char ring_[];
   __shared__ alignas(8) uint64_t bars[2 * kStages + 5];
@@ -457,7 +459,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
           ok = tc::bar_wait(taken + 8 * buf, (turn / 2 + 1) & 1, gave_up);
           if (!ok) break;
           tc::fence_after();
-          const int end = i + part_of<(kPairs > 1), BACKWARD>(i, w.depth, steps);
+          const int end = i + part_of<(kPairs > 1)>(w.kind, i, w.depth, steps);
           for (int j = 0; i < end; ++j, ++i, ++n) {
             const unsigned s = n % kStages;
             ok = tc::bar_wait(full + 8 * s, (n / kStages) & 1, gave_up);
@@ -602,55 +604,37 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
       const auto at = [&](int c) {
         return tmem + (turn & 1) * kXentCols + half * cols + c + (uint32_t(quarter * 32) << 16);
       };
-      // (cols is 64 or 128: an even number of 32s)
-      if constexpr (kSums) {
-        float acc[kXentCols / 64][32];
-        if (!await()) break;
+      float acc[kXentCols / 64][32];
+      if (!await()) break;
 #pragma unroll
-        for (int j = 0; j < kXentCols / 64; ++j)
-          if (32 * j < cols) tc::tmem_load32(at(32 * j), acc[j]);
+      for (int j = 0; j < kXentCols / 64; ++j)
+        if (32 * j < cols) tc::tmem_load32(at(32 * j), acc[j]);
 #pragma unroll
-        for (int j = 0; j < kXentCols / 64; ++j) tc::tmem_wait(acc[j]);
-        give();
-        for (int i = part_of<(kPairs > 1), BACKWARD>(0, w.depth, steps); i < steps;
-             i += part_of<(kPairs > 1), BACKWARD>(i, w.depth, steps)) {
-          if (!await()) break;
-          float v[2][32];
-          tc::tmem_load32(at(0), v[0]);
-#pragma unroll
-          for (int j = 0; j < kXentCols / 64; ++j) {
-            if (32 * j >= cols) break;
-            tc::tmem_wait(v[j & 1]);
-            if (j + 1 < kXentCols / 64 && 32 * (j + 1) < cols) tc::tmem_load32(at(32 * (j + 1)), v[(j + 1) & 1]);
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              const float2 s = add2(make_float2(acc[j][e], acc[j][e + 1]), make_float2(v[j & 1][e], v[j & 1][e + 1]));
-              acc[j][e] = s.x;
-              acc[j][e + 1] = s.y;
-            }
-          }
-          give();
-        }
-        if (!ok) break;
-#pragma unroll
-        for (int j = 0; j < kXentCols / 64; ++j)
-          if (32 * j < cols) put(32 * j, acc[j]);
-      } else {
+      for (int j = 0; j < kXentCols / 64; ++j) tc::tmem_wait(acc[j]);
+      give();
+      for (int i = part_of<(kPairs > 1)>(w.kind, 0, w.depth, steps); i < steps;
+           i += part_of<(kPairs > 1)>(w.kind, i, w.depth, steps)) {
         if (!await()) break;
         float v[2][32];
         tc::tmem_load32(at(0), v[0]);
-        for (int c = 0; c < cols; c += 64) {
-          tc::tmem_wait(v[0]);
-          tc::tmem_load32(at(c + 32), v[1]);
-          put(c, v[0]);
-          __syncwarp();
-          tc::tmem_wait(v[1]);
-          if (c + 64 < cols) tc::tmem_load32(at(c + 64), v[0]);
-          else give();
-          put(c + 32, v[1]);
-          __syncwarp();
+#pragma unroll
+        for (int j = 0; j < kXentCols / 64; ++j) {
+          if (32 * j >= cols) break;
+          tc::tmem_wait(v[j & 1]);
+          if (j + 1 < kXentCols / 64 && 32 * (j + 1) < cols) tc::tmem_load32(at(32 * (j + 1)), v[(j + 1) & 1]);
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const float2 s = add2(make_float2(acc[j][e], acc[j][e + 1]), make_float2(v[j & 1][e], v[j & 1][e + 1]));
+            acc[j][e] = s.x;
+            acc[j][e + 1] = s.y;
+          }
         }
+        give();
       }
+      if (!ok) break;
+#pragma unroll
+      for (int j = 0; j < kXentCols / 64; ++j)
+        if (32 * j < cols) put(32 * j, acc[j]);
       if constexpr (!BACKWARD)
         p.part[(long long)row * p.parts + w.part * 2 + half] = make_float2(stats.top, stats.total);
       __syncwarp();

@@ -72,3 +72,41 @@ def test_the_mean_loss_is_not_biased(n, d, v, dtype, most):
     want = definition(hidden, weight, targets)[6].mean()
     got = B().cross_entropy_forward(hidden, weight, targets)[0].double()
     assert abs(got - want) <= most * want
+
+
+@pytest.mark.parametrize("n", [3000, 2 ** 17])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_sums_over_many_tokens_are_not_cut(n, dtype):
+    """The layer's gradient from contributions of one sign, as many as there are tokens: on average over its entries it is a small part
+    of the result's half step off, however many."""
+    d, v = 96, 32
+    g = torch.Generator(device="cuda").manual_seed(3)
+    hidden = ((torch.rand(n, d, device="cuda", generator=g) + 0.5) * torch.exp2(torch.rand(d, device="cuda", generator=g))).to(dtype)
+    weight, targets = torch.zeros(v, d, device="cuda", dtype=dtype), torch.randint(0, v // 2, (n,), device="cuda", generator=g)
+    _, lse = B().cross_entropy_forward(hidden, weight, targets, -100, "none")
+    dw = B().cross_entropy_backward(torch.full((n,), 2.0 ** -10, device="cuda"), hidden, weight, targets, lse, -100, "none")[1]
+    # all classes are as likely: 1 / 32, which is exact
+    G = torch.full((n, v), 2.0 ** -15, dtype=torch.float64, device="cuda")
+    G[torch.arange(n), targets] -= 2.0 ** -10
+    want = G.t() @ hidden.double()
+    off = (dw.double() - want) / want
+    for rows in (off[:v // 2], off[v // 2:]):
+        assert rows.mean().abs() <= HALF[dtype] / 4
+
+
+@pytest.mark.parametrize("d", [64, 512, 4096])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_a_row_of_the_logits_gradient_adds_up_to_zero(d, dtype):
+    """Logits of 30 from products of one sign.  A further column holds ones for the classes and zeros for the tokens: the gradient of
+    the tokens' part of it is the sum of the logits' gradient over the classes."""
+    n, v = 700, 300
+    g = torch.Generator(device="cuda").manual_seed(4)
+    hidden = torch.rand(n, d, device="cuda", generator=g) + 0.5
+    weight = (torch.rand(v, d, device="cuda", generator=g) + 0.5) * (30 / d)
+    hidden = torch.cat((hidden, torch.zeros(n, 1, device="cuda")), 1).to(dtype)
+    weight = torch.cat((weight, torch.ones(v, 1, device="cuda")), 1).to(dtype)
+    targets = torch.randint(0, v, (n,), device="cuda", generator=g)
+    _, lse = B().cross_entropy_forward(hidden, weight, targets, -100, "none")
+    dh = B().cross_entropy_backward(torch.ones(n, device="cuda"), hidden, weight, targets, lse, -100, "none")[0]
+    # on average: the roundings of a row's 300 entries, and of lse, which is 36: two units of it
+    assert dh[:, -1].double().mean().abs() <= (HALF[dtype] / 16 if dtype != torch.float32 else 2 * 36 * U)
