@@ -20,7 +20,9 @@ namespace {
 constexpr unsigned kAllLanes = 0xFFFFFFFFu;
 
 // lse and loss of a token from the statistics of its logits' parts (their largest values are in units of log2(e)); a
-// warp takes a token.  The last steps are in 64 bits: lse is several times as large as the loss.
+// warp takes a token.  The last steps are in 64 bits: lse is several times as large as the loss.  (The largest value is
+// taken back by the factor that it has got, rounding and all: that is 1e-8 off log2(e), and the loss is what little
+// lse is above the target's logit.)
 __global__ void __launch_bounds__(256) k_xent_join(const XentPrep p) {
   take_turn();
   const int lane = threadIdx.x & 31, count = *p.count;
@@ -51,7 +53,7 @@ __global__ void __launch_bounds__(256) k_xent_join(const XentPrep p) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAllLanes, sum, o);
     if (lane) continue;
-    const double lse = (double(top) + log2(double(sum))) * 0.69314718055994530942;
+    const double lse = double(top) / double(kLog2e) + log(double(sum));
     const float loss =
         p.target[i] < 0 ? __int_as_float(0x7FC00000) : float(lse - double(p.target_logit[i]));
     p.lse_out[p.order[i]] = float(lse);

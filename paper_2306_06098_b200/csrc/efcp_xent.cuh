@@ -46,7 +46,6 @@ constexpr uint32_t kStageBytes = kABytes + kBBytes;
 constexpr uint32_t kOutBytes = 32 * 128;        // a warp's box of results
 constexpr size_t kXentSmem = kStages * kStageBytes + kOutWarps * kOutBytes + 1024;
 constexpr int kSquare = 8;                      // rows of tiles that pairs work on side by side
-constexpr float kLog2e = 1.4426950408889634f;
 
 template <typename T>
 using Operand = std::conditional_t<std::is_same_v<T, __half>, __half, __nv_bfloat16>;

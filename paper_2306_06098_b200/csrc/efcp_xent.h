@@ -11,6 +11,7 @@ namespace efcp {
 // A tile of a product (256 x up to 256, of a pair of blocks), and a step along the sum.
 constexpr int kXentRows = 256, kXentCols = 256, kXentDepth = 64;
 constexpr int kXentShifts = 3;
+constexpr float kLog2e = 1.4426950408889634f;  // e^x = 2^(x log2(e)), up to this one's rounding: see k_xent_join
 constexpr int kXentSplits = 32;  // parts of the sum over a piece that are added up apart, at most
 
 // The products of tiles that a launch works on, in this order:

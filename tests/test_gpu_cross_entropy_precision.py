@@ -110,3 +110,25 @@ def test_a_row_of_the_logits_gradient_adds_up_to_zero(d, dtype):
     dh = B().cross_entropy_backward(torch.ones(n, device="cuda"), hidden, weight, targets, lse, -100, "none")[0]
     # on average: the roundings of a row's 300 entries, and of lse, which is 36: two units of it
     assert dh[:, -1].double().mean().abs() <= (HALF[dtype] / 16 if dtype != torch.float32 else 2 * 36 * U)
+
+
+def sure(size, dtype, n=40, v=300, d=16):
+    """Tokens that are as good as certain of their targets: logits of +size and -size, exactly."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    targets = torch.randint(0, d, (n,), device="cuda", generator=g)
+    hidden, weight = torch.zeros(n, d, device="cuda"), torch.full((v, d), -1.0, device="cuda")
+    hidden[torch.arange(n), targets] = size
+    weight[:d] += 2 * torch.eye(d, device="cuda")
+    return hidden.to(dtype), weight.to(dtype), targets
+
+
+@pytest.mark.parametrize("size", [20.0, 92.0, 500.0, 6000.0])
+@pytest.mark.parametrize("n", [3, 40])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_the_loss_of_a_sure_token(size, n, dtype):
+    hidden, weight, targets = sure(size, dtype, n)
+    size = hidden.amax().item()
+    losses, lse = B().cross_entropy_forward(hidden, weight, targets, -100, "none")
+    assert (lse.double() - size).abs().max() <= 2 * U * size
+    # the exponential of about 0 (2^-22) and the rounding of the sum: nothing that grows with the logits
+    assert losses.abs().max() <= 2.0 ** -22 + 2 * U
