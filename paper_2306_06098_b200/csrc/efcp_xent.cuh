@@ -187,6 +187,13 @@ __device__ __forceinline__ float2 exp_pair(float a, float b, float base) {
   return make_float2(pow2(x.x), pow2(x.y));
 }
 
+// e^(v - lse), two at a time.  (The difference first: it is exact where the probability is large, while lse times log2(e) is rounded
+// to its own size.)
+__device__ __forceinline__ float2 probability_pair(float a, float b, float lse) {
+  const float2 x = mul2(add2(make_float2(a, b), both(-lse)), both(kLog2e));
+  return make_float2(pow2(x.x), pow2(x.y));
+}
+
 // What becomes of 32 columns of a row of logits, forward: their largest value (times log2(e)) and the sum of
 // exponentials relative to it are joined to the row's.
 struct RowStats {
@@ -502,7 +509,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
       if (w.kind == kLogits) {
         target = p.target[row];
         if constexpr (BACKWARD) {
-          lse = p.lse[row] * kLog2e;
+          lse = p.lse[row];
           coef = p.coef[row];
         }
       }
@@ -521,12 +528,12 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
           if (mine) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) x = i == hit ? v[i] : x;
-            x = (exp_pair(x, x, lse).x - 1.f) * coef;
+            x = (probability_pair(x, x, lse).x - 1.f) * coef;
             if constexpr (kPairs == 1) p.rest[row] = x - rounded<O>(x);
           }
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
-            const float2 e = mul2(exp_pair(v[i], v[i + 1], lse), both(coef));
+            const float2 e = mul2(probability_pair(v[i], v[i + 1], lse), both(coef));
             v[i] = e.x;
             v[i + 1] = e.y;
           }

@@ -132,3 +132,16 @@ def test_the_loss_of_a_sure_token(size, n, dtype):
     assert (lse.double() - size).abs().max() <= 2 * U * size
     # the exponential of about 0 (2^-22) and the rounding of the sum: nothing that grows with the logits
     assert losses.abs().max() <= 2.0 ** -22 + 2 * U
+
+
+@pytest.mark.parametrize("size", [20.0, 92.0, 500.0, 6000.0])
+@pytest.mark.parametrize("n", [3, 40])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_the_gradient_of_a_sure_token(size, n, dtype):
+    """lse is the target's logit, exactly: a probability of 1 and others of 0, so gradients of 0."""
+    hidden, weight, targets = sure(size, dtype, n)
+    lse = hidden.amax(1).float()
+    dh, dw = B().cross_entropy_backward(torch.ones(n, device="cuda"), hidden, weight, targets, lse, -100, "none")
+    # the exponential of 0 (2^-22), times a weight of 1; of `size` for the layer, n tokens of which may have one target
+    assert dh.double().abs().max() <= 2.0 ** -22 + 2 * U
+    assert dw.double().abs().max() <= (2.0 ** -22 + 2 * U) * n * hidden.amax().item()
