@@ -80,26 +80,6 @@ __global__ void __launch_bounds__(1024) k_xent_total(const XentPrep p) {
   if (lane == 0) p.losses[0] = float(p.reduction == 1 ? sum / count : sum);
 }
 
-// Which steps of 64 tokens have a target in which tile of rows of W: a warp looks at 32 steps for a tile.
-__global__ void __launch_bounds__(256) k_xent_hits(const XentPrep p) {
-  take_turn();
-  const int lane = threadIdx.x & 31, count = *p.count;
-  const long long all = (p.vocab + kXentRows - 1ll) / kXentRows * p.hit_words, warps = (long long)gridDim.x * 8;
-  for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < all; i += warps) {
-    const long long tile = i / p.hit_words;
-    const int first = int(i - tile * p.hit_words) * 32 * kXentDepth;
-    unsigned word = 0;
-#pragma unroll 4
-    for (int s = 0; s < 32; ++s) {
-      const int a = first + s * kXentDepth + lane, b = a + 32;
-      const int t = a < count ? p.target[a] : -1, u = b < count ? p.target[b] : -1;
-      const bool here = (t >= 0 && t / kXentRows == tile) || (u >= 0 && u / kXentRows == tile);
-      if (__any_sync(kAllLanes, here)) word |= 1u << s;
-    }
-    if (lane == 0) p.hits[i] = word;
-  }
-}
-
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 
@@ -133,10 +113,9 @@ struct Plan {
   int parts;
   int d_tiles, d_tile;
   int pairs;
-  int hit_words;
   int64_t sum_row, sum_rows;
   // offsets
-  int64_t count, scale, order, target, lse, coef, rest, place, logit, each, part, hits, hidden, weight, g[2], sum, bytes;
+  int64_t count, scale, order, target, lse, coef, rest, place, logit, each, part, bounds, hidden, weight, g[2], sum, bytes;
 };
 
 // Whether the tensor copies can read the weight where it lies.
@@ -184,10 +163,7 @@ Plan make_plan(const efcp_cross_entropy& d, const void* weight, bool backward, i
     p.coef = take(4 * p.padded);
     p.rest = take(4 * p.padded);
     p.place = take(4 * p.padded);
-    if (p.planes == 1) {
-      p.hit_words = int(ceil_div(p.padded, 32 * kXentDepth));
-      p.hits = take(4 * ceil_div(d.vocab, kXentRows) * p.hit_words);
-    }
+    p.bounds = take(4 * (kXentBuckets + 1));
     for (int i = 0; i < std::min(2, p.pieces); ++i) p.g[i] = take(2 * p.planes * p.padded * p.piece);
     // how many rows count is not known here: the most that any number of them takes with its parts
     const int64_t rows = p.padded / kXentRows;
@@ -495,9 +471,9 @@ int efcp_cross_entropy_backward(const efcp_cross_entropy* desc, const float* gra
   c.prep.sum = sum;
   c.prep.sum_row = p.sum_row;
   c.prep.dhidden = dhidden;
-  c.prep.hits = p.planes == 1 && dweight ? c.at<unsigned>(workspace, p.hits) : nullptr;
-  c.prep.hit_words = m.hit_words = p.hit_words;
-  m.hits = c.prep.hits;
+  m.bounds = c.prep.bounds = p.planes == 1 && dweight ? c.at<int>(workspace, p.bounds) : nullptr;
+  while ((desc->vocab - 1) / kXentRows >> c.prep.wide >= kXentBuckets) ++c.prep.wide;
+  m.wide = c.prep.wide;
   m.lse = c.prep.lse;
   m.coef = c.prep.coef;
   m.dweight = dweight;
@@ -519,7 +495,6 @@ int efcp_cross_entropy_backward(const efcp_cross_entropy* desc, const float* gra
        !make_map(&m.dweight_out, desc->dtype, dweight, desc->d, desc->vocab, desc->d, 1, 0, 32)))
     return failed();
   if (!c.prepare(true)) return failed();
-  if (c.prep.hits && xent_hits(c.prep, c.sms, c.st) != cudaSuccess) return failed();
   m.hidden = dhidden != nullptr;
   m.weight = dweight != nullptr;
   // (where pieces are wider than they might be, the last launches find nothing to do)
@@ -538,11 +513,6 @@ cudaError_t xent_join(const XentPrep& p, int sms, cudaStream_t st) {
   cudaError_t e = launch(k_xent_join, Shape{unsigned(rows < 8ll * sms ? rows : 8ll * sms), 256, 0, 0}, st, p);
   if (e != cudaSuccess || !p.reduction) return e;
   return launch(k_xent_total, Shape{1, 1024, 0, 0}, st, p);
-}
-
-cudaError_t xent_hits(const XentPrep& p, int sms, cudaStream_t st) {
-  const long long warps = (p.vocab + kXentRows - 1ll) / kXentRows * p.hit_words;
-  return launch(k_xent_hits, Shape{unsigned(std::min<long long>(warps / 8 + 1, 8ll * sms)), 256, 0, 0}, st, p);
 }
 
 }  // namespace efcp

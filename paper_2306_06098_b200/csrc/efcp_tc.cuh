@@ -63,6 +63,21 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
   }
 }
 
+// Waits for a counter in shared memory that another warp of the block moves on; false as above.
+__device__ __forceinline__ bool count_wait(const volatile unsigned* counter, unsigned least, volatile int* gave_up) {
+  const uint64_t start = clock_ns();
+  while (int(*counter - least) < 0) {
+    if (*gave_up) return false;
+    if (clock_ns() - start > kWaitNs) {
+      *gave_up = 1;
+      return false;
+    }
+    __nanosleep(64);
+  }
+  __threadfence_block();
+  return true;
+}
+
 // ------------------------------------------------------------------ pairs of blocks
 __device__ __forceinline__ uint32_t pair_rank() {
   uint32_t r;
@@ -83,11 +98,20 @@ __device__ __forceinline__ uint32_t of_first(uint32_t addr) {
 __device__ __forceinline__ void bar_arrive_pair(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// What this thread wrote to shared memory comes before; the waiting thread fences.
+// What this thread wrote to shared memory comes before, for a thread that sees the phase done by bar_acquire_pair.  (A fence for
+// the whole cluster in its place takes as long as two steps of a product.)
 __device__ __forceinline__ void bar_release_pair(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void fence_pair() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
+__device__ __forceinline__ void bar_acquire_pair(uint32_t bar, uint32_t parity) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n"
+      "}\n" ::"r"(bar),
+      "r"(parity)
+      : "memory");
+}
 
 // ------------------------------------------------------------------ tensor copies
 // One box of a three-dimensional map into this block's shared memory, counted on a barrier of the pair's first

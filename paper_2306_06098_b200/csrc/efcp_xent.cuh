@@ -16,7 +16,7 @@
 // With 16-bit operands the logits' gradient is rounded to their type, but for the entries of the targets, by far the largest: without
 // what that rounding leaves of them the gradients are 0.0017 off (2-norm, 2458 x 256 x 30522 bf16), with it below 0.0001, where the
 // results' own rounding is 0.0017.  The gradient of H gets it in k_xent_finish, the gradient of W in steps of its own, with the tokens
-// whose targets are near (XentGemm::hits).
+// whose targets are near (XentGemm::bounds).
 //
 // fp32 values are held as three bfloat16 ones (8 bits of the significand each), of whose nine products the six
 // largest are added up, the small ones first; what is left out is below 2^-24 of the result.
@@ -45,6 +45,7 @@ constexpr uint32_t kABytes = kBlockRows / 64 * kBoxBytes, kBBytes = kXentCols / 
 constexpr uint32_t kStageBytes = kABytes + kBBytes;
 constexpr uint32_t kOutBytes = 32 * 128;        // a warp's box of results
 constexpr size_t kXentSmem = kStages * kStageBytes + kOutWarps * kOutBytes + 1024;
+constexpr int kRestWarps = 3;                   // see load_rests
 constexpr int kSquare = 8;                      // rows of tiles that pairs work on side by side
 
 template <typename T>
@@ -89,7 +90,7 @@ struct XentTile {
   int m0, n0;     // rows and columns of the result
   int cols;       // width of the tile
   int k0, depth;  // first step along the sum, and steps
-  int rests;      // steps more, of what the rounding of G left (weight)
+  int rest0, rests;  // the same of the steps that bring what the rounding of G left (weight)
   int part;       // of the sum over the piece (hidden); tile of the columns (logits)
 };
 
@@ -101,11 +102,6 @@ struct XentWork {
   int rows, next_cols;                       // of them: rows of W, columns
   long long hidden, weight, all;             // tiles of hidden; and of weight; and of logits
   bool six;                                  // products for each step
-
-  // the words that tell of the rests for the piece's rows of W from m0 on
-  __device__ __forceinline__ const unsigned* hits(const XentGemm& p, int m0) const {
-    return p.hits + (long long)((v0 + m0) / kXentRows) * p.hit_words;
-  }
 
   __device__ __forceinline__ XentWork(const XentGemm& p, int count, int pairs, bool backward, bool six_) {
     six = six_;
@@ -138,7 +134,7 @@ struct XentWork {
   }
   __device__ __forceinline__ XentTile tile(const XentGemm& p, long long t) const {
     XentTile r;
-    r.rests = 0;
+    r.rest0 = r.rests = 0;
     if (t < hidden) {
       const int2 mn = square(int(t), row_tiles, p.d_tiles * splits);
       const int n = mn.y / splits;
@@ -158,8 +154,11 @@ struct XentWork {
       r.cols = p.d_tile;
       r.part = r.k0 = 0;
       r.depth = token_steps;
-      if (!six)
-        for (int i = 0; i < p.hit_words; ++i) r.rests += __popc(hits(p, r.m0)[i]);
+      if (!six) {
+        const int bucket = (v0 + r.m0) / kXentRows >> p.wide, first = p.bounds[bucket], last = p.bounds[bucket + 1];
+        r.rest0 = first / kXentDepth;
+        r.rests = last > first ? (last - 1) / kXentDepth - r.rest0 + 1 : 0;
+      }
     } else {
       t -= weight;
       const int c = int(t / row_tiles);
@@ -338,51 +337,54 @@ __device__ __forceinline__ bool load_tile(const XentGemm& p, const XentWork& wor
   return true;
 }
 
-// (a warp) The steps of a tile of the layer's gradient that bring the rests of the targets' entries: of G's part of 64 tokens there is
-// one value a token, which is written to shared memory next to zeros.
+// The steps of a tile of the layer's gradient that bring the rests of the targets' entries, every kRestWarps-th of them from `which`
+// on: of G's part of 64 tokens there is one value a token, which a warp writes to shared memory next to zeros.  (262144 tokens x
+// 64 x 32 classes, gradients: 3.6 ms, 5.8 with one warp, 1.6 without the rests; 65536 x 768 x 5000: 3.00, 3.14 and 2.70.)
 template <typename O>
 __device__ __forceinline__ bool load_rests(const XentGemm& p, const XentWork& work, const XentTile& w, const Ring& r, int count,
-                                           int rank, int lane, unsigned& n, volatile int* gave_up) {
+                                           int rank, int which, int lane, unsigned n, volatile int* gave_up) {
   const int first = work.v0 + w.m0 + rank * kBlockRows, bn = w.n0 + rank * (w.cols / 2);
-  const unsigned* const hits = work.hits(p, w.m0);
-  const bool wide = w.cols > 128;
-  for (int i = 0, left = w.rests; left; ++i)
-    for (unsigned word = hits[i]; word; word &= word - 1, --left, ++n) {
-      const int k = (i * 32 + __ffs(word) - 1) * kXentDepth;
-      const unsigned s = n % kStages;
-      if (!__all_sync(kAll, tc::bar_wait(r.empty + 8 * s, (n / kStages + 1) & 1, gave_up))) return false;
-      const uint32_t bar = r.full + 8 * s, a = r.stages + s * kStageBytes, b = a + kABytes;
-      int col[2];  // of this lane's two tokens
-      float rest[2];
+  int col[2];  // of this lane's two tokens, one step ahead
+  float rest[2];
+  const auto fetch = [&](int i) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int token = k + 32 * j + lane;
-        col[j] = token < count ? p.target[token] - first : -1;
-        rest[j] = col[j] >= 0 && col[j] < kBlockRows ? p.rest[token] : 0.f;
-      }
-#pragma unroll 8
-      for (uint32_t at = lane * 16; at < kABytes; at += 512)
-        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(a + at), "r"(0) : "memory");
-      __syncwarp();
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int row = 32 * j + lane, c = col[j];
-        if (c < 0 || c >= kBlockRows) continue;
-        const O v = from_f32<O>(rest[j]);
-        asm volatile("st.shared.u16 [%0], %1;" ::"r"(a + (c >> 6) * kBoxBytes + row * 128 +
-                                                     ((((c & 63) >> 3) ^ (row & 7)) << 4) + (c & 7) * 2),
-                     "h"(reinterpret_cast<const uint16_t&>(v))
-                     : "memory");
-      }
-      tc::fence_copies();
-      __syncwarp();
-      if (lane == 0) {
-        if (rank == 0) tc::bar_expect(r.full_here + 8 * s, 2 * uint32_t(w.cols) * 64);
-        else tc::bar_release_pair(bar);
-        tc::load_box(&p.hidden_cols, b, bar, bn, k, 0);
-        if (wide) tc::load_box(&p.hidden_cols, b + kBoxBytes, bar, bn + 64, k, 0);
-      }
+    for (int j = 0; j < 2; ++j) {
+      const int token = (w.rest0 + i) * kXentDepth + 32 * j + lane;
+      const bool on = i < w.rests && token < count;
+      col[j] = on ? p.target[token] - first : -1;
+      rest[j] = on ? p.rest[token] : 0.f;
     }
+  };
+  fetch(which);
+  for (int i = which; i < w.rests; i += kRestWarps) {
+    const unsigned s = (n + i) % kStages;
+    if (!__all_sync(kAll, tc::bar_wait(r.empty + 8 * s, ((n + i) / kStages + 1) & 1, gave_up))) return false;
+    const uint32_t bar = r.full + 8 * s, a = r.stages + s * kStageBytes, b = a + kABytes;
+#pragma unroll 8
+    for (uint32_t at = lane * 16; at < kABytes; at += 512)
+      asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(a + at), "r"(0) : "memory");
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int row = 32 * j + lane, c = col[j];
+      if (c < 0 || c >= kBlockRows) continue;
+      const O v = from_f32<O>(rest[j]);
+      asm volatile("st.shared.u16 [%0], %1;" ::"r"(a + (c >> 6) * kBoxBytes + row * 128 +
+                                                   ((((c & 63) >> 3) ^ (row & 7)) << 4) + (c & 7) * 2),
+                   "h"(reinterpret_cast<const uint16_t&>(v))
+                   : "memory");
+    }
+    fetch(i + kRestWarps);
+    tc::fence_copies();
+    __syncwarp();
+    if (lane == 0) {
+      const int token = (w.rest0 + i) * kXentDepth;
+      if (rank == 0) tc::bar_expect(r.full_here + 8 * s, 2 * uint32_t(w.cols) * 64);
+      else tc::bar_release_pair(bar);
+      tc::load_box(&p.hidden_cols, b, bar, bn, token, 0);
+      if (w.cols > 128) tc::load_box(&p.hidden_cols, b + kBoxBytes, bar, bn + 64, token, 0);
+    }
+  }
   return true;
 }
 
@@ -394,6 +396,8 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
   __shared__ alignas(8) uint64_t bars[2 * kStages + 5];
   __shared__ uint32_t tmem_at;
   __shared__ int gave_up_;
+  __shared__ unsigned loaded_;  // steps that the copying warp has come to, before each tile with rests
+  volatile unsigned* loaded = &loaded_;
   volatile int* gave_up = &gave_up_;
   const uint32_t ring = (tc::smem_of(ring_) + 1023) & ~1023u;
   const uint32_t full = tc::smem_of(bars), empty = full + 8 * kStages, done = empty + 8 * kStages,
@@ -402,6 +406,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
   const int rank = int(tc::pair_rank());
   if (threadIdx.x == 0) {
     gave_up_ = 0;
+    loaded_ = 0;
     for (int i = 0; i < kStages; ++i) {
       tc::bar_init(full + 8 * i, 2);  // a thread of either block
       tc::bar_init(empty + 8 * i, 1);
@@ -424,6 +429,11 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
   const XentWork work(p, count, pairs, BACKWARD, kPairs > 1);
 
   // Registers go where the sums are held: 128 x 72 + 256 x 216 of the launch's 384 x 168.
+  const auto drain = [] {  // nothing may land in shared memory that the block has left: copies take microseconds
+    const uint64_t start = tc::clock_ns();
+    while (tc::clock_ns() - start < tc::kDrainNs) {
+    }
+  };
   if (warp >= kOutWarps) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
   if (warp == kOutWarps) {
@@ -433,7 +443,14 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
     for (long long t = pair; t < work.all && ok; t += pairs) {
       const XentTile w = work.tile(p, t);
       if constexpr (BACKWARD && kPairs == 1)
-        if (w.rests) ok = load_rests<O>(p, work, w, ring_of, count, rank, lane, n, gave_up);
+        if (w.rests) {
+          if (lane == 0) {
+            __threadfence_block();
+            *loaded = n;
+          }
+          ok = load_rests<O>(p, work, w, ring_of, count, rank, 0, lane, n, gave_up);
+          n += unsigned(w.rests);
+        }
       if (ok && lane == 0) {
         unsigned m = n;
         if (w.kind == kLogits) ok = load_tile<kLogits, kPairs>(p, work, w, ring_of, rank, m, gave_up);
@@ -443,11 +460,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
       n += unsigned(w.depth * kPairs);
       ok = __all_sync(kAll, ok);
     }
-    if (!ok && lane == 0) {  // nothing may land in shared memory that the block has left: copies take microseconds
-      const uint64_t start = tc::clock_ns();
-      while (tc::clock_ns() - start < tc::kDrainNs) {
-      }
-    }
+    if (!ok && lane == 0) drain();
     __syncwarp();
   } else if (warp == kOutWarps + 1) {
     if (lane == 0 && rank == 0) {
@@ -470,7 +483,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
             const unsigned s = n % kStages;
             ok = tc::bar_wait(full + 8 * s, (n / kStages) & 1, gave_up);
             if (!ok) break;
-            if (i < w.rests) tc::fence_pair();  // (operands that threads of both blocks have written)
+            if (i < w.rests) tc::bar_acquire_pair(full + 8 * s, (n / kStages) & 1);  // (threads of both blocks wrote operands)
             tc::fence_after();
             const uint32_t a = ring + s * kStageBytes, b = a + kABytes;
 #pragma unroll
@@ -489,6 +502,22 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
         (void)tc::bar_wait(drained, 0, gave_up, tc::kDrainNs);
       }
     }
+    __syncwarp();
+  } else if constexpr (BACKWARD && kPairs == 1) {
+    const Ring ring_of{ring, empty, tc::of_first(full), full};
+    unsigned n = 0;
+    bool ok = true;
+    for (long long t = pair; t < work.weight && ok; t += pairs) {  // (no rests in the tiles behind)
+      const XentTile w = work.tile(p, t);
+      const int which = warp - kOutWarps - 1;
+      if (which < w.rests) {
+        // (a place's barrier tells of its last use only: the uses before these steps have to be under way)
+        ok = __all_sync(kAll, tc::count_wait(loaded, n, gave_up)) &&
+             load_rests<O>(p, work, w, ring_of, count, rank, which, lane, n, gave_up);
+      }
+      n += unsigned(w.rests + w.depth);
+    }
+    if (!ok && lane == 0) drain();
     __syncwarp();
   }
   } else {
@@ -655,12 +684,10 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
   if (threadIdx.x == 0 && gave_up_) atomicExch(p.status, EFCP_ETIMEOUT);
 }
 
-constexpr int kBuckets = 1024;  // of targets
-
 // What comes before the products: which tokens have a target, in order; their rows of H, one behind the other (and
 // zeros up to whole tiles), as the copies of tiles want them; backward also the factors on their gradients, times a
 // power of two that brings the largest near 1 (near 2^14 for fp16, whose probabilities would vanish otherwise); and
-// zeros for what belongs to the other tokens.  Where the rests of the targets' entries are asked for (p.hits) the order goes by
+// zeros for what belongs to the other tokens.  Where the rests of the targets' entries are asked for (p.bounds) the order goes by
 // the targets' tiles first, so that a tile of rows of W meets its targets in few steps (2458 tokens x 30522 classes: in one or two of
 // 39; in the tokens' own order it would be 16).
 //
@@ -673,7 +700,7 @@ __global__ void __launch_bounds__(512) k_xent_prepare(const XentPrep p, bool bac
   constexpr int kPlanes = std::is_same_v<T, float> ? 3 : 1;
   constexpr bool kHalf = std::is_same_v<T, __half>;
   __shared__ int before_, all_, places[512 / 32], tokens[512], rows[512];
-  __shared__ int bucket[512], bucket_all[kBuckets], bucket_at[kBuckets];  // (sorted)
+  __shared__ int bucket[512], bucket_all[kXentBuckets], bucket_at[kXentBuckets];  // (sorted)
   __shared__ unsigned most_;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long lo = (long long)blockIdx.x * per, hi = min(p.tokens, lo + per);
@@ -684,28 +711,35 @@ __global__ void __launch_bounds__(512) k_xent_prepare(const XentPrep p, bool bac
   __syncthreads();
   int before = 0, all = 0;
   float big = 0.f;
-  const bool each = backward && p.reduction == 0, sorted = p.hits;
-  const int tiles = (p.vocab - 1) / kXentRows;
-  int wide = 0;  // a bucket's tiles of rows of W: 2^wide
-  while (tiles >> wide >= kBuckets) ++wide;
-  const auto bucket_of = [&](long long t) { return t >= 0 && t < p.vocab ? int(t / kXentRows) >> wide : 0; };
+  const bool each = backward && p.reduction == 0, sorted = p.bounds;
+  const auto bucket_of = [&](long long t) { return t >= 0 && t < p.vocab ? int(t / kXentRows) >> p.wide : 0; };
   if (sorted) {
-    for (int i = threadIdx.x; i < kBuckets; i += 512) bucket_all[i] = bucket_at[i] = 0;
+    for (int i = threadIdx.x; i < kXentBuckets; i += 512) bucket_all[i] = bucket_at[i] = 0;
     __syncthreads();
   }
-#pragma unroll 8
-  for (long long i = threadIdx.x; i < p.tokens; i += 512) {
-    const long long t = p.targets[i];
-    const bool used = t != p.ignore;
-    all += used;
-    before += used && i < lo;
-    if (sorted && used) {  // (whole numbers: any order)
-      atomicAdd(&bucket_all[bucket_of(t)], 1);
-      if (i < lo) atomicAdd(&bucket_at[bucket_of(t)], 1);
+  constexpr int kAhead = 8;  // loads on their way: counting in shared memory would wait for each
+  for (long long i0 = threadIdx.x; i0 < p.tokens; i0 += 512 * kAhead) {
+    long long t[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) t[k] = i0 + 512 * k < p.tokens ? p.targets[i0 + 512 * k] : p.ignore;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const long long i = i0 + 512 * k;
+      const bool used = t[k] != p.ignore;
+      all += used;
+      before += used && i < lo;
+      if (each && used) {
+        const float g = fabsf(p.grad[i * p.grad_step]);
+        if (g < INFINITY) big = fmaxf(big, g);
+      }
     }
-    if (each && used) {
-      const float g = fabsf(p.grad[i * p.grad_step]);
-      if (g < INFINITY) big = fmaxf(big, g);
+    if (sorted) {  // (whole numbers: any order)
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (t[k] == p.ignore) continue;
+        atomicAdd(&bucket_all[bucket_of(t[k])], 1);
+        if (i0 + 512 * k < lo) atomicAdd(&bucket_at[bucket_of(t[k])], 1);
+      }
     }
   }
   before = __reduce_add_sync(kAll, before);
@@ -728,6 +762,11 @@ __global__ void __launch_bounds__(512) k_xent_prepare(const XentPrep p, bool bac
     if (lane == 31) places[warp] = sum;
     __syncthreads();
     for (int w = 0; w < warp; ++w) sum += places[w];
+    if (blockIdx.x == 0) {
+      p.bounds[k] = sum - two;
+      p.bounds[k + 1] = sum - two + bucket_all[k];
+      if (k + 2 == kXentBuckets) p.bounds[k + 2] = sum;
+    }
     bucket_at[k] += sum - two;
     bucket_at[k + 1] += sum - two + bucket_all[k];
     __syncthreads();

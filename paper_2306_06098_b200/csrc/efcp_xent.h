@@ -11,6 +11,7 @@ namespace efcp {
 // A tile of a product (256 x up to 256, of a pair of blocks), and a step along the sum.
 constexpr int kXentRows = 256, kXentCols = 256, kXentDepth = 64;
 constexpr int kXentShifts = 3;
+constexpr int kXentBuckets = 1024;  // of targets, at most
 constexpr float kLog2e = 1.4426950408889634f;  // e^x = 2^(x log2(e)), up to this one's rounding: see k_xent_join
 constexpr int kXentSplits = 32;  // parts of the sum over a piece that are added up apart, at most
 
@@ -34,8 +35,8 @@ struct XentGemm {
   const float* coef;   // factor on a token's gradient
   const float* scale;  // [0]: the factor that coef holds, [1]: its inverse
   float* rest;         // what the rounding of G left of the targets' entries (16 bits)
-  const unsigned* hits;  // for each tile of rows of W `hit_words` words: the steps of 64 tokens that have a target there (16 bits)
-  int hit_words;
+  const int* bounds;   // tokens lie in the order of their targets' tiles of rows of W: where the tokens of a bucket of
+  int wide;            // 2^wide tiles begin (16 bits)
   float2* part;        // statistics, a row of `parts` for each token
   float* target_logit;
   void* dweight;
@@ -72,8 +73,8 @@ struct XentPrep {
   float* rest;                     // see XentGemm
   const void* layer;               // the weight as it was given
   int* place;                      // a token's place in the order, -1: none
-  unsigned* hits;                  // see XentGemm; null: not wanted
-  int hit_words;
+  int* bounds;                     // see XentGemm, kXentBuckets + 1 of them; null: not wanted
+  int wide;
   const float* sum;                // gradient of H: parts of the whole tiles' rows, sum_row elements each
   long long sum_row;
   int d_tiles, piece, tiles, shifts, pairs;
@@ -143,6 +144,5 @@ cudaError_t few_launch_f32(const XentFew& p, bool vec, bool backward, cudaStream
 cudaError_t few_launch_bf16(const XentFew& p, bool vec, bool backward, cudaStream_t st);
 cudaError_t few_launch_f16(const XentFew& p, bool vec, bool backward, cudaStream_t st);
 cudaError_t xent_join(const XentPrep& p, int sms, cudaStream_t st);
-cudaError_t xent_hits(const XentPrep& p, int sms, cudaStream_t st);
 
 }  // namespace efcp

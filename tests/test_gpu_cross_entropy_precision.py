@@ -17,7 +17,8 @@ def inside(got, want, bound, dtype):
 # few tokens next to the classes, so that the targets' entries make up the gradients; d that is no multiple of a tile; one tile of
 # classes; several pieces of the vocabulary, as they are and widened
 @pytest.mark.parametrize("n,d,v,labelled", [(40, 64, 3000, 1.0), (300, 72, 5003, 1.0), (130, 300, 4096, 0.5), (14, 40, 120, 1.0),
-                                            (16300, 24, 30011, 1.0), (16300, 24, 30011, 0.1), (16300, 40, 9001, 0.01), (2500, 128, 30522, 1.0), (40, 8, 300000, 1.0)])
+                                            (16300, 24, 30011, 1.0), (16300, 24, 30011, 0.1), (16300, 40, 9001, 0.01), (2500, 128, 30522, 1.0), (40, 8, 300000, 1.0),
+                                            (200, 520, 60000, 1.0), (12, 24, 100000, 1.0)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_entries_of_the_targets(n, d, v, labelled, dtype):
     """Both gradients, where the other entries of the logits' gradient are rounded to the operands' type once, and those of the
@@ -59,6 +60,28 @@ def test_entries_of_the_targets(n, d, v, labelled, dtype):
         assert not inside((once @ w).to(dtype), want_h, bound_h, dtype)
     assert inside(dh[used], want_h, bound_h, dtype)
     assert inside(dw, want_w, bound_w, dtype)
+
+
+@pytest.mark.parametrize("n,d,v,near", [(5000, 300, 9001, 700), (5000, 300, 9001, 1), (700, 72, 5003, 300), (9000, 24, 300000, 5000), (130, 600, 40000, 3)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_targets_that_lie_together(n, d, v, near, dtype):
+    """Many tokens for few tiles of classes, in any order, the last class among them."""
+    hidden, weight, targets = inputs(n, d, v, dtype, 7, size=0.05)
+    targets = v - 1 - targets % near
+    grad = grads(n)
+    _, lse = B().cross_entropy_forward(hidden, weight, targets, -100, "none")
+    dh, dw = B().cross_entropy_backward(grad, hidden, weight, targets, lse, -100, "none")
+    for _ in range(3):
+        assert torch.equal(B().cross_entropy_backward(grad, hidden, weight, targets, lse, -100, "none")[1], dw)
+    h, w = hidden.double(), weight.double()
+    G = torch.softmax(h @ w.t(), 1)
+    G[torch.arange(n), targets] -= 1
+    G *= grad.double()[:, None]
+    # the 2-norm of the errors: the results' own roundings, uniform within half a step (at most: over the square root of three), and
+    # a tenth more for the roundings of the other entries of the logits' gradient
+    for got, want in ((dh, G @ w), (dw, G.t() @ h)):
+        assert (got.double() - want).norm() <= 1.1 * HALF[dtype] / 3 ** 0.5 * want.norm()
+    B().operators_status()
 
 
 # Roundings to nearest average out over many tokens, and their number grows with the depth of a sum only below its size; what is cut off
