@@ -186,12 +186,16 @@ __device__ __forceinline__ float2 exp_pair(float a, float b, float base) {
   return make_float2(pow2(x.x), pow2(x.y));
 }
 
-// e^(v - lse), two at a time.  (The difference first: it is exact where the probability is large, while lse times log2(e) is rounded
-// to its own size.)
-__device__ __forceinline__ float2 probability_pair(float a, float b, float lse) {
-  const float2 x = mul2(add2(make_float2(a, b), both(-lse)), both(kLog2e));
-  return make_float2(pow2(x.x), pow2(x.y));
-}
+// A row's lse, for its probabilities: e^(v - lse) = 2^(v log2(e) - base) scale.  (lse times log2(e) is rounded to its own size, by much
+// more than a probability near 1 may be off; what that leaves is in the scale, which is a little off 1.)
+struct RowLse {
+  float base = 0.f, scale = 1.f;
+  __device__ __forceinline__ void set(float lse) {
+    base = lse * kLog2e;
+    const float x = -0.69314718f * fmaf(lse, kLog2e, -base);  // (below 2^-24 of lse: two terms of the exponential)
+    scale = fmaf(fmaf(0.5f, x, 1.f), x, 1.f);
+  }
+};
 
 // What becomes of 32 columns of a row of logits, forward: their largest value (times log2(e)) and the sum of
 // exponentials relative to it are joined to the row's.
@@ -534,12 +538,14 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
       const int cols = w.cols / 2, n0 = w.n0 + half * cols;
       const int steps = w.depth * kPairs + w.rests;
       int target = -1;
-      float lse = 0.f, coef = 0.f;
+      RowLse lse;
+      float coef = 0.f, times = 0.f;
       if (w.kind == kLogits) {
         target = p.target[row];
         if constexpr (BACKWARD) {
-          lse = p.lse[row];
+          lse.set(p.lse[row]);
           coef = p.coef[row];
+          times = coef * lse.scale;
         }
       }
       RowStats stats;
@@ -557,12 +563,12 @@ __global__ void __launch_bounds__(kXentThreads, 1) k_xent(const __grid_constant_
           if (mine) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) x = i == hit ? v[i] : x;
-            x = (probability_pair(x, x, lse).x - 1.f) * coef;
+            x = (exp_pair(x, x, lse.base).x * lse.scale - 1.f) * coef;
             if constexpr (kPairs == 1) p.rest[row] = x - rounded<O>(x);
           }
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
-            const float2 e = mul2(probability_pair(v[i], v[i + 1], lse), both(coef));
+            const float2 e = mul2(exp_pair(v[i], v[i + 1], lse.base), both(times));
             v[i] = e.x;
             v[i + 1] = e.y;
           }
