@@ -550,12 +550,14 @@ int efcp_group_norm_backward(const efcp_group_norm* desc, const void* dy, const 
  *                    afterwards; not needed (NULL) without dweight.
  * efcp_rms_norm_quantize gives y in 8 bits: with `block` columns sharing a scale (32, 64, 128; 0: the whole
  * row; the last block of a row may be shorter) and m their largest |h r w| in fp32,
- *     scale = m / 448 (EFCP_E4M3) or m / 127 (EFCP_INT8), q = h r w / scale to the nearest, ties to even;
- * scale 1 where m is 0, and scale NaN with q 0 where m is not finite.
+ *     scale = m / 448 (EFCP_E4M3) or m / 127 (EFCP_INT8), q = h r w / scale to the nearest;
+ * the quotient is taken by the inverse of scale, so that one within a few roundings of fp32 of the middle between two
+ * values may go to either; scale 1 where m is 0, and scale NaN with q 0 where m is not finite.
  *   q        device, rows * d bytes.   scales   device, rows * ceil(d / block) floats (rows, when block is 0).
- * Squares and sums are fp32 (a mean of squares beyond its range, rows of 2^64 and more, gives r = 0), in a fixed
- * order, so results repeat bit for bit; outputs are rounded to their type once.  Outputs overlap no input.  Work runs on the current device and on `stream`, asynchronously, and can be
- * captured in a graph.  rows == 0 enqueues nothing but the zeroing of dweight.
+ * Squares and sums are fp32 (where the squares of eight values add up to more than its range, r is 0), in a fixed
+ * order, so results repeat bit for bit; outputs are rounded to their type once.  Outputs overlap no input.  Work runs
+ * on the current device and on `stream`, asynchronously, and can be captured in a graph.  rows == 0 enqueues nothing but
+ * the zeroing of dweight.
  * EFCP_EINVAL (nothing enqueued): null or misaligned pointers, rows < 0, d outside 1 .. 2^30 - 1, a
  * product above 2^40, negative strides, eps negative or not finite, p outside 0 .. 1, unknown types, formats or blocks;
  * EFCP_ENOMEM: a workspace that is too small; EFCP_ETOOBIG: more than 2^31 - 1 thread blocks.
@@ -608,7 +610,9 @@ int efcp_dropout(const efcp_rms_norm* desc, const void* x, int64_t x_row, const 
  *                    aligned, undefined afterwards.  The backward call holds the gradient of as many columns of the
  *                    logits as fit in 256 MB (256 at least); operands that the tensor copies cannot read
  *                    where they lie, fp32 among them, are laid out there.
- * Products are exact and added up in fp32; fp32 operands are multiplied in three parts each, to about 2^-22.
+ * Products are exact and added up in fp32; of fp32 operands, which are multiplied in three parts each, what is left out
+ * is below 2^-22 of the sum of the products' magnitudes.  lse is one fp32 number: a probability is off by half a unit of
+ * its size, |lse| 2^-24, next to the error of its logit.
  * The logits' gradient is rounded to bf16 or fp16 (with a common factor that keeps it in range) before the two
  * products that read it, except for the entries of the targets, which have about twice as many bits; it has all of fp32
  * where the operands do.  All sums have a fixed order, so results repeat bit

@@ -1,7 +1,8 @@
 // Root-mean-square norm of a residual stream, forward, backward and with an output in 8 bits, and dropout of
 // rows (the formulas stand in include/efcp.h).
 //
-// Memory bounds them: every input is read once, every output written once.  A row is shared out over one
+// Every input is read once, every output written once.  The plain kernels here, for what is little and for rows that are long, wait
+// on latency more than on the memory (1531 x 1111 fp32 backward: 21 % of its rate, 36 % of the issue slots).  A row is shared out over one
 // to 32 warps whose lanes keep it in registers between the sum and the result (K chunks a warp); rows longer than
 // that (K == 0) are walked twice, the second time out of the cache.  Backward a thread keeps its columns
 // over all rows that its block takes, so the weight's gradient grows in registers; the blocks' sums are

@@ -12,10 +12,11 @@
 // those pieces' elements are copied one by one.
 //
 // The memory bounds rows that begin on 16 bytes without dropout, forward and backward: 16384 x 4096 bf16 with a residual
-// 90 us (5.96 TB/s) and 108 us (4.97 TB/s); 16384 x 768, 16 us.  Instructions bound the rest, with 16 warps on an SM, which
-// is what the registers allow: dropout's ten rounds for eight elements (16384 x 768, 24 us), the maxima and conversions of 8-bit
-// outputs (8192 x 4096: 58 us, blocks of 128), the shifts and the rows' ends of rows that begin anywhere (20000 x 1111 bf16:
-// 53 us forward, 79 us backward; 117 and 153 with loads of single elements).
+// 90 us (5.96 TB/s) and 108 us (4.97 TB/s); 16384 x 768, 16 us.  The rest waits on chains of instructions one behind the other, which
+// the 16 warps on an SM that the registers allow do not hide (about half of the issue slots are used): dropout's ten rounds for eight
+// elements (16384 x 768, 25 us, 53 % of them), the maxima and conversions of 8-bit outputs (8192 x 4096: 59 us, blocks of 128, 48 %),
+// the shifts and the rows' ends of rows that begin anywhere (20000 x 1111 bf16: 53 us forward, 79 us backward; 117 and 153 with
+// loads of single elements).
 #pragma once
 
 #include <cuda_runtime.h>

@@ -19,7 +19,8 @@
 // whose targets are near (XentGemm::bounds).
 //
 // fp32 values are held as three bfloat16 ones (8 bits of the significand each), of whose nine products the six
-// largest are added up, the small ones first; what is left out is below 2^-24 of the result.
+// largest are added up, the small ones first.  What is left out is below 2^-22 of the sum of the products' magnitudes: two products
+// of at most 2^-24 each, and a smaller one.
 #pragma once
 
 #include <cuda_runtime.h>

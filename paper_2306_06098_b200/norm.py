@@ -100,7 +100,7 @@ def add_rms_norm(x: torch.Tensor, residual: torch.Tensor, weight: Optional[torch
 
 
 class RMSNorm(WithGenerator):
-    """Root-mean-square norm of the last dimension, of size d.  forward(x) normalises x;
+    """Root-mean-square norm of the last dimension, of size d.  forward(x) normalises x, and drops nothing;
     forward(x, residual) returns the norm of h = dropout(x) + residual, and h.  The dropout of share p is
     active in training, with a generator of its own (inside of torch.utils.checkpoint: see
     dropout.checkpoint_contexts)."""
