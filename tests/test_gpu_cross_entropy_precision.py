@@ -62,7 +62,8 @@ def test_entries_of_the_targets(n, d, v, labelled, dtype):
     assert inside(dw, want_w, bound_w, dtype)
 
 
-@pytest.mark.parametrize("n,d,v,near", [(5000, 300, 9001, 700), (5000, 300, 9001, 1), (700, 72, 5003, 300), (9000, 24, 300000, 5000), (130, 600, 40000, 3)])
+@pytest.mark.parametrize("n,d,v,near", [(5000, 300, 9001, 700), (5000, 300, 9001, 1), (700, 72, 5003, 300), (9000, 24, 300000, 5000), (130, 600, 40000, 3),
+                                          (200000, 16, 600, 600)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_targets_that_lie_together(n, d, v, near, dtype):
     """Many tokens for few tiles of classes, in any order, the last class among them."""
